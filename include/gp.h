@@ -403,6 +403,69 @@ gp_status gp_lc_forward_branches(const void *stack, int64_t ld, gp_dtype dtype, 
 gp_status gp_lc_softmax(float *H, int64_t B, int32_t C, int64_t ld, void *hip_stream);
 
 /* ---------------------------------------------------------------------------
+ * What a model over the stack learns: a table of embedding rows (one per word, category or node: the features of
+ * slot 0 where nodes bring none of their own) and weight matrices.  Four operators carry a training step:
+ * gp_embedding, gp_embedding_grad, gp_orthogonalize, gp_muon_step.  (Between a lookup and its gradient, a filter
+ * over a symmetric operator is its own transpose: gp_propagate_combine serves both directions.)
+ * They keep nothing between calls and allocate nothing: scratch is the caller's, `workspace` (DEVICE, of the size the
+ * *_workspace call names, on a 256-byte boundary; what it holds is of no use afterwards; calls that overlap in time need one
+ * each).  All may be captured in a HIP graph.  Deterministic: the same inputs give the same bits.
+ */
+typedef enum { GP_I32 = 0, GP_I64 = 1 } gp_index;
+
+/* gp_embedding -- out[i, :] = scale * table[token[i], :], in fp32, rounded once to out_dtype.
+ *  table   DEVICE, V x d of `dtype`, rows ldt elements apart (ldt >= d >= 1, V >= 1).
+ *  tokens  DEVICE, N row numbers of type `index` (N >= 0).  A number outside [0, V) is not an error: its row of out is zero.
+ *  out     DEVICE, N x d of `out_dtype`, rows ldo elements apart (ldo >= d); may be a slab of a hop stack; must not overlap the inputs.
+ * Rows may start on any element.  Enqueued on hip_stream.  Errors: INVALID_ARG, OVERFLOW, DEVICE. */
+gp_status gp_embedding(const void *table, int64_t ldt, gp_dtype dtype, int64_t V, int32_t d, const void *tokens,
+                       gp_index index, int64_t N, float scale, void *out, int64_t ldo, gp_dtype out_dtype, void *hip_stream);
+
+/* gp_embedding_grad -- the gradient of gp_embedding with respect to the table:
+ *     table_grad[v, :] = scale * (sum of grad[i, :] over all i with token[i] = v)     (accumulate = 0: all V rows written)
+ *     table_grad[v, :] += the same                    (accumulate = 1: rows without a token are neither read nor written)
+ *  tokens      DEVICE, N row numbers; those outside [0, V) take no part.
+ *  grad        DEVICE, N x d of `dtype`, rows ldg elements apart.
+ *  table_grad  DEVICE, V x d of `out_dtype`, rows ldt elements apart; must not overlap the inputs.
+ * Sums are held in fp32 and rounded once.  The tokens are sorted, so a token's rows are added in an order that depends on
+ * the tokens alone.  N and V at most 2^31 - 1 (else UNSUPPORTED).  Enqueued on hip_stream.
+ * Errors: INVALID_ARG, UNSUPPORTED, DEVICE.  gp_embedding_grad_workspace: bytes; -1 for sizes that the call rejects. */
+int64_t gp_embedding_grad_workspace(int64_t N, int64_t V, int32_t d);
+gp_status gp_embedding_grad(const void *tokens, gp_index index, int64_t N, const void *grad, int64_t ldg, gp_dtype dtype,
+                            int32_t d, float scale, int64_t V, void *table_grad, int64_t ldt, gp_dtype out_dtype,
+                            int32_t accumulate, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/* gp_orthogonalize -- Newton-Schulz steps on `count` matrices of one shape:
+ *     X = G / (|G|_F + eps),  then `steps` times  A = X X^T,  X <- a X + (b A + c A A) X
+ * on G or its transpose, whichever has no more rows than columns: singular vectors stay, singular values go to
+ * a s + b s^3 + c s^5, step by step.
+ *  G      DEVICE, rows x cols of `dtype`, rows ldg elements apart, matrices stride_g elements apart.
+ *  coeff  HOST, 3 * steps floats (a, b, c of every step), read during the call; NULL: 3.4445, -4.7750, 2.0315 for all
+ *         (five steps take singular values of 0.01 .. 1 to about 0.7 .. 1.2).  Steps that take [0, 1] beyond 10^6 are
+ *         INVALID_ARG.  1 <= steps <= 32.
+ *  out    DEVICE, the same shape and dtype, rows ldo, matrices stride_o elements apart; may be G itself (same strides).  Matrices
+ *         of out must not overlap (INVALID_ARG).
+ * Products are taken in about 22 bits with fp32 accumulation whatever `dtype` is, X is held in as many; bf16 results are rounded once.  The
+ * sum of squares is held in fp64.  rows, cols <= 2^20, count <= 65535 (else UNSUPPORTED); nothing is done where one of them is 0.
+ * A matrix with an infinity or NaN gives NaN, and leaves the others alone.  Enqueued on hip_stream.
+ * Errors: INVALID_ARG, UNSUPPORTED, DEVICE.  gp_orthogonalize_workspace: bytes; -1 for sizes that the call rejects. */
+int64_t gp_orthogonalize_workspace(int64_t rows, int64_t cols, int64_t count);
+gp_status gp_orthogonalize(const void *G, int64_t ldg, int64_t stride_g, gp_dtype dtype, int64_t rows, int64_t cols,
+                           int64_t count, int32_t steps, const float *coeff, float eps, void *out, int64_t ldo,
+                           int64_t stride_o, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/* gp_muon_step -- a step of weight matrices along such directions:
+ *     M_out = momentum * M + G,   U = nesterov ? G + momentum * M_out : M_out,
+ *     W_out = (1 - lr * weight_decay) * W - lr * orthogonalize(U)
+ *  W, W_out  DEVICE fp32, rows ldw, matrices stride_w elements apart; W_out may be W.   M, M_out  the same with ldm, stride_m.
+ *  G         DEVICE, of `dtype`.  Everything else, the workspace too (gp_orthogonalize_workspace), as gp_orthogonalize. */
+gp_status gp_muon_step(const float *W, float *W_out, int64_t ldw, int64_t stride_w, const float *M, float *M_out, int64_t ldm,
+                       int64_t stride_m, const void *G, int64_t ldg, int64_t stride_g, gp_dtype dtype, int64_t rows,
+                       int64_t cols, int64_t count, float lr, float momentum, float weight_decay, int32_t nesterov,
+                       int32_t steps, const float *coeff, float eps, void *workspace, int64_t workspace_bytes,
+                       void *hip_stream);
+
+/* ---------------------------------------------------------------------------
  * Optimal graph decomposition (Section 3.2, Eq. 11 and Eq. 12): block counts
  * from byte volumes, the available GPU volume and the environment's coefficients
  * (all in the same unit, e.g. bytes or GB; coefficients are measured by watching

@@ -5,6 +5,7 @@ an error (build it with `python -m paper_2207_12000_amd.build`).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -62,6 +63,20 @@ _SIGNATURES = {
                                           _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int, _c.c_int32, _c.c_void_p,
                                           _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p]),
     "gp_lc_softmax": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int32, _c.c_int64, _c.c_void_p]),
+    "gp_embedding": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int, _c.c_int64, _c.c_int32, _c.c_void_p, _c.c_int, _c.c_int64,
+                                _c.c_float, _c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p]),
+    "gp_embedding_grad_workspace": (_c.c_int64, [_c.c_int64, _c.c_int64, _c.c_int32]),
+    "gp_embedding_grad": (_c.c_int, [_c.c_void_p, _c.c_int, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_int, _c.c_int32, _c.c_float,
+                                     _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_int, _c.c_int32, _c.c_void_p, _c.c_int64,
+                                     _c.c_void_p]),
+    "gp_orthogonalize_workspace": (_c.c_int64, [_c.c_int64, _c.c_int64, _c.c_int64]),
+    "gp_orthogonalize": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_int32,
+                                    _c.c_void_p, _c.c_float, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_int64,
+                                    _c.c_void_p]),
+    "gp_muon_step": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64,
+                                _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_float,
+                                _c.c_float, _c.c_float, _c.c_int32, _c.c_int32, _c.c_void_p, _c.c_float, _c.c_void_p, _c.c_int64,
+                                _c.c_void_p]),
     "gp_solve_normalisation_blocks": (_c.c_int, [_c.c_double] * 7 + [_c.POINTER(_c.c_int64)]),
     "gp_solve_aggregation_blocks": (_c.c_int, [_c.c_double] * 5 + [_c.c_int64, _c.POINTER(_c.c_int64),
                                                                   _c.POINTER(_c.c_int64)]),
@@ -429,6 +444,227 @@ def lc_forward_tensors(stack, batch, gamma, weights, out=None, stream=None, dept
         gp_lc_forward_branches(stack.data_ptr(), d, dtype, n, d, K1 - 1, bp, B, gamma, depth, comb, wp, ww, out.data_ptr(),
                                out.stride(0), stream)
     return out
+
+
+GP_I32, GP_I64 = 0, 1
+
+
+def gp_embedding(table_ptr: int, ldt: int, dtype: int, V: int, d: int, tokens_ptr: int, index: int, N: int, scale: float,
+                 out_ptr: int, ldo: int, out_dtype: int, stream: Optional[int] = None):
+    """Raw-pointer form: out[i, :] = scale * table[token[i], :]; all addresses are device addresses."""
+    st = lib().gp_embedding(table_ptr or None, ldt, dtype, V, d, tokens_ptr or None, index, N, scale, out_ptr or None, ldo,
+                            out_dtype, stream or None)
+    _check(st, "gp_embedding")
+
+
+def gp_embedding_grad_workspace(N: int, V: int, d: int) -> int:
+    return lib().gp_embedding_grad_workspace(N, V, d)
+
+
+def gp_embedding_grad(tokens_ptr: int, index: int, N: int, grad_ptr: int, ldg: int, dtype: int, d: int, scale: float, V: int,
+                      table_grad_ptr: int, ldt: int, out_dtype: int, accumulate: bool, workspace_ptr: int, workspace_bytes: int,
+                      stream: Optional[int] = None):
+    """Raw-pointer form of the gradient of gp_embedding; all addresses are device addresses."""
+    st = lib().gp_embedding_grad(tokens_ptr or None, index, N, grad_ptr or None, ldg, dtype, d, scale, V, table_grad_ptr or None,
+                                 ldt, out_dtype, int(accumulate), workspace_ptr or None, workspace_bytes, stream or None)
+    _check(st, "gp_embedding_grad")
+
+
+def gp_orthogonalize_workspace(rows: int, cols: int, count: int = 1) -> int:
+    return lib().gp_orthogonalize_workspace(rows, cols, count)
+
+
+def _coefficients(coeff, steps: int):
+    """(steps, 3) host floats from one triple for all steps, one for each, or None (the library's own)."""
+    if coeff is None:
+        return None
+    c = np.ascontiguousarray(coeff, dtype=np.float32)
+    if c.shape == (3,):
+        c = np.ascontiguousarray(np.broadcast_to(c, (max(steps, 0), 3)))
+    if c.shape != (steps, 3):
+        raise ValueError("coeff must hold three values, or three for every step")
+    return c
+
+
+def gp_orthogonalize(G_ptr: int, ldg: int, stride_g: int, dtype: int, rows: int, cols: int, count: int, steps: int, coeff, eps: float,
+                     out_ptr: int, ldo: int, stride_o: int, workspace_ptr: int, workspace_bytes: int, stream: Optional[int] = None):
+    """Raw-pointer form.  coeff: three host floats, three for every step, or None."""
+    c = _coefficients(coeff, steps)
+    st = lib().gp_orthogonalize(G_ptr or None, ldg, stride_g, dtype, rows, cols, count, steps, None if c is None else c.ctypes.data,
+                                eps, out_ptr or None, ldo, stride_o, workspace_ptr or None, workspace_bytes, stream or None)
+    _check(st, "gp_orthogonalize")
+
+
+def gp_muon_step(W_ptr: int, W_out_ptr: int, ldw: int, stride_w: int, M_ptr: int, M_out_ptr: int, ldm: int, stride_m: int, G_ptr: int,
+                 ldg: int, stride_g: int, dtype: int, rows: int, cols: int, count: int, lr: float, momentum: float,
+                 weight_decay: float, nesterov: bool, steps: int, coeff, eps: float, workspace_ptr: int, workspace_bytes: int,
+                 stream: Optional[int] = None):
+    """Raw-pointer form.  coeff: three host floats, three for every step, or None."""
+    c = _coefficients(coeff, steps)
+    st = lib().gp_muon_step(W_ptr or None, W_out_ptr or None, ldw, stride_w, M_ptr or None, M_out_ptr or None, ldm, stride_m,
+                            G_ptr or None, ldg, stride_g, dtype, rows, cols, count, lr, momentum, weight_decay, int(nesterov), steps,
+                            None if c is None else c.ctypes.data, eps, workspace_ptr or None, workspace_bytes, stream or None)
+    _check(st, "gp_muon_step")
+
+
+@contextlib.contextmanager
+def _other_stream(handle, device):
+    import torch
+    with torch.cuda.stream(torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)):
+        yield handle
+
+
+def _on_stream(tensor, stream):
+    """Context: the tensor's device and the stream a call is enqueued on (torch's current one unless given) are current while what the
+    call needs is allocated, so that torch gives its memory to no other stream before the call is done with it."""
+    import torch
+    if not tensor.is_cuda:
+        raise ValueError("tensors must be on the GPU")
+    current = torch.cuda.current_stream(tensor.device).cuda_stream
+    handle = current if stream is None else int(stream)
+    if handle == current and tensor.device.index == torch.cuda.current_device():
+        return contextlib.nullcontext(handle)
+    return _other_stream(handle, tensor.device)
+
+
+def _float_type(t):
+    import torch
+    kinds = {torch.float32: GP_F32, torch.bfloat16: GP_BF16}
+    dtype = t if isinstance(t, torch.dtype) else t.dtype
+    if dtype not in kinds:
+        raise ValueError("values must be float32 or bfloat16")
+    return kinds[dtype]
+
+
+def _index_type(tokens):
+    import torch
+    kinds = {torch.int32: GP_I32, torch.int64: GP_I64}
+    if tokens.dtype not in kinds or not tokens.is_contiguous():
+        raise ValueError("tokens must be a contiguous int32 or int64 tensor")
+    return kinds[tokens.dtype]
+
+
+def _one_device(*tensors):
+    if len({t.device for t in tensors if t is not None}) > 1:
+        raise ValueError("tensors must be on one device")
+
+
+def _row_stride(t, what):
+    """The distance of a matrix's rows, in elements (that of a single row, or of none, is whatever its width asks for)."""
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what} must have unit column stride")
+    return max(t.shape[-1], 1) if t.shape[-2] <= 1 else t.stride(-2)
+
+
+def _workspace(workspace, need, device):
+    import torch
+    if workspace is None:
+        return torch.empty(max(need, 0), dtype=torch.uint8, device=device)
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor")
+    return workspace
+
+
+def embedding_tensors(table, tokens, scale=1.0, out=None, out_dtype=None, stream=None):
+    """Convenience for torch tensors: table is a (V, d) float32 / bfloat16 GPU tensor, tokens an int32 / int64 GPU tensor of
+    any shape.  Returns scale * table[tokens], of shape tokens.shape + (d,), in out_dtype (the table's unless given); a
+    token outside the table gives zeros.  out: a (tokens.numel(), d) tensor with unit column stride, filled and returned."""
+    import torch
+    if table.dim() != 2:
+        raise ValueError("table must be a (V, d) tensor")
+    V, d = table.shape
+    dtype, index, ldt = _float_type(table), _index_type(tokens), _row_stride(table, "table")
+    N = tokens.numel()
+    if out is not None and (out.dim() != 2 or out.shape != (N, d) or out_dtype not in (None, out.dtype)):
+        raise ValueError("out must be a (tokens, d) tensor of out_dtype")
+    _one_device(table, tokens, out)
+    with _on_stream(table, stream) as handle:
+        result = out
+        if out is None:
+            result = torch.empty(tuple(tokens.shape) + (d,), dtype=out_dtype or table.dtype, device=table.device)
+            out = result.view(N, d)
+        gp_embedding(table.data_ptr(), ldt, dtype, V, d, tokens.data_ptr(), index, N, scale, out.data_ptr(), _row_stride(out, "out"),
+                     _float_type(out), handle)
+    return result
+
+
+def embedding_grad_tensors(tokens, grad, V, scale=1.0, out=None, out_dtype=None, accumulate=False, workspace=None, stream=None):
+    """Convenience for torch tensors: the gradient of embedding_tensors with respect to its table of V rows, from grad, the
+    gradient of what it returned ((N, d), or tokens.shape + (d,) contiguous).  Returns a (V, d) tensor of out_dtype (grad's
+    unless given), or adds to out (accumulate=True).  workspace: a uint8 GPU tensor of gp_embedding_grad_workspace(N, V, d)
+    bytes or more, kept by the caller; without one the call takes its memory from torch."""
+    import torch
+    N, index, dtype = tokens.numel(), _index_type(tokens), _float_type(grad)
+    if grad.dim() < 2:
+        raise ValueError("grad must hold one row per token")
+    if grad.dim() > 2:
+        if tuple(grad.shape[:-1]) != tuple(tokens.shape) or not grad.is_contiguous():
+            raise ValueError("grad of more than two dimensions must be contiguous, of shape tokens.shape + (d,)")
+        grad = grad.view(N, grad.shape[-1])
+    if grad.shape[0] != N:
+        raise ValueError("grad must hold one row per token")
+    d = grad.shape[1]
+    if accumulate and out is None:
+        raise ValueError("accumulate needs a tensor to add to")
+    if out is not None and (out.dim() != 2 or out.shape != (V, d) or out_dtype not in (None, out.dtype)):
+        raise ValueError("out must be a (V, d) tensor of out_dtype")
+    _one_device(tokens, grad, out, workspace)
+    with _on_stream(grad, stream) as handle:
+        if out is None:
+            out = torch.empty((V, d), dtype=out_dtype or grad.dtype, device=grad.device)
+        ws = _workspace(workspace, gp_embedding_grad_workspace(N, V, d), grad.device)
+        gp_embedding_grad(tokens.data_ptr(), index, N, grad.data_ptr(), _row_stride(grad, "grad"), dtype, d, scale, V, out.data_ptr(),
+                          _row_stride(out, "out"), _float_type(out), accumulate, ws.data_ptr(), ws.numel(), handle)
+    return out
+
+
+def _matrices(t, shape, dtype, what):
+    """(rows, cols, count, row distance, matrix distance) of a (rows, cols) or (count, rows, cols) tensor."""
+    if t.dim() not in (2, 3) or (shape is not None and t.shape != shape) or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{what} must be a (rows, cols) or (count, rows, cols) tensor, all of one shape, of the right type")
+    count = t.shape[0] if t.dim() == 3 else 1
+    return t.shape[-2], t.shape[-1], count, _row_stride(t, what), t.stride(0) if t.dim() == 3 and count > 1 else 0
+
+
+def orthogonalize_tensors(G, steps=5, coeff=None, eps=1e-7, out=None, workspace=None, stream=None):
+    """Convenience for torch tensors: Newton-Schulz steps on G, a (rows, cols) or (count, rows, cols) float32 / bfloat16 GPU
+    tensor.  coeff: (a, b, c), or three for every step, or None (3.4445, -4.7750, 2.0315).  Returns out (made if not given;
+    G itself will do).  workspace: a uint8 GPU tensor of gp_orthogonalize_workspace(rows, cols, count) bytes or more."""
+    import torch
+    rows, cols, count, ldg, sg = _matrices(G, None, None, "G")
+    dtype = _float_type(G)
+    if out is not None:
+        _matrices(out, G.shape, G.dtype, "out")
+    _one_device(G, out, workspace)
+    with _on_stream(G, stream) as handle:
+        if out is None:
+            out = torch.empty(G.shape, dtype=G.dtype, device=G.device)
+        _, _, _, ldo, so = _matrices(out, G.shape, G.dtype, "out")
+        ws = _workspace(workspace, gp_orthogonalize_workspace(rows, cols, count), G.device)
+        gp_orthogonalize(G.data_ptr(), ldg, sg, dtype, rows, cols, count, steps, coeff, eps, out.data_ptr(), ldo, so, ws.data_ptr(),
+                         ws.numel(), handle)
+    return out
+
+
+def muon_step_tensors(W, M, G, lr, momentum=0.95, weight_decay=0.0, nesterov=True, steps=5, coeff=None, eps=1e-7, W_out=None,
+                      M_out=None, workspace=None, stream=None):
+    """Convenience for torch tensors: one step of weight matrices W (float32) with momentum M (float32) and gradient G (float32 /
+    bfloat16), all (rows, cols) or (count, rows, cols).  W and M are stepped in place unless W_out, M_out are given (of the
+    same strides).  Returns (W_out, M_out).  coeff, workspace: as orthogonalize_tensors."""
+    import torch
+    rows, cols, count, ldg, sg = _matrices(G, None, None, "G")
+    dtype = _float_type(G)
+    W_out, M_out = W if W_out is None else W_out, M if M_out is None else M_out
+    _, _, _, ldw, sw = _matrices(W, G.shape, torch.float32, "W")
+    _, _, _, ldm, sm = _matrices(M, G.shape, torch.float32, "M")
+    if _matrices(W_out, G.shape, torch.float32, "W_out")[3:] != (ldw, sw) or _matrices(M_out, G.shape, torch.float32, "M_out")[3:] != (ldm, sm):
+        raise ValueError("W_out and M_out must have the strides of W and M")
+    _one_device(G, W, M, W_out, M_out, workspace)
+    with _on_stream(G, stream) as handle:
+        ws = _workspace(workspace, gp_orthogonalize_workspace(rows, cols, count), G.device)
+        gp_muon_step(W.data_ptr(), W_out.data_ptr(), ldw, sw, M.data_ptr(), M_out.data_ptr(), ldm, sm, G.data_ptr(), ldg, sg, dtype, rows,
+                     cols, count, lr, momentum, weight_decay, nesterov, steps, coeff, eps, ws.data_ptr(), ws.numel(), handle)
+    return W_out, M_out
 
 
 def gp_solve_normalisation_blocks(B_A, B_S, B_D, B_GPU, alpha_A=1.0, alpha_S=1.0, alpha_D=1.0) -> int:

@@ -1,0 +1,426 @@
+// Update directions of weight matrices by Newton-Schulz products, and the step of a weight matrix around them.
+//
+//     X = U / (|U|_F + eps),   then, step by step,   A = X X^T,   B = b A + c A A,   X <- a X + B X,
+//
+// X being U or its transpose, whichever has no more rows (m) than columns (n).  Every step maps each singular value s of X to
+// a s + b s^3 + c s^5 and leaves the singular vectors alone.  (K. Jordan's Muon optimiser takes such directions from
+// the momentum of a weight matrix's gradient.)
+//
+// Arithmetic.  What the steps leave of a direction that is weak in U is its share times a^steps (485 for five steps of the
+// usual a = 3.4445), and so are the roundings on the way: with bf16 operands the result was 1.4e-2 off for normal matrices and
+// 0.35 off (relative error in the Frobenius norm) for gradients of low rank over a floor of noise; with single f16
+// operands 1.3e-3 and 2.8e-2.  So every matrix is held as two f16 parts, x = hi + lo with 22 bits between them, and a product is three
+// f16 products with fp32 accumulation, hi hi + hi lo + lo hi: 3.7e-7 and 9e-6, where fp32 arithmetic itself left 1.6e-6 and
+// 1.7e-5.  A singular value after any number of steps is at most what the polynomial makes of [0, 1], and no element exceeds
+// the largest singular value: a power of two per matrix and step, known beforehand, keeps every part inside f16's range
+// and lo above its subnormal numbers where it counts.
+//
+// Every product is taken as rows times rows (both operands consecutive along the summed dimension): A and B are symmetric,
+// and X is kept in both orientations.
+#include <algorithm>
+#include <cmath>
+#include <exception>
+
+#include "gp_internal.h"
+
+namespace gp {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTile = 64;          // sides of planes are multiples of it; what is added is zero
+constexpr int kNormBlocks = 256;   // partial sums of squares per matrix
+constexpr int kMaxSteps = 32;
+
+typedef unsigned short bf16_t;
+typedef _Float16 f16;
+typedef f16 v8h __attribute__((ext_vector_type(8)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ float widen(bf16_t v) { return __uint_as_float((unsigned)v << 16); }
+
+struct Update {  // U, element by element: G, or the momentum step M <- mu M + G and U = G + mu M (Nesterov) or M
+    const void* G;
+    int64_t ldg, stride_g;
+    const float* M;
+    float* M_out;
+    int64_t ldm, stride_m;
+    float mu;
+    int nesterov;
+    int64_t rows, cols;
+};
+
+// ---- the sum of squares, and the new momentum ---------------------------------------------------------
+
+__device__ __forceinline__ double block_sum(double v, double* part)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    double s = 0.0;
+    for (int w = 0; w < kThreads / 64; ++w) s += part[w];
+    return s;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void gp_ns_norms(Update u, double* __restrict__ partial)
+{
+    __shared__ double part[kThreads / 64];
+    const int64_t z = blockIdx.y, total = u.rows * u.cols;
+    const T* const G = (const T*)u.G + z * u.stride_g;
+    double s = 0.0;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)kNormBlocks * kThreads) {
+        const int64_t r = i / u.cols, c = i - r * u.cols;
+        float v = widen(G[r * u.ldg + c]);
+        if (u.M) {
+            const int64_t e = z * u.stride_m + r * u.ldm + c;
+            const float m = u.mu * u.M[e] + v;
+            u.M_out[e] = m;
+            v = u.nesterov ? v + u.mu * m : m;
+        }
+        s += (double)v * v;
+    }
+    s = block_sum(s, part);
+    if (threadIdx.x == 0) partial[z * kNormBlocks + blockIdx.x] = s;
+}
+
+// ---- the first X, in two parts and both orientations --------------------------------------------------
+
+__device__ __forceinline__ void split(float v, f16& hi, f16& lo)
+{
+    hi = (f16)v;
+    lo = (f16)(v - (float)hi);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void gp_ns_start(Update u, const double* __restrict__ partial, float eps, float scale, f16* natural,
+                                                        f16* transposed, int64_t lo, int64_t stride, int ldn, int ldt)
+{
+    __shared__ double part[kThreads / 64];
+    __shared__ float tile[kTile][kTile + 1];
+    const int64_t z = blockIdx.z;
+    static_assert(kNormBlocks == kThreads, "one partial sum per thread");
+    const double norm = sqrt(block_sum(partial[z * kNormBlocks + threadIdx.x], part));
+    const float factor = (float)((double)scale / (norm + (double)eps));
+    const T* const G = (const T*)u.G + z * u.stride_g;
+    const int64_t r0 = (int64_t)blockIdx.y * kTile, c0 = (int64_t)blockIdx.x * kTile;
+    f16* const pn = natural + z * stride;
+    f16* const pt = transposed + z * stride;
+    for (int i = threadIdx.x; i < kTile * kTile; i += kThreads) {
+        const int64_t r = r0 + i / kTile, c = c0 + i % kTile;
+        float v = 0.0f;
+        if (r < u.rows && c < u.cols) {
+            v = widen(G[r * u.ldg + c]);
+            if (u.M) {
+                const float m = u.M_out[z * u.stride_m + r * u.ldm + c];
+                v = u.nesterov ? v + u.mu * m : m;
+            }
+            v *= factor;
+        }
+        tile[i / kTile][i % kTile] = v;
+        f16 h, l;
+        split(v, h, l);
+        pn[r * ldn + c] = h, pn[lo + r * ldn + c] = l;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kTile * kTile; i += kThreads) {
+        const int64_t c = c0 + i / kTile, r = r0 + i % kTile;
+        f16 h, l;
+        split(tile[i % kTile][i / kTile], h, l);
+        pt[c * ldt + r] = h, pt[lo + c * ldt + r] = l;
+    }
+}
+
+// ---- products ----------------------------------------------------------------------------------------
+
+// D = alpha P Q^T + beta E over planes of parts (the second lo elements behind the first), D into its own planes and, transposed,
+// into others; or, at the end, into the caller's matrix.
+struct Product {
+    const f16 *P, *Q, *E;
+    int ldp, ldq, lde, K;
+    int64_t lo, stride;  // elements from first to second parts, from one matrix of the call to the next
+    float alpha, beta;
+    f16 *D, *Dt;
+    int ldd, lddt;
+    int symmetric;  // D and Dt are one plane: tiles on and above the diagonal will do
+    // the last product
+    int64_t rows, cols;
+    void* out;
+    int64_t ldo, stride_o;
+    const float* W;
+    float keep, lr;
+};
+
+template <typename TO, bool LAST>
+__global__ __launch_bounds__(kThreads) void gp_ns_product(Product a)
+{
+    const int bi = blockIdx.y, bj = blockIdx.x;
+    if (a.symmetric && bi > bj) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t base = (int64_t)blockIdx.z * a.stride;
+    const int r0 = bi * kTile + (wave >> 1) * 32, c0 = bj * kTile + (wave & 1) * 32;
+    const f16* p = a.P + base + (int64_t)(r0 + (lane & 31)) * a.ldp + (lane >> 5) * 8;
+    const f16* q = a.Q + base + (int64_t)(c0 + (lane & 31)) * a.ldq + (lane >> 5) * 8;
+    v16f acc;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
+    for (int k = 0; k < a.K; k += 16) {
+        const v8h ph = *(const v8h*)(p + k), pl = *(const v8h*)(p + a.lo + k);
+        const v8h qh = *(const v8h*)(q + k), ql = *(const v8h*)(q + a.lo + k);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
+    }
+    const int c = c0 + (lane & 31);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int r = r0 + (i >> 2) * 8 + (lane >> 5) * 4 + (i & 3);
+        float v = acc[i] * a.alpha;
+        if (a.E) {
+            const f16* const e = a.E + base + (int64_t)r * a.lde + c;
+            v += a.beta * ((float)e[0] + (float)e[a.lo]);
+        }
+        if constexpr (LAST) {
+            if (r >= a.rows || c >= a.cols) continue;
+            const int64_t o = blockIdx.z * a.stride_o + r * a.ldo + c;
+            if (a.W) v = a.keep * a.W[o] - a.lr * v;
+            if constexpr (sizeof(TO) == 4)
+                ((float*)a.out)[o] = v;
+            else
+                ((bf16_t*)a.out)[o] = __builtin_bit_cast(bf16_t, (__bf16)v);
+        } else {
+            f16 h, l;
+            split(v, h, l);
+            f16* const d = a.D + base + (int64_t)r * a.ldd + c;
+            d[0] = h, d[a.lo] = l;
+            if (a.symmetric && bi == bj) continue;  // (the tile holds both halves)
+            f16* const t = a.Dt + base + (int64_t)c * a.lddt + r;
+            t[0] = h, t[a.lo] = l;
+        }
+    }
+}
+
+// ---- ranges ------------------------------------------------------------------------------------------
+
+// the largest |a s + b s^3 + c s^5| over 0 <= s <= top
+double polynomial_bound(double a, double b, double c, double top)
+{
+    auto value = [&](double s) { return std::fabs(s * (a + s * s * (b + s * s * c))); };
+    double best = value(top);
+    double roots[2] = {-1.0, -1.0};  // s^2 where the slope a + 3 b s^2 + 5 c s^4 is zero
+    if (c != 0.0) {
+        const double disc = 9.0 * b * b - 20.0 * a * c;
+        if (disc >= 0.0) roots[0] = (-3.0 * b + std::sqrt(disc)) / (10.0 * c), roots[1] = (-3.0 * b - std::sqrt(disc)) / (10.0 * c);
+    } else if (b != 0.0) {
+        roots[0] = -a / (3.0 * b);
+    }
+    for (double r : roots)
+        if (r > 0.0 && r < top * top) best = std::max(best, value(std::sqrt(r)));
+    return best;
+}
+// the largest |b t + c t^2| over 0 <= t <= top
+double quadratic_bound(double b, double c, double top)
+{
+    double best = std::fabs(top * (b + top * c));
+    if (c != 0.0) {
+        const double t = -b / (2.0 * c);
+        if (t > 0.0 && t < top) best = std::max(best, std::fabs(t * (b + t * c)));
+    }
+    return best;
+}
+// the exponent that brings numbers up to `bound` just under 2^15 (f16 ends at 2^16)
+int exponent_for(double bound)
+{
+    int e = 0;
+    (void)std::frexp(bound * 1.01, &e);  // bound * 1.01 <= 2^e; the rest of the factor of two takes the roundings
+    return std::min(100, std::max(-100, 15 - e));
+}
+
+// ---- the call ----------------------------------------------------------------------------------------
+
+struct NsLayout {
+    int64_t m, n;                    // shorter and longer side, of whole tiles
+    int64_t X[2], Xt[2], A, B;       // planes of a matrix, in elements; second parts `lo` elements behind
+    int64_t lo, stride;              // elements
+    int64_t planes, total;           // bytes
+};
+NsLayout ns_layout(int64_t rows, int64_t cols, int64_t count)
+{
+    NsLayout l;
+    l.m = (std::min(rows, cols) + kTile - 1) / kTile * kTile;
+    l.n = (std::max(rows, cols) + kTile - 1) / kTile * kTile;
+    int64_t at = 0;
+    for (int i = 0; i < 2; ++i) l.X[i] = at, l.Xt[i] = at + l.m * l.n, at += 2 * l.m * l.n;
+    l.A = at, l.B = at + l.m * l.m, at += 2 * l.m * l.m;
+    l.lo = at, l.stride = 2 * at;
+    l.planes = (count * kNormBlocks * 8 + 255) / 256 * 256;
+    l.total = l.planes + count * l.stride * 2;
+    return l;
+}
+
+constexpr int64_t kMaxSide = 1 << 20;
+constexpr float kDefaultCoeff[3] = {3.4445f, -4.7750f, 2.0315f};
+
+// what is written: matrices one behind the other, or side by side in rows long enough for all of them
+gp_status check_apart(const char* what, int64_t rows, int64_t cols, int64_t count, int64_t ld, int64_t stride)
+{
+    if (count <= 1 || rows == 0 || cols == 0) return GP_OK;
+    if (stride >= (rows - 1) * ld + cols || (stride >= cols && ld >= (count - 1) * stride + cols)) return GP_OK;
+    return fail(GP_ERR_INVALID_ARG, "matrices of %s overlap", what);
+}
+
+gp_status check_shape(int64_t rows, int64_t cols, int64_t count)
+{
+    if (rows < 0 || cols < 0 || count < 0) return fail(GP_ERR_INVALID_ARG, "negative size");
+    if (rows > kMaxSide || cols > kMaxSide || count > 65535)
+        return fail(GP_ERR_UNSUPPORTED, "%lld matrices of %lld x %lld: at most 65535 of 2^20 x 2^20", (long long)count, (long long)rows, (long long)cols);
+    return GP_OK;
+}
+
+template <bool LAST>
+gp_status launch_product(const Product& a, int64_t rows, int64_t cols, int64_t count, gp_dtype dtype, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(cols / kTile), (unsigned)(rows / kTile), (unsigned)count);
+    profile_begin("gp_ns_product", stream);
+    if (LAST && dtype == GP_BF16)
+        hipLaunchKernelGGL((gp_ns_product<bf16_t, LAST>), grid, dim3(kThreads), 0, stream, a);
+    else
+        hipLaunchKernelGGL((gp_ns_product<float, LAST>), grid, dim3(kThreads), 0, stream, a);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    return GP_OK;
+}
+
+// out: the direction itself (W null, of dtype out_dtype), or the stepped weights
+gp_status newton_schulz(const Update& u, gp_dtype dtype, int64_t count, int32_t steps, const float* coeff, float eps, const float* W, float keep,
+                        float lr, void* out, int64_t ldo, int64_t stride_o, gp_dtype out_dtype, void* workspace, int64_t bytes, hipStream_t stream)
+{
+    if (steps < 1 || steps > kMaxSteps) return fail(GP_ERR_INVALID_ARG, "steps = %d: 1 .. %d", steps, kMaxSteps);
+    if (!(eps >= 0.0f)) return fail(GP_ERR_INVALID_ARG, "eps must not be negative");
+    int ex[kMaxSteps + 1], ea[kMaxSteps], eb[kMaxSteps];
+    double top = 1.0;
+    for (int k = 0; k < steps; ++k) {
+        const float* const p = coeff ? coeff + 3 * k : kDefaultCoeff;
+        ex[k] = exponent_for(top), ea[k] = exponent_for(top * top), eb[k] = exponent_for(quadratic_bound(p[1], p[2], top * top));
+        top = polynomial_bound(p[0], p[1], p[2], top);
+        if (!(top <= 1e6)) return fail(GP_ERR_INVALID_ARG, "step %d takes singular values of 0 .. 1 out to %g", k + 1, top);
+    }
+    if (u.rows == 0 || u.cols == 0 || count == 0) return GP_OK;
+    const NsLayout l = ns_layout(u.rows, u.cols, count);
+    if (!workspace || bytes < l.total || (uintptr_t)workspace % 256 != 0)
+        return fail(GP_ERR_INVALID_ARG, "need a workspace of %lld bytes on a 256-byte boundary", (long long)l.total);
+    double* const partial = (double*)workspace;
+    f16* const ws = (f16*)((char*)workspace + l.planes);
+    const bool tall = u.rows > u.cols;
+
+    profile_begin("gp_ns_norms", stream);
+    if (dtype == GP_F32)
+        hipLaunchKernelGGL(gp_ns_norms<float>, dim3(kNormBlocks, (unsigned)count), dim3(kThreads), 0, stream, u, partial);
+    else
+        hipLaunchKernelGGL(gp_ns_norms<bf16_t>, dim3(kNormBlocks, (unsigned)count), dim3(kThreads), 0, stream, u, partial);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    {
+        const int64_t pr = tall ? l.n : l.m, pc = tall ? l.m : l.n;
+        const dim3 grid((unsigned)(pc / kTile), (unsigned)(pr / kTile), (unsigned)count);
+        f16 *const natural = ws + (tall ? l.Xt[0] : l.X[0]), *const transposed = ws + (tall ? l.X[0] : l.Xt[0]);
+        const float scale = std::ldexp(1.0f, ex[0]);
+        profile_begin("gp_ns_start", stream);
+        if (dtype == GP_F32)
+            hipLaunchKernelGGL(gp_ns_start<float>, grid, dim3(kThreads), 0, stream, u, partial, eps, scale, natural, transposed, l.lo, l.stride, (int)pc, (int)pr);
+        else
+            hipLaunchKernelGGL(gp_ns_start<bf16_t>, grid, dim3(kThreads), 0, stream, u, partial, eps, scale, natural, transposed, l.lo, l.stride, (int)pc, (int)pr);
+        profile_end(stream);
+        GP_HIP(hipGetLastError());
+    }
+    const int m = (int)l.m, n = (int)l.n;
+    for (int k = 0; k < steps; ++k) {
+        const float* const p = coeff ? coeff + 3 * k : kDefaultCoeff;
+        f16 *const X = ws + l.X[k & 1], *const Xt = ws + l.Xt[k & 1], *const A = ws + l.A, *const B = ws + l.B;
+        Product a{};
+        a.lo = l.lo, a.stride = l.stride;
+        a.P = a.Q = X, a.ldp = a.ldq = n, a.K = n;
+        a.alpha = std::ldexp(1.0f, ea[k] - 2 * ex[k]);
+        a.D = a.Dt = A, a.ldd = a.lddt = m, a.symmetric = 1;
+        gp_status st = launch_product<false>(a, m, m, count, GP_F32, stream);
+        if (st != GP_OK) return st;
+        a.P = a.Q = a.E = A, a.ldp = a.ldq = a.lde = m, a.K = m;
+        a.alpha = std::ldexp(p[2], eb[k] - 2 * ea[k]), a.beta = std::ldexp(p[1], eb[k] - ea[k]);
+        a.D = a.Dt = B;
+        if ((st = launch_product<false>(a, m, m, count, GP_F32, stream)) != GP_OK) return st;
+        a.symmetric = 0;
+        const bool last = k == steps - 1;
+        const int next = last ? 0 : ex[k + 1] - ex[k];
+        if (!last) {
+            a.P = B, a.ldp = m, a.Q = Xt, a.ldq = m, a.E = X, a.lde = n, a.K = m;
+            a.alpha = std::ldexp(1.0f, next - eb[k]), a.beta = std::ldexp(p[0], next);
+            a.D = ws + l.X[(k + 1) & 1], a.ldd = n, a.Dt = ws + l.Xt[(k + 1) & 1], a.lddt = m;
+            if ((st = launch_product<false>(a, m, n, count, GP_F32, stream)) != GP_OK) return st;
+        } else {  // in the orientation of the caller's matrix
+            a.P = tall ? Xt : B, a.Q = tall ? B : Xt, a.ldp = a.ldq = m, a.K = m;
+            a.E = tall ? Xt : X, a.lde = tall ? m : n;
+            a.alpha = std::ldexp(1.0f, -ex[k] - eb[k]), a.beta = std::ldexp(p[0], -ex[k]);
+            a.rows = u.rows, a.cols = u.cols, a.out = out, a.ldo = ldo, a.stride_o = stride_o, a.W = W, a.keep = keep, a.lr = lr;
+            if ((st = launch_product<true>(a, tall ? n : m, tall ? m : n, count, out_dtype, stream)) != GP_OK) return st;
+        }
+    }
+    return GP_OK;
+}
+
+}  // namespace
+
+}  // namespace gp
+
+extern "C" int64_t gp_orthogonalize_workspace(int64_t rows, int64_t cols, int64_t count)
+{
+    if (rows < 0 || cols < 0 || count < 0 || rows > gp::kMaxSide || cols > gp::kMaxSide || count > 65535) return -1;
+    return rows == 0 || cols == 0 || count == 0 ? 0 : gp::ns_layout(rows, cols, count).total;
+}
+
+extern "C" gp_status gp_orthogonalize(const void* G, int64_t ldg, int64_t stride_g, gp_dtype dtype, int64_t rows, int64_t cols, int64_t count,
+                                      int32_t steps, const float* coeff, float eps, void* out, int64_t ldo, int64_t stride_o, void* workspace,
+                                      int64_t workspace_bytes, void* hip_stream)
+{
+    using namespace gp;
+    try {
+        if (dtype != GP_F32 && dtype != GP_BF16) return fail(GP_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+        gp_status st = check_shape(rows, cols, count);
+        if (st != GP_OK) return st;
+        if (ldg < cols || ldo < cols) return fail(GP_ERR_INVALID_ARG, "need ldg >= cols, ldo >= cols");
+        if ((st = check_apart("out", rows, cols, count, ldo, stride_o)) != GP_OK) return st;
+        if ((!G || !out) && rows > 0 && cols > 0 && count > 0) return fail(GP_ERR_INVALID_ARG, "NULL argument");
+        Update u{};
+        u.G = G, u.ldg = ldg, u.stride_g = stride_g, u.rows = rows, u.cols = cols;
+        return newton_schulz(u, dtype, count, steps, coeff, eps, nullptr, 0.0f, 0.0f, out, ldo, stride_o, dtype, workspace, workspace_bytes,
+                             (hipStream_t)hip_stream);
+    } catch (const std::exception& e) {
+        return fail(GP_ERR_OOM_HOST, "gp_orthogonalize: %s", e.what());
+    }
+}
+
+extern "C" gp_status gp_muon_step(const float* W, float* W_out, int64_t ldw, int64_t stride_w, const float* M, float* M_out, int64_t ldm,
+                                  int64_t stride_m, const void* G, int64_t ldg, int64_t stride_g, gp_dtype dtype, int64_t rows, int64_t cols,
+                                  int64_t count, float lr, float momentum, float weight_decay, int32_t nesterov, int32_t steps,
+                                  const float* coeff, float eps, void* workspace, int64_t workspace_bytes, void* hip_stream)
+{
+    using namespace gp;
+    try {
+        if (dtype != GP_F32 && dtype != GP_BF16) return fail(GP_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+        gp_status st = check_shape(rows, cols, count);
+        if (st != GP_OK) return st;
+        if (ldg < cols || ldw < cols || ldm < cols) return fail(GP_ERR_INVALID_ARG, "need ldg >= cols, ldw >= cols, ldm >= cols");
+        if ((st = check_apart("W", rows, cols, count, ldw, stride_w)) != GP_OK) return st;
+        if ((st = check_apart("M", rows, cols, count, ldm, stride_m)) != GP_OK) return st;
+        if ((!G || !W || !W_out || !M || !M_out) && rows > 0 && cols > 0 && count > 0) return fail(GP_ERR_INVALID_ARG, "NULL argument");
+        Update u{};
+        u.G = G, u.ldg = ldg, u.stride_g = stride_g, u.rows = rows, u.cols = cols;
+        u.M = M, u.M_out = M_out, u.ldm = ldm, u.stride_m = stride_m, u.mu = momentum, u.nesterov = nesterov != 0;
+        return newton_schulz(u, dtype, count, steps, coeff, eps, W, (float)(1.0 - (double)lr * (double)weight_decay), lr, W_out, ldw, stride_w,
+                             GP_F32, workspace, workspace_bytes, (hipStream_t)hip_stream);
+    } catch (const std::exception& e) {
+        return fail(GP_ERR_OOM_HOST, "gp_muon_step: %s", e.what());
+    }
+}

@@ -1,0 +1,421 @@
+"""The training operators on the GPU against their definitions in 64 bits.
+
+Tolerances.  A looked-up row is one fp32 product, rounded once: equal bits.  A gradient row of t terms is a sum in fp32 in some
+order: at most t roundings of 2^-24 of the terms' magnitudes (and one for the scale), then one of the result (2^-24, or 2^-8 in bf16).
+Newton-Schulz steps: with operands of 22 bits, step k leaves an error of a few 2^-22 of |X_k|, which the steps after it stretch by at
+most the polynomial's largest slope L each: 4 * 2^-22 * sum_k L^(steps - k) |X_k| / |X_steps| in the Frobenius norm, and 2^-9 for a
+result in bf16.  (Operands of 11 bits would be a thousand times that.)
+"""
+import numpy as np
+import pytest
+
+import paper_2207_12000_amd as gp
+from oracle import training
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu(gpu_or_skip):
+    yield
+
+
+def types():
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "i32": torch.int32, "i64": torch.int64}
+
+
+def padded(rows, cols, ld, dtype, skew=0, fill=float("nan")):
+    """A (rows, cols) view with rows ld elements apart, `skew` elements into its memory; the rest is `fill`."""
+    import torch
+    flat = torch.full((rows * ld + skew + 64,), fill, dtype=dtype, device="cuda")
+    return flat, flat[skew:skew + rows * ld].view(rows, ld)[:, :cols]
+
+
+def same_bits(a, b):
+    import torch
+    assert a.dtype == b.dtype and a.shape == b.shape
+    return torch.equal(a.contiguous().view(torch.int16 if a.element_size() == 2 else torch.int32),
+                       b.contiguous().view(torch.int16 if a.element_size() == 2 else torch.int32))
+
+
+# ---- lookup ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("index", ["i32", "i64"])
+@pytest.mark.parametrize("kinds", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("N,V,d,pad,skew", [(1, 1, 1, 0, 0), (5, 3, 2, 1, 1), (1, 7, 128, 0, 0), (3, 9, 3, 0, 1), (77, 50, 4, 0, 0), (64, 11, 5, 0, 0),
+                                            (130, 1000, 8, 3, 1), (257, 40, 47, 0, 1), (1000, 333, 100, 5, 3), (65, 13, 129, 0, 0),
+                                            (33, 77, 602, 2, 0), (4096, 500, 256, 0, 0), (9, 5, 4097, 0, 1)])
+def test_lookup(N, V, d, pad, skew, kinds, index):
+    import torch
+    ty = types()
+    rng = np.random.default_rng(N * 31 + d)
+    _, table = padded(V, d, d + pad, ty[kinds[0]], skew)
+    table.copy_(torch.from_numpy(rng.normal(size=(V, d)).astype(np.float32)))
+    tokens = torch.from_numpy(rng.integers(-2, V + 2, N)).to(ty[index]).cuda()
+    flat, out = padded(N, d, d + 2 * pad, ty[kinds[1]], skew, fill=7.0)
+    for scale in (1.0, -0.37):
+        got = gp.embedding_tensors(table, tokens, scale=scale, out=out)
+        assert got is out
+        known = (tokens >= 0) & (tokens < V)
+        want = (table.float()[tokens.long().clamp(0, V - 1)] * torch.tensor(scale, device="cuda") * known[:, None].float())
+        want = torch.where(known[:, None], want, torch.zeros_like(want)).to(ty[kinds[1]])
+        assert same_bits(out, want)
+        if pad:  # between the rows, before and behind them: untouched
+            flat[skew:skew + N * (d + 2 * pad)].view(N, -1)[:, :d] = 7.0
+            assert bool((flat == 7.0).all())
+
+
+def test_lookup_against_the_oracle():
+    import torch
+    rng = np.random.default_rng(5)
+    table, tokens = rng.normal(size=(40, 19)).astype(np.float32), rng.integers(-1, 41, 100)
+    got = gp.embedding_tensors(torch.from_numpy(table).cuda(), torch.from_numpy(tokens).cuda(), scale=0.5).cpu().numpy()
+    assert np.array_equal(got, training.embedding(table, tokens, 0.5))
+
+
+def test_lookup_keeps_the_shape_of_tokens_and_takes_none():
+    import torch
+    table = torch.randn(10, 6, device="cuda")
+    tokens = torch.randint(0, 10, (3, 4), device="cuda")
+    assert torch.equal(gp.embedding_tensors(table, tokens), table[tokens])
+    assert gp.embedding_tensors(table, tokens[:0].contiguous()).shape == (0, 4, 6)
+    far = torch.tensor([2 ** 40, -2 ** 63, 2 ** 32 + 1, 3], device="cuda")  # (2^32 + 1 is no 1)
+    assert torch.equal(gp.embedding_tensors(table, far), torch.cat([torch.zeros(3, 6, device="cuda"), table[3:4]]))
+
+
+def test_special_values_of_the_table():
+    import torch
+    table = torch.tensor([[float("inf"), float("nan"), -0.0, 3e38]], device="cuda")
+    got = gp.embedding_tensors(table, torch.tensor([0, -1], device="cuda"), scale=2.0)
+    assert got[0, 0] == float("inf") and got[0, 1].isnan() and got[0, 3] == float("inf") and torch.equal(got[1], torch.zeros(4, device="cuda"))
+    nothing = gp.embedding_tensors(table, torch.tensor([-1], device="cuda"), scale=float("inf"))
+    assert torch.equal(nothing, torch.zeros(1, 4, device="cuda"))
+
+
+def test_lookup_and_gradient_past_32_bit_offsets():
+    import torch
+    V, d = 17_000_003, 260   # 4.4e9 elements of bf16
+    table = torch.empty(V, d, dtype=torch.bfloat16, device="cuda")
+    rows = torch.tensor([0, 16_500_000, V - 1, 9_000_001], device="cuda")
+    table[rows] = torch.randn(4, d, device="cuda").bfloat16()
+    assert torch.equal(gp.embedding_tensors(table, rows), table[rows])
+    up = torch.randn(4, d, device="cuda").bfloat16()
+    gp.embedding_grad_tensors(rows.to(torch.int32), up, V, out=table)
+    assert torch.equal(table[rows], up)
+    assert int(torch.count_nonzero(table[16_500_001:V - 1])) == 0 and int(torch.count_nonzero(table[1:9_000_001])) == 0
+
+
+# ---- gradient ----------------------------------------------------------------------------------------------
+
+def check_gradient(got, tokens, up, V, scale, before=None):
+    want, size, terms = training.embedding_grad(tokens.cpu().numpy(), up.float().cpu().numpy(), V, scale)
+    if before is not None:
+        want, size = want + before, size + np.abs(before)
+    last = 2.0 ** -24 if got.element_size() == 4 else 2.0 ** -8
+    bound = (terms[:, None] + 2) * 2.0 ** -24 * size + last * np.abs(want) + 1e-37
+    err = np.abs(got.float().cpu().numpy() - want)
+    assert (err <= bound).all(), f"worst {np.nanmax(err / bound):.2f} of the bound"
+
+
+def tokens_of(kind, N, V, rng):
+    if kind == "uniform":
+        return rng.integers(0, V, N)
+    if kind == "one":      # every position names one row
+        return np.full(N, V // 2)
+    if kind == "none":
+        return np.full(N, -1)
+    if kind == "hot":      # half of them name one row, some name none
+        t = rng.integers(0, V, N)
+        t[rng.random(N) < 0.5] = V - 1
+        t[rng.random(N) < 0.1] = V
+        return t
+    if kind == "sorted":
+        return np.sort(rng.integers(0, V, N))
+    return np.arange(N)[::-1] % V
+
+
+@pytest.mark.parametrize("tokens_kind", ["uniform", "one", "none", "hot", "sorted", "falling"])
+@pytest.mark.parametrize("N,V,d", [(1, 1, 1), (2, 3, 4), (15, 5, 47), (16, 16, 8), (17, 300, 128), (64, 2, 3), (1000, 70, 100), (1025, 5000, 33),
+                                   (4096, 257, 64), (20_011, 47, 47), (70_001, 65_536, 16)])
+def test_gradient(N, V, d, tokens_kind):
+    import torch
+    rng = np.random.default_rng(N + V)
+    tokens = torch.from_numpy(tokens_of(tokens_kind, N, V, rng)).to(torch.int32).cuda()
+    up = torch.from_numpy(rng.normal(size=(N, d)).astype(np.float32)).cuda()
+    out = torch.full((V, d), float("nan"), device="cuda")
+    gp.embedding_grad_tensors(tokens, up, V, scale=0.3, out=out)
+    check_gradient(out, tokens, up, V, np.float32(0.3).astype(np.float64))
+
+
+@pytest.mark.parametrize("index", ["i32", "i64"])
+@pytest.mark.parametrize("kinds", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("N,V,d,pad,skew", [(600, 41, 1, 0, 1), (600, 41, 5, 1, 1), (3000, 900, 47, 0, 1), (2500, 30, 100, 4, 0), (900, 77, 130, 3, 1),
+                                            (500, 29, 602, 1, 1), (300, 11, 1031, 0, 0)])
+def test_gradient_types_and_strides(N, V, d, pad, skew, kinds, accumulate, index):
+    import torch
+    ty = types()
+    rng = np.random.default_rng(d)
+    tokens = torch.from_numpy(rng.integers(-1, V - 3, N)).to(ty[index]).cuda()   # (the last rows have no token)
+    _, up = padded(N, d, d + pad, ty[kinds[0]], skew)
+    up.copy_(torch.from_numpy(rng.normal(size=(N, d)).astype(np.float32)))
+    flat, out = padded(V, d, d + 2 * pad, ty[kinds[1]], skew, fill=0.25)
+    ws = torch.full((gp.gp_embedding_grad_workspace(N, V, d),), 255, dtype=torch.uint8, device="cuda")
+    gp.embedding_grad_tensors(tokens, up, V, scale=2.0, out=out, accumulate=accumulate, workspace=ws)
+    check_gradient(out, tokens, up, V, 2.0, before=0.25 if accumulate else None)
+    first = out.clone()
+    flat[skew:skew + V * (d + 2 * pad)].view(V, -1)[:, :d] = 0.25
+    assert bool((flat == 0.25).all())                                            # nothing beside the rows was written
+    gp.embedding_grad_tensors(tokens, up, V, scale=2.0, out=out, accumulate=accumulate)
+    assert same_bits(out, first)
+
+
+@pytest.mark.parametrize("N,V,d,tokens_kind", [(262_143, 1000, 16, "hot"), (262_145, 3, 20, "uniform"), (600_000, 2_000_000, 8, "uniform"),
+                                               (1_000_003, 200_000, 12, "one")])
+def test_gradient_of_long_lists(N, V, d, tokens_kind):
+    import torch
+    rng = np.random.default_rng(7)
+    tokens = torch.from_numpy(tokens_of(tokens_kind, N, V, rng)).to(torch.int32).cuda()
+    up = torch.from_numpy(rng.normal(size=(N, d)).astype(np.float32)).cuda()
+    out = gp.embedding_grad_tensors(tokens, up, V)
+    check_gradient(out, tokens, up, V, 1.0)
+    assert same_bits(out, gp.embedding_grad_tensors(tokens, up, V))
+
+
+def test_a_gradient_row_with_infinity_or_nan_stays_alone():
+    import torch
+    tokens = torch.tensor([3, 1, 3, 2, -1, 1], device="cuda")
+    up = torch.ones(6, 9, device="cuda")
+    up[0, 2], up[3, 4], up[4] = float("inf"), float("nan"), float("nan")
+    got = gp.embedding_grad_tensors(tokens, up, 5)
+    want = torch.tensor([0.0, 2.0, 1.0, 2.0, 0.0], device="cuda")[:, None].repeat(1, 9)
+    want[3, 2], want[2, 4] = float("inf"), float("nan")
+    assert torch.allclose(got, want, rtol=0, atol=0, equal_nan=True)
+
+
+def test_no_tokens():
+    import torch
+    tokens, up = torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty(0, 7, device="cuda")
+    out = torch.ones(5, 7, device="cuda")
+    gp.embedding_grad_tensors(tokens, up, 5, out=out, accumulate=True)
+    assert bool((out == 1).all())
+    gp.embedding_grad_tensors(tokens, up, 5, out=out)
+    assert bool((out == 0).all())
+
+
+def test_gradient_agrees_with_differences():
+    """<lookup(table + D), up> - <lookup(table), up> = <grad, D>: the lookup is linear."""
+    import torch
+    rng = np.random.default_rng(3)
+    table, step = (torch.from_numpy(rng.integers(-8, 9, (50, 21)).astype(np.float32)).cuda() for _ in range(2))   # (exact in fp32)
+    tokens = torch.from_numpy(rng.integers(-1, 51, 400)).cuda()
+    up = torch.from_numpy(rng.integers(-8, 9, (400, 21)).astype(np.float32)).cuda()
+    moved = gp.embedding_tensors(table + step, tokens, scale=0.5) - gp.embedding_tensors(table, tokens, scale=0.5)
+    grad = gp.embedding_grad_tensors(tokens, up, 50, scale=0.5)
+    assert float((moved.double() * up.double()).sum()) == float((grad.double() * step.double()).sum())
+
+
+# ---- Newton-Schulz -------------------------------------------------------------------------------------------
+
+def tolerance(iterates, steps, coeff, out_bytes):
+    coeff = np.broadcast_to(np.asarray(coeff, dtype=np.float64), (steps, 3))
+    s = np.linspace(0.0, 1.25, 2001)
+    slope = [np.abs(a + 3 * b * s ** 2 + 5 * c * s ** 4).max() for a, b, c in coeff]
+    norms = [np.linalg.norm(x) for x in iterates]
+    total = sum(np.prod(slope[k:]) * norms[k] for k in range(steps + 1)) / norms[-1]
+    return 4 * 2.0 ** -22 * total + (2.0 ** -9 if out_bytes == 2 else 0.0)
+
+
+def check_direction(got, G, steps=5, coeff=training.COEFF, eps=1e-7):
+    iterates = training.newton_schulz(G.double().cpu().numpy(), steps, coeff, eps)
+    err = np.linalg.norm(got.double().cpu().numpy() - iterates[-1]) / np.linalg.norm(iterates[-1])
+    tol = tolerance(iterates, steps, coeff, got.element_size())
+    assert err <= tol, f"{err:.3g} against {tol:.3g}"
+
+
+def gradient_like(shape, rng, floor=0.2):
+    """A few strong directions over a floor of noise."""
+    k = max(1, min(shape) // 8)
+    return 1e-3 * (rng.normal(size=(shape[0], k)) @ rng.normal(size=(k, shape[1])) + floor * rng.normal(size=shape))
+
+
+SHAPES = [(1, 1), (1, 7), (7, 1), (16, 16), (16, 40), (63, 65), (64, 64), (65, 63), (128, 128), (130, 257), (256, 40), (40, 256), (256, 256), (602, 256),
+          (100, 1023), (511, 513)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_orthogonalize(shape, dtype):
+    import torch
+    rng = np.random.default_rng(shape[0])
+    for G in (rng.normal(size=shape), gradient_like(shape, rng)):
+        G = torch.from_numpy(G).to(types()[dtype]).cuda()
+        check_direction(gp.orthogonalize_tensors(G), G)
+
+
+@pytest.mark.parametrize("shape", [(300, 1100), (1500, 700), (1024, 1024)])
+def test_orthogonalize_larger(shape):
+    import torch
+    G = torch.from_numpy(gradient_like(shape, np.random.default_rng(4))).float().cuda()
+    check_direction(gp.orthogonalize_tensors(G), G)
+
+
+@pytest.mark.parametrize("steps,coeff", [(1, (1.5, -0.5, 0.0)), (2, (3.0, -16 / 5, 6 / 5)), (3, [(4.0, -6.0, 2.5), (3.0, -3.5, 1.4), (15 / 8, -10 / 8, 3 / 8)]),
+                                         (8, (15 / 8, -10 / 8, 3 / 8)), (2, (0.0, 0.0, 0.0)), (4, (30.0, 0.0, 0.0)), (1, (-2.0, 1.0, 0.5))])
+@pytest.mark.parametrize("shape", [(70, 90), (90, 70)])
+def test_other_polynomials(shape, steps, coeff):
+    import torch
+    G = torch.from_numpy(gradient_like(shape, np.random.default_rng(6))).float().cuda()
+    got = gp.orthogonalize_tensors(G, steps=steps, coeff=coeff)
+    if not np.any(coeff):
+        assert bool((got == 0).all())
+    else:
+        c32 = np.asarray(coeff, dtype=np.float32).astype(np.float64)
+        check_direction(got, G, steps, c32)
+
+
+@pytest.mark.parametrize("power", [-30, -12, 12, 30])
+def test_any_magnitude(power):
+    import torch
+    G = torch.from_numpy(gradient_like((48, 130), np.random.default_rng(8)) * 10.0 ** power).float().cuda()
+    check_direction(gp.orthogonalize_tensors(G, eps=0.0), G, eps=0.0)
+
+
+def test_eps_rules_over_a_small_matrix_and_zero_stays_zero():
+    import torch
+    G = torch.from_numpy(np.random.default_rng(9).normal(size=(20, 30)) * 1e-9).float().cuda()
+    check_direction(gp.orthogonalize_tensors(G, eps=1e-7), G, eps=1e-7)
+    assert bool((gp.orthogonalize_tensors(torch.zeros(20, 30, device="cuda")) == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(33, 70), (70, 33), (200, 200)])
+def test_batches_strides_and_in_place(shape, dtype):
+    import torch
+    rng = np.random.default_rng(10)
+    ty = types()[dtype]
+    G = torch.from_numpy(np.stack([gradient_like(shape, rng) for _ in range(3)])).to(ty).cuda()
+    alone = torch.stack([gp.orthogonalize_tensors(g) for g in G])
+    assert same_bits(gp.orthogonalize_tensors(G), alone)
+    # matrices side by side in long rows, from an odd address; the rest is left alone
+    flat = torch.full((1 + shape[0] * (3 * shape[1] + 5),), 9.0, dtype=ty, device="cuda")
+    wide = flat[1:].view(shape[0], 3 * shape[1] + 5)
+    side = wide[:, :3 * shape[1]].unflatten(1, (3, shape[1])).permute(1, 0, 2)
+    side.copy_(G)
+    ws = torch.full((gp.gp_orthogonalize_workspace(*shape, 3),), 255, dtype=torch.uint8, device="cuda")
+    gp.orthogonalize_tensors(side, out=side, workspace=ws)
+    assert same_bits(side, alone)
+    assert bool((wide[:, 3 * shape[1]:] == 9.0).all()) and float(flat[0]) == 9.0
+    one = G[0].clone()
+    gp.orthogonalize_tensors(one, out=one)
+    assert same_bits(one, alone[0])
+    same = gp.orthogonalize_tensors(G[:1].expand(2, *shape))   # one matrix read twice
+    assert same_bits(same, alone[:1].expand(2, *shape).contiguous())
+
+
+def test_a_matrix_with_nan_or_infinity_spoils_no_other():
+    import torch
+    G = torch.from_numpy(np.random.default_rng(11).normal(size=(4, 50, 80))).float().cuda()
+    want = gp.orthogonalize_tensors(G)
+    G[1, 3, 4], G[2, 0, 0] = float("nan"), float("inf")
+    got = gp.orthogonalize_tensors(G)
+    assert bool(got[1].isnan().all()) and bool(got[2].isnan().all())
+    assert same_bits(got[0], want[0]) and same_bits(got[3], want[3])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("shape", [(1, 1), (256, 40), (96, 130), (130, 96)])
+def test_muon_step(shape, nesterov, dtype):
+    import torch
+    rng = np.random.default_rng(12)
+    W, M = (torch.from_numpy(x).float().cuda() for x in (rng.normal(size=shape) / shape[0] ** 0.5, 5 * gradient_like(shape, rng)))
+    G = torch.from_numpy(gradient_like(shape, rng)).to(types()[dtype]).cuda()
+    lr, mu, wd = (float(np.float32(x)) for x in (0.02, 0.95, 0.1))
+    W2, M2 = gp.muon_step_tensors(W, M, G, lr, mu, wd, nesterov, W_out=torch.empty_like(W), M_out=torch.empty_like(M))
+    w, m, g = (x.double().cpu().numpy() for x in (W, M, G))
+    want_W, want_M = training.muon_step(w, m, g, lr, mu, wd, nesterov)
+    # M: two roundings; W: the direction's tolerance (U itself has three roundings, which the steps stretch no further than
+    # they do their own), times lr, and three roundings of its own
+    assert (np.abs(M2.double().cpu().numpy() - want_M) <= 2.0 ** -23 * (np.abs(mu * m) + np.abs(g))).all()
+    iterates = training.newton_schulz(g + mu * want_M if nesterov else want_M)
+    tol = lr * 2 * tolerance(iterates, 5, training.COEFF, 4) * np.linalg.norm(iterates[-1]) + 3 * 2.0 ** -24 * (np.linalg.norm(w) + lr * np.linalg.norm(iterates[-1]))
+    assert np.linalg.norm(W2.double().cpu().numpy() - want_W) <= tol
+    gp.muon_step_tensors(W, M, G, lr, mu, wd, nesterov)     # in place
+    assert same_bits(W, W2) and same_bits(M, M2)
+
+
+def test_muon_steps_of_several_matrices():
+    import torch
+    rng = np.random.default_rng(13)
+    W, M, G = (torch.from_numpy(rng.normal(size=(3, 66, 50))).float().cuda() for _ in range(3))
+    alone = [gp.muon_step_tensors(W[i], M[i], G[i], 0.1, W_out=torch.empty(66, 50, device="cuda"), M_out=torch.empty(66, 50, device="cuda"))
+             for i in range(3)]
+    W2, M2 = gp.muon_step_tensors(W, M, G, 0.1, W_out=torch.empty_like(W), M_out=torch.empty_like(M))
+    for i in range(3):
+        assert same_bits(W2[i], alone[i][0]) and same_bits(M2[i], alone[i][1])
+
+
+# ---- streams and graphs --------------------------------------------------------------------------------------
+
+def all_four(s):
+    gp.embedding_tensors(s["table"], s["tokens"], scale=2.0, out=s["rows"])
+    gp.embedding_grad_tensors(s["tokens"], s["rows"], s["table"].shape[0], out=s["grad"], workspace=s["ws1"])
+    gp.orthogonalize_tensors(s["G"], out=s["O"], workspace=s["ws2"])
+    gp.muon_step_tensors(s["W"], s["M"], s["G"], 0.1, W_out=s["W2"], M_out=s["M2"], workspace=s["ws2"])
+
+
+def state(N=3000, V=500, d=36):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    s = dict(table=torch.randn(V, d, generator=gen, device="cuda"), tokens=torch.randint(-1, V, (N,), generator=gen, device="cuda"),
+             rows=torch.empty(N, d, device="cuda"), grad=torch.empty(V, d, device="cuda"), G=torch.randn(70, 90, generator=gen, device="cuda"),
+             W=torch.randn(70, 90, generator=gen, device="cuda"), M=torch.randn(70, 90, generator=gen, device="cuda"))
+    s.update(O=torch.empty_like(s["G"]), W2=torch.empty_like(s["W"]), M2=torch.empty_like(s["M"]),
+             ws1=torch.empty(gp.gp_embedding_grad_workspace(N, V, d), dtype=torch.uint8, device="cuda"),
+             ws2=torch.empty(gp.gp_orthogonalize_workspace(70, 90), dtype=torch.uint8, device="cuda"))
+    return s
+
+
+def results(s):
+    return [s[k].clone() for k in ("rows", "grad", "O", "W2", "M2")]
+
+
+def test_replays_of_a_captured_step():
+    import torch
+    s = state()
+    all_four(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        all_four(s)
+    for seed in range(4):   # other inputs in the same places, eager work and waits in between
+        gen = torch.Generator(device="cuda").manual_seed(10 + seed)
+        for k in ("table", "G", "W", "M"):
+            s[k].copy_(torch.randn(s[k].shape, generator=gen, device="cuda"))
+        s["tokens"].copy_(torch.randint(-1, 500 if seed % 2 else 4, s["tokens"].shape, generator=gen, device="cuda"))
+        for k in ("rows", "grad", "O", "W2", "M2"):
+            s[k].fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = results(s)
+        all_four(s)
+        torch.cuda.synchronize()
+        assert all(same_bits(a, b) for a, b in zip(replayed, results(s)))
+
+
+def test_another_stream_than_the_current_one():
+    import torch
+    s = state()
+    all_four(s)
+    want = results(s)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    rows = gp.embedding_tensors(s["table"], s["tokens"], scale=2.0, stream=side.cuda_stream)
+    grad = gp.embedding_grad_tensors(s["tokens"], rows, 500, stream=side.cuda_stream)
+    O = gp.orthogonalize_tensors(s["G"], stream=side.cuda_stream)
+    filler = [torch.full((1 << 22,), 3.0, device="cuda") for _ in range(8)]   # (the current stream's memory is others')
+    side.synchronize()
+    assert same_bits(rows, want[0]) and same_bits(grad, want[1]) and same_bits(O, want[2])
+    del filler
