@@ -18,6 +18,7 @@
 // Every product is taken as rows times rows (both operands consecutive along the summed dimension): A and B are symmetric,
 // and X is kept in both orientations.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <exception>
 
@@ -34,6 +35,7 @@ constexpr int kMaxSteps = 32;
 
 typedef unsigned short bf16_t;
 typedef _Float16 f16;
+typedef f16 v4h __attribute__((ext_vector_type(4)));
 typedef f16 v8h __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
@@ -95,9 +97,12 @@ __device__ __forceinline__ void split(float v, f16& hi, f16& lo)
     lo = (f16)(v - (float)hi);
 }
 
+constexpr int kParts = 32;  // from a first part to its second
+__device__ __forceinline__ int64_t place(int64_t c) { return (c >> 5) * (2 * kParts) + (c & 31); }
+
 template <typename T>
 __global__ __launch_bounds__(kThreads) void gp_ns_start(Update u, const double* __restrict__ partial, float eps, float scale, f16* natural,
-                                                        f16* transposed, int64_t lo, int64_t stride, int ldn, int ldt)
+                                                        f16* transposed, int64_t stride, int ldn, int ldt)
 {
     __shared__ double part[kThreads / 64];
     __shared__ float tile[kTile][kTile + 1];
@@ -123,29 +128,32 @@ __global__ __launch_bounds__(kThreads) void gp_ns_start(Update u, const double* 
         tile[i / kTile][i % kTile] = v;
         f16 h, l;
         split(v, h, l);
-        pn[r * ldn + c] = h, pn[lo + r * ldn + c] = l;
+        pn[r * ldn + place(c)] = h, pn[r * ldn + place(c) + kParts] = l;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < kTile * kTile; i += kThreads) {
         const int64_t c = c0 + i / kTile, r = r0 + i % kTile;
         f16 h, l;
         split(tile[i % kTile][i / kTile], h, l);
-        pt[c * ldt + r] = h, pt[lo + c * ldt + r] = l;
+        pt[c * ldt + place(r)] = h, pt[c * ldt + place(r) + kParts] = l;
     }
 }
 
 // ---- products ----------------------------------------------------------------------------------------
 
-// D = alpha P Q^T + beta E over planes of parts (the second lo elements behind the first), D into its own planes and, transposed,
-// into others; or, at the end, into the caller's matrix.
+// D = alpha P Q^T + beta E over planes, D into its own plane and, transposed, into another; or, at the end, into the caller's
+// matrix.  A plane's row holds, 32 columns after 32 columns, their first parts and then their second parts (place()): what a step
+// of the sum takes of a row is one 128-byte line.
 struct Product {
     const f16 *P, *Q, *E;
-    int ldp, ldq, lde, K;
-    int64_t lo, stride;  // elements from first to second parts, from one matrix of the call to the next
+    int ldp, ldq, lde;   // halves from row to row
+    int M, N, K;         // rows of P, rows of Q, summed columns: multiples of 64
+    int64_t stride;      // halves from one matrix of the call to the next
     float alpha, beta;
     f16 *D, *Dt;
     int ldd, lddt;
-    int symmetric;  // D and Dt are one plane: tiles on and above the diagonal will do
+    int symmetric;       // D and Dt are one plane: tiles on and above the diagonal will do
+    int tiles_n;
     // the last product
     int64_t rows, cols;
     void* out;
@@ -154,53 +162,142 @@ struct Product {
     float keep, lr;
 };
 
-template <typename TO, bool LAST>
-__global__ __launch_bounds__(kThreads) void gp_ns_product(Product a)
+typedef __attribute__((address_space(1))) const void* GlobalPtr;
+typedef __attribute__((address_space(3))) void* LdsPtr;
+
+// BM x BN tiles of D by WM x WN waves.  A step sums over 32 columns: BM + BN lines of 128 bytes, which go straight from memory to one
+// half of LDS while the matrix cores work on the other half.  A line's 16-byte pieces lie in LDS in the order
+// piece ^ (row / 2 mod 8), with which the 16 lanes that LDS serves together read different banks.
+// A wave's registers hold its BM / WM x BN / WN sums as 32 x 32 blocks: lane l has column l mod 32, rows 8 (i / 4) + 4 (l / 32) + i mod 4.
+template <int BM, int BN, int WM, int WN, typename TO, bool LAST>
+__global__ __launch_bounds__(64 * WM * WN) void gp_ns_product(Product a)
 {
-    const int bi = blockIdx.y, bj = blockIdx.x;
-    if (a.symmetric && bi > bj) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int kWaves = WM * WN;
+    constexpr int RB = BM / WM / 32, CB = BN / WN / 32;  // blocks of a wave
+    constexpr int kLoads = (BM + BN) / 8 / kWaves;       // eight lines per wave and load
+    constexpr int kHalf = (BM + BN) * 64;
+    extern __shared__ __align__(128) f16 lds[];
+    int bi, bj;
+    if (a.symmetric) {  // tiles of the upper triangle, row by row
+        const int t = blockIdx.x, T = a.tiles_n;
+        bi = (int)((2 * T + 1 - sqrtf((float)((2 * T + 1) * (2 * T + 1) - 8 * t))) * 0.5f);
+        while (bi * T - bi * (bi - 1) / 2 > t) --bi;
+        while ((bi + 1) * T - (bi + 1) * bi / 2 <= t) ++bi;
+        bj = bi + t - (bi * T - bi * (bi - 1) / 2);
+    } else {
+        bi = blockIdx.x / a.tiles_n, bj = blockIdx.x - bi * a.tiles_n;
+    }
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t base = (int64_t)blockIdx.z * a.stride;
-    const int r0 = bi * kTile + (wave >> 1) * 32, c0 = bj * kTile + (wave & 1) * 32;
-    const f16* p = a.P + base + (int64_t)(r0 + (lane & 31)) * a.ldp + (lane >> 5) * 8;
-    const f16* q = a.Q + base + (int64_t)(c0 + (lane & 31)) * a.ldq + (lane >> 5) * 8;
-    v16f acc;
+    // lines this lane takes part in loading; those past the planes' ends repeat the last one (and are not used)
+    const f16* src[kLoads];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
-    for (int k = 0; k < a.K; k += 16) {
-        const v8h ph = *(const v8h*)(p + k), pl = *(const v8h*)(p + a.lo + k);
-        const v8h qh = *(const v8h*)(q + k), ql = *(const v8h*)(q + a.lo + k);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
+    for (int u = 0; u < kLoads; ++u) {
+        const int line = (u * kWaves + wave) * 8 + (lane >> 3);
+        const int piece = (lane & 7) ^ ((line >> 1) & 7);
+        src[u] = line < BM ? a.P + base + (int64_t)min(bi * BM + line, a.M - 1) * a.ldp + piece * 8
+                           : a.Q + base + (int64_t)min(bj * BN + line - BM, a.N - 1) * a.ldq + piece * 8;
     }
-    const int c = c0 + (lane & 31);
+    auto load = [&](int half, int step) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int r = r0 + (i >> 2) * 8 + (lane >> 5) * 4 + (i & 3);
-        float v = acc[i] * a.alpha;
-        if (a.E) {
-            const f16* const e = a.E + base + (int64_t)r * a.lde + c;
-            v += a.beta * ((float)e[0] + (float)e[a.lo]);
-        }
-        if constexpr (LAST) {
-            if (r >= a.rows || c >= a.cols) continue;
-            const int64_t o = blockIdx.z * a.stride_o + r * a.ldo + c;
-            if (a.W) v = a.keep * a.W[o] - a.lr * v;
-            if constexpr (sizeof(TO) == 4)
-                ((float*)a.out)[o] = v;
-            else
-                ((bf16_t*)a.out)[o] = __builtin_bit_cast(bf16_t, (__bf16)v);
-        } else {
-            f16 h, l;
-            split(v, h, l);
-            f16* const d = a.D + base + (int64_t)r * a.ldd + c;
-            d[0] = h, d[a.lo] = l;
-            if (a.symmetric && bi == bj) continue;  // (the tile holds both halves)
-            f16* const t = a.Dt + base + (int64_t)c * a.lddt + r;
-            t[0] = h, t[a.lo] = l;
+        for (int u = 0; u < kLoads; ++u)
+            __builtin_amdgcn_global_load_lds((GlobalPtr)(src[u] + (int64_t)step * 64), (LdsPtr)(lds + half * kHalf + (u * kWaves + wave) * 512), 16, 0, 0);
+    };
+    const int wr = wave / WN * (RB * 32), wc = wave % WN * (CB * 32);
+    // where this lane reads: line wr + lane mod 32, pieces lane / 32 + 2 s (+ 4: second parts), s = 0, 1
+    const int swap = (lane >> 1) & 7;
+    const f16* const pl = lds + (wr + (lane & 31)) * 64;
+    const f16* const ql = lds + (BM + wc + (lane & 31)) * 64;
+    v16f acc[RB][CB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[r][c][i] = 0.0f;
+    const int steps = a.K / 32;
+    load(0, 0);
+    for (int k = 0; k < steps; ++k) {
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's lines are there; behind the barrier, everyone's
+        __syncthreads();
+        const int h = (k & 1) * kHalf;
+        if (k + 1 < steps) load(~k & 1, k + 1);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            v8h p[2][RB], q[2][CB];
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                const int at = (((lane >> 5) + 2 * s + 4 * part) ^ swap) * 8 + h;
+#pragma unroll
+                for (int r = 0; r < RB; ++r) p[part][r] = *(const v8h*)(pl + r * 32 * 64 + at);
+#pragma unroll
+                for (int c = 0; c < CB; ++c) q[part][c] = *(const v8h*)(ql + c * 32 * 64 + at);
+            }
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int c = 0; c < CB; ++c) {
+                    acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[1][r], q[0][c], acc[r][c], 0, 0, 0);
+                    acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[0][r], q[1][c], acc[r][c], 0, 0, 0);
+                    acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[0][r], q[0][c], acc[r][c], 0, 0, 0);
+                }
         }
     }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            const int r0 = bi * BM + wr + rb * 32, c0 = bj * BN + wc + cb * 32;
+            if (r0 >= a.M || c0 >= a.N) continue;
+            const int c = c0 + (lane & 31), rl = r0 + (lane >> 5) * 4;  // element i: row rl + 8 (i / 4) + i mod 4
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = acc[rb][cb][i] * a.alpha;
+            if (a.E) {
+                const f16* const e = a.E + base + (int64_t)rl * a.lde + place(c);
+                f16 hi[16], lo[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) hi[i] = e[(int64_t)(8 * (i >> 2) + (i & 3)) * a.lde], lo[i] = e[(int64_t)(8 * (i >> 2) + (i & 3)) * a.lde + kParts];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] += a.beta * ((float)hi[i] + (float)lo[i]);
+            }
+            if constexpr (LAST) {
+                if (c >= a.cols) continue;
+                const int64_t o = blockIdx.z * a.stride_o + rl * a.ldo + c;
+                float w[16];
+                if (a.W) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[i] = rl + 8 * (i >> 2) + (i & 3) < a.rows ? a.W[o + (8 * (i >> 2) + (i & 3)) * a.ldo] : 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = a.keep * w[i] - a.lr * v[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int dr = 8 * (i >> 2) + (i & 3);
+                    if (rl + dr >= a.rows) continue;
+                    if constexpr (sizeof(TO) == 4)
+                        ((float*)a.out)[o + dr * a.ldo] = v[i];
+                    else
+                        ((bf16_t*)a.out)[o + dr * a.ldo] = __builtin_bit_cast(bf16_t, (__bf16)v[i]);
+                }
+            } else {
+                f16* const d = a.D + base + (int64_t)rl * a.ldd + place(c);
+                f16* const t = a.Dt + base + (int64_t)c * a.lddt + place(rl);
+                const bool both = !a.symmetric || bi != bj;  // (a tile on the diagonal holds both halves)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    v4h hi, lo;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        f16 x, y;
+                        split(v[4 * g + i], x, y);
+                        hi[i] = x, lo[i] = y;
+                        d[(int64_t)(8 * g + i) * a.ldd] = x, d[(int64_t)(8 * g + i) * a.ldd + kParts] = y;
+                    }
+                    if (both) *(v4h*)(t + 8 * g) = hi, *(v4h*)(t + 8 * g + kParts) = lo;
+                }
+            }
+        }
 }
 
 // ---- ranges ------------------------------------------------------------------------------------------
@@ -242,10 +339,10 @@ int exponent_for(double bound)
 // ---- the call ----------------------------------------------------------------------------------------
 
 struct NsLayout {
-    int64_t m, n;                    // shorter and longer side, of whole tiles
-    int64_t X[2], Xt[2], A, B;       // planes of a matrix, in elements; second parts `lo` elements behind
-    int64_t lo, stride;              // elements
-    int64_t planes, total;           // bytes
+    int64_t m, n;               // shorter and longer side, of whole tiles
+    int64_t X[2], Xt[2], A, B;  // planes of a matrix, in halves
+    int64_t stride;             // halves
+    int64_t planes, total;      // bytes
 };
 NsLayout ns_layout(int64_t rows, int64_t cols, int64_t count)
 {
@@ -253,9 +350,9 @@ NsLayout ns_layout(int64_t rows, int64_t cols, int64_t count)
     l.m = (std::min(rows, cols) + kTile - 1) / kTile * kTile;
     l.n = (std::max(rows, cols) + kTile - 1) / kTile * kTile;
     int64_t at = 0;
-    for (int i = 0; i < 2; ++i) l.X[i] = at, l.Xt[i] = at + l.m * l.n, at += 2 * l.m * l.n;
-    l.A = at, l.B = at + l.m * l.m, at += 2 * l.m * l.m;
-    l.lo = at, l.stride = 2 * at;
+    for (int i = 0; i < 2; ++i) l.X[i] = at, l.Xt[i] = at + 2 * l.m * l.n, at += 4 * l.m * l.n;
+    l.A = at, l.B = at + 2 * l.m * l.m, at += 4 * l.m * l.m;
+    l.stride = at;
     l.planes = (count * kNormBlocks * 8 + 255) / 256 * 256;
     l.total = l.planes + count * l.stride * 2;
     return l;
@@ -280,18 +377,43 @@ gp_status check_shape(int64_t rows, int64_t cols, int64_t count)
     return GP_OK;
 }
 
-template <bool LAST>
-gp_status launch_product(const Product& a, int64_t rows, int64_t cols, int64_t count, gp_dtype dtype, hipStream_t stream)
+template <int BM, int BN, int WM, int WN, typename TO, bool LAST>
+gp_status launch_tiles(Product a, int64_t count, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(cols / kTile), (unsigned)(rows / kTile), (unsigned)count);
+    constexpr size_t lds = 2 * (BM + BN) * 128;
+    if constexpr (lds > 65536) {  // above what a kernel gets by default: asked for once per device
+        static std::atomic<uint64_t> done{0};
+        int dev = 0;
+        GP_HIP(hipGetDevice(&dev));
+        if (dev < 0 || dev >= 64) return fail(GP_ERR_UNSUPPORTED, "device ordinal %d not supported", dev);
+        if (!(done.load(std::memory_order_acquire) >> dev & 1)) {
+            GP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gp_ns_product<BM, BN, WM, WN, TO, LAST>),
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+            done.fetch_or(UINT64_C(1) << dev, std::memory_order_release);
+        }
+    }
+    const int64_t tm = (a.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
+    a.tiles_n = (int)tn;
+    const dim3 grid((unsigned)(a.symmetric ? tn * (tn + 1) / 2 : tm * tn), 1, (unsigned)count);
     profile_begin("gp_ns_product", stream);
-    if (LAST && dtype == GP_BF16)
-        hipLaunchKernelGGL((gp_ns_product<bf16_t, LAST>), grid, dim3(kThreads), 0, stream, a);
-    else
-        hipLaunchKernelGGL((gp_ns_product<float, LAST>), grid, dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((gp_ns_product<BM, BN, WM, WN, TO, LAST>), grid, dim3(64 * WM * WN), lds, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     return GP_OK;
+}
+
+template <typename TO, bool LAST>
+gp_status launch_product(const Product& a, int64_t count, hipStream_t stream)
+{
+    // the largest tiles of which there are enough for three quarters of the 256 compute units
+    auto enough = [&](int64_t side) {
+        const int64_t tm = (a.M + side - 1) / side, tn = (a.N + side - 1) / side;
+        return (a.symmetric ? tn * (tn + 1) / 2 : tm * tn) * count >= 192;
+    };
+    const int side = enough(256) ? 256 : enough(128) ? 128 : 64;
+    if (side == 256) return launch_tiles<256, 256, 2, 4, TO, LAST>(a, count, stream);
+    if (side == 128) return launch_tiles<128, 128, 2, 2, TO, LAST>(a, count, stream);
+    return launch_tiles<64, 64, 2, 2, TO, LAST>(a, count, stream);
 }
 
 // out: the direction itself (W null, of dtype out_dtype), or the stepped weights
@@ -330,9 +452,9 @@ gp_status newton_schulz(const Update& u, gp_dtype dtype, int64_t count, int32_t 
         const float scale = std::ldexp(1.0f, ex[0]);
         profile_begin("gp_ns_start", stream);
         if (dtype == GP_F32)
-            hipLaunchKernelGGL(gp_ns_start<float>, grid, dim3(kThreads), 0, stream, u, partial, eps, scale, natural, transposed, l.lo, l.stride, (int)pc, (int)pr);
+            hipLaunchKernelGGL(gp_ns_start<float>, grid, dim3(kThreads), 0, stream, u, partial, eps, scale, natural, transposed, l.stride, 2 * (int)pc, 2 * (int)pr);
         else
-            hipLaunchKernelGGL(gp_ns_start<bf16_t>, grid, dim3(kThreads), 0, stream, u, partial, eps, scale, natural, transposed, l.lo, l.stride, (int)pc, (int)pr);
+            hipLaunchKernelGGL(gp_ns_start<bf16_t>, grid, dim3(kThreads), 0, stream, u, partial, eps, scale, natural, transposed, l.stride, 2 * (int)pc, 2 * (int)pr);
         profile_end(stream);
         GP_HIP(hipGetLastError());
     }
@@ -341,30 +463,30 @@ gp_status newton_schulz(const Update& u, gp_dtype dtype, int64_t count, int32_t 
         const float* const p = coeff ? coeff + 3 * k : kDefaultCoeff;
         f16 *const X = ws + l.X[k & 1], *const Xt = ws + l.Xt[k & 1], *const A = ws + l.A, *const B = ws + l.B;
         Product a{};
-        a.lo = l.lo, a.stride = l.stride;
-        a.P = a.Q = X, a.ldp = a.ldq = n, a.K = n;
+        a.stride = l.stride;
+        a.P = a.Q = X, a.ldp = a.ldq = 2 * n, a.M = a.N = m, a.K = n;
         a.alpha = std::ldexp(1.0f, ea[k] - 2 * ex[k]);
-        a.D = a.Dt = A, a.ldd = a.lddt = m, a.symmetric = 1;
-        gp_status st = launch_product<false>(a, m, m, count, GP_F32, stream);
+        a.D = a.Dt = A, a.ldd = a.lddt = 2 * m, a.symmetric = 1;
+        gp_status st = launch_product<float, false>(a, count, stream);
         if (st != GP_OK) return st;
-        a.P = a.Q = a.E = A, a.ldp = a.ldq = a.lde = m, a.K = m;
+        a.P = a.Q = a.E = A, a.ldp = a.ldq = a.lde = 2 * m, a.K = m;
         a.alpha = std::ldexp(p[2], eb[k] - 2 * ea[k]), a.beta = std::ldexp(p[1], eb[k] - ea[k]);
         a.D = a.Dt = B;
-        if ((st = launch_product<false>(a, m, m, count, GP_F32, stream)) != GP_OK) return st;
+        if ((st = launch_product<float, false>(a, count, stream)) != GP_OK) return st;
         a.symmetric = 0;
-        const bool last = k == steps - 1;
-        const int next = last ? 0 : ex[k + 1] - ex[k];
-        if (!last) {
-            a.P = B, a.ldp = m, a.Q = Xt, a.ldq = m, a.E = X, a.lde = n, a.K = m;
+        if (k < steps - 1) {
+            const int next = ex[k + 1] - ex[k];
+            a.P = B, a.Q = Xt, a.N = n, a.E = X, a.lde = 2 * n;
             a.alpha = std::ldexp(1.0f, next - eb[k]), a.beta = std::ldexp(p[0], next);
-            a.D = ws + l.X[(k + 1) & 1], a.ldd = n, a.Dt = ws + l.Xt[(k + 1) & 1], a.lddt = m;
-            if ((st = launch_product<false>(a, m, n, count, GP_F32, stream)) != GP_OK) return st;
+            a.D = ws + l.X[(k + 1) & 1], a.ldd = 2 * n, a.Dt = ws + l.Xt[(k + 1) & 1], a.lddt = 2 * m;
+            if ((st = launch_product<float, false>(a, count, stream)) != GP_OK) return st;
         } else {  // in the orientation of the caller's matrix
-            a.P = tall ? Xt : B, a.Q = tall ? B : Xt, a.ldp = a.ldq = m, a.K = m;
-            a.E = tall ? Xt : X, a.lde = tall ? m : n;
+            a.P = tall ? Xt : B, a.Q = tall ? B : Xt, a.M = tall ? n : m, a.N = tall ? m : n;
+            a.E = tall ? Xt : X, a.lde = tall ? 2 * m : 2 * n;
             a.alpha = std::ldexp(1.0f, -ex[k] - eb[k]), a.beta = std::ldexp(p[0], -ex[k]);
             a.rows = u.rows, a.cols = u.cols, a.out = out, a.ldo = ldo, a.stride_o = stride_o, a.W = W, a.keep = keep, a.lr = lr;
-            if ((st = launch_product<true>(a, tall ? n : m, tall ? m : n, count, out_dtype, stream)) != GP_OK) return st;
+            st = out_dtype == GP_F32 ? launch_product<float, true>(a, count, stream) : launch_product<bf16_t, true>(a, count, stream);
+            if (st != GP_OK) return st;
         }
     }
     return GP_OK;
