@@ -139,23 +139,203 @@ gp_status launch_lookup(const LookupArgs& a, hipStream_t stream)
 
 // ---- gradient -----------------------------------------------------------------------------------------
 
-// a sorted list's entry: token << 32 | position; a token that names no row counts as V, behind all that do
-__global__ __launch_bounds__(kThreads) void gp_token_keys(const void* __restrict__ tokens, int wide, int64_t N, int64_t V, uint64_t* __restrict__ keys)
+// The sort: least significant digit first, digits of up to 11 bits of the token, equal digits keep their order.  An entry is
+// token << 32 | position; a token that names no row counts as V, behind all that do.  A pass of a long list: (1) every workgroup counts
+// the digits of its tile of consecutive entries, (2) one wavefront per digit adds up the tiles before each tile, (3) every workgroup
+// ranks its tile's entries -- a wavefront takes 64 at a time, finds the lanes with its own digit by one ballot per bit, and
+// keeps counts of its own in LDS, so that no barrier stands between its steps -- and writes each to its place.
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMaxDigits = 2048;
+
+struct SortArgs {
+    const void* tokens;    // the first pass reads these,
+    int wide;
+    const uint64_t* keys;  // the others these
+    uint64_t* out;
+    int64_t N, V;
+    int shift, bits;       // the digit
+    int64_t tiles;
+    uint32_t* table;       // [digit][tile]
+    uint32_t* totals;      // [digit]
+};
+
+__device__ __forceinline__ uint64_t entry_of(int64_t token, int64_t i, int64_t V)
 {
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < N; i += (int64_t)gridDim.x * kThreads) {
-        const int64_t t = token_at(tokens, wide, i);
-        keys[i] = (uint64_t)(t >= 0 && t < V ? t : V) << 32 | (uint64_t)i;
+    return (uint64_t)(token >= 0 && token < V ? token : V) << 32 | (uint64_t)i;
+}
+template <bool FIRST>
+__device__ __forceinline__ uint64_t entry_at(const SortArgs& a, int64_t i)
+{
+    if constexpr (FIRST)
+        return entry_of(token_at(a.tokens, a.wide, i), i, a.V);
+    else
+        return a.keys[i];
+}
+
+// lanes of the wavefront that are valid and hold the same digit
+__device__ __forceinline__ unsigned long long peers_of(unsigned digit, int bits, bool valid)
+{
+    unsigned long long peers = __ballot(valid);
+    for (int b = 0; b < bits; ++b) {
+        const bool bit = (digit >> b) & 1u;
+        const unsigned long long with = __ballot(bit);
+        peers &= bit ? with : ~with;
+    }
+    return peers;
+}
+
+// Ranks a wavefront's next 64 entries among its own; count: the wavefront's digit counts in LDS (volatile: its lanes hand them on
+// without a barrier).
+__device__ __forceinline__ uint32_t rank_in_wave(volatile uint16_t* count, unsigned digit, int bits, bool valid, int lane)
+{
+    const unsigned long long peers = peers_of(digit, bits, valid);
+    const uint32_t before = (uint32_t)__popcll(peers & ((1ull << lane) - 1ull));
+    uint32_t r = 0;
+    if (valid) {
+        r = count[digit] + before;
+        if (before == 0) count[digit] = (uint16_t)(r + (uint32_t)__popcll(peers));
+    }
+    __builtin_amdgcn_wave_barrier();
+    return r;
+}
+
+// exclusive prefix of v over the workgroup's threads; part: kSortWaves words of LDS
+__device__ __forceinline__ uint32_t exclusive_1024(uint32_t v, uint32_t* part)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t incl = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t up = __shfl_up(incl, o, 64);
+        if (lane >= o) incl += up;
+    }
+    __syncthreads();
+    if (lane == 63) part[wave] = incl;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int w = 0; w < wave; ++w) before += part[w];
+    return before + incl - v;
+}
+
+template <int ITEMS, bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void gp_token_count(SortArgs a)
+{
+    __shared__ uint32_t h[kMaxDigits];
+    const int digits = 1 << a.bits;
+    for (int i = threadIdx.x; i < digits; i += kSortThreads) h[i] = 0;
+    __syncthreads();
+    const int64_t t0 = (int64_t)blockIdx.x * (ITEMS * kSortThreads);
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+        const int64_t i = t0 + j * kSortThreads + threadIdx.x;
+        if (i < a.N) atomicAdd(&h[(unsigned)(entry_at<FIRST>(a, i) >> a.shift) & (digits - 1)], 1u);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < digits; i += kSortThreads) a.table[i * a.tiles + blockIdx.x] = h[i];
+}
+
+__global__ __launch_bounds__(kThreads) void gp_token_prefix(SortArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t digit = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    if (digit >= 1 << a.bits) return;
+    uint32_t* const row = a.table + digit * a.tiles;
+    uint32_t run = 0;
+    for (int64_t t0 = 0; t0 < a.tiles; t0 += 64) {
+        const int64_t t = t0 + lane;
+        const uint32_t v = t < a.tiles ? row[t] : 0;
+        uint32_t incl = v;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t up = __shfl_up(incl, o, 64);
+            if (lane >= o) incl += up;
+        }
+        if (t < a.tiles) row[t] = run + incl - v;
+        run += __shfl(incl, 63, 64);
+    }
+    if (lane == 0) a.totals[digit] = run;
+}
+
+// LDS of a scatter: where the workgroup's first entry of each digit goes, and counts [wave][digit], at first of the wavefront's own entries,
+// then of those in the wavefronts before it (a tile has fewer than 2^16).
+constexpr size_t scatter_lds(int digits) { return (size_t)digits * (4 + 2 * kSortWaves) + kSortWaves * 4; }
+
+template <int ITEMS, bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void gp_token_scatter(SortArgs a)
+{
+    extern __shared__ __align__(16) uint32_t sort_lds[];
+    const int digits = 1 << a.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t *const part = sort_lds, *const base = part + kSortWaves;
+    uint16_t* const count = (uint16_t*)(base + digits);
+    for (int i = threadIdx.x; i < kSortWaves / 2 * digits; i += kSortThreads) ((uint32_t*)count)[i] = 0;
+    // where each digit begins: thread t looks after digits per t .. per t + per - 1
+    const int per = (digits + kSortThreads - 1) / kSortThreads, d0 = threadIdx.x * per;
+    uint32_t mine = 0;
+    for (int j = 0; j < per; ++j)
+        if (d0 + j < digits) mine += a.totals[d0 + j];
+    uint32_t begin = exclusive_1024(mine, part);
+    for (int j = 0; j < per; ++j)
+        if (d0 + j < digits) base[d0 + j] = begin + a.table[(d0 + j) * a.tiles + blockIdx.x], begin += a.totals[d0 + j];
+    __syncthreads();
+    uint64_t key[ITEMS];
+    uint32_t rank[ITEMS];
+    const int64_t w0 = (int64_t)blockIdx.x * (ITEMS * kSortThreads) + wave * (ITEMS * 64) + lane;
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) key[j] = w0 + j * 64 < a.N ? entry_at<FIRST>(a, w0 + j * 64) : 0;
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j)
+        rank[j] = rank_in_wave(count + wave * digits, (unsigned)(key[j] >> a.shift) & (digits - 1), a.bits, w0 + j * 64 < a.N, lane);
+    __syncthreads();
+    for (int d = threadIdx.x; d < digits; d += kSortThreads) {
+        uint32_t n[kSortWaves], before = 0;
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) n[w] = count[w * digits + d];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) count[w * digits + d] = (uint16_t)before, before += n[w];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+        if (w0 + j * 64 >= a.N) continue;
+        const unsigned digit = (unsigned)(key[j] >> a.shift) & (digits - 1);
+        const int64_t place = (int64_t)base[digit] + count[wave * digits + digit] + rank[j];
+        if (place < a.N) a.out[place] = key[j];  // (always true)
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void gp_zero_rows(T* __restrict__ p, int64_t ld, int64_t rows, int d)
+// A short list takes its places by counting, for every entry, those that are smaller (entries are all different): N^2 comparisons,
+// but one launch.  A workgroup ranks 64 entries, one per lane, against the whole list in LDS, a sixteenth of it per wavefront.
+constexpr int64_t kShortList = 8192;
+
+__global__ __launch_bounds__(kSortThreads) void gp_token_rank(SortArgs a)
 {
-    const int64_t total = rows * d;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
-        const int64_t r = i / d;
-        p[r * ld + (i - r * d)] = 0;
+    __shared__ __align__(16) uint32_t list[kShortList];
+    __shared__ uint32_t smaller[kSortWaves][64];
+    const int N = (int)a.N, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int each = (N + kSortWaves * 4 - 1) / (kSortWaves * 4) * 4;  // tokens per wavefront
+    for (int i = threadIdx.x; i < each * kSortWaves; i += kSortThreads) list[i] = i < N ? (uint32_t)(entry_at<true>(a, i) >> 32) : 0xFFFFFFFFu;
+    __syncthreads();
+    const int i = blockIdx.x * 64 + lane;
+    const uint32_t own = i < N ? list[i] : 0;
+    uint32_t n = 0;
+    const int j0 = wave * each, j1 = j0 + each, i0 = blockIdx.x * 64;
+    // before this workgroup's entries an equal token is the smaller entry, behind them it is not
+    int j = j0;
+    for (; j < min(j1, i0); j += 4) {
+        const uint4 t = *(const uint4*)(list + j);
+        n += (t.x <= own) + (t.y <= own) + (t.z <= own) + (t.w <= own);
     }
+    for (; j < min(j1, i0 + 64); ++j) n += list[j] < own || (list[j] == own && j < i);
+    for (; j < j1; j += 4) {
+        const uint4 t = *(const uint4*)(list + j);
+        n += (t.x < own) + (t.y < own) + (t.z < own) + (t.w < own);
+    }
+    smaller[wave][lane] = n;
+    __syncthreads();
+    if (wave > 0 || i >= N) return;
+    uint32_t place = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) place += smaller[w][lane];
+    if (place < (uint32_t)N) a.out[place] = (uint64_t)own << 32 | (uint64_t)i;  // (always true)
 }
 
 struct GradArgs {
@@ -195,6 +375,9 @@ __device__ __forceinline__ void finish(const GradArgs& a, int64_t v, int c, cons
     }
 }
 
+// rows of zeros: those of a gap in the tokens that is at most kGap rows long are written beside the run behind it, others by gp_join_tiles
+constexpr int64_t kGap = 256;
+
 // G lanes walk one tile; a lane holds one vector of the sums.
 template <typename TG, typename TO, int VEC, int G>
 __global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
@@ -210,6 +393,11 @@ __global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
     float acc[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
+    auto fill_gap = [&](int64_t before, int64_t token) {
+        if (a.accumulate || token >= a.V || token - before > kGap + 1) return;
+        for (int64_t r = before + 1; r < token; ++r) store_vec<TO, VEC>((TO*)a.out + r * a.ldt + min(c * VEC, a.d - VEC), acc);
+    };
+    if (lo > 0 && !came_in) fill_gap((int64_t)(a.keys[lo - 1] >> 32), cur);
     for (int64_t p = lo; p < hi; p += U) {
         uint64_t key[U];
         float v[U][VEC];
@@ -230,9 +418,10 @@ __global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
                     store_vec<float, VEC>(a.carry + ((2 * t) * a.nvec + c) * VEC, acc);
                 else
                     finish<TO, VEC>(a, cur, c, acc);
-                cur = tok, came_in = false;
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
+                fill_gap(cur, tok);
+                cur = tok, came_in = false;
             }
 #pragma unroll
             for (int i = 0; i < VEC; ++i) acc[i] += v[u][i];
@@ -247,45 +436,150 @@ __global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
         finish<TO, VEC>(a, cur, c, acc);
 }
 
-// One workgroup per tile in which a run begins that goes on: its partial rows, added up in the order of (tile mod groups,
-// tile), then over the groups.
+// the first place of the sorted list whose token is not below v, by all lanes of a wavefront (64 probes a round)
+__device__ __forceinline__ int64_t first_not_below(const uint64_t* keys, int64_t N, int64_t v, int lane)
+{
+    int64_t lo = 0, n = N;  // it lies in lo .. lo + n
+    while (n > 0) {
+        const int64_t step = (n + 64) / 65, p = lo + (lane + 1) * step - 1;
+        const int below = __popcll(__ballot(p < lo + n && (int64_t)(keys[p < lo + n ? p : lo] >> 32) < v));
+        lo += below * step, n = below == 64 ? n - 64 * step : min(step - 1, n - below * step);
+    }
+    return lo;
+}
+
+// zeros in rows [r, end), by the lanes of a wavefront
+template <typename TO>
+__device__ __forceinline__ void zero_rows(const GradArgs& a, int64_t r, int64_t end, int lane)
+{
+    constexpr int N = 16 / sizeof(TO);
+    float zero[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) zero[i] = 0.0f;
+    const bool whole = a.ldt == a.d;  // one stretch
+    const int64_t len = whole ? max((end - r) * a.d, (int64_t)0) : a.d;
+    for (; r < end; r = whole ? end : r + 1) {
+        TO* const p = (TO*)a.out + r * a.ldt;
+        for (int64_t i = (int64_t)lane * N; i + N <= len; i += 64 * N) store_vec<TO, N>(p + i, zero);
+        const int64_t i = len - len % N + lane;
+        if (i < len) p[i] = 0;
+    }
+}
+
+template <typename TO>
+__global__ __launch_bounds__(kThreads) void gp_zero_table(GradArgs a)
+{
+    constexpr int kWaves = kThreads / 64;
+    const int64_t per = (a.V + gridDim.x * kWaves - 1) / (gridDim.x * kWaves), r0 = ((int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6)) * per;
+    zero_rows<TO>(a, min(r0, a.V), min(r0 + per, a.V), threadIdx.x & 63);
+}
+
+// Wavefronts behind the tiles' workgroups look after kGap rows each: a gap of more than kGap rows, or one before the first token or behind
+// the last, covers at most the rows up to the first token among them and those behind the last.
+template <typename TO>
+__device__ __forceinline__ void fill_long_gaps(const GradArgs& a, int64_t chunk, int lane)
+{
+    const int64_t r0 = chunk * kGap, r1 = min(r0 + kGap, a.V);
+    if (r0 >= a.V) return;
+    const int64_t p = first_not_below(a.keys, a.N, r0, lane), q = first_not_below(a.keys, a.N, r1, lane);
+    const int64_t before = p > 0 ? (int64_t)(a.keys[p - 1] >> 32) : -1, first = p < a.N ? min((int64_t)(a.keys[p] >> 32), a.V) : a.V;
+    if (p == 0 || first == a.V || first - before > kGap + 1) zero_rows<TO>(a, r0, min(first, r1), lane);
+    if (first >= r1) return;
+    const int64_t last = (int64_t)(a.keys[q - 1] >> 32), next = q < a.N ? min((int64_t)(a.keys[q] >> 32), a.V) : a.V;
+    if (next == a.V || next - last > kGap + 1) zero_rows<TO>(a, last + 1, r1, lane);
+}
+
+// Runs that go on into other tiles.  G lanes look at one tile: where such a run begins in it, its partial rows are added up in tile order;
+// a run of more than kShortRun further tiles is left to the whole workgroup, whose groups take every kGroups-th tile each.
+constexpr int kShortRun = 8;
+
 template <typename TO, int VEC, int G>
-__global__ __launch_bounds__(kThreads) void gp_join_tiles(GradArgs a)
+__global__ __launch_bounds__(kThreads) void gp_join_tiles(GradArgs a, int64_t tile_blocks)
 {
     constexpr int kGroups = kThreads / G;
     __shared__ float part[kThreads][VEC];
-    const int64_t t = blockIdx.x;
-    const int64_t lo = t * a.tile, hi = min(lo + a.tile, a.N);
-    const int64_t tok = (int64_t)(a.keys[hi - 1] >> 32);
-    if (tok >= a.V || hi >= a.N || (int64_t)(a.keys[hi] >> 32) != tok) return;                   // nothing goes on
-    if (lo > 0 && (int64_t)(a.keys[lo - 1] >> 32) == tok) return;                                // it began before
-    int64_t first = t + 1, last = a.tiles;  // the first tile whose list does not start with the token: between these
-    while (first < last) {
-        const int64_t mid = (first + last) / 2;
-        if ((int64_t)(a.keys[mid * a.tile] >> 32) == tok) first = mid + 1;
-        else last = mid;
+    __shared__ int64_t longer[kGroups];
+    __shared__ int longer_count;
+    if (blockIdx.x >= tile_blocks) {
+        if (blockIdx.y == 0) fill_long_gaps<TO>(a, (blockIdx.x - tile_blocks) * (kThreads / 64) + (threadIdx.x >> 6), threadIdx.x & 63);
+        return;
     }
+    if (threadIdx.x == 0) longer_count = 0;
+    __syncthreads();
     const int g = threadIdx.x / G, c = blockIdx.y * G + threadIdx.x % G;
-    float acc[VEC];
+    const int64_t row = (int64_t)a.nvec * VEC, at = (int64_t)c * VEC;  // floats of a partial row; this lane's place in it
+    const int64_t t = (int64_t)blockIdx.x * kGroups + g, lo = t * a.tile, hi = lo + a.tile;
+    if (hi < a.N) {
+        const int64_t tok = (int64_t)(a.keys[hi - 1] >> 32);
+        const bool begins = lo == 0 || (int64_t)(a.keys[lo - 1] >> 32) != tok;
+        if (tok < a.V && begins && (int64_t)(a.keys[hi] >> 32) == tok) {
+            int more = 0;  // tiles that start with the token
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
-    if (c < a.nvec) {
-        if (g == 0) load_vec<float, VEC>(a.carry + ((2 * t + 1) * a.nvec + c) * VEC, acc);
-        for (int64_t s = t + 1 + g; s < last; s += kGroups) {
-            float v[VEC];
-            load_vec<float, VEC>(a.carry + ((2 * s) * a.nvec + c) * VEC, v);
+            for (int i = 0; i <= kShortRun; ++i) {
+                const int64_t p = hi + i * a.tile;
+                more += p < a.N && (int64_t)(a.keys[p] >> 32) == tok;
+            }
+            if (more > kShortRun) {
+                if (threadIdx.x % G == 0) longer[atomicAdd(&longer_count, 1)] = t;
+            } else if (c < a.nvec) {
+                float acc[VEC], v[kShortRun][VEC];
+                load_vec<float, VEC>(a.carry + (2 * t + 1) * row + at, acc);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) acc[i] += v[i];
+                for (int i = 0; i < kShortRun; ++i) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) v[i][e] = 0.0f;
+                    if (i < more) load_vec<float, VEC>(a.carry + 2 * (t + 1 + i) * row + at, v[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < kShortRun; ++i)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        if (i < more) acc[e] += v[i][e];
+                finish<TO, VEC>(a, tok, c, acc);
+            }
         }
     }
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) part[threadIdx.x][i] = acc[i];
     __syncthreads();
-    if (g > 0 || c >= a.nvec) return;
-    for (int o = 1; o < kGroups; ++o)
+    const int count = longer_count;
+    for (int k = 0; k < count; ++k) {
+        const int64_t t = longer[k];
+        const int64_t tok = (int64_t)(a.keys[t * a.tile + a.tile - 1] >> 32);
+        int64_t first = t + 1, last = a.tiles;  // the first tile whose list does not start with the token: between these
+        while (first < last) {
+            const int64_t mid = (first + last) / 2;
+            if ((int64_t)(a.keys[mid * a.tile] >> 32) == tok) first = mid + 1;
+            else last = mid;
+        }
+        float acc[VEC];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) acc[i] += part[o * G + threadIdx.x][i];
-    finish<TO, VEC>(a, tok, c, acc);
+        for (int e = 0; e < VEC; ++e) acc[e] = 0.0f;
+        if (c < a.nvec) {
+            if (g == 0) load_vec<float, VEC>(a.carry + (2 * t + 1) * row + at, acc);
+            constexpr int U = 8;
+            for (int64_t s = t + 1 + g; s < last; s += U * kGroups) {
+                float v[U][VEC];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) v[u][e] = 0.0f;
+                    if (s + u * kGroups < last) load_vec<float, VEC>(a.carry + 2 * (s + u * kGroups) * row + at, v[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) acc[e] += v[u][e];
+            }
+        }
+        __syncthreads();  // (the run before is read to its end)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) part[threadIdx.x][e] = acc[e];
+        __syncthreads();
+        if (g > 0 || c >= a.nvec) continue;
+        for (int o = 1; o < kGroups; ++o)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) acc[e] += part[o * G + threadIdx.x][e];
+        finish<TO, VEC>(a, tok, c, acc);
+    }
 }
 
 template <typename TG, typename TO, int VEC, int G>
@@ -297,9 +591,11 @@ gp_status launch_sums(const GradArgs& a, hipStream_t stream)
     hipLaunchKernelGGL((gp_sum_tiles<TG, TO, VEC, G>), dim3((unsigned)((a.tiles + per - 1) / per), ny), dim3(kThreads), 0, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
-    if (a.tiles > 1) {
+    const int64_t fills = a.accumulate ? 0 : ((a.V + kGap - 1) / kGap + kThreads / 64 - 1) / (kThreads / 64);
+    if (a.tiles > 1 || fills > 0) {
         profile_begin("gp_join_tiles", stream);
-        hipLaunchKernelGGL((gp_join_tiles<TO, VEC, G>), dim3((unsigned)a.tiles, ny), dim3(kThreads), 0, stream, a);
+        const int64_t tile_blocks = (a.tiles + per - 1) / per;
+        hipLaunchKernelGGL((gp_join_tiles<TO, VEC, G>), dim3((unsigned)(tile_blocks + fills), ny), dim3(kThreads), 0, stream, a, tile_blocks);
         profile_end(stream);
         GP_HIP(hipGetLastError());
     }
@@ -322,7 +618,7 @@ gp_status launch_sums(const GradArgs& a, hipStream_t stream)
 }
 
 // Tiles: equal lengths; enough of them to fill the chip, few enough that the partial rows of one token are added up fast.
-constexpr int64_t kMinTile = 16, kMaxTiles = 16384;
+constexpr int64_t kMinTile = 4, kMaxTiles = 16384;
 int64_t tile_length(int64_t N) { return std::max(kMinTile, (N + kMaxTiles - 1) / kMaxTiles); }
 
 int bits_of(int64_t v)
@@ -332,19 +628,83 @@ int bits_of(int64_t v)
     return b;
 }
 
-struct GradLayout {
-    int64_t other, scratch, carry, total;
+// the digits of tokens 0 .. V (V: those that name no row)
+struct SortPlan {
+    int passes, bits, items;
+    int64_t tiles;
 };
-GradLayout grad_layout(int64_t N, int32_t d)
+SortPlan sort_plan(int64_t N, int64_t V)
+{
+    SortPlan p;
+    const int all = bits_of(V);
+    p.passes = (all + 10) / 11, p.bits = (all + p.passes - 1) / p.passes;
+    p.items = N <= (1 << 20) ? 4 : 8;
+    p.tiles = (N + p.items * kSortThreads - 1) / (p.items * kSortThreads);
+    return p;
+}
+
+struct GradLayout {
+    int64_t other, table, totals, carry, total;
+};
+GradLayout grad_layout(int64_t N, int64_t V, int32_t d)
 {
     auto up = [](int64_t b) { return (b + 255) / 256 * 256; };
     const int64_t tiles = (N + tile_length(N) - 1) / tile_length(N);
+    const SortPlan p = sort_plan(N, V);
     GradLayout l;
     l.other = up(8 * N);
-    l.scratch = l.other + up(8 * N);
-    l.carry = l.scratch + up((int64_t)device_sort_scratch_words(N) * 4);
+    l.table = l.other + up(N <= kShortList ? 0 : 8 * N);
+    l.totals = l.table + up(N <= kShortList ? 0 : (p.tiles << p.bits) * 4);
+    l.carry = l.totals + up(N <= kShortList ? 0 : (4 << p.bits));
     l.total = l.carry + up(2 * tiles * (((int64_t)d + 7) / 8 * 8) * 4);
     return l;
+}
+
+template <int ITEMS, bool FIRST>
+gp_status launch_pass(const SortArgs& a, hipStream_t stream)
+{
+    const size_t lds = scatter_lds(1 << a.bits);
+    gp_status st = raise_lds<&gp_token_scatter<ITEMS, FIRST>>(scatter_lds(kMaxDigits));
+    if (st != GP_OK) return st;
+    profile_begin("gp_token_count", stream);
+    hipLaunchKernelGGL((gp_token_count<ITEMS, FIRST>), dim3((unsigned)a.tiles), dim3(kSortThreads), 0, stream, a);
+    profile_end(stream);
+    profile_begin("gp_token_prefix", stream);
+    hipLaunchKernelGGL(gp_token_prefix, dim3((unsigned)(((1 << a.bits) + 3) / 4)), dim3(kThreads), 0, stream, a);
+    profile_end(stream);
+    profile_begin("gp_token_scatter", stream);
+    hipLaunchKernelGGL((gp_token_scatter<ITEMS, FIRST>), dim3((unsigned)a.tiles), dim3(kSortThreads), lds, stream, a);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    return GP_OK;
+}
+
+// *sorted: whichever of the two lists of the workspace holds the result
+gp_status sort_tokens(const void* tokens, int wide, int64_t N, int64_t V, char* ws, const GradLayout& l, hipStream_t stream, const uint64_t** sorted)
+{
+    const SortPlan p = sort_plan(N, V);
+    SortArgs a{};
+    a.tokens = tokens, a.wide = wide, a.N = N, a.V = V, a.bits = p.bits, a.tiles = p.tiles;
+    a.table = (uint32_t*)(ws + l.table), a.totals = (uint32_t*)(ws + l.totals);
+    a.shift = 32;
+    if (N <= kShortList) {
+        a.out = (uint64_t*)ws;
+        profile_begin("gp_token_rank", stream);
+        hipLaunchKernelGGL(gp_token_rank, dim3((unsigned)((N + 63) / 64)), dim3(kSortThreads), 0, stream, a);
+        profile_end(stream);
+        GP_HIP(hipGetLastError());
+        *sorted = a.out;
+        return GP_OK;
+    }
+    uint64_t* lists[2] = {(uint64_t*)ws, (uint64_t*)(ws + l.other)};
+    for (int pass = 0; pass < p.passes; ++pass) {
+        a.shift = 32 + pass * p.bits, a.keys = lists[(pass + 1) & 1], a.out = lists[pass & 1];
+        gp_status st = p.items == 4 ? (pass == 0 ? launch_pass<4, true>(a, stream) : launch_pass<4, false>(a, stream))
+                                    : (pass == 0 ? launch_pass<8, true>(a, stream) : launch_pass<8, false>(a, stream));
+        if (st != GP_OK) return st;
+    }
+    *sorted = a.out;
+    return GP_OK;
 }
 
 constexpr int64_t kMaxCount = (INT64_C(1) << 31) - 1;
@@ -376,29 +736,26 @@ gp_status embedding_grad(const void* tokens, gp_index index, int64_t N, const vo
     if (N < 0 || V < 1 || d < 1 || ldg < d || ldt < d) return fail(GP_ERR_INVALID_ARG, "need N >= 0, V >= 1, d >= 1, ldg >= d, ldt >= d");
     if (N > kMaxCount || V > kMaxCount) return fail(GP_ERR_UNSUPPORTED, "more than 2^31 - 1 tokens or rows");
     if (!out || (N > 0 && (!tokens || !up))) return fail(GP_ERR_INVALID_ARG, "NULL argument");
-    const GradLayout l = grad_layout(N, d);
+    const GradLayout l = grad_layout(N, V, d);
     if (N > 0 && (!workspace || bytes < l.total || (uintptr_t)workspace % 256 != 0))
         return fail(GP_ERR_INVALID_ARG, "need a workspace of %lld bytes on a 256-byte boundary", (long long)l.total);
-    if (!accumulate) {
-        const unsigned grid = (unsigned)std::min<int64_t>((V * d + kThreads - 1) / kThreads, 256 * 16);
-        profile_begin("gp_zero_rows", stream);
+    if (N == 0) {
+        if (accumulate) return GP_OK;
+        const unsigned grid = (unsigned)std::min<int64_t>((V + 3) / 4, 256 * 16);
+        GradArgs a{};
+        a.V = V, a.d = d, a.out = out, a.ldt = ldt;
+        profile_begin("gp_zero_table", stream);
         if (out_dtype == GP_F32)
-            hipLaunchKernelGGL(gp_zero_rows<float>, dim3(grid), dim3(kThreads), 0, stream, (float*)out, ldt, V, d);
+            hipLaunchKernelGGL(gp_zero_table<float>, dim3(grid), dim3(kThreads), 0, stream, a);
         else
-            hipLaunchKernelGGL(gp_zero_rows<bf16_t>, dim3(grid), dim3(kThreads), 0, stream, (bf16_t*)out, ldt, V, d);
+            hipLaunchKernelGGL(gp_zero_table<bf16_t>, dim3(grid), dim3(kThreads), 0, stream, a);
         profile_end(stream);
         GP_HIP(hipGetLastError());
+        return GP_OK;
     }
-    if (N == 0) return GP_OK;
     char* const ws = (char*)workspace;
-    uint64_t* const keys = (uint64_t*)ws;
-    profile_begin("gp_token_keys", stream);
-    hipLaunchKernelGGL(gp_token_keys, dim3((unsigned)std::min<int64_t>((N + kThreads - 1) / kThreads, 256 * 16)), dim3(kThreads), 0, stream, tokens,
-                       (int)(index == GP_I64), N, V, keys);
-    profile_end(stream);
-    GP_HIP(hipGetLastError());
-    uint64_t* sorted = nullptr;
-    gp_status st = device_sort_keys(keys, (uint64_t*)(ws + l.other), N, 0, bits_of(V), (uint32_t*)(ws + l.scratch), stream, &sorted);
+    const uint64_t* sorted = nullptr;
+    gp_status st = sort_tokens(tokens, (int)(index == GP_I64), N, V, ws, l, stream, &sorted);
     if (st != GP_OK) return st;
     GradArgs a{};
     a.keys = sorted, a.N = N, a.V = V, a.tile = tile_length(N), a.tiles = (N + a.tile - 1) / a.tile, a.up = up, a.ldg = ldg, a.d = d,
@@ -420,7 +777,7 @@ extern "C" gp_status gp_embedding(const void* table, int64_t ldt, gp_dtype dtype
 extern "C" int64_t gp_embedding_grad_workspace(int64_t N, int64_t V, int32_t d)
 {
     if (N < 0 || N > gp::kMaxCount || V < 1 || V > gp::kMaxCount || d < 1) return -1;
-    return N == 0 ? 0 : gp::grad_layout(N, d).total;
+    return N == 0 ? 0 : gp::grad_layout(N, V, d).total;
 }
 
 extern "C" gp_status gp_embedding_grad(const void* tokens, gp_index index, int64_t N, const void* grad, int64_t ldg, gp_dtype dtype, int32_t d,

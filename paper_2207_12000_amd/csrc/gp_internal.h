@@ -5,6 +5,7 @@
 
 #include <sys/mman.h>
 
+#include <atomic>
 #include <cstdarg>
 #include <cstdint>
 #include <cstdlib>
@@ -28,6 +29,21 @@ gp_status fail(gp_status s, const char* fmt, ...) __attribute__((format(printf, 
             return gp::fail(e_ == hipErrorOutOfMemory ? GP_ERR_OOM_DEVICE : GP_ERR_DEVICE, \
                             "%s failed: %s", #call, hipGetErrorString(e_));               \
     } while (0)
+
+// Dynamic LDS above the 64 KB a kernel gets by default: asked for once per device (the attribute belongs to the device's copy of the kernel).
+template <auto Kernel>
+gp_status raise_lds(size_t bytes)
+{
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    GP_HIP(hipGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return fail(GP_ERR_UNSUPPORTED, "device ordinal %d not supported", dev);
+    if (!(done.load(std::memory_order_acquire) >> dev & 1)) {
+        GP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(Kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+        done.fetch_or(UINT64_C(1) << dev, std::memory_order_release);
+    }
+    return GP_OK;
+}
 
 // ---- options ------------------------------------------------------------
 struct Options {

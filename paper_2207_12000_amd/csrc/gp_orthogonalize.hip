@@ -18,7 +18,6 @@
 // Every product is taken as rows times rows (both operands consecutive along the summed dimension): A and B are symmetric,
 // and X is kept in both orientations.
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <exception>
 
@@ -381,16 +380,9 @@ template <int BM, int BN, int WM, int WN, typename TO, bool LAST>
 gp_status launch_tiles(Product a, int64_t count, hipStream_t stream)
 {
     constexpr size_t lds = 2 * (BM + BN) * 128;
-    if constexpr (lds > 65536) {  // above what a kernel gets by default: asked for once per device
-        static std::atomic<uint64_t> done{0};
-        int dev = 0;
-        GP_HIP(hipGetDevice(&dev));
-        if (dev < 0 || dev >= 64) return fail(GP_ERR_UNSUPPORTED, "device ordinal %d not supported", dev);
-        if (!(done.load(std::memory_order_acquire) >> dev & 1)) {
-            GP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gp_ns_product<BM, BN, WM, WN, TO, LAST>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-            done.fetch_or(UINT64_C(1) << dev, std::memory_order_release);
-        }
+    if constexpr (lds > 65536) {
+        gp_status st = raise_lds<&gp_ns_product<BM, BN, WM, WN, TO, LAST>>(lds);
+        if (st != GP_OK) return st;
     }
     const int64_t tm = (a.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
     a.tiles_n = (int)tn;
