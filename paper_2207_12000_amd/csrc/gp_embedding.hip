@@ -255,17 +255,22 @@ __global__ __launch_bounds__(kThreads) void gp_token_prefix(SortArgs a)
     if (lane == 0) a.totals[digit] = run;
 }
 
-// LDS of a scatter: where the workgroup's first entry of each digit goes, and counts [wave][digit], at first of the wavefront's own entries,
-// then of those in the wavefronts before it (a tile has fewer than 2^16).
-constexpr size_t scatter_lds(int digits) { return (size_t)digits * (4 + 2 * kSortWaves) + kSortWaves * 4; }
+// LDS of a scatter: what leads from an entry's place among the workgroup's to its place in the list, by digit; then counts [wave][digit],
+// at first of the wavefront's own entries, later the place of its first one (a tile has fewer than 2^16); then, over these, the
+// workgroup's entries in the new order: neighbours there are neighbours in the list, and their stores share lines.
+constexpr size_t scatter_lds(int digits, int items)
+{
+    return kSortWaves * 4 + (size_t)digits * 4 + std::max((size_t)digits * 2 * kSortWaves, (size_t)items * kSortThreads * 8);
+}
 
 template <int ITEMS, bool FIRST>
 __global__ __launch_bounds__(kSortThreads) void gp_token_scatter(SortArgs a)
 {
     extern __shared__ __align__(16) uint32_t sort_lds[];
     const int digits = 1 << a.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t *const part = sort_lds, *const base = part + kSortWaves;
-    uint16_t* const count = (uint16_t*)(base + digits);
+    uint32_t *const part = sort_lds, *const lead = part + kSortWaves;
+    uint16_t* const count = (uint16_t*)(lead + digits);
+    uint64_t* const list = (uint64_t*)count;
     for (int i = threadIdx.x; i < kSortWaves / 2 * digits; i += kSortThreads) ((uint32_t*)count)[i] = 0;
     // where each digit begins: thread t looks after digits per t .. per t + per - 1
     const int per = (digits + kSortThreads - 1) / kSortThreads, d0 = threadIdx.x * per;
@@ -274,31 +279,50 @@ __global__ __launch_bounds__(kSortThreads) void gp_token_scatter(SortArgs a)
         if (d0 + j < digits) mine += a.totals[d0 + j];
     uint32_t begin = exclusive_1024(mine, part);
     for (int j = 0; j < per; ++j)
-        if (d0 + j < digits) base[d0 + j] = begin + a.table[(d0 + j) * a.tiles + blockIdx.x], begin += a.totals[d0 + j];
+        if (d0 + j < digits) lead[d0 + j] = begin + a.table[(d0 + j) * a.tiles + blockIdx.x], begin += a.totals[d0 + j];
     __syncthreads();
     uint64_t key[ITEMS];
     uint32_t rank[ITEMS];
-    const int64_t w0 = (int64_t)blockIdx.x * (ITEMS * kSortThreads) + wave * (ITEMS * 64) + lane;
+    const int64_t t0 = (int64_t)blockIdx.x * (ITEMS * kSortThreads), w0 = t0 + wave * (ITEMS * 64) + lane;
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) key[j] = w0 + j * 64 < a.N ? entry_at<FIRST>(a, w0 + j * 64) : 0;
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j)
         rank[j] = rank_in_wave(count + wave * digits, (unsigned)(key[j] >> a.shift) & (digits - 1), a.bits, w0 + j * 64 < a.N, lane);
     __syncthreads();
-    for (int d = threadIdx.x; d < digits; d += kSortThreads) {
-        uint32_t n[kSortWaves], before = 0;
+    mine = 0;
+    for (int j = 0; j < per; ++j)
+        if (d0 + j < digits)
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) mine += count[w * digits + d0 + j];
+    begin = exclusive_1024(mine, part);
+    for (int j = 0; j < per; ++j) {
+        const int d = d0 + j;
+        if (d >= digits) break;
+        lead[d] -= begin;
+        uint32_t n[kSortWaves];
 #pragma unroll
         for (int w = 0; w < kSortWaves; ++w) n[w] = count[w * digits + d];
 #pragma unroll
-        for (int w = 0; w < kSortWaves; ++w) count[w * digits + d] = (uint16_t)before, before += n[w];
+        for (int w = 0; w < kSortWaves; ++w) count[w * digits + d] = (uint16_t)begin, begin += n[w];
     }
     __syncthreads();
 #pragma unroll
+    for (int j = 0; j < ITEMS; ++j)
+        if (w0 + j * 64 < a.N) rank[j] += count[wave * digits + ((unsigned)(key[j] >> a.shift) & (digits - 1))];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j)
+        if (w0 + j * 64 < a.N) list[rank[j]] = key[j];
+    __syncthreads();
+    const int here = (int)min((int64_t)ITEMS * kSortThreads, a.N - t0);
+#pragma unroll
     for (int j = 0; j < ITEMS; ++j) {
-        if (w0 + j * 64 >= a.N) continue;
-        const unsigned digit = (unsigned)(key[j] >> a.shift) & (digits - 1);
-        const int64_t place = (int64_t)base[digit] + count[wave * digits + digit] + rank[j];
-        if (place < a.N) a.out[place] = key[j];  // (always true)
+        const int i = j * kSortThreads + threadIdx.x;
+        if (i >= here) continue;
+        const uint64_t k = list[i];
+        const uint32_t place = lead[(unsigned)(k >> a.shift) & (digits - 1)] + (uint32_t)i;
+        if (place < a.N) a.out[place] = k;  // (always true)
     }
 }
 
@@ -320,11 +344,14 @@ __global__ __launch_bounds__(kSortThreads) void gp_token_rank(SortArgs a)
     const int j0 = wave * each, j1 = j0 + each, i0 = blockIdx.x * 64;
     // before this workgroup's entries an equal token is the smaller entry, behind them it is not
     int j = j0;
+#pragma unroll 8
     for (; j < min(j1, i0); j += 4) {
         const uint4 t = *(const uint4*)(list + j);
         n += (t.x <= own) + (t.y <= own) + (t.z <= own) + (t.w <= own);
     }
+#pragma unroll 8
     for (; j < min(j1, i0 + 64); ++j) n += list[j] < own || (list[j] == own && j < i);
+#pragma unroll 8
     for (; j < j1; j += 4) {
         const uint4 t = *(const uint4*)(list + j);
         n += (t.x < own) + (t.y < own) + (t.z < own) + (t.w < own);
@@ -340,7 +367,7 @@ __global__ __launch_bounds__(kSortThreads) void gp_token_rank(SortArgs a)
 
 struct GradArgs {
     const uint64_t* keys;  // sorted
-    int64_t N, V, tile, tiles;
+    int64_t N, V, tile, tiles;  // places of a tile (before the launch: of a stretch of it)
     const void* up;
     int64_t ldg;
     int d, nvec;
@@ -378,60 +405,94 @@ __device__ __forceinline__ void finish(const GradArgs& a, int64_t v, int c, cons
 // rows of zeros: those of a gap in the tokens that is at most kGap rows long are written beside the run behind it, others by gp_join_tiles
 constexpr int64_t kGap = 256;
 
-// G lanes walk one tile; a lane holds one vector of the sums.
+// G lanes walk one stretch of a.tile / kGroups places, a lane holds one vector of the sums; the workgroup's stretches are one tile.  A run
+// that goes on from stretch to stretch is put together by the lanes in whose stretch it begins (or, where it came into the tile, by
+// the first ones), from what the others leave in LDS; only what leaves the tile goes through memory.
 template <typename TG, typename TO, int VEC, int G>
 __global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
 {
-    constexpr int U = 8;
-    const int64_t t = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
-    const int c = blockIdx.y * G + threadIdx.x % G;
-    if (t >= a.tiles || c >= a.nvec) return;
-    const int64_t lo = t * a.tile, hi = min(lo + a.tile, a.N);
-    const TG* const up = (const TG*)a.up + min(c * VEC, a.d - VEC);
-    int64_t cur = (int64_t)(a.keys[lo] >> 32);
-    bool came_in = lo > 0 && (int64_t)(a.keys[lo - 1] >> 32) == cur;
+    constexpr int U = 8, kGroups = kThreads / G;
+    __shared__ float head[kThreads][VEC];   // what a stretch adds to the run that comes into it
+    __shared__ int passes[kGroups];         // that run goes on behind the stretch
+    const int g = threadIdx.x / G, c = blockIdx.y * G + threadIdx.x % G;
+    const int64_t stretch = a.tile / kGroups, lo = blockIdx.x * a.tile + g * stretch, hi = min(lo + stretch, a.N);
+    const bool active = c < a.nvec;
+    const int col = min(min(c, a.nvec - 1) * VEC, a.d - VEC);
+    const TG* const up = (const TG*)a.up + col;
+    float* const carry = a.carry + (2 * (int64_t)blockIdx.x * a.nvec + c) * VEC;  // of the run that came in; the other's is one row on
     float acc[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
     auto fill_gap = [&](int64_t before, int64_t token) {
         if (a.accumulate || token >= a.V || token - before > kGap + 1) return;
-        for (int64_t r = before + 1; r < token; ++r) store_vec<TO, VEC>((TO*)a.out + r * a.ldt + min(c * VEC, a.d - VEC), acc);
+        float zero[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) zero[i] = 0.0f;
+        for (int64_t r = before + 1; r < token; ++r) store_vec<TO, VEC>((TO*)a.out + r * a.ldt + col, zero);
     };
-    if (lo > 0 && !came_in) fill_gap((int64_t)(a.keys[lo - 1] >> 32), cur);
-    for (int64_t p = lo; p < hi; p += U) {
-        uint64_t key[U];
-        float v[U][VEC];
-#pragma unroll
-        for (int u = 0; u < U; ++u) key[u] = p + u < hi ? a.keys[p + u] : ~UINT64_C(0);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) v[u][i] = 0.0f;
-            if ((int64_t)(key[u] >> 32) < a.V) load_vec<TG, VEC>(up + (int64_t)(key[u] & 0xFFFFFFFFu) * a.ldg, v[u]);
+    int64_t cur = a.V;
+    bool came_in = false, open = false;
+    if (lo < a.N && active) {
+        cur = (int64_t)(a.keys[lo] >> 32);
+        if (lo > 0) {
+            const int64_t before = (int64_t)(a.keys[lo - 1] >> 32);
+            came_in = before == cur;
+            if (!came_in) fill_gap(before, cur);
         }
+        for (int64_t p = lo; p < hi; p += U) {
+            uint64_t key[U];
+            float v[U][VEC];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (p + u >= hi) break;
-            const int64_t tok = (int64_t)(key[u] >> 32);
-            if (tok != cur) {  // (cur < tok <= V)
-                if (came_in)
-                    store_vec<float, VEC>(a.carry + ((2 * t) * a.nvec + c) * VEC, acc);
-                else
-                    finish<TO, VEC>(a, cur, c, acc);
+            for (int u = 0; u < U; ++u) key[u] = p + u < hi ? a.keys[p + u] : ~UINT64_C(0);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
-                fill_gap(cur, tok);
-                cur = tok, came_in = false;
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[u][i] = 0.0f;
+                if ((int64_t)(key[u] >> 32) < a.V) load_vec<TG, VEC>(up + (int64_t)(key[u] & 0xFFFFFFFFu) * a.ldg, v[u]);
             }
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) acc[i] += v[u][i];
+            for (int u = 0; u < U; ++u) {
+                if (p + u >= hi) break;
+                const int64_t tok = (int64_t)(key[u] >> 32);
+                if (tok != cur) {  // (cur < tok <= V)
+                    if (!came_in)
+                        finish<TO, VEC>(a, cur, c, acc);
+                    else if (g == 0)
+                        store_vec<float, VEC>(carry, acc);
+                    else
+                        store_vec<float, VEC>(head[threadIdx.x], acc);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
+                    fill_gap(cur, tok);
+                    cur = tok, came_in = false;
+                }
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) acc[i] += v[u][i];
+            }
+        }
+        open = cur < a.V && hi < a.N && (int64_t)(a.keys[hi] >> 32) == cur;
+        if (came_in && g > 0) {
+            store_vec<float, VEC>(head[threadIdx.x], acc);
+            if (threadIdx.x % G == 0) passes[g] = open;
+            cur = a.V;  // (another's run)
+        } else if (threadIdx.x % G == 0) {
+            passes[g] = false;
         }
     }
+    __syncthreads();
     if (cur >= a.V) return;
+    if (open)
+        for (int h = g + 1; h < kGroups && open; ++h) {
+            float v[VEC];
+            load_vec<float, VEC>(head[h * G + threadIdx.x % G], v);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) acc[i] += v[i];
+            open = passes[h];
+        }
     if (came_in)
-        store_vec<float, VEC>(a.carry + ((2 * t) * a.nvec + c) * VEC, acc);
-    else if (hi < a.N && (int64_t)(a.keys[hi] >> 32) == cur)
-        store_vec<float, VEC>(a.carry + ((2 * t + 1) * a.nvec + c) * VEC, acc);
+        store_vec<float, VEC>(carry, acc);
+    else if (open)
+        store_vec<float, VEC>(carry + (int64_t)a.nvec * VEC, acc);
     else
         finish<TO, VEC>(a, cur, c, acc);
 }
@@ -583,12 +644,13 @@ __global__ __launch_bounds__(kThreads) void gp_join_tiles(GradArgs a, int64_t ti
 }
 
 template <typename TG, typename TO, int VEC, int G>
-gp_status launch_sums(const GradArgs& a, hipStream_t stream)
+gp_status launch_sums(GradArgs a, hipStream_t stream)
 {
     const unsigned ny = (unsigned)((a.nvec + G - 1) / G);
     constexpr int per = kThreads / G;
+    a.tile *= per, a.tiles = (a.N + a.tile - 1) / a.tile;
     profile_begin("gp_sum_tiles", stream);
-    hipLaunchKernelGGL((gp_sum_tiles<TG, TO, VEC, G>), dim3((unsigned)((a.tiles + per - 1) / per), ny), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((gp_sum_tiles<TG, TO, VEC, G>), dim3((unsigned)a.tiles, ny), dim3(kThreads), 0, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     const int64_t fills = a.accumulate ? 0 : ((a.V + kGap - 1) / kGap + kThreads / 64 - 1) / (kThreads / 64);
@@ -617,9 +679,9 @@ gp_status launch_sums(const GradArgs& a, hipStream_t stream)
     return a.d >= VEC ? launch_sums<TG, TO, VEC>(a, stream) : launch_sums<TG, TO, 1>(a, stream);
 }
 
-// Tiles: equal lengths; enough of them to fill the chip, few enough that the partial rows of one token are added up fast.
-constexpr int64_t kMinTile = 4, kMaxTiles = 16384;
-int64_t tile_length(int64_t N) { return std::max(kMinTile, (N + kMaxTiles - 1) / kMaxTiles); }
+// Stretches: equal lengths; enough of them to fill the chip, few enough that the partial rows of one token are added up fast.
+constexpr int64_t kMinStretch = 4, kMaxStretches = 16384;
+int64_t stretch_length(int64_t N) { return std::max(kMinStretch, (N + kMaxStretches - 1) / kMaxStretches); }
 
 int bits_of(int64_t v)
 {
@@ -649,7 +711,7 @@ struct GradLayout {
 GradLayout grad_layout(int64_t N, int64_t V, int32_t d)
 {
     auto up = [](int64_t b) { return (b + 255) / 256 * 256; };
-    const int64_t tiles = (N + tile_length(N) - 1) / tile_length(N);
+    const int64_t tile = stretch_length(N) * 4, tiles = (N + tile - 1) / tile;  // (four stretches to a tile, or more)
     const SortPlan p = sort_plan(N, V);
     GradLayout l;
     l.other = up(8 * N);
@@ -663,8 +725,8 @@ GradLayout grad_layout(int64_t N, int64_t V, int32_t d)
 template <int ITEMS, bool FIRST>
 gp_status launch_pass(const SortArgs& a, hipStream_t stream)
 {
-    const size_t lds = scatter_lds(1 << a.bits);
-    gp_status st = raise_lds<&gp_token_scatter<ITEMS, FIRST>>(scatter_lds(kMaxDigits));
+    const size_t lds = scatter_lds(1 << a.bits, ITEMS);
+    gp_status st = raise_lds<&gp_token_scatter<ITEMS, FIRST>>(scatter_lds(kMaxDigits, ITEMS));
     if (st != GP_OK) return st;
     profile_begin("gp_token_count", stream);
     hipLaunchKernelGGL((gp_token_count<ITEMS, FIRST>), dim3((unsigned)a.tiles), dim3(kSortThreads), 0, stream, a);
@@ -758,7 +820,7 @@ gp_status embedding_grad(const void* tokens, gp_index index, int64_t N, const vo
     gp_status st = sort_tokens(tokens, (int)(index == GP_I64), N, V, ws, l, stream, &sorted);
     if (st != GP_OK) return st;
     GradArgs a{};
-    a.keys = sorted, a.N = N, a.V = V, a.tile = tile_length(N), a.tiles = (N + a.tile - 1) / a.tile, a.up = up, a.ldg = ldg, a.d = d,
+    a.keys = sorted, a.N = N, a.V = V, a.tile = stretch_length(N), a.up = up, a.ldg = ldg, a.d = d,
     a.scale = scale, a.out = out, a.ldt = ldt, a.accumulate = accumulate != 0, a.carry = (float*)(ws + l.carry);
     if (dtype == GP_F32) return out_dtype == GP_F32 ? launch_sums<float, float>(a, stream) : launch_sums<float, bf16_t>(a, stream);
     return out_dtype == GP_F32 ? launch_sums<bf16_t, float>(a, stream) : launch_sums<bf16_t, bf16_t>(a, stream);
