@@ -141,7 +141,7 @@ gp_status launch_lookup(const LookupArgs& a, hipStream_t stream)
 
 // The sort: least significant digit first, digits of up to 11 bits of the token, equal digits keep their order.  An entry is
 // token << 32 | position; a token that names no row counts as V, behind all that do.  A pass of a long list: (1) every workgroup counts
-// the digits of its tile of consecutive entries, (2) one wavefront per digit adds up the tiles before each tile, (3) every workgroup
+// the digits of its tile of consecutive entries, (2) for every digit the tiles before each tile are added up, (3) every workgroup
 // ranks its tile's entries -- a wavefront takes 64 at a time, finds the lanes with its own digit by one ballot per bit, and
 // keeps counts of its own in LDS, so that no barrier stands between its steps -- and writes each to its place.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMaxDigits = 2048;
@@ -154,7 +154,7 @@ struct SortArgs {
     int64_t N, V;
     int shift, bits;       // the digit
     int64_t tiles;
-    uint32_t* table;       // [digit][tile]
+    uint32_t* table;       // [tile][digit]
     uint32_t* totals;      // [digit]
 };
 
@@ -230,29 +230,38 @@ __global__ __launch_bounds__(kSortThreads) void gp_token_count(SortArgs a)
         if (i < a.N) atomicAdd(&h[(unsigned)(entry_at<FIRST>(a, i) >> a.shift) & (digits - 1)], 1u);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < digits; i += kSortThreads) a.table[i * a.tiles + blockIdx.x] = h[i];
+    for (int i = threadIdx.x; i < digits; i += kSortThreads) a.table[(int64_t)blockIdx.x * digits + i] = h[i];
 }
 
-__global__ __launch_bounds__(kThreads) void gp_token_prefix(SortArgs a)
+// A workgroup looks after kPrefixDigits digits: its threads stand side by side over them, and each row of threads over a range of tiles.
+constexpr int kPrefixDigits = 32, kPrefixRows = kSortThreads / kPrefixDigits;
+
+__global__ __launch_bounds__(kSortThreads) void gp_token_prefix(SortArgs a)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t digit = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-    if (digit >= 1 << a.bits) return;
-    uint32_t* const row = a.table + digit * a.tiles;
-    uint32_t run = 0;
-    for (int64_t t0 = 0; t0 < a.tiles; t0 += 64) {
-        const int64_t t = t0 + lane;
-        const uint32_t v = t < a.tiles ? row[t] : 0;
-        uint32_t incl = v;
+    __shared__ uint32_t sums[kPrefixRows][kPrefixDigits];
+    const int col = threadIdx.x % kPrefixDigits, row = threadIdx.x / kPrefixDigits;
+    const int64_t digits = 1 << a.bits, d = (int64_t)blockIdx.x * kPrefixDigits + col;
+    const int64_t each = (a.tiles + kPrefixRows - 1) / kPrefixRows, t0 = min(row * each, a.tiles), t1 = min(t0 + each, a.tiles);
+    uint32_t sum = 0;
+    if (d < digits)
+#pragma unroll 8
+        for (int64_t t = t0; t < t1; ++t) sum += a.table[t * digits + d];
+    sums[row][col] = sum;
+    __syncthreads();
+    uint32_t before = 0, all = 0;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t up = __shfl_up(incl, o, 64);
-            if (lane >= o) incl += up;
-        }
-        if (t < a.tiles) row[t] = run + incl - v;
-        run += __shfl(incl, 63, 64);
+    for (int r = 0; r < kPrefixRows; ++r) {
+        const uint32_t v = sums[r][col];
+        before += r < row ? v : 0, all += v;
     }
-    if (lane == 0) a.totals[digit] = run;
+    if (d >= digits) return;
+    if (row == 0) a.totals[d] = all;
+#pragma unroll 8
+    for (int64_t t = t0; t < t1; ++t) {
+        const uint32_t v = a.table[t * digits + d];
+        a.table[t * digits + d] = before;
+        before += v;
+    }
 }
 
 // LDS of a scatter: what leads from an entry's place among the workgroup's to its place in the list, by digit; then counts [wave][digit],
@@ -279,7 +288,7 @@ __global__ __launch_bounds__(kSortThreads) void gp_token_scatter(SortArgs a)
         if (d0 + j < digits) mine += a.totals[d0 + j];
     uint32_t begin = exclusive_1024(mine, part);
     for (int j = 0; j < per; ++j)
-        if (d0 + j < digits) lead[d0 + j] = begin + a.table[(d0 + j) * a.tiles + blockIdx.x], begin += a.totals[d0 + j];
+        if (d0 + j < digits) lead[d0 + j] = begin + a.table[(int64_t)blockIdx.x * digits + d0 + j], begin += a.totals[d0 + j];
     __syncthreads();
     uint64_t key[ITEMS];
     uint32_t rank[ITEMS];
@@ -330,32 +339,41 @@ __global__ __launch_bounds__(kSortThreads) void gp_token_scatter(SortArgs a)
 // but one launch.  A workgroup ranks 64 entries, one per lane, against the whole list in LDS, a sixteenth of it per wavefront.
 constexpr int64_t kShortList = 8192;
 
+// how many of list[j0 .. j1) are below `own`, or, where EQUAL, not above it; j0, j1 multiples of 16
+template <bool EQUAL>
+__device__ __forceinline__ uint32_t count_below(const uint32_t* list, int j0, int j1, uint32_t own)
+{
+    uint32_t n = 0;
+    for (int j = j0; j < j1; j += 16) {
+        uint4 t[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) t[u] = *(const uint4*)(list + j + 4 * u);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            n += EQUAL ? (t[u].x <= own) + (t[u].y <= own) + (t[u].z <= own) + (t[u].w <= own) : (t[u].x < own) + (t[u].y < own) + (t[u].z < own) + (t[u].w < own);
+    }
+    return n;
+}
+
 __global__ __launch_bounds__(kSortThreads) void gp_token_rank(SortArgs a)
 {
     __shared__ __align__(16) uint32_t list[kShortList];
     __shared__ uint32_t smaller[kSortWaves][64];
-    const int N = (int)a.N, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int each = (N + kSortWaves * 4 - 1) / (kSortWaves * 4) * 4;  // tokens per wavefront
-    for (int i = threadIdx.x; i < each * kSortWaves; i += kSortThreads) list[i] = i < N ? (uint32_t)(entry_at<true>(a, i) >> 32) : 0xFFFFFFFFu;
+    const int N = (int)a.N, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int all = (N + 63) / 64 * 64;  // (behind the list: tokens above any)
+    for (int i = threadIdx.x; i < all; i += kSortThreads) list[i] = i < N ? (uint32_t)(entry_at<true>(a, i) >> 32) : 0xFFFFFFFFu;
     __syncthreads();
-    const int i = blockIdx.x * 64 + lane;
-    const uint32_t own = i < N ? list[i] : 0;
-    uint32_t n = 0;
-    const int j0 = wave * each, j1 = j0 + each, i0 = blockIdx.x * 64;
-    // before this workgroup's entries an equal token is the smaller entry, behind them it is not
-    int j = j0;
-#pragma unroll 8
-    for (; j < min(j1, i0); j += 4) {
-        const uint4 t = *(const uint4*)(list + j);
-        n += (t.x <= own) + (t.y <= own) + (t.z <= own) + (t.w <= own);
-    }
-#pragma unroll 8
-    for (; j < min(j1, i0 + 64); ++j) n += list[j] < own || (list[j] == own && j < i);
-#pragma unroll 8
-    for (; j < j1; j += 4) {
-        const uint4 t = *(const uint4*)(list + j);
-        n += (t.x < own) + (t.y < own) + (t.z < own) + (t.w < own);
-    }
+    const int i0 = blockIdx.x * 64, i = i0 + lane;
+    const int each = ((all + kSortWaves - 1) / kSortWaves + 15) / 16 * 16, j0 = min(wave * each, all), j1 = min(j0 + each, all);
+    const uint32_t own = list[i];
+    // before the workgroup's own entries an equal token is the smaller entry, behind them it is not
+    uint32_t n = count_below<true>(list, j0, min(j1, i0), own) + count_below<false>(list, max(j0, i0 + 64), j1, own);
+    if (wave == 0)
+#pragma unroll 16
+        for (int u = 0; u < 64; ++u) {
+            const uint32_t t = __builtin_amdgcn_readlane(own, u);
+            n += t < own || (t == own && u < lane);
+        }
     smaller[wave][lane] = n;
     __syncthreads();
     if (wave > 0 || i >= N) return;
@@ -732,7 +750,7 @@ gp_status launch_pass(const SortArgs& a, hipStream_t stream)
     hipLaunchKernelGGL((gp_token_count<ITEMS, FIRST>), dim3((unsigned)a.tiles), dim3(kSortThreads), 0, stream, a);
     profile_end(stream);
     profile_begin("gp_token_prefix", stream);
-    hipLaunchKernelGGL(gp_token_prefix, dim3((unsigned)(((1 << a.bits) + 3) / 4)), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL(gp_token_prefix, dim3((unsigned)(((1 << a.bits) + kPrefixDigits - 1) / kPrefixDigits)), dim3(kSortThreads), 0, stream, a);
     profile_end(stream);
     profile_begin("gp_token_scatter", stream);
     hipLaunchKernelGGL((gp_token_scatter<ITEMS, FIRST>), dim3((unsigned)a.tiles), dim3(kSortThreads), lds, stream, a);
