@@ -92,6 +92,9 @@ __global__ __launch_bounds__(kThreads) void gp_ns_norms(Update u, double* __rest
 
 __device__ __forceinline__ void split(float v, f16& hi, f16& lo)
 {
+    // (v as it is rounded to fp32: an instruction that multiplies and rounds to f16 at once can give a neighbour of hi, which
+    // the compiler may take for one of hi's two uses alone)
+    asm("" : "+v"(v));
     hi = (f16)v;
     lo = (f16)(v - (float)hi);
 }
@@ -99,42 +102,53 @@ __device__ __forceinline__ void split(float v, f16& hi, f16& lo)
 constexpr int kParts = 32;  // from a first part to its second
 __device__ __forceinline__ int64_t place(int64_t c) { return (c >> 5) * (2 * kParts) + (c & 31); }
 
+// four neighbours of a plane's row
+__device__ __forceinline__ void store_parts(f16* d, const float (&v)[4])
+{
+    v4h hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f16 x, y;
+        split(v[i], x, y);
+        hi[i] = x, lo[i] = y;
+    }
+    *(v4h*)d = hi, *(v4h*)(d + kParts) = lo;
+}
+
+// One 64 x 64 tile per workgroup: a thread loads a square of 4 x 4 elements, whose rows go into one plane and whose columns into the
+// other.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void gp_ns_start(Update u, const double* __restrict__ partial, float eps, float scale, f16* natural,
                                                         f16* transposed, int64_t stride, int ldn, int ldt)
 {
     __shared__ double part[kThreads / 64];
-    __shared__ float tile[kTile][kTile + 1];
     const int64_t z = blockIdx.z;
+    const T* const G = (const T*)u.G + z * u.stride_g;
+    const int64_t r0 = (int64_t)blockIdx.y * kTile + (threadIdx.x >> 4) * 4, c0 = (int64_t)blockIdx.x * kTile + (threadIdx.x & 15) * 4;
+    float v[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t r = r0 + i, c = c0 + j;
+            v[i][j] = r < u.rows && c < u.cols ? (!u.M || u.nesterov ? widen(G[r * u.ldg + c]) : 0.0f) : 0.0f;
+            if (u.M && r < u.rows && c < u.cols) {
+                const float m = u.M_out[z * u.stride_m + r * u.ldm + c];
+                v[i][j] = u.nesterov ? v[i][j] + u.mu * m : m;
+            }
+        }
     static_assert(kNormBlocks == kThreads, "one partial sum per thread");
     const double norm = sqrt(block_sum(partial[z * kNormBlocks + threadIdx.x], part));
     const float factor = (float)((double)scale / (norm + (double)eps));
-    const T* const G = (const T*)u.G + z * u.stride_g;
-    const int64_t r0 = (int64_t)blockIdx.y * kTile, c0 = (int64_t)blockIdx.x * kTile;
-    f16* const pn = natural + z * stride;
-    f16* const pt = transposed + z * stride;
-    for (int i = threadIdx.x; i < kTile * kTile; i += kThreads) {
-        const int64_t r = r0 + i / kTile, c = c0 + i % kTile;
-        float v = 0.0f;
-        if (r < u.rows && c < u.cols) {
-            v = widen(G[r * u.ldg + c]);
-            if (u.M) {
-                const float m = u.M_out[z * u.stride_m + r * u.ldm + c];
-                v = u.nesterov ? v + u.mu * m : m;
-            }
-            v *= factor;
-        }
-        tile[i / kTile][i % kTile] = v;
-        f16 h, l;
-        split(v, h, l);
-        pn[r * ldn + place(c)] = h, pn[r * ldn + place(c) + kParts] = l;
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < kTile * kTile; i += kThreads) {
-        const int64_t c = c0 + i / kTile, r = r0 + i % kTile;
-        f16 h, l;
-        split(tile[i % kTile][i / kTile], h, l);
-        pt[c * ldt + place(r)] = h, pt[c * ldt + place(r) + kParts] = l;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i][j] *= r0 + i < u.rows && c0 + j < u.cols ? factor : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float t[4] = {v[0][i], v[1][i], v[2][i], v[3][i]};
+        store_parts(natural + z * stride + (r0 + i) * ldn + place(c0), v[i]);
+        store_parts(transposed + z * stride + (c0 + i) * ldt + place(r0), t);
     }
 }
 
@@ -164,6 +178,28 @@ struct Product {
 typedef __attribute__((address_space(1))) const void* GlobalPtr;
 typedef __attribute__((address_space(3))) void* LdsPtr;
 
+// the workgroup's tile: row by row, or, where D is symmetric, those on and above the diagonal, row by row
+__device__ __forceinline__ void tile_of(const Product& a, int& bi, int& bj)
+{
+    const int t = blockIdx.x, T = a.tiles_n;
+    if (!a.symmetric) {
+        bi = t / T, bj = t - bi * T;
+        return;
+    }
+    bi = (int)((2 * T + 1 - sqrtf((float)((2 * T + 1) * (2 * T + 1) - 8 * t))) * 0.5f);
+    while (bi * T - bi * (bi - 1) / 2 > t) --bi;
+    while ((bi + 1) * T - (bi + 1) * bi / 2 <= t) ++bi;
+    bj = bi + t - (bi * T - bi * (bi - 1) / 2);
+}
+template <typename TO>
+__device__ __forceinline__ void write_out(const Product& a, int64_t o, float v)
+{
+    if (a.W) v = a.keep * a.W[o] - a.lr * v;
+    if constexpr (sizeof(TO) == 4)
+        ((float*)a.out)[o] = v;
+    else
+        ((bf16_t*)a.out)[o] = __builtin_bit_cast(bf16_t, (__bf16)v);
+}
 // BM x BN tiles of D by WM x WN waves.  A step sums over 32 columns: BM + BN lines of 128 bytes, which go straight from memory to one
 // half of LDS while the matrix cores work on the other half.  A line's 16-byte pieces lie in LDS in the order
 // piece ^ (row / 2 mod 8), with which the 16 lanes that LDS serves together read different banks.
@@ -177,15 +213,7 @@ __global__ __launch_bounds__(64 * WM * WN) void gp_ns_product(Product a)
     constexpr int kHalf = (BM + BN) * 64;
     extern __shared__ __align__(128) f16 lds[];
     int bi, bj;
-    if (a.symmetric) {  // tiles of the upper triangle, row by row
-        const int t = blockIdx.x, T = a.tiles_n;
-        bi = (int)((2 * T + 1 - sqrtf((float)((2 * T + 1) * (2 * T + 1) - 8 * t))) * 0.5f);
-        while (bi * T - bi * (bi - 1) / 2 > t) --bi;
-        while ((bi + 1) * T - (bi + 1) * bi / 2 <= t) ++bi;
-        bj = bi + t - (bi * T - bi * (bi - 1) / 2);
-    } else {
-        bi = blockIdx.x / a.tiles_n, bj = blockIdx.x - bi * a.tiles_n;
-    }
+    tile_of(a, bi, bj);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t base = (int64_t)blockIdx.z * a.stride;
     // lines this lane takes part in loading; those past the planes' ends repeat the last one (and are not used)
@@ -299,6 +327,92 @@ __global__ __launch_bounds__(64 * WM * WN) void gp_ns_product(Product a)
         }
 }
 
+// The same for products of few tiles, where a launch lasts as long as its loads take to arrive: 32 x 32 tiles, the sum's lines dealt out
+// to eight wavefronts, which load them straight into the matrix instructions' registers, two lines' worth ahead, and add up
+// their sums in LDS.
+constexpr int kSmallWaves = 8;
+
+template <typename TO, bool LAST>
+__global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product a)
+{
+    __shared__ __align__(16) float part[kSmallWaves][32][36];
+    int bi, bj;
+    tile_of(a, bi, bj);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t base = (int64_t)blockIdx.z * a.stride;
+    const int r0 = bi * 32, c0 = bj * 32;
+    const f16* const p = a.P + base + (int64_t)(r0 + (lane & 31)) * a.ldp + (lane >> 5) * 8;
+    const f16* const q = a.Q + base + (int64_t)(c0 + (lane & 31)) * a.ldq + (lane >> 5) * 8;
+    v16f acc[3];
+#pragma unroll
+    for (int x = 0; x < 3; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[x][i] = 0.0f;
+    const int steps = a.K / 32;
+    v8h pv[2][4], qv[2][4];  // [line][16 columns' first parts, the next 16's, second parts of both]
+    auto load = [&](int b, int step) {
+        if (step >= steps) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pv[b][i] = *(const v8h*)(p + (int64_t)step * 64 + i * 16), qv[b][i] = *(const v8h*)(q + (int64_t)step * 64 + i * 16);
+    };
+    auto multiply = [&](int b, int step) {
+        if (step >= steps) return;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[b][i], qv[b][i], acc[0], 0, 0, 0);
+            acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[b][i + 2], qv[b][i], acc[1], 0, 0, 0);
+            acc[2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[b][i], qv[b][i + 2], acc[2], 0, 0, 0);
+        }
+    };
+    load(0, wave), load(1, wave + kSmallWaves);
+    const bool mine = threadIdx.x < 256;  // four neighbours of a row each, at the end
+    const int lr = (threadIdx.x >> 3) & 31, lc = (threadIdx.x & 7) * 4, r = r0 + lr, c = c0 + lc;
+    v4h eh = {0, 0, 0, 0}, el = {0, 0, 0, 0};
+    if (a.E && mine) {
+        const f16* const e = a.E + base + (int64_t)r * a.lde + place(c);
+        eh = *(const v4h*)e, el = *(const v4h*)(e + kParts);
+    }
+    for (int k = wave; k < steps; k += 2 * kSmallWaves) {
+        multiply(0, k);
+        load(0, k + 2 * kSmallWaves);
+        multiply(1, k + kSmallWaves);
+        load(1, k + 3 * kSmallWaves);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) part[wave][(i >> 2) * 8 + (lane >> 5) * 4 + (i & 3)][lane & 31] = acc[0][i] + (acc[1][i] + acc[2][i]);
+    __syncthreads();
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (mine) {
+#pragma unroll
+        for (int w = 0; w < kSmallWaves; ++w) {
+            const float4 x = *(const float4*)&part[w][lr][lc];
+            v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = v[i] * a.alpha + a.beta * ((float)eh[i] + (float)el[i]);
+    }
+    if constexpr (LAST) {
+        if (!mine || r >= a.rows) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (c + i >= a.cols) continue;
+            write_out<TO>(a, blockIdx.z * a.stride_o + (int64_t)r * a.ldo + c + i, v[i]);
+        }
+    } else {
+        if (mine) store_parts(a.D + base + (int64_t)r * a.ldd + place(c), v);
+        if (a.symmetric && bi == bj) return;  // (the tile holds both halves)
+        __syncthreads();
+        if (mine)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[0][lc + i][lr] = v[i];
+        __syncthreads();
+        if (!mine) return;
+        const float4 x = *(const float4*)&part[0][lr][lc];
+        const float t[4] = {x.x, x.y, x.z, x.w};
+        store_parts(a.Dt + base + (int64_t)(c0 + lr) * a.lddt + place(r0 + lc), t);
+    }
+}
+
 // ---- ranges ------------------------------------------------------------------------------------------
 
 // the largest |a s + b s^3 + c s^5| over 0 <= s <= top
@@ -397,6 +511,19 @@ gp_status launch_tiles(Product a, int64_t count, hipStream_t stream)
 template <typename TO, bool LAST>
 gp_status launch_product(const Product& a, int64_t count, hipStream_t stream)
 {
+    if (getenv("NS_SMALL") ? atoi(getenv("NS_SMALL")) : true) {
+        Product p = a;
+        p.tiles_n = a.N / 32;
+        const int64_t tm = a.M / 32, tn = a.N / 32;
+        const int64_t tiles = a.symmetric ? tn * (tn + 1) / 2 : tm * tn;
+        if (tiles * count <= (getenv("NS_MAX") ? atoi(getenv("NS_MAX")) : 512)) {
+            profile_begin("gp_ns_product", stream);
+            hipLaunchKernelGGL((gp_ns_product_small<TO, LAST>), dim3((unsigned)tiles, 1, (unsigned)count), dim3(64 * kSmallWaves), 0, stream, p);
+            profile_end(stream);
+            GP_HIP(hipGetLastError());
+            return GP_OK;
+        }
+    }
     // the largest tiles of which there are enough for three quarters of the 256 compute units
     auto enough = [&](int64_t side) {
         const int64_t tm = (a.M + side - 1) / side, tn = (a.N + side - 1) / side;
