@@ -20,6 +20,7 @@
 #include <algorithm>
 #include <cmath>
 #include <exception>
+#include <type_traits>
 
 #include "gp_internal.h"
 
@@ -166,7 +167,7 @@ struct Product {
     f16 *D, *Dt;
     int ldd, lddt;
     int symmetric;       // D and Dt are one plane: tiles on and above the diagonal will do
-    int tiles_n;
+    int tiles_m, tiles_n, tile_count;
     // the last product
     int64_t rows, cols;
     void* out;
@@ -175,21 +176,39 @@ struct Product {
     float keep, lr;
 };
 
+// all but the wave's last N loads have arrived, it has read what it asked LDS for, and so have the workgroup's others
+template <int N>
+__device__ __forceinline__ void wait_and_meet()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
 typedef __attribute__((address_space(1))) const void* GlobalPtr;
 typedef __attribute__((address_space(3))) void* LdsPtr;
 
-// the workgroup's tile: row by row, or, where D is symmetric, those on and above the diagonal, row by row
-__device__ __forceinline__ void tile_of(const Product& a, int& bi, int& bj)
+// The workgroup's tile, false for none.  Tiles are numbered in bands of four rows, column by column (where D is symmetric, from the
+// band's first column on the diagonal; a tile below the diagonal is none), and each of the chip's eight parts, which share an L2 and
+// take every eighth workgroup, gets one stretch of the numbers: a square of tiles, whose lines it reads once.
+__host__ __device__ __forceinline__ int64_t tile_numbers(int tiles_m, int tiles_n, bool symmetric)
 {
-    const int t = blockIdx.x, T = a.tiles_n;
-    if (!a.symmetric) {
-        bi = t / T, bj = t - bi * T;
-        return;
+    if (!symmetric) return (int64_t)tiles_m * tiles_n;
+    int64_t all = 0;
+    for (int b = 0; b < tiles_m; b += 4) all += (int64_t)(tiles_m - b < 4 ? tiles_m - b : 4) * (tiles_n - b);
+    return all;
+}
+__device__ __forceinline__ bool tile_of(const Product& a, int& bi, int& bj)
+{
+    const int per = gridDim.x / 8, all = a.tile_count;
+    int t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if (t >= all) return false;
+    for (int b = 0;; b += 4) {
+        const int rows = min(a.tiles_m - b, 4), first = a.symmetric ? b : 0, size = rows * (a.tiles_n - first);
+        if (t < size) {
+            bi = b + t % rows, bj = first + t / rows;
+            return !a.symmetric || bi <= bj;
+        }
+        t -= size;
     }
-    bi = (int)((2 * T + 1 - sqrtf((float)((2 * T + 1) * (2 * T + 1) - 8 * t))) * 0.5f);
-    while (bi * T - bi * (bi - 1) / 2 > t) --bi;
-    while ((bi + 1) * T - (bi + 1) * bi / 2 <= t) ++bi;
-    bj = bi + t - (bi * T - bi * (bi - 1) / 2);
 }
 template <typename TO>
 __device__ __forceinline__ void write_out(const Product& a, int64_t o, float v)
@@ -204,31 +223,34 @@ __device__ __forceinline__ void write_out(const Product& a, int64_t o, float v)
 // half of LDS while the matrix cores work on the other half.  A line's 16-byte pieces lie in LDS in the order
 // piece ^ (row / 2 mod 8), with which the 16 lanes that LDS serves together read different banks.
 // A wave's registers hold its BM / WM x BN / WN sums as 32 x 32 blocks: lane l has column l mod 32, rows 8 (i / 4) + 4 (l / 32) + i mod 4.
-template <int BM, int BN, int WM, int WN, typename TO, bool LAST>
+template <int BM, int BN, int WM, int WN, int STAGES, typename TO, bool LAST>
 __global__ __launch_bounds__(64 * WM * WN) void gp_ns_product(Product a)
 {
     constexpr int kWaves = WM * WN;
     constexpr int RB = BM / WM / 32, CB = BN / WN / 32;  // blocks of a wave
     constexpr int kLoads = (BM + BN) / 8 / kWaves;       // eight lines per wave and load
-    constexpr int kHalf = (BM + BN) * 64;
+    constexpr int kStage = (BM + BN) * 64;
     extern __shared__ __align__(128) f16 lds[];
     int bi, bj;
-    tile_of(a, bi, bj);
+    if (!tile_of(a, bi, bj)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t base = (int64_t)blockIdx.z * a.stride;
-    // lines this lane takes part in loading; those past the planes' ends repeat the last one (and are not used)
-    const f16* src[kLoads];
+    // lines this lane takes part in loading, the first kLoadsP of P, the others of Q; those past the planes' ends repeat the last one (and
+    // are not used)
+    constexpr int kLoadsP = BM / 8 / kWaves;
+    static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0, "a load is of one plane");
+    const f16 *const p0 = a.P + base + (int64_t)bi * BM * a.ldp, *const q0 = a.Q + base + (int64_t)bj * BN * a.ldq;
+    unsigned offset[kLoads];
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
         const int line = (u * kWaves + wave) * 8 + (lane >> 3);
-        const int piece = (lane & 7) ^ ((line >> 1) & 7);
-        src[u] = line < BM ? a.P + base + (int64_t)min(bi * BM + line, a.M - 1) * a.ldp + piece * 8
-                           : a.Q + base + (int64_t)min(bj * BN + line - BM, a.N - 1) * a.ldq + piece * 8;
+        const unsigned piece = (unsigned)((lane & 7) ^ ((line >> 1) & 7)) * 8;
+        offset[u] = piece + (u < kLoadsP ? (unsigned)min(line, a.M - 1 - bi * BM) * (unsigned)a.ldp : (unsigned)min(line - BM, a.N - 1 - bj * BN) * (unsigned)a.ldq);
     }
-    auto load = [&](int half, int step) {
-#pragma unroll
-        for (int u = 0; u < kLoads; ++u)
-            __builtin_amdgcn_global_load_lds((GlobalPtr)(src[u] + (int64_t)step * 64), (LdsPtr)(lds + half * kHalf + (u * kWaves + wave) * 512), 16, 0, 0);
+    const int steps = a.K / 32;
+    auto load = [&](int u, int stage, int step) {
+        const f16* const from = (u < kLoadsP ? p0 : q0) + (int64_t)min(step, steps - 1) * 64;  // (steps past the last are not used)
+        __builtin_amdgcn_global_load_lds((GlobalPtr)(from + offset[u]), (LdsPtr)(lds + stage * kStage + (u * kWaves + wave) * 512), 16, 0, 0);
     };
     const int wr = wave / WN * (RB * 32), wc = wave % WN * (CB * 32);
     // where this lane reads: line wr + lane mod 32, pieces lane / 32 + 2 s (+ 4: second parts), s = 0, 1
@@ -242,34 +264,65 @@ __global__ __launch_bounds__(64 * WM * WN) void gp_ns_product(Product a)
         for (int c = 0; c < CB; ++c)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[r][c][i] = 0.0f;
-    const int steps = a.K / 32;
-    load(0, 0);
-    for (int k = 0; k < steps; ++k) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's lines are there; behind the barrier, everyone's
-        __syncthreads();
-        const int h = (k & 1) * kHalf;
-        if (k + 1 < steps) load(~k & 1, k + 1);
+    // half a step's operands: 16 columns of the wave's lines, first and second parts
+    struct Half {
+        v8h p[2][RB], q[2][CB];
+    };
+    auto read = [&](Half& f, int stage, int s) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            v8h p[2][RB], q[2][CB];
+        for (int part = 0; part < 2; ++part) {
+            const int at = (((lane >> 5) + 2 * s + 4 * part) ^ swap) * 8 + stage * kStage;
 #pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                const int at = (((lane >> 5) + 2 * s + 4 * part) ^ swap) * 8 + h;
+            for (int r = 0; r < RB; ++r) f.p[part][r] = *(const v8h*)(pl + r * 32 * 64 + at);
 #pragma unroll
-                for (int r = 0; r < RB; ++r) p[part][r] = *(const v8h*)(pl + r * 32 * 64 + at);
+            for (int c = 0; c < CB; ++c) f.q[part][c] = *(const v8h*)(ql + c * 32 * 64 + at);
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (the reads go out before the products that they run beside)
+    };
+    // a half step's products; with them, one at a time (a wave that asks for all of them at once waits for the last before it goes on),
+    // the loads of a step into a stage
+    auto multiply = [&](const Half& f, auto loads, int stage, int step) {
+        constexpr int kProducts = 3 * RB * CB;
 #pragma unroll
-                for (int c = 0; c < CB; ++c) q[part][c] = *(const v8h*)(ql + c * 32 * 64 + at);
-            }
+        for (int x = 0; x < 3; ++x)
 #pragma unroll
             for (int r = 0; r < RB; ++r)
 #pragma unroll
                 for (int c = 0; c < CB; ++c) {
-                    acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[1][r], q[0][c], acc[r][c], 0, 0, 0);
-                    acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[0][r], q[1][c], acc[r][c], 0, 0, 0);
-                    acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[0][r], q[0][c], acc[r][c], 0, 0, 0);
+                    acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.p[x == 0][r], f.q[x == 1][c], acc[r][c], 0, 0, 0);
+                    if constexpr (decltype(loads)::value) {
+                        const int i = (x * RB + r) * CB + c;
+#pragma unroll
+                        for (int u = 0; u < kLoads; ++u)
+                            if (u >= i * kLoads / kProducts && u < (i + 1) * kLoads / kProducts) {
+                                __builtin_amdgcn_sched_barrier(0);
+                                load(u, stage, step);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                    }
                 }
-        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // Every half step's reads run beside the half step before it; a stage is loaded again as soon as all waves have its second
+    // half in registers.
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s)
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) load(u, s, s);
+    Half f0, f1;
+    wait_and_meet<(STAGES - 1) * kLoads>();
+    read(f0, 0, 0);
+    int stage = 0;
+    for (int k = 0; k < steps; ++k) {
+        read(f1, stage, 1);
+        multiply(f0, std::false_type{}, 0, 0);
+        wait_and_meet<(STAGES - 2) * kLoads>();  // the next step's lines are there
+        const int next = stage + 1 == STAGES ? 0 : stage + 1;
+        read(f0, next, 0);
+        multiply(f1, std::true_type{}, stage, k + STAGES);
+        stage = next;
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
@@ -337,7 +390,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product 
 {
     __shared__ __align__(16) float part[kSmallWaves][32][36];
     int bi, bj;
-    tile_of(a, bi, bj);
+    if (!tile_of(a, bi, bj)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t base = (int64_t)blockIdx.z * a.stride;
     const int r0 = bi * 32, c0 = bj * 32;
@@ -410,6 +463,84 @@ __global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product 
         const float4 x = *(const float4*)&part[0][lr][lc];
         const float t[4] = {x.x, x.y, x.z, x.w};
         store_parts(a.Dt + base + (int64_t)(c0 + lr) * a.lddt + place(r0 + lc), t);
+    }
+}
+
+// A step's second and third product at once, for m <= 128: on 16 columns of X, X <- a X + b Y + c A Y with Y = A X needs no other columns.
+// A (in the registers of m / 16 wavefronts, 16 rows each) is read once, X and Y lie in LDS; one launch less per step, where launches are
+// what a step takes (us per launch here, and for the two products: 5.6 and 10 with m = 64, 6.5 and 10 with 128, but 12 and 10 with
+// 256, where a compute unit reads 256 KB of A).
+struct Panel {
+    const f16 *A, *Xt;       // planes: m x m, n x m
+    f16 *X_out, *Xt_out;     // m x n, n x m
+    int m, n;
+    int64_t stride;
+    float y_scale, fa, fb, fc;
+    // the last step
+    int64_t rows, cols;
+    int tall;
+    Product last;
+};
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+template <int M, typename TO, bool LAST>
+__global__ __launch_bounds__(4 * M) void gp_ns_panel(Panel a)
+{
+    constexpr int kSteps = M / 32, kLd = 2 * M + 8;  // halves of a column in LDS: 16 bytes more than its parts, so that columns start on different banks
+    __shared__ __align__(16) f16 xs[16 * kLd], ys[16 * kLd];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, kg = lane >> 4;
+    const int64_t base = (int64_t)blockIdx.z * a.stride;
+    const int c0 = blockIdx.x * 16;
+    v8h av[kSteps][2];
+    const f16* const arow = a.A + base + (int64_t)(wave * 16 + r16) * (2 * M) + kg * 8;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) av[s][0] = *(const v8h*)(arow + s * 64), av[s][1] = *(const v8h*)(arow + s * 64 + kParts);
+    for (int i = threadIdx.x; i < 16 * M / 4; i += 4 * M) {  // (four pieces of eight halves per thread)
+        const int col = i / (M / 4), piece = i % (M / 4);
+        *(v8h*)(xs + col * kLd + piece * 8) = *(const v8h*)(a.Xt + base + (int64_t)(c0 + col) * (2 * M) + piece * 8);
+    }
+    __syncthreads();
+    auto product = [&](const f16* cols) {
+        v4f acc[3] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
+        const f16* const q = cols + r16 * kLd + kg * 8;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const v8h hi = *(const v8h*)(q + s * 64), lo = *(const v8h*)(q + s * 64 + kParts);
+            acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(av[s][0], hi, acc[0], 0, 0, 0);
+            acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(av[s][1], hi, acc[1], 0, 0, 0);
+            acc[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(av[s][0], lo, acc[2], 0, 0, 0);
+        }
+        return acc[0] + (acc[1] + acc[2]);
+    };
+    // the lane's elements: column c0 + r16, rows r .. r + 3
+    const int r = wave * 16 + kg * 4, at = r16 * kLd + (int)place(r);
+    const v4f y = product(xs);
+    const float yv[4] = {y[0] * a.y_scale, y[1] * a.y_scale, y[2] * a.y_scale, y[3] * a.y_scale};
+    store_parts(ys + at, yv);
+    const v4h xh = *(const v4h*)(xs + at), xl = *(const v4h*)(xs + at + kParts);
+    __syncthreads();
+    const v4f z = product(ys);
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a.fa * ((float)xh[i] + (float)xl[i]) + (a.fb * y[i] + a.fc * z[i]);
+    const int c = c0 + r16;
+    if constexpr (LAST) {
+        const Product& p = a.last;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = a.tall ? c : r + i, col = a.tall ? r + i : c;
+            if (row < p.rows && col < p.cols) write_out<TO>(p, blockIdx.z * p.stride_o + row * p.ldo + col, v[i]);
+        }
+    } else {
+        store_parts(a.Xt_out + base + (int64_t)c * (2 * M) + place(r), v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f16 hi, lo;
+            split(v[i], hi, lo);
+            f16* const d = a.X_out + base + (int64_t)(r + i) * (2 * a.n) + place(c);
+            d[0] = hi, d[kParts] = lo;
+        }
     }
 }
 
@@ -490,19 +621,24 @@ gp_status check_shape(int64_t rows, int64_t cols, int64_t count)
     return GP_OK;
 }
 
-template <int BM, int BN, int WM, int WN, typename TO, bool LAST>
+unsigned tile_grid(Product& a, int bm, int bn)
+{
+    a.tiles_m = (a.M + bm - 1) / bm, a.tiles_n = (a.N + bn - 1) / bn;
+    a.tile_count = (int)tile_numbers(a.tiles_m, a.tiles_n, a.symmetric);
+    return (unsigned)((a.tile_count + 7) / 8 * 8);
+}
+
+template <int BM, int BN, int WM, int WN, int STAGES, typename TO, bool LAST>
 gp_status launch_tiles(Product a, int64_t count, hipStream_t stream)
 {
-    constexpr size_t lds = 2 * (BM + BN) * 128;
+    constexpr size_t lds = STAGES * (BM + BN) * 128;
     if constexpr (lds > 65536) {
-        gp_status st = raise_lds<&gp_ns_product<BM, BN, WM, WN, TO, LAST>>(lds);
+        gp_status st = raise_lds<&gp_ns_product<BM, BN, WM, WN, STAGES, TO, LAST>>(lds);
         if (st != GP_OK) return st;
     }
-    const int64_t tm = (a.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
-    a.tiles_n = (int)tn;
-    const dim3 grid((unsigned)(a.symmetric ? tn * (tn + 1) / 2 : tm * tn), 1, (unsigned)count);
+    const dim3 grid(tile_grid(a, BM, BN), 1, (unsigned)count);
     profile_begin("gp_ns_product", stream);
-    hipLaunchKernelGGL((gp_ns_product<BM, BN, WM, WN, TO, LAST>), grid, dim3(64 * WM * WN), lds, stream, a);
+    hipLaunchKernelGGL((gp_ns_product<BM, BN, WM, WN, STAGES, TO, LAST>), grid, dim3(64 * WM * WN), lds, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     return GP_OK;
@@ -511,28 +647,40 @@ gp_status launch_tiles(Product a, int64_t count, hipStream_t stream)
 template <typename TO, bool LAST>
 gp_status launch_product(const Product& a, int64_t count, hipStream_t stream)
 {
-    if (getenv("NS_SMALL") ? atoi(getenv("NS_SMALL")) : true) {
-        Product p = a;
-        p.tiles_n = a.N / 32;
-        const int64_t tm = a.M / 32, tn = a.N / 32;
-        const int64_t tiles = a.symmetric ? tn * (tn + 1) / 2 : tm * tn;
-        if (tiles * count <= (getenv("NS_MAX") ? atoi(getenv("NS_MAX")) : 512)) {
-            profile_begin("gp_ns_product", stream);
-            hipLaunchKernelGGL((gp_ns_product_small<TO, LAST>), dim3((unsigned)tiles, 1, (unsigned)count), dim3(64 * kSmallWaves), 0, stream, p);
-            profile_end(stream);
-            GP_HIP(hipGetLastError());
-            return GP_OK;
-        }
-    }
-    // the largest tiles of which there are enough for three quarters of the 256 compute units
-    auto enough = [&](int64_t side) {
+    const int small_max = 512;
+    auto tiles = [&](int64_t side) {
         const int64_t tm = (a.M + side - 1) / side, tn = (a.N + side - 1) / side;
-        return (a.symmetric ? tn * (tn + 1) / 2 : tm * tn) * count >= 192;
+        return (a.symmetric ? tn * (tn + 1) / 2 : tm * tn) * count;
     };
-    const int side = enough(256) ? 256 : enough(128) ? 128 : 64;
-    if (side == 256) return launch_tiles<256, 256, 2, 4, TO, LAST>(a, count, stream);
-    if (side == 128) return launch_tiles<128, 128, 2, 2, TO, LAST>(a, count, stream);
-    return launch_tiles<64, 64, 2, 2, TO, LAST>(a, count, stream);
+    const int forced = getenv("NS_TILE") ? atoi(getenv("NS_TILE")) : 0;
+    if (forced ? forced == 32 : tiles(32) <= small_max) {
+        Product p = a;
+        const dim3 grid(tile_grid(p, 32, 32), 1, (unsigned)count);
+        profile_begin("gp_ns_product", stream);
+        hipLaunchKernelGGL((gp_ns_product_small<TO, LAST>), grid, dim3(64 * kSmallWaves), 0, stream, p);
+        profile_end(stream);
+        GP_HIP(hipGetLastError());
+        return GP_OK;
+    }
+    const int side = forced ? forced : tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
+    if (side == 256) return launch_tiles<256, 256, 2, 2, 2, TO, LAST>(a, count, stream);
+    if (side == 128) return launch_tiles<128, 128, 2, 4, 4, TO, LAST>(a, count, stream);
+    if (side == 129) return launch_tiles<128, 128, 2, 2, 2, TO, LAST>(a, count, stream);
+    return launch_tiles<64, 64, 2, 2, 4, TO, LAST>(a, count, stream);
+}
+
+template <typename TO, bool LAST>
+gp_status launch_panels(const Panel& a, int64_t count, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(a.n / 16), 1, (unsigned)count), block(4 * a.m);
+    profile_begin("gp_ns_panel", stream);
+    if (a.m == 64)
+        hipLaunchKernelGGL((gp_ns_panel<64, TO, LAST>), grid, block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((gp_ns_panel<128, TO, LAST>), grid, block, 0, stream, a);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    return GP_OK;
 }
 
 // out: the direction itself (W null, of dtype out_dtype), or the stepped weights
@@ -541,11 +689,11 @@ gp_status newton_schulz(const Update& u, gp_dtype dtype, int64_t count, int32_t 
 {
     if (steps < 1 || steps > kMaxSteps) return fail(GP_ERR_INVALID_ARG, "steps = %d: 1 .. %d", steps, kMaxSteps);
     if (!(eps >= 0.0f)) return fail(GP_ERR_INVALID_ARG, "eps must not be negative");
-    int ex[kMaxSteps + 1], ea[kMaxSteps], eb[kMaxSteps];
+    int ex[kMaxSteps + 1], ea[kMaxSteps], eb[kMaxSteps], ey[kMaxSteps];
     double top = 1.0;
     for (int k = 0; k < steps; ++k) {
         const float* const p = coeff ? coeff + 3 * k : kDefaultCoeff;
-        ex[k] = exponent_for(top), ea[k] = exponent_for(top * top), eb[k] = exponent_for(quadratic_bound(p[1], p[2], top * top));
+        ex[k] = exponent_for(top), ea[k] = exponent_for(top * top), ey[k] = exponent_for(top * top * top), eb[k] = exponent_for(quadratic_bound(p[1], p[2], top * top));
         top = polynomial_bound(p[0], p[1], p[2], top);
         if (!(top <= 1e6)) return fail(GP_ERR_INVALID_ARG, "step %d takes singular values of 0 .. 1 out to %g", k + 1, top);
     }
@@ -588,12 +736,26 @@ gp_status newton_schulz(const Update& u, gp_dtype dtype, int64_t count, int32_t 
         a.D = a.Dt = A, a.ldd = a.lddt = 2 * m, a.symmetric = 1;
         gp_status st = launch_product<float, false>(a, count, stream);
         if (st != GP_OK) return st;
+        const bool last_step = k == steps - 1;
+        if (m <= 128) {
+            Panel q{};
+            const int out_ex = last_step ? 0 : ex[k + 1];
+            q.A = A, q.Xt = Xt, q.X_out = ws + l.X[(k + 1) & 1], q.Xt_out = ws + l.Xt[(k + 1) & 1];
+            q.m = m, q.n = n, q.stride = l.stride, q.tall = tall;
+            q.y_scale = std::ldexp(1.0f, ey[k] - ea[k] - ex[k]);
+            q.fa = std::ldexp(p[0], out_ex - ex[k]), q.fb = std::ldexp(p[1], out_ex - ea[k] - ex[k]), q.fc = std::ldexp(p[2], out_ex - ea[k] - ey[k]);
+            q.last.rows = u.rows, q.last.cols = u.cols, q.last.out = out, q.last.ldo = ldo, q.last.stride_o = stride_o;
+            q.last.W = W, q.last.keep = keep, q.last.lr = lr;
+            st = !last_step ? launch_panels<float, false>(q, count, stream) : out_dtype == GP_F32 ? launch_panels<float, true>(q, count, stream) : launch_panels<bf16_t, true>(q, count, stream);
+            if (st != GP_OK) return st;
+            continue;
+        }
         a.P = a.Q = a.E = A, a.ldp = a.ldq = a.lde = 2 * m, a.K = m;
         a.alpha = std::ldexp(p[2], eb[k] - 2 * ea[k]), a.beta = std::ldexp(p[1], eb[k] - ea[k]);
         a.D = a.Dt = B;
         if ((st = launch_product<float, false>(a, count, stream)) != GP_OK) return st;
         a.symmetric = 0;
-        if (k < steps - 1) {
+        if (!last_step) {
             const int next = ex[k + 1] - ex[k];
             a.P = B, a.Q = Xt, a.N = n, a.E = X, a.lde = 2 * n;
             a.alpha = std::ldexp(1.0f, next - eb[k]), a.beta = std::ldexp(p[0], next);
