@@ -116,6 +116,22 @@ __device__ __forceinline__ void store_parts(f16* d, const float (&v)[4])
     *(v4h*)d = hi, *(v4h*)(d + kParts) = lo;
 }
 
+// sixteen
+__device__ __forceinline__ void store_parts16(f16* d, const float (&v)[16])
+{
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+        v8h hi, lo;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            f16 x, y;
+            split(v[8 * g + i], x, y);
+            hi[i] = x, lo[i] = y;
+        }
+        *(v8h*)(d + 8 * g) = hi, *(v8h*)(d + 8 * g + kParts) = lo;
+    }
+}
+
 // One 64 x 64 tile per workgroup: a thread loads a square of 4 x 4 elements, whose rows go into one plane and whose columns into the
 // other.
 template <typename T>
@@ -219,6 +235,43 @@ __device__ __forceinline__ void write_out(const Product& a, int64_t o, float v)
     else
         ((bf16_t*)a.out)[o] = __builtin_bit_cast(bf16_t, (__bf16)v);
 }
+// the first `count` of sixteen neighbours of a row, from any element's boundary
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef bf16_t v8b_any __attribute__((ext_vector_type(8), aligned(2)));
+template <typename TO>
+__device__ __forceinline__ void write_row(const Product& a, int64_t o, int count, const float (&v)[16])
+{
+    if (count < 16) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (i < count) write_out<TO>(a, o + i, v[i]);
+        return;
+    }
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = v[i];
+    if (a.W) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const v4f_any w = *(const v4f_any*)(a.W + o + 4 * g);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * g + i] = a.keep * w[i] - a.lr * v[4 * g + i];
+        }
+    }
+    if constexpr (sizeof(TO) == 4) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) *(v4f_any*)((float*)a.out + o + 4 * g) = (v4f_any){x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]};
+    } else {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            v8b_any y;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = __builtin_bit_cast(bf16_t, (__bf16)x[8 * g + i]);
+            *(v8b_any*)((bf16_t*)a.out + o + 8 * g) = y;
+        }
+    }
+}
+
 // BM x BN tiles of D by WM x WN waves.  A step sums over 32 columns: BM + BN lines of 128 bytes, which go straight from memory to one
 // half of LDS while the matrix cores work on the other half.  A line's 16-byte pieces lie in LDS in the order
 // piece ^ (row / 2 mod 8), with which the 16 lanes that LDS serves together read different banks.
@@ -322,62 +375,51 @@ __global__ __launch_bounds__(64 * WM * WN) void gp_ns_product(Product a)
         multiply(f1, std::true_type{}, stage, k + STAGES);
         stage = next;
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // The sums, 32 x 32 at a time, turned through LDS so that a lane has 16 neighbours of a row (and, for Dt, of a column): requests
+    // of 16 bytes instead of 2.  The stages are free behind this barrier: no load is on its way, and every wave has read its last.
+    wait_and_meet<0>();
+    float* const turn = (float*)lds + wave * (32 * 33);
+    const int lr = lane >> 1, lc = (lane & 1) * 16;
+    v8h e[2][4];  // of this block and the next: first and second parts of 16 neighbours
+    auto fetch = [&](int n) {
+        const int r0 = bi * BM + wr + n / CB * 32, c0 = bj * BN + wc + n % CB * 32;
+        if (!a.E || r0 >= a.M || c0 >= a.N) return;
+        const f16* const p = a.E + base + (int64_t)(r0 + lr) * a.lde + place(c0 + lc);
+        e[n & 1][0] = *(const v8h*)p, e[n & 1][1] = *(const v8h*)(p + 8);
+        e[n & 1][2] = *(const v8h*)(p + kParts), e[n & 1][3] = *(const v8h*)(p + kParts + 8);
+    };
+    fetch(0);
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
+    for (int n = 0; n < RB * CB; ++n) {
+        if (n + 1 < RB * CB) fetch(n + 1);
+        const int rb = n / CB, cb = n % CB;
+        const int r0 = bi * BM + wr + rb * 32, c0 = bj * BN + wc + cb * 32;
+        if (r0 >= a.M || c0 >= a.N) continue;
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            const int r0 = bi * BM + wr + rb * 32, c0 = bj * BN + wc + cb * 32;
-            if (r0 >= a.M || c0 >= a.N) continue;
-            const int c = c0 + (lane & 31), rl = r0 + (lane >> 5) * 4;  // element i: row rl + 8 (i / 4) + i mod 4
-            float v[16];
+        for (int i = 0; i < 16; ++i) turn[((i >> 2) * 8 + (lane >> 5) * 4 + (i & 3)) * 33 + (lane & 31)] = acc[rb][cb][i];
+        __builtin_amdgcn_wave_barrier();
+        float v[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = acc[rb][cb][i] * a.alpha;
-            if (a.E) {
-                const f16* const e = a.E + base + (int64_t)rl * a.lde + place(c);
-                f16 hi[16], lo[16];
+        for (int i = 0; i < 16; ++i) v[i] = turn[lr * 33 + lc + i] * a.alpha;
+        if (a.E)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) hi[i] = e[(int64_t)(8 * (i >> 2) + (i & 3)) * a.lde], lo[i] = e[(int64_t)(8 * (i >> 2) + (i & 3)) * a.lde + kParts];
+            for (int i = 0; i < 16; ++i) v[i] += a.beta * ((float)e[n & 1][i >> 3][i & 7] + (float)e[n & 1][2 + (i >> 3)][i & 7]);
+        __builtin_amdgcn_wave_barrier();
+        if constexpr (LAST) {
+            if (r0 + lr >= a.rows) continue;
+            write_row<TO>(a, blockIdx.z * a.stride_o + (int64_t)(r0 + lr) * a.ldo + c0 + lc, (int)min(a.cols - c0 - lc, (int64_t)16), v);
+        } else {
+            store_parts16(a.D + base + (int64_t)(r0 + lr) * a.ldd + place(c0 + lc), v);
+            if (a.symmetric && bi == bj) continue;  // (the tile holds both halves)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] += a.beta * ((float)hi[i] + (float)lo[i]);
-            }
-            if constexpr (LAST) {
-                if (c >= a.cols) continue;
-                const int64_t o = blockIdx.z * a.stride_o + rl * a.ldo + c;
-                float w[16];
-                if (a.W) {
+            for (int i = 0; i < 16; ++i) turn[lr * 33 + lc + i] = v[i];
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) w[i] = rl + 8 * (i >> 2) + (i & 3) < a.rows ? a.W[o + (8 * (i >> 2) + (i & 3)) * a.ldo] : 0.0f;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = a.keep * w[i] - a.lr * v[i];
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int dr = 8 * (i >> 2) + (i & 3);
-                    if (rl + dr >= a.rows) continue;
-                    if constexpr (sizeof(TO) == 4)
-                        ((float*)a.out)[o + dr * a.ldo] = v[i];
-                    else
-                        ((bf16_t*)a.out)[o + dr * a.ldo] = __builtin_bit_cast(bf16_t, (__bf16)v[i]);
-                }
-            } else {
-                f16* const d = a.D + base + (int64_t)rl * a.ldd + place(c);
-                f16* const t = a.Dt + base + (int64_t)c * a.lddt + place(rl);
-                const bool both = !a.symmetric || bi != bj;  // (a tile on the diagonal holds both halves)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    v4h hi, lo;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        f16 x, y;
-                        split(v[4 * g + i], x, y);
-                        hi[i] = x, lo[i] = y;
-                        d[(int64_t)(8 * g + i) * a.ldd] = x, d[(int64_t)(8 * g + i) * a.ldd + kParts] = y;
-                    }
-                    if (both) *(v4h*)(t + 8 * g) = hi, *(v4h*)(t + 8 * g + kParts) = lo;
-                }
-            }
+            for (int i = 0; i < 16; ++i) v[i] = turn[(lc + i) * 33 + lr];
+            __builtin_amdgcn_wave_barrier();
+            store_parts16(a.Dt + base + (int64_t)(c0 + lr) * a.lddt + place(r0 + lc), v);
         }
+    }
 }
 
 // The same for products of few tiles, where a launch lasts as long as its loads take to arrive: 32 x 32 tiles, the sum's lines dealt out
