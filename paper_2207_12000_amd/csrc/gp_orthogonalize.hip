@@ -32,11 +32,14 @@ constexpr int kThreads = 256;
 constexpr int kTile = 64;          // sides of planes are multiples of it; what is added is zero
 constexpr int kNormBlocks = 256;   // partial sums of squares per matrix
 constexpr int kMaxSteps = 32;
+constexpr int kMaxShared = 1024;    // tiles of a product that several workgroups may share
 
 typedef unsigned short bf16_t;
 typedef _Float16 f16;
 typedef f16 v4h __attribute__((ext_vector_type(4)));
 typedef f16 v8h __attribute__((ext_vector_type(8)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ float widen(float v) { return v; }
@@ -55,6 +58,7 @@ struct Update {  // U, element by element: G, or the momentum step M <- mu M + G
 
 // ---- the sum of squares, and the new momentum ---------------------------------------------------------
 
+template <int THREADS>
 __device__ __forceinline__ double block_sum(double v, double* part)
 {
 #pragma unroll
@@ -63,29 +67,83 @@ __device__ __forceinline__ double block_sum(double v, double* part)
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
     double s = 0.0;
-    for (int w = 0; w < kThreads / 64; ++w) s += part[w];
+    for (int w = 0; w < THREADS / 64; ++w) s += part[w];
     return s;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void gp_ns_norms(Update u, double* __restrict__ partial)
+// Four neighbours of a row per thread and step, four steps' requests at once (4096 x 4096 fp32: 19 us, 3.5 TB/s; one element at a time
+// took 130).  Workgroups of 256 threads where these have no more than one step to do (256 x 256: 3 us, 5 with 1024), else of 1024.
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef bf16_t v4b_any __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ void load_some(const float* p, int count, float (&v)[4])
 {
-    __shared__ double part[kThreads / 64];
-    const int64_t z = blockIdx.y, total = u.rows * u.cols;
+    if (count >= 4) {
+        const v4f_any x = *(const v4f_any*)p;
+        v[0] = x[0], v[1] = x[1], v[2] = x[2], v[3] = x[3];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i < count ? p[i] : 0.0f;
+    }
+}
+__device__ __forceinline__ void load_some(const bf16_t* p, int count, float (&v)[4])
+{
+    if (count >= 4) {
+        const v4b_any x = *(const v4b_any*)p;
+        v[0] = widen(x[0]), v[1] = widen(x[1]), v[2] = widen(x[2]), v[3] = widen(x[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i < count ? widen(p[i]) : 0.0f;
+    }
+}
+__device__ __forceinline__ void store_some(float* p, int count, const float (&v)[4])
+{
+    if (count >= 4) {
+        *(v4f_any*)p = (v4f_any){v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < count) p[i] = v[i];
+    }
+}
+
+template <int kNormThreads, typename T>
+__global__ __launch_bounds__(kNormThreads) void gp_ns_norms(Update u, double* __restrict__ partial, int* __restrict__ arrived)
+{
+    __shared__ double part[kNormThreads / 64];
+    if (blockIdx.x == 0 && blockIdx.y == 0)
+        for (int i = threadIdx.x; i < kMaxShared; i += kNormThreads) arrived[i] = 0;
+    constexpr int U = 4;
+    const int64_t z = blockIdx.y, groups = (u.cols + 3) / 4, total = u.rows * groups;
     const T* const G = (const T*)u.G + z * u.stride_g;
     double s = 0.0;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)kNormBlocks * kThreads) {
-        const int64_t r = i / u.cols, c = i - r * u.cols;
-        float v = widen(G[r * u.ldg + c]);
-        if (u.M) {
-            const int64_t e = z * u.stride_m + r * u.ldm + c;
-            const float m = u.mu * u.M[e] + v;
-            u.M_out[e] = m;
-            v = u.nesterov ? v + u.mu * m : m;
+    for (int64_t i = (int64_t)blockIdx.x * kNormThreads + threadIdx.x; i < total; i += (int64_t)U * kNormBlocks * kNormThreads) {
+        float g[U][4], m[U][4];
+        int64_t at[U];
+        int count[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t e = i + (int64_t)k * kNormBlocks * kNormThreads;
+            const int64_t r = total <= 0xFFFFFFFFll ? (int64_t)((uint32_t)e / (uint32_t)groups) : e / groups, c = (e - r * groups) * 4;
+            count[k] = e < total ? (int)min(u.cols - c, (int64_t)4) : 0;
+            at[k] = z * u.stride_m + r * u.ldm + c;
+            load_some(G + (count[k] ? r * u.ldg + c : 0), count[k], g[k]);
+            if (u.M) load_some(u.M + (count[k] ? at[k] : 0), count[k], m[k]);
         }
-        s += (double)v * v;
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (u.M) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    m[k][j] = u.mu * m[k][j] + g[k][j];
+                    g[k][j] = u.nesterov ? g[k][j] + u.mu * m[k][j] : m[k][j];
+                }
+                if (count[k]) store_some(u.M_out + at[k], count[k], m[k]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s += (double)g[k][j] * g[k][j];
+        }
     }
-    s = block_sum(s, part);
+    s = block_sum<kNormThreads>(s, part);
     if (threadIdx.x == 0) partial[z * kNormBlocks + blockIdx.x] = s;
 }
 
@@ -155,7 +213,7 @@ __global__ __launch_bounds__(kThreads) void gp_ns_start(Update u, const double* 
             }
         }
     static_assert(kNormBlocks == kThreads, "one partial sum per thread");
-    const double norm = sqrt(block_sum(partial[z * kNormBlocks + threadIdx.x], part));
+    const double norm = sqrt(block_sum<kThreads>(partial[z * kNormBlocks + threadIdx.x], part));
     const float factor = (float)((double)scale / (norm + (double)eps));
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -183,7 +241,12 @@ struct Product {
     f16 *D, *Dt;
     int ldd, lddt;
     int symmetric;       // D and Dt are one plane: tiles on and above the diagonal will do
-    int tiles_m, tiles_n, tile_count;
+    int tiles_m, tiles_n, tile_count;  // of one matrix
+    int64_t workers;     // workgroups that share the call's steps
+    int64_t units;       // tiles of all matrices x steps
+    int split;           // their shares end inside tiles
+    float* partial;      // two tiles' sums per worker
+    int* arrived;        // per tile: workers whose sums are there (zero between launches)
     // the last product
     int64_t rows, cols;
     void* out;
@@ -202,30 +265,32 @@ __device__ __forceinline__ void wait_and_meet()
 typedef __attribute__((address_space(1))) const void* GlobalPtr;
 typedef __attribute__((address_space(3))) void* LdsPtr;
 
-// The workgroup's tile, false for none.  Tiles are numbered in bands of four rows, column by column (where D is symmetric, from the
-// band's first column on the diagonal; a tile below the diagonal is none), and each of the chip's eight parts, which share an L2 and
-// take every eighth workgroup, gets one stretch of the numbers: a square of tiles, whose lines it reads once.
-__host__ __device__ __forceinline__ int64_t tile_numbers(int tiles_m, int tiles_n, bool symmetric)
+// Tiles of a matrix are numbered in bands of four rows, column by column; where D is symmetric, those on and above the diagonal, a
+// band's triangle first.  Each of the chip's eight parts, which share an L2 and take every eighth workgroup, gets one stretch of the
+// numbers: a square of tiles, whose lines it reads once.
+constexpr int kBand = 4;
+int64_t tile_numbers(int64_t tiles_m, int64_t tiles_n, bool symmetric) { return symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n; }
+__device__ __forceinline__ void tile_at(const Product& a, int t, int& bi, int& bj)
 {
-    if (!symmetric) return (int64_t)tiles_m * tiles_n;
-    int64_t all = 0;
-    for (int b = 0; b < tiles_m; b += 4) all += (int64_t)(tiles_m - b < 4 ? tiles_m - b : 4) * (tiles_n - b);
-    return all;
-}
-__device__ __forceinline__ bool tile_of(const Product& a, int& bi, int& bj)
-{
-    const int per = gridDim.x / 8, all = a.tile_count;
-    int t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if (t >= all) return false;
-    for (int b = 0;; b += 4) {
-        const int rows = min(a.tiles_m - b, 4), first = a.symmetric ? b : 0, size = rows * (a.tiles_n - first);
-        if (t < size) {
-            bi = b + t % rows, bj = first + t / rows;
-            return !a.symmetric || bi <= bj;
+    for (int b = 0;; b += kBand) {
+        const int rows = min(a.tiles_m - b, kBand), corner = a.symmetric ? rows * (rows + 1) / 2 : 0;
+        const int first = a.symmetric ? b + rows : 0, size = corner + rows * (a.tiles_n - first);
+        if (t >= size) {
+            t -= size;
+            continue;
         }
-        t -= size;
+        if (t >= corner) {
+            t -= corner;
+            bi = b + t % rows, bj = first + t / rows;
+            return;
+        }
+        int c = 0;  // column c of the triangle has c + 1 tiles
+        while (t > c) t -= ++c;
+        bi = b + t, bj = b + c;
+        return;
     }
 }
+__device__ __forceinline__ int64_t stretched_block() { return (int64_t)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3); }
 template <typename TO>
 __device__ __forceinline__ void write_out(const Product& a, int64_t o, float v)
 {
@@ -236,7 +301,6 @@ __device__ __forceinline__ void write_out(const Product& a, int64_t o, float v)
         ((bf16_t*)a.out)[o] = __builtin_bit_cast(bf16_t, (__bf16)v);
 }
 // the first `count` of sixteen neighbours of a row, from any element's boundary
-typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef bf16_t v8b_any __attribute__((ext_vector_type(8), aligned(2)));
 template <typename TO>
 __device__ __forceinline__ void write_row(const Product& a, int64_t o, int count, const float (&v)[16])
@@ -283,141 +347,202 @@ __global__ __launch_bounds__(64 * WM * WN) void gp_ns_product(Product a)
     constexpr int RB = BM / WM / 32, CB = BN / WN / 32;  // blocks of a wave
     constexpr int kLoads = (BM + BN) / 8 / kWaves;       // eight lines per wave and load
     constexpr int kStage = (BM + BN) * 64;
+    constexpr int kThreadsHere = 64 * kWaves;
     extern __shared__ __align__(128) f16 lds[];
-    int bi, bj;
-    if (!tile_of(a, bi, bj)) return;
+    __shared__ int arrivals;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t base = (int64_t)blockIdx.z * a.stride;
-    // lines this lane takes part in loading, the first kLoadsP of P, the others of Q; those past the planes' ends repeat the last one (and
-    // are not used)
-    constexpr int kLoadsP = BM / 8 / kWaves;
-    static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0, "a load is of one plane");
-    const f16 *const p0 = a.P + base + (int64_t)bi * BM * a.ldp, *const q0 = a.Q + base + (int64_t)bj * BN * a.ldq;
-    unsigned offset[kLoads];
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-        const int line = (u * kWaves + wave) * 8 + (lane >> 3);
-        const unsigned piece = (unsigned)((lane & 7) ^ ((line >> 1) & 7)) * 8;
-        offset[u] = piece + (u < kLoadsP ? (unsigned)min(line, a.M - 1 - bi * BM) * (unsigned)a.ldp : (unsigned)min(line - BM, a.N - 1 - bj * BN) * (unsigned)a.ldq);
-    }
     const int steps = a.K / 32;
-    auto load = [&](int u, int stage, int step) {
-        const f16* const from = (u < kLoadsP ? p0 : q0) + (int64_t)min(step, steps - 1) * 64;  // (steps past the last are not used)
-        __builtin_amdgcn_global_load_lds((GlobalPtr)(from + offset[u]), (LdsPtr)(lds + stage * kStage + (u * kWaves + wave) * 512), 16, 0, 0);
-    };
     const int wr = wave / WN * (RB * 32), wc = wave % WN * (CB * 32);
     // where this lane reads: line wr + lane mod 32, pieces lane / 32 + 2 s (+ 4: second parts), s = 0, 1
     const int swap = (lane >> 1) & 7;
     const f16* const pl = lds + (wr + (lane & 31)) * 64;
     const f16* const ql = lds + (BM + wc + (lane & 31)) * 64;
-    v16f acc[RB][CB];
+    // the worker's share of all tiles' steps, tile by tile
+    const int64_t worker = stretched_block(), units = a.units;
+    if (worker >= a.workers) return;
+    auto begin = [&](int64_t w) { return a.split ? w * units / a.workers : w * steps; };
+    const int64_t end = begin(worker + 1);
+    for (int64_t unit = begin(worker); unit < end;) {
+        const int64_t tile = unit / steps;
+        const int k0 = (int)(unit - tile * steps), k1 = (int)min((int64_t)steps, k0 + end - unit);
+        unit += k1 - k0;
+        int bi, bj;
+        const int64_t z = tile / a.tile_count;
+        tile_at(a, (int)(tile - z * a.tile_count), bi, bj);
+        const int64_t base = z * a.stride;
+        // lines this lane takes part in loading, the first kLoadsP of P, the others of Q; those past the planes' ends repeat the last one (and
+        // are not used)
+        constexpr int kLoadsP = BM / 8 / kWaves;
+        static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0, "a load is of one plane");
+        const f16 *const p0 = a.P + base + (int64_t)bi * BM * a.ldp, *const q0 = a.Q + base + (int64_t)bj * BN * a.ldq;
+        unsigned offset[kLoads];
 #pragma unroll
-    for (int r = 0; r < RB; ++r)
-#pragma unroll
-        for (int c = 0; c < CB; ++c)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[r][c][i] = 0.0f;
-    // half a step's operands: 16 columns of the wave's lines, first and second parts
-    struct Half {
-        v8h p[2][RB], q[2][CB];
-    };
-    auto read = [&](Half& f, int stage, int s) {
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            const int at = (((lane >> 5) + 2 * s + 4 * part) ^ swap) * 8 + stage * kStage;
-#pragma unroll
-            for (int r = 0; r < RB; ++r) f.p[part][r] = *(const v8h*)(pl + r * 32 * 64 + at);
-#pragma unroll
-            for (int c = 0; c < CB; ++c) f.q[part][c] = *(const v8h*)(ql + c * 32 * 64 + at);
+        for (int u = 0; u < kLoads; ++u) {
+            const int line = (u * kWaves + wave) * 8 + (lane >> 3);
+            const unsigned piece = (unsigned)((lane & 7) ^ ((line >> 1) & 7)) * 8;
+            offset[u] = piece + (u < kLoadsP ? (unsigned)min(line, a.M - 1 - bi * BM) * (unsigned)a.ldp : (unsigned)min(line - BM, a.N - 1 - bj * BN) * (unsigned)a.ldq);
         }
-        __builtin_amdgcn_sched_barrier(0);  // (the reads go out before the products that they run beside)
-    };
-    // a half step's products; with them, one at a time (a wave that asks for all of them at once waits for the last before it goes on),
-    // the loads of a step into a stage
-    auto multiply = [&](const Half& f, auto loads, int stage, int step) {
-        constexpr int kProducts = 3 * RB * CB;
+        auto load = [&](int u, int stage, int step) {
+            const f16* const from = (u < kLoadsP ? p0 : q0) + (int64_t)min(step, k1 - 1) * 64;  // (steps past the last are not used)
+            __builtin_amdgcn_global_load_lds((GlobalPtr)(from + offset[u]), (LdsPtr)(lds + stage * kStage + (u * kWaves + wave) * 512), 16, 0, 0);
+        };
+        v16f acc[RB][CB];
 #pragma unroll
-        for (int x = 0; x < 3; ++x)
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int c = 0; c < CB; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[r][c][i] = 0.0f;
+        // half a step's operands: 16 columns of the wave's lines, first and second parts
+        struct Half {
+            v8h p[2][RB], q[2][CB];
+        };
+        auto read = [&](Half& f, int stage, int s) {
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                const int at = (((lane >> 5) + 2 * s + 4 * part) ^ swap) * 8 + stage * kStage;
+#pragma unroll
+                for (int r = 0; r < RB; ++r) f.p[part][r] = *(const v8h*)(pl + r * 32 * 64 + at);
+#pragma unroll
+                for (int c = 0; c < CB; ++c) f.q[part][c] = *(const v8h*)(ql + c * 32 * 64 + at);
+            }
+            __builtin_amdgcn_sched_barrier(0);  // (the reads go out before the products that they run beside)
+        };
+        // a half step's products; with them, one at a time (a wave that asks for all of them at once waits for the last before it goes on),
+        // the loads of a step into a stage
+        auto multiply = [&](const Half& f, auto loads, int stage, int step) {
+            constexpr int kProducts = 3 * RB * CB;
+#pragma unroll
+            for (int x = 0; x < 3; ++x)
+#pragma unroll
+                for (int r = 0; r < RB; ++r)
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) {
+                        acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.p[x == 0][r], f.q[x == 1][c], acc[r][c], 0, 0, 0);
+                        if constexpr (decltype(loads)::value) {
+                            const int i = (x * RB + r) * CB + c;
+#pragma unroll
+                            for (int u = 0; u < kLoads; ++u)
+                                if (u >= i * kLoads / kProducts && u < (i + 1) * kLoads / kProducts) {
+                                    __builtin_amdgcn_sched_barrier(0);
+                                    load(u, stage, step);
+                                    __builtin_amdgcn_sched_barrier(0);
+                                }
+                        }
+                    }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        // Every half step's reads run beside the half step before it; a stage is loaded again as soon as all waves have its second
+        // half in registers.
+        wait_and_meet<0>();  // (all are done with LDS)
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s)
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) load(u, s, k0 + s);
+        Half f0, f1;
+        wait_and_meet<(STAGES - 1) * kLoads>();
+        read(f0, 0, 0);
+        int stage = 0;
+        for (int k = k0; k < k1; ++k) {
+            read(f1, stage, 1);
+            multiply(f0, std::false_type{}, 0, 0);
+            wait_and_meet<(STAGES - 2) * kLoads>();  // the next step's lines are there
+            const int next = stage + 1 == STAGES ? 0 : stage + 1;
+            read(f0, next, 0);
+            multiply(f1, std::true_type{}, stage, k + STAGES);
+            stage = next;
+        }
+        // The sums, 32 x 32 at a time, turned through LDS so that a lane has 16 neighbours of a row (and, for Dt, of a column): requests
+        // of 16 bytes instead of 2.  The stages are free behind this barrier: no load is on its way, and every wave has read its last.
+        wait_and_meet<0>();
+        if (k1 - k0 < steps) {
+            // A tile of several workers: each leaves its sums in memory, and whoever comes last adds them up, in the workers' order whoever
+            // that is, and goes on.  Nobody waits for another.
+            // (Sums go through memory by device-wide atomic stores and loads, which pass by the L2s that the chip's parts do not share: a fence
+            // instead would write back and empty these, 10 to 20 us where all workgroups do it.)
+            auto slot = [&](int64_t w) { return (uint64_t*)a.partial + ((w * 2 + (begin(w) <= tile * steps)) * (BM * BN / 2) + threadIdx.x); };
+            uint64_t* const own = slot(worker);
+#pragma unroll
+            for (int n = 0; n < RB * CB; ++n)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const v2f x = {acc[n / CB][n % CB][2 * q], acc[n / CB][n % CB][2 * q + 1]};
+                    __hip_atomic_store(own + (n * 8 + q) * kThreadsHere, __builtin_bit_cast(uint64_t, x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
+            int64_t w0 = tile * steps * a.workers / units;  // the first and, at last, the one behind the last worker of the tile
+            while (begin(w0 + 1) <= tile * steps) ++w0;
+            int64_t w1 = w0 + 1;
+            while (begin(w1) < (tile + 1) * steps) ++w1;
+            wait_and_meet<0>();  // (all of the workgroup's stores are done before it counts as arrived)
+            if (threadIdx.x == 0) arrivals = __hip_atomic_fetch_add(a.arrived + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
+            __syncthreads();
+            if (arrivals < w1 - w0) continue;
+            if (threadIdx.x == 0) __hip_atomic_store(a.arrived + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
             for (int r = 0; r < RB; ++r)
 #pragma unroll
-                for (int c = 0; c < CB; ++c) {
-                    acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.p[x == 0][r], f.q[x == 1][c], acc[r][c], 0, 0, 0);
-                    if constexpr (decltype(loads)::value) {
-                        const int i = (x * RB + r) * CB + c;
+                for (int c = 0; c < CB; ++c)
 #pragma unroll
-                        for (int u = 0; u < kLoads; ++u)
-                            if (u >= i * kLoads / kProducts && u < (i + 1) * kLoads / kProducts) {
-                                __builtin_amdgcn_sched_barrier(0);
-                                load(u, stage, step);
-                                __builtin_amdgcn_sched_barrier(0);
-                            }
+                    for (int i = 0; i < 16; ++i) acc[r][c][i] = 0.0f;
+            for (int64_t w = w0; w < w1; ++w) {
+                uint64_t* const from = slot(w);
+                constexpr int kAtOnce = RB * CB % 4 == 0 ? 4 : RB * CB % 3 == 0 ? 3 : RB * CB % 2 == 0 ? 2 : 1;  // blocks on their way
+#pragma unroll
+                for (int n = 0; n < RB * CB; n += kAtOnce) {
+                    uint64_t x[8 * kAtOnce];
+#pragma unroll
+                    for (int q = 0; q < 8 * kAtOnce; ++q) x[q] = __hip_atomic_load(from + (n * 8 + q) * kThreadsHere, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int q = 0; q < 8 * kAtOnce; ++q) {
+                        const v2f y = __builtin_bit_cast(v2f, x[q]);
+                        v16f& to = acc[(n + q / 8) / CB][(n + q / 8) % CB];
+                        to[2 * (q % 8)] += y[0], to[2 * (q % 8) + 1] += y[1];
                     }
                 }
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    // Every half step's reads run beside the half step before it; a stage is loaded again as soon as all waves have its second
-    // half in registers.
+            }
+        }
+        float* const turn = (float*)lds + wave * (32 * 33);
+        const int lr = lane >> 1, lc = (lane & 1) * 16;
+        v8h e[2][4];  // of this block and the next: first and second parts of 16 neighbours
+        auto fetch = [&](int n) {
+            const int r0 = bi * BM + wr + n / CB * 32, c0 = bj * BN + wc + n % CB * 32;
+            if (!a.E || r0 >= a.M || c0 >= a.N) return;
+            const f16* const p = a.E + base + (int64_t)(r0 + lr) * a.lde + place(c0 + lc);
+            e[n & 1][0] = *(const v8h*)p, e[n & 1][1] = *(const v8h*)(p + 8);
+            e[n & 1][2] = *(const v8h*)(p + kParts), e[n & 1][3] = *(const v8h*)(p + kParts + 8);
+        };
+        fetch(0);
 #pragma unroll
-    for (int s = 0; s < STAGES; ++s)
+        for (int n = 0; n < RB * CB; ++n) {
+            if (n + 1 < RB * CB) fetch(n + 1);
+            const int rb = n / CB, cb = n % CB;
+            const int r0 = bi * BM + wr + rb * 32, c0 = bj * BN + wc + cb * 32;
+            if (r0 >= a.M || c0 >= a.N) continue;
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) load(u, s, s);
-    Half f0, f1;
-    wait_and_meet<(STAGES - 1) * kLoads>();
-    read(f0, 0, 0);
-    int stage = 0;
-    for (int k = 0; k < steps; ++k) {
-        read(f1, stage, 1);
-        multiply(f0, std::false_type{}, 0, 0);
-        wait_and_meet<(STAGES - 2) * kLoads>();  // the next step's lines are there
-        const int next = stage + 1 == STAGES ? 0 : stage + 1;
-        read(f0, next, 0);
-        multiply(f1, std::true_type{}, stage, k + STAGES);
-        stage = next;
-    }
-    // The sums, 32 x 32 at a time, turned through LDS so that a lane has 16 neighbours of a row (and, for Dt, of a column): requests
-    // of 16 bytes instead of 2.  The stages are free behind this barrier: no load is on its way, and every wave has read its last.
-    wait_and_meet<0>();
-    float* const turn = (float*)lds + wave * (32 * 33);
-    const int lr = lane >> 1, lc = (lane & 1) * 16;
-    v8h e[2][4];  // of this block and the next: first and second parts of 16 neighbours
-    auto fetch = [&](int n) {
-        const int r0 = bi * BM + wr + n / CB * 32, c0 = bj * BN + wc + n % CB * 32;
-        if (!a.E || r0 >= a.M || c0 >= a.N) return;
-        const f16* const p = a.E + base + (int64_t)(r0 + lr) * a.lde + place(c0 + lc);
-        e[n & 1][0] = *(const v8h*)p, e[n & 1][1] = *(const v8h*)(p + 8);
-        e[n & 1][2] = *(const v8h*)(p + kParts), e[n & 1][3] = *(const v8h*)(p + kParts + 8);
-    };
-    fetch(0);
-#pragma unroll
-    for (int n = 0; n < RB * CB; ++n) {
-        if (n + 1 < RB * CB) fetch(n + 1);
-        const int rb = n / CB, cb = n % CB;
-        const int r0 = bi * BM + wr + rb * 32, c0 = bj * BN + wc + cb * 32;
-        if (r0 >= a.M || c0 >= a.N) continue;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) turn[((i >> 2) * 8 + (lane >> 5) * 4 + (i & 3)) * 33 + (lane & 31)] = acc[rb][cb][i];
-        __builtin_amdgcn_wave_barrier();
-        float v[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = turn[lr * 33 + lc + i] * a.alpha;
-        if (a.E)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] += a.beta * ((float)e[n & 1][i >> 3][i & 7] + (float)e[n & 1][2 + (i >> 3)][i & 7]);
-        __builtin_amdgcn_wave_barrier();
-        if constexpr (LAST) {
-            if (r0 + lr >= a.rows) continue;
-            write_row<TO>(a, blockIdx.z * a.stride_o + (int64_t)(r0 + lr) * a.ldo + c0 + lc, (int)min(a.cols - c0 - lc, (int64_t)16), v);
-        } else {
-            store_parts16(a.D + base + (int64_t)(r0 + lr) * a.ldd + place(c0 + lc), v);
-            if (a.symmetric && bi == bj) continue;  // (the tile holds both halves)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) turn[lr * 33 + lc + i] = v[i];
+            for (int i = 0; i < 16; ++i) turn[((i >> 2) * 8 + (lane >> 5) * 4 + (i & 3)) * 33 + (lane & 31)] = acc[rb][cb][i];
             __builtin_amdgcn_wave_barrier();
+            float v[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = turn[(lc + i) * 33 + lr];
+            for (int i = 0; i < 16; ++i) v[i] = turn[lr * 33 + lc + i] * a.alpha;
+            if (a.E)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] += a.beta * ((float)e[n & 1][i >> 3][i & 7] + (float)e[n & 1][2 + (i >> 3)][i & 7]);
             __builtin_amdgcn_wave_barrier();
-            store_parts16(a.Dt + base + (int64_t)(c0 + lr) * a.lddt + place(r0 + lc), v);
+            if constexpr (LAST) {
+                if (r0 + lr >= a.rows) continue;
+                write_row<TO>(a, z * a.stride_o + (int64_t)(r0 + lr) * a.ldo + c0 + lc, (int)min(a.cols - c0 - lc, (int64_t)16), v);
+            } else {
+                store_parts16(a.D + base + (int64_t)(r0 + lr) * a.ldd + place(c0 + lc), v);
+                if (a.symmetric && bi == bj) continue;  // (the tile holds both halves)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) turn[lr * 33 + lc + i] = v[i];
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = turn[(lc + i) * 33 + lr];
+                __builtin_amdgcn_wave_barrier();
+                store_parts16(a.Dt + base + (int64_t)(c0 + lr) * a.lddt + place(r0 + lc), v);
+            }
         }
     }
 }
@@ -432,7 +557,9 @@ __global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product 
 {
     __shared__ __align__(16) float part[kSmallWaves][32][36];
     int bi, bj;
-    if (!tile_of(a, bi, bj)) return;
+    const int64_t t = stretched_block();
+    if (t >= a.tile_count) return;
+    tile_at(a, (int)t, bi, bj);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t base = (int64_t)blockIdx.z * a.stride;
     const int r0 = bi * 32, c0 = bj * 32;
@@ -523,8 +650,6 @@ struct Panel {
     int tall;
     Product last;
 };
-
-typedef float v4f __attribute__((ext_vector_type(4)));
 
 template <int M, typename TO, bool LAST>
 __global__ __launch_bounds__(4 * M) void gp_ns_panel(Panel a)
@@ -624,22 +749,77 @@ int exponent_for(double bound)
 
 // ---- the call ----------------------------------------------------------------------------------------
 
+// How a product is cut: tiles of 32 (gp_ns_product_small), 64, 128, 192 or 256, and how many workgroups share their steps: as many as there
+// are tiles, each a whole one, or up to one per compute unit, with equal shares that end inside tiles (of 64 or 128: larger tiles'
+// sums take longer to hand over than that saves).  The cut of the least time by what its parts take, in us as measured: a step of 32
+// columns where few compute units are at work and where all are (power is what the large ones run out of), a tile's end, and,
+// where tiles are shared, handing over one worker's sums.  us a launch, model / measured:
+//     m x n, K                  64          128          192          256
+//   1024 x 1024, 1024       14 / 16      26 / 26      44 / 48      61 / 79
+//   2048 x 2048, 2048       71 / 72      59 / 60      88 / 87     121 / 138
+//   the same, X X^T         53 / 54      50 / 50      82 / 78     112 / 131
+//   4096 x 4096, 4096      537 / 500    442 / 396    394 / 400    345 / 350
+//   the same, X X^T        311 / 275    287 / 259    196 / 198    273 / 262
+struct Cut {
+    int side;
+    int64_t workers;
+    bool split;
+    double us;
+};
+constexpr int kUnits = 256;  // compute units
+Cut choose_cut(int64_t m, int64_t n, int64_t k, bool symmetric, int64_t count)
+{
+    const int64_t steps = k / 32;
+    auto tiles = [&](int64_t side) { return tile_numbers((m + side - 1) / side, (n + side - 1) / side, symmetric) * count; };
+    Cut best{32, tiles(32), false, 1e30};
+    if (best.workers <= 4 * kUnits) best.us = (double)((best.workers + kUnits - 1) / kUnits) * (2.5 + 0.22 * steps);
+    struct Kind {
+        int side;
+        double few, all, finish, hand_over;
+    };
+    static const Kind kinds[] = {{256, 1.4, 2.6, 12.0, 0.0}, {192, 1.0, 1.46, 10.0, 0.0}, {128, 0.5, 0.8, 8.0, 0.9}, {64, 0.3, 0.36, 4.0, 0.5}};
+    for (const Kind& c : kinds) {
+        const int64_t T = tiles(c.side);
+        auto step = [&](int64_t units) { return c.few + (c.all - c.few) * (double)units / kUnits; };
+        // rounds of workgroups; two of those with tiles of 64 share a compute unit
+        const int64_t full = c.side == 64 ? 2 * kUnits : kUnits, rest = T % full;
+        double us = (double)(T / full) * (steps * (c.side == 64 ? 0.52 : c.all) + c.finish);
+        if (rest) us += steps * (rest > kUnits ? 0.52 : step(rest)) + c.finish;
+        if (us < best.us) best = {c.side, T, false, us};
+        if (c.hand_over == 0.0 || T > kMaxShared) continue;
+        for (int64_t W = kUnits; W >= 16; W /= 2) {
+            const double share = (double)T * steps / W;
+            if (share < 2.0 || T % W == 0) continue;
+            us = share * step(W) + c.finish * (std::ceil(share / steps) + 1.0) + c.hand_over * (std::min((double)W, steps / share) + 2.0);
+            if (us < best.us) best = {c.side, W, true, us};
+        }
+    }
+    return best;
+}
+int64_t cut_bytes(const Cut& c) { return c.split ? c.workers * 2 * c.side * c.side * 4 : 0; }
+
 struct NsLayout {
     int64_t m, n;               // shorter and longer side, of whole tiles
+    Cut gram, square, update;   // of a step's three products
     int64_t X[2], Xt[2], A, B;  // planes of a matrix, in halves
     int64_t stride;             // halves
-    int64_t planes, total;      // bytes
+    int64_t arrived, partial, planes, total;  // bytes
 };
 NsLayout ns_layout(int64_t rows, int64_t cols, int64_t count)
 {
     NsLayout l;
     l.m = (std::min(rows, cols) + kTile - 1) / kTile * kTile;
     l.n = (std::max(rows, cols) + kTile - 1) / kTile * kTile;
+    l.gram = choose_cut(l.m, l.m, l.n, true, count);
+    l.square = choose_cut(l.m, l.m, l.m, true, count);
+    l.update = choose_cut(l.m, l.n, l.m, false, count);
     int64_t at = 0;
     for (int i = 0; i < 2; ++i) l.X[i] = at, l.Xt[i] = at + 2 * l.m * l.n, at += 4 * l.m * l.n;
     l.A = at, l.B = at + 2 * l.m * l.m, at += 4 * l.m * l.m;
     l.stride = at;
-    l.planes = (count * kNormBlocks * 8 + 255) / 256 * 256;
+    l.arrived = (count * kNormBlocks * 8 + 255) / 256 * 256;
+    l.partial = l.arrived + kMaxShared * 4;
+    l.planes = l.partial + std::max(cut_bytes(l.gram), l.m <= 128 ? 0 : std::max(cut_bytes(l.square), cut_bytes(l.update)));
     l.total = l.planes + count * l.stride * 2;
     return l;
 }
@@ -663,52 +843,36 @@ gp_status check_shape(int64_t rows, int64_t cols, int64_t count)
     return GP_OK;
 }
 
-unsigned tile_grid(Product& a, int bm, int bn)
+template <int SIDE, int WM, int WN, int STAGES, typename TO, bool LAST>
+gp_status launch_tiles(const Product& a, int64_t count, hipStream_t stream)
 {
-    a.tiles_m = (a.M + bm - 1) / bm, a.tiles_n = (a.N + bn - 1) / bn;
-    a.tile_count = (int)tile_numbers(a.tiles_m, a.tiles_n, a.symmetric);
-    return (unsigned)((a.tile_count + 7) / 8 * 8);
-}
-
-template <int BM, int BN, int WM, int WN, int STAGES, typename TO, bool LAST>
-gp_status launch_tiles(Product a, int64_t count, hipStream_t stream)
-{
-    constexpr size_t lds = STAGES * (BM + BN) * 128;
+    constexpr size_t lds = STAGES * 2 * SIDE * 128;
     if constexpr (lds > 65536) {
-        gp_status st = raise_lds<&gp_ns_product<BM, BN, WM, WN, STAGES, TO, LAST>>(lds);
+        gp_status st = raise_lds<&gp_ns_product<SIDE, SIDE, WM, WN, STAGES, TO, LAST>>(lds);
         if (st != GP_OK) return st;
     }
-    const dim3 grid(tile_grid(a, BM, BN), 1, (unsigned)count);
     profile_begin("gp_ns_product", stream);
-    hipLaunchKernelGGL((gp_ns_product<BM, BN, WM, WN, STAGES, TO, LAST>), grid, dim3(64 * WM * WN), lds, stream, a);
+    hipLaunchKernelGGL((gp_ns_product<SIDE, SIDE, WM, WN, STAGES, TO, LAST>), dim3((unsigned)((a.workers + 7) / 8 * 8)), dim3(64 * WM * WN), lds, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     return GP_OK;
 }
 
 template <typename TO, bool LAST>
-gp_status launch_product(const Product& a, int64_t count, hipStream_t stream)
+gp_status launch_product(Product a, const Cut& cut, int64_t count, hipStream_t stream)
 {
-    const int small_max = 512;
-    auto tiles = [&](int64_t side) {
-        const int64_t tm = (a.M + side - 1) / side, tn = (a.N + side - 1) / side;
-        return (a.symmetric ? tn * (tn + 1) / 2 : tm * tn) * count;
-    };
-    const int forced = getenv("NS_TILE") ? atoi(getenv("NS_TILE")) : 0;
-    if (forced ? forced == 32 : tiles(32) <= small_max) {
-        Product p = a;
-        const dim3 grid(tile_grid(p, 32, 32), 1, (unsigned)count);
-        profile_begin("gp_ns_product", stream);
-        hipLaunchKernelGGL((gp_ns_product_small<TO, LAST>), grid, dim3(64 * kSmallWaves), 0, stream, p);
-        profile_end(stream);
-        GP_HIP(hipGetLastError());
-        return GP_OK;
-    }
-    const int side = forced ? forced : tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
-    if (side == 256) return launch_tiles<256, 256, 2, 2, 2, TO, LAST>(a, count, stream);
-    if (side == 128) return launch_tiles<128, 128, 2, 4, 4, TO, LAST>(a, count, stream);
-    if (side == 129) return launch_tiles<128, 128, 2, 2, 2, TO, LAST>(a, count, stream);
-    return launch_tiles<64, 64, 2, 2, 4, TO, LAST>(a, count, stream);
+    a.tiles_m = (a.M + cut.side - 1) / cut.side, a.tiles_n = (a.N + cut.side - 1) / cut.side;
+    a.tile_count = (int)tile_numbers(a.tiles_m, a.tiles_n, a.symmetric);
+    a.workers = cut.workers, a.split = cut.split, a.units = a.tile_count * count * (a.K / 32);
+    if (cut.side == 256) return launch_tiles<256, 2, 2, 2, TO, LAST>(a, count, stream);
+    if (cut.side == 192) return launch_tiles<192, 2, 2, 3, TO, LAST>(a, count, stream);
+    if (cut.side == 128) return launch_tiles<128, 2, 4, 4, TO, LAST>(a, count, stream);
+    if (cut.side == 64) return launch_tiles<64, 2, 2, 4, TO, LAST>(a, count, stream);
+    profile_begin("gp_ns_product", stream);
+    hipLaunchKernelGGL((gp_ns_product_small<TO, LAST>), dim3((unsigned)((a.tile_count + 7) / 8 * 8), 1, (unsigned)count), dim3(64 * kSmallWaves), 0, stream, a);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    return GP_OK;
 }
 
 template <typename TO, bool LAST>
@@ -745,13 +909,20 @@ gp_status newton_schulz(const Update& u, gp_dtype dtype, int64_t count, int32_t 
         return fail(GP_ERR_INVALID_ARG, "need a workspace of %lld bytes on a 256-byte boundary", (long long)l.total);
     double* const partial = (double*)workspace;
     f16* const ws = (f16*)((char*)workspace + l.planes);
+    int* const arrived = (int*)((char*)workspace + l.arrived);
     const bool tall = u.rows > u.cols;
 
+    const dim3 norm_grid(kNormBlocks, (unsigned)count);
+    const bool small = u.rows * ((u.cols + 3) / 4) <= 4 * kNormBlocks * kThreads;
     profile_begin("gp_ns_norms", stream);
-    if (dtype == GP_F32)
-        hipLaunchKernelGGL(gp_ns_norms<float>, dim3(kNormBlocks, (unsigned)count), dim3(kThreads), 0, stream, u, partial);
+    if (dtype == GP_F32 && small)
+        hipLaunchKernelGGL((gp_ns_norms<kThreads, float>), norm_grid, dim3(kThreads), 0, stream, u, partial, arrived);
+    else if (dtype == GP_F32)
+        hipLaunchKernelGGL((gp_ns_norms<1024, float>), norm_grid, dim3(1024), 0, stream, u, partial, arrived);
+    else if (small)
+        hipLaunchKernelGGL((gp_ns_norms<kThreads, bf16_t>), norm_grid, dim3(kThreads), 0, stream, u, partial, arrived);
     else
-        hipLaunchKernelGGL(gp_ns_norms<bf16_t>, dim3(kNormBlocks, (unsigned)count), dim3(kThreads), 0, stream, u, partial);
+        hipLaunchKernelGGL((gp_ns_norms<1024, bf16_t>), norm_grid, dim3(1024), 0, stream, u, partial, arrived);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     {
@@ -772,11 +943,11 @@ gp_status newton_schulz(const Update& u, gp_dtype dtype, int64_t count, int32_t 
         const float* const p = coeff ? coeff + 3 * k : kDefaultCoeff;
         f16 *const X = ws + l.X[k & 1], *const Xt = ws + l.Xt[k & 1], *const A = ws + l.A, *const B = ws + l.B;
         Product a{};
-        a.stride = l.stride;
+        a.stride = l.stride, a.arrived = arrived, a.partial = (float*)((char*)workspace + l.partial);
         a.P = a.Q = X, a.ldp = a.ldq = 2 * n, a.M = a.N = m, a.K = n;
         a.alpha = std::ldexp(1.0f, ea[k] - 2 * ex[k]);
         a.D = a.Dt = A, a.ldd = a.lddt = 2 * m, a.symmetric = 1;
-        gp_status st = launch_product<float, false>(a, count, stream);
+        gp_status st = launch_product<float, false>(a, l.gram, count, stream);
         if (st != GP_OK) return st;
         const bool last_step = k == steps - 1;
         if (m <= 128) {
@@ -795,20 +966,20 @@ gp_status newton_schulz(const Update& u, gp_dtype dtype, int64_t count, int32_t 
         a.P = a.Q = a.E = A, a.ldp = a.ldq = a.lde = 2 * m, a.K = m;
         a.alpha = std::ldexp(p[2], eb[k] - 2 * ea[k]), a.beta = std::ldexp(p[1], eb[k] - ea[k]);
         a.D = a.Dt = B;
-        if ((st = launch_product<float, false>(a, count, stream)) != GP_OK) return st;
+        if ((st = launch_product<float, false>(a, l.square, count, stream)) != GP_OK) return st;
         a.symmetric = 0;
         if (!last_step) {
             const int next = ex[k + 1] - ex[k];
             a.P = B, a.Q = Xt, a.N = n, a.E = X, a.lde = 2 * n;
             a.alpha = std::ldexp(1.0f, next - eb[k]), a.beta = std::ldexp(p[0], next);
             a.D = ws + l.X[(k + 1) & 1], a.ldd = 2 * n, a.Dt = ws + l.Xt[(k + 1) & 1], a.lddt = 2 * m;
-            if ((st = launch_product<float, false>(a, count, stream)) != GP_OK) return st;
+            if ((st = launch_product<float, false>(a, l.update, count, stream)) != GP_OK) return st;
         } else {  // in the orientation of the caller's matrix
             a.P = tall ? Xt : B, a.Q = tall ? B : Xt, a.M = tall ? n : m, a.N = tall ? m : n;
             a.E = tall ? Xt : X, a.lde = tall ? 2 * m : 2 * n;
             a.alpha = std::ldexp(1.0f, -ex[k] - eb[k]), a.beta = std::ldexp(p[0], -ex[k]);
             a.rows = u.rows, a.cols = u.cols, a.out = out, a.ldo = ldo, a.stride_o = stride_o, a.W = W, a.keep = keep, a.lr = lr;
-            st = out_dtype == GP_F32 ? launch_product<float, true>(a, count, stream) : launch_product<bf16_t, true>(a, count, stream);
+            st = out_dtype == GP_F32 ? launch_product<float, true>(a, l.update, count, stream) : launch_product<bf16_t, true>(a, l.update, count, stream);
             if (st != GP_OK) return st;
         }
     }

@@ -419,3 +419,29 @@ def test_another_stream_than_the_current_one():
     side.synchronize()
     assert same_bits(rows, want[0]) and same_bits(grad, want[1]) and same_bits(O, want[2])
     del filler
+
+
+@pytest.mark.parametrize("shape,count", [((64, 8192), 1), (((256, 4096)), 1), ((1000, 4097), 1), ((768, 768), 4), ((2048, 2048), 1), ((2300, 1900), 1),
+                                         ((1024, 4096), 2), ((4096, 4096), 1)])
+def test_orthogonalize_large(shape, count):
+    """Every tile and every way to share one: against fp64 on the GPU; twice, with the same bits."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    k = min(shape) // 8
+    G = 1e-3 * (torch.randn(count, shape[0], k, generator=gen, device="cuda") @ torch.randn(count, k, shape[1], generator=gen, device="cuda")
+                + 0.2 * torch.randn(count, *shape, generator=gen, device="cuda"))
+    got = gp.orthogonalize_tensors(G)
+    assert same_bits(got, gp.orthogonalize_tensors(G))
+    a, b, c = training.COEFF
+    slope = np.abs([a + 3 * b * s ** 2 + 5 * c * s ** 4 for s in np.linspace(0.0, 1.25, 2001)]).max()
+    for i in range(count):
+        X = G[i].double() if shape[0] <= shape[1] else G[i].double().t().contiguous()
+        X = X / (X.norm() + 1e-7)
+        norms = [float(X.norm())]
+        for _ in range(5):
+            A = X @ X.t().contiguous()
+            X = a * X + (b * A + c * (A @ A)) @ X
+            norms.append(float(X.norm()))
+        want = X if shape[0] <= shape[1] else X.t()
+        tol = 4 * 2.0 ** -22 * sum(slope ** (5 - k) * norms[k] for k in range(6)) / norms[-1]
+        assert float((got[i].double() - want).norm()) <= tol * norms[-1]
