@@ -32,7 +32,7 @@ constexpr int kThreads = 256;
 constexpr int kTile = 64;          // sides of planes are multiples of it; what is added is zero
 constexpr int kNormBlocks = 256;   // partial sums of squares per matrix
 constexpr int kMaxSteps = 32;
-constexpr int kMaxShared = 1024;    // tiles of a product that several workgroups may share
+constexpr int kMaxShared = 256;     // tiles of a product that several workgroups may share
 
 typedef unsigned short bf16_t;
 typedef _Float16 f16;
@@ -242,11 +242,10 @@ struct Product {
     int ldd, lddt;
     int symmetric;       // D and Dt are one plane: tiles on and above the diagonal will do
     int tiles_m, tiles_n, tile_count;  // of one matrix
-    int64_t workers;     // workgroups that share the call's steps
-    int64_t units;       // tiles of all matrices x steps
-    int split;           // their shares end inside tiles
-    float* partial;      // two tiles' sums per worker
-    int* arrived;        // per tile: workers whose sums are there (zero between launches)
+    int64_t all_tiles;   // of all matrices of the call
+    int parts;           // workgroups to a tile: each sums over a part of the columns
+    float* partial;      // a tile's sums per workgroup
+    int* arrived;        // per tile: workgroups whose sums are there (zero between launches)
     // the last product
     int64_t rows, cols;
     void* out;
@@ -357,192 +356,179 @@ __global__ __launch_bounds__(64 * WM * WN) void gp_ns_product(Product a)
     const int swap = (lane >> 1) & 7;
     const f16* const pl = lds + (wr + (lane & 31)) * 64;
     const f16* const ql = lds + (BM + wc + (lane & 31)) * 64;
-    // the worker's share of all tiles' steps, tile by tile
-    const int64_t worker = stretched_block(), units = a.units;
-    if (worker >= a.workers) return;
-    auto begin = [&](int64_t w) { return a.split ? w * units / a.workers : w * steps; };
-    const int64_t end = begin(worker + 1);
-    for (int64_t unit = begin(worker); unit < end;) {
-        const int64_t tile = unit / steps;
-        const int k0 = (int)(unit - tile * steps), k1 = (int)min((int64_t)steps, k0 + end - unit);
-        unit += k1 - k0;
-        int bi, bj;
-        const int64_t z = tile / a.tile_count;
-        tile_at(a, (int)(tile - z * a.tile_count), bi, bj);
-        const int64_t base = z * a.stride;
-        // lines this lane takes part in loading, the first kLoadsP of P, the others of Q; those past the planes' ends repeat the last one (and
-        // are not used)
-        constexpr int kLoadsP = BM / 8 / kWaves;
-        static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0, "a load is of one plane");
-        const f16 *const p0 = a.P + base + (int64_t)bi * BM * a.ldp, *const q0 = a.Q + base + (int64_t)bj * BN * a.ldq;
-        unsigned offset[kLoads];
+    constexpr bool kShared = BM * BN <= 128 * 128;  // (choose_cut)
+    const int64_t worker = stretched_block();
+    if (worker >= a.all_tiles * a.parts) return;
+    const int part = kShared ? (int)(worker / a.all_tiles) : 0;
+    const int64_t tile = kShared ? worker - part * a.all_tiles : worker;
+    const int k0 = kShared ? (int)((int64_t)steps * part / a.parts) : 0, k1 = kShared ? (int)((int64_t)steps * (part + 1) / a.parts) : steps;
+    int bi, bj;
+    const int64_t z = tile / a.tile_count;
+    tile_at(a, (int)(tile - z * a.tile_count), bi, bj);
+    const int64_t base = z * a.stride;
+    // lines this lane takes part in loading, the first kLoadsP of P, the others of Q; those past the planes' ends repeat the last one (and
+    // are not used)
+    constexpr int kLoadsP = BM / 8 / kWaves;
+    static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0, "a load is of one plane");
+    const f16 *const p0 = a.P + base + (int64_t)bi * BM * a.ldp, *const q0 = a.Q + base + (int64_t)bj * BN * a.ldq;
+    unsigned offset[kLoads];
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) {
-            const int line = (u * kWaves + wave) * 8 + (lane >> 3);
-            const unsigned piece = (unsigned)((lane & 7) ^ ((line >> 1) & 7)) * 8;
-            offset[u] = piece + (u < kLoadsP ? (unsigned)min(line, a.M - 1 - bi * BM) * (unsigned)a.ldp : (unsigned)min(line - BM, a.N - 1 - bj * BN) * (unsigned)a.ldq);
+    for (int u = 0; u < kLoads; ++u) {
+        const int line = (u * kWaves + wave) * 8 + (lane >> 3);
+        const unsigned piece = (unsigned)((lane & 7) ^ ((line >> 1) & 7)) * 8;
+        offset[u] = piece + (u < kLoadsP ? (unsigned)min(line, a.M - 1 - bi * BM) * (unsigned)a.ldp : (unsigned)min(line - BM, a.N - 1 - bj * BN) * (unsigned)a.ldq);
+    }
+    auto load = [&](int u, int stage, int step) {
+        const f16* const from = (u < kLoadsP ? p0 : q0) + (int64_t)min(step, k1 - 1) * 64;  // (steps past the last are not used)
+        __builtin_amdgcn_global_load_lds((GlobalPtr)(from + offset[u]), (LdsPtr)(lds + stage * kStage + (u * kWaves + wave) * 512), 16, 0, 0);
+    };
+    v16f acc[RB][CB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[r][c][i] = 0.0f;
+    // half a step's operands: 16 columns of the wave's lines, first and second parts
+    struct Half {
+        v8h p[2][RB], q[2][CB];
+    };
+    auto read = [&](Half& f, int stage, int s) {
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const int at = (((lane >> 5) + 2 * s + 4 * part) ^ swap) * 8 + stage * kStage;
+#pragma unroll
+            for (int r = 0; r < RB; ++r) f.p[part][r] = *(const v8h*)(pl + r * 32 * 64 + at);
+#pragma unroll
+            for (int c = 0; c < CB; ++c) f.q[part][c] = *(const v8h*)(ql + c * 32 * 64 + at);
         }
-        auto load = [&](int u, int stage, int step) {
-            const f16* const from = (u < kLoadsP ? p0 : q0) + (int64_t)min(step, k1 - 1) * 64;  // (steps past the last are not used)
-            __builtin_amdgcn_global_load_lds((GlobalPtr)(from + offset[u]), (LdsPtr)(lds + stage * kStage + (u * kWaves + wave) * 512), 16, 0, 0);
-        };
-        v16f acc[RB][CB];
+        __builtin_amdgcn_sched_barrier(0);  // (the reads go out before the products that they run beside)
+    };
+    // a half step's products; with them, one at a time (a wave that asks for all of them at once waits for the last before it goes on),
+    // the loads of a step into a stage
+    auto multiply = [&](const Half& f, auto loads, int stage, int step) {
+        constexpr int kProducts = 3 * RB * CB;
 #pragma unroll
-        for (int r = 0; r < RB; ++r)
-#pragma unroll
-            for (int c = 0; c < CB; ++c)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[r][c][i] = 0.0f;
-        // half a step's operands: 16 columns of the wave's lines, first and second parts
-        struct Half {
-            v8h p[2][RB], q[2][CB];
-        };
-        auto read = [&](Half& f, int stage, int s) {
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                const int at = (((lane >> 5) + 2 * s + 4 * part) ^ swap) * 8 + stage * kStage;
-#pragma unroll
-                for (int r = 0; r < RB; ++r) f.p[part][r] = *(const v8h*)(pl + r * 32 * 64 + at);
-#pragma unroll
-                for (int c = 0; c < CB; ++c) f.q[part][c] = *(const v8h*)(ql + c * 32 * 64 + at);
-            }
-            __builtin_amdgcn_sched_barrier(0);  // (the reads go out before the products that they run beside)
-        };
-        // a half step's products; with them, one at a time (a wave that asks for all of them at once waits for the last before it goes on),
-        // the loads of a step into a stage
-        auto multiply = [&](const Half& f, auto loads, int stage, int step) {
-            constexpr int kProducts = 3 * RB * CB;
-#pragma unroll
-            for (int x = 0; x < 3; ++x)
-#pragma unroll
-                for (int r = 0; r < RB; ++r)
-#pragma unroll
-                    for (int c = 0; c < CB; ++c) {
-                        acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.p[x == 0][r], f.q[x == 1][c], acc[r][c], 0, 0, 0);
-                        if constexpr (decltype(loads)::value) {
-                            const int i = (x * RB + r) * CB + c;
-#pragma unroll
-                            for (int u = 0; u < kLoads; ++u)
-                                if (u >= i * kLoads / kProducts && u < (i + 1) * kLoads / kProducts) {
-                                    __builtin_amdgcn_sched_barrier(0);
-                                    load(u, stage, step);
-                                    __builtin_amdgcn_sched_barrier(0);
-                                }
-                        }
-                    }
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        // Every half step's reads run beside the half step before it; a stage is loaded again as soon as all waves have its second
-        // half in registers.
-        wait_and_meet<0>();  // (all are done with LDS)
-#pragma unroll
-        for (int s = 0; s < STAGES; ++s)
-#pragma unroll
-            for (int u = 0; u < kLoads; ++u) load(u, s, k0 + s);
-        Half f0, f1;
-        wait_and_meet<(STAGES - 1) * kLoads>();
-        read(f0, 0, 0);
-        int stage = 0;
-        for (int k = k0; k < k1; ++k) {
-            read(f1, stage, 1);
-            multiply(f0, std::false_type{}, 0, 0);
-            wait_and_meet<(STAGES - 2) * kLoads>();  // the next step's lines are there
-            const int next = stage + 1 == STAGES ? 0 : stage + 1;
-            read(f0, next, 0);
-            multiply(f1, std::true_type{}, stage, k + STAGES);
-            stage = next;
-        }
-        // The sums, 32 x 32 at a time, turned through LDS so that a lane has 16 neighbours of a row (and, for Dt, of a column): requests
-        // of 16 bytes instead of 2.  The stages are free behind this barrier: no load is on its way, and every wave has read its last.
-        wait_and_meet<0>();
-        if (k1 - k0 < steps) {
-            // A tile of several workers: each leaves its sums in memory, and whoever comes last adds them up, in the workers' order whoever
-            // that is, and goes on.  Nobody waits for another.
-            // (Sums go through memory by device-wide atomic stores and loads, which pass by the L2s that the chip's parts do not share: a fence
-            // instead would write back and empty these, 10 to 20 us where all workgroups do it.)
-            auto slot = [&](int64_t w) { return (uint64_t*)a.partial + ((w * 2 + (begin(w) <= tile * steps)) * (BM * BN / 2) + threadIdx.x); };
-            uint64_t* const own = slot(worker);
-#pragma unroll
-            for (int n = 0; n < RB * CB; ++n)
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const v2f x = {acc[n / CB][n % CB][2 * q], acc[n / CB][n % CB][2 * q + 1]};
-                    __hip_atomic_store(own + (n * 8 + q) * kThreadsHere, __builtin_bit_cast(uint64_t, x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                }
-            int64_t w0 = tile * steps * a.workers / units;  // the first and, at last, the one behind the last worker of the tile
-            while (begin(w0 + 1) <= tile * steps) ++w0;
-            int64_t w1 = w0 + 1;
-            while (begin(w1) < (tile + 1) * steps) ++w1;
-            wait_and_meet<0>();  // (all of the workgroup's stores are done before it counts as arrived)
-            if (threadIdx.x == 0) arrivals = __hip_atomic_fetch_add(a.arrived + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
-            __syncthreads();
-            if (arrivals < w1 - w0) continue;
-            if (threadIdx.x == 0) __hip_atomic_store(a.arrived + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (int x = 0; x < 3; ++x)
 #pragma unroll
             for (int r = 0; r < RB; ++r)
 #pragma unroll
-                for (int c = 0; c < CB; ++c)
+                for (int c = 0; c < CB; ++c) {
+                    acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.p[x == 0][r], f.q[x == 1][c], acc[r][c], 0, 0, 0);
+                    if constexpr (decltype(loads)::value) {
+                        const int i = (x * RB + r) * CB + c;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[r][c][i] = 0.0f;
-            for (int64_t w = w0; w < w1; ++w) {
-                uint64_t* const from = slot(w);
-                constexpr int kAtOnce = RB * CB % 4 == 0 ? 4 : RB * CB % 3 == 0 ? 3 : RB * CB % 2 == 0 ? 2 : 1;  // blocks on their way
-#pragma unroll
-                for (int n = 0; n < RB * CB; n += kAtOnce) {
-                    uint64_t x[8 * kAtOnce];
-#pragma unroll
-                    for (int q = 0; q < 8 * kAtOnce; ++q) x[q] = __hip_atomic_load(from + (n * 8 + q) * kThreadsHere, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int q = 0; q < 8 * kAtOnce; ++q) {
-                        const v2f y = __builtin_bit_cast(v2f, x[q]);
-                        v16f& to = acc[(n + q / 8) / CB][(n + q / 8) % CB];
-                        to[2 * (q % 8)] += y[0], to[2 * (q % 8) + 1] += y[1];
+                        for (int u = 0; u < kLoads; ++u)
+                            if (u >= i * kLoads / kProducts && u < (i + 1) * kLoads / kProducts) {
+                                __builtin_amdgcn_sched_barrier(0);
+                                load(u, stage, step);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
                     }
+                }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // Every half step's reads run beside the half step before it; a stage is loaded again as soon as all waves have its second
+    // half in registers.
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s)
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) load(u, s, k0 + s);
+    Half f0, f1;
+    wait_and_meet<(STAGES - 1) * kLoads>();
+    read(f0, 0, 0);
+    int stage = 0;
+    for (int k = k0; k < k1; ++k) {
+        read(f1, stage, 1);
+        multiply(f0, std::false_type{}, 0, 0);
+        wait_and_meet<(STAGES - 2) * kLoads>();  // the next step's lines are there
+        const int next = stage + 1 == STAGES ? 0 : stage + 1;
+        read(f0, next, 0);
+        multiply(f1, std::true_type{}, stage, k + STAGES);
+        stage = next;
+    }
+    // The sums, 32 x 32 at a time, turned through LDS so that a lane has 16 neighbours of a row (and, for Dt, of a column): requests
+    // of 16 bytes instead of 2.  The stages are free behind this barrier: no load is on its way, and every wave has read its last.
+    wait_and_meet<0>();
+    if (kShared && a.parts > 1) {
+        // Each workgroup of the tile leaves its sums in memory, and whoever comes last adds them up, in the parts' order whoever that is, and
+        // goes on.  Nobody waits for another.  (Sums go through memory by device-wide atomic stores and loads, which pass by the L2s that
+        // the chip's parts do not share: a fence instead would write back and empty these, 10 to 20 us where all workgroups do it.)
+        constexpr int kBlocks = RB * CB, kTogether = 4;  // parts whose sums are on their way
+        uint64_t* const sums = (uint64_t*)a.partial + tile * a.parts * (BM * BN / 2) + threadIdx.x;
+#pragma unroll
+        for (int q = 0; q < 8 * kBlocks; ++q) {
+            const v16f& from = acc[q / 8 / CB][q / 8 % CB];
+            const v2f x = {from[2 * (q % 8)], from[2 * (q % 8) + 1]};
+            __hip_atomic_store(sums + part * (BM * BN / 2) + q * kThreadsHere, __builtin_bit_cast(uint64_t, x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        wait_and_meet<0>();  // (all of the workgroup's stores are done before it counts as arrived)
+        if (threadIdx.x == 0) arrivals = __hip_atomic_fetch_add(a.arrived + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
+        __syncthreads();
+        if (arrivals < a.parts) return;
+        if (threadIdx.x == 0) __hip_atomic_store(a.arrived + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+        for (int q = 0; q < 16 * kBlocks; ++q) acc[q / 16 / CB][q / 16 % CB][q % 16] = 0.0f;
+        for (int w = 0; w < a.parts; w += kTogether) {
+            uint64_t x[kTogether][8 * kBlocks];
+#pragma unroll
+            for (int t = 0; t < kTogether; ++t)
+#pragma unroll
+                for (int q = 0; q < 8 * kBlocks; ++q)
+                    x[t][q] = __hip_atomic_load(sums + min(w + t, a.parts - 1) * (BM * BN / 2) + q * kThreadsHere, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < kTogether; ++t) {
+                if (w + t >= a.parts) break;
+#pragma unroll
+                for (int q = 0; q < 8 * kBlocks; ++q) {
+                    const v2f y = __builtin_bit_cast(v2f, x[t][q]);
+                    v16f& to = acc[q / 8 / CB][q / 8 % CB];
+                    to[2 * (q % 8)] += y[0], to[2 * (q % 8) + 1] += y[1];
                 }
             }
         }
-        float* const turn = (float*)lds + wave * (32 * 33);
-        const int lr = lane >> 1, lc = (lane & 1) * 16;
-        v8h e[2][4];  // of this block and the next: first and second parts of 16 neighbours
-        auto fetch = [&](int n) {
-            const int r0 = bi * BM + wr + n / CB * 32, c0 = bj * BN + wc + n % CB * 32;
-            if (!a.E || r0 >= a.M || c0 >= a.N) return;
-            const f16* const p = a.E + base + (int64_t)(r0 + lr) * a.lde + place(c0 + lc);
-            e[n & 1][0] = *(const v8h*)p, e[n & 1][1] = *(const v8h*)(p + 8);
-            e[n & 1][2] = *(const v8h*)(p + kParts), e[n & 1][3] = *(const v8h*)(p + kParts + 8);
-        };
-        fetch(0);
+    }
+    float* const turn = (float*)lds + wave * (32 * 33);
+    const int lr = lane >> 1, lc = (lane & 1) * 16;
+    v8h e[2][4];  // of this block and the next: first and second parts of 16 neighbours
+    auto fetch = [&](int n) {
+        const int r0 = bi * BM + wr + n / CB * 32, c0 = bj * BN + wc + n % CB * 32;
+        if (!a.E || r0 >= a.M || c0 >= a.N) return;
+        const f16* const p = a.E + base + (int64_t)(r0 + lr) * a.lde + place(c0 + lc);
+        e[n & 1][0] = *(const v8h*)p, e[n & 1][1] = *(const v8h*)(p + 8);
+        e[n & 1][2] = *(const v8h*)(p + kParts), e[n & 1][3] = *(const v8h*)(p + kParts + 8);
+    };
+    fetch(0);
 #pragma unroll
-        for (int n = 0; n < RB * CB; ++n) {
-            if (n + 1 < RB * CB) fetch(n + 1);
-            const int rb = n / CB, cb = n % CB;
-            const int r0 = bi * BM + wr + rb * 32, c0 = bj * BN + wc + cb * 32;
-            if (r0 >= a.M || c0 >= a.N) continue;
+    for (int n = 0; n < RB * CB; ++n) {
+        if (n + 1 < RB * CB) fetch(n + 1);
+        const int rb = n / CB, cb = n % CB;
+        const int r0 = bi * BM + wr + rb * 32, c0 = bj * BN + wc + cb * 32;
+        if (r0 >= a.M || c0 >= a.N) continue;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) turn[((i >> 2) * 8 + (lane >> 5) * 4 + (i & 3)) * 33 + (lane & 31)] = acc[rb][cb][i];
+        for (int i = 0; i < 16; ++i) turn[((i >> 2) * 8 + (lane >> 5) * 4 + (i & 3)) * 33 + (lane & 31)] = acc[rb][cb][i];
+        __builtin_amdgcn_wave_barrier();
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = turn[lr * 33 + lc + i] * a.alpha;
+        if (a.E)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] += a.beta * ((float)e[n & 1][i >> 3][i & 7] + (float)e[n & 1][2 + (i >> 3)][i & 7]);
+        __builtin_amdgcn_wave_barrier();
+        if constexpr (LAST) {
+            if (r0 + lr >= a.rows) continue;
+            write_row<TO>(a, z * a.stride_o + (int64_t)(r0 + lr) * a.ldo + c0 + lc, (int)min(a.cols - c0 - lc, (int64_t)16), v);
+        } else {
+            store_parts16(a.D + base + (int64_t)(r0 + lr) * a.ldd + place(c0 + lc), v);
+            if (a.symmetric && bi == bj) continue;  // (the tile holds both halves)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) turn[lr * 33 + lc + i] = v[i];
             __builtin_amdgcn_wave_barrier();
-            float v[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = turn[lr * 33 + lc + i] * a.alpha;
-            if (a.E)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] += a.beta * ((float)e[n & 1][i >> 3][i & 7] + (float)e[n & 1][2 + (i >> 3)][i & 7]);
+            for (int i = 0; i < 16; ++i) v[i] = turn[(lc + i) * 33 + lr];
             __builtin_amdgcn_wave_barrier();
-            if constexpr (LAST) {
-                if (r0 + lr >= a.rows) continue;
-                write_row<TO>(a, z * a.stride_o + (int64_t)(r0 + lr) * a.ldo + c0 + lc, (int)min(a.cols - c0 - lc, (int64_t)16), v);
-            } else {
-                store_parts16(a.D + base + (int64_t)(r0 + lr) * a.ldd + place(c0 + lc), v);
-                if (a.symmetric && bi == bj) continue;  // (the tile holds both halves)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) turn[lr * 33 + lc + i] = v[i];
-                __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = turn[(lc + i) * 33 + lr];
-                __builtin_amdgcn_wave_barrier();
-                store_parts16(a.Dt + base + (int64_t)(c0 + lr) * a.lddt + place(r0 + lc), v);
-            }
+            store_parts16(a.Dt + base + (int64_t)(c0 + lr) * a.lddt + place(r0 + lc), v);
         }
     }
 }
@@ -749,11 +735,10 @@ int exponent_for(double bound)
 
 // ---- the call ----------------------------------------------------------------------------------------
 
-// How a product is cut: tiles of 32 (gp_ns_product_small), 64, 128, 192 or 256, and how many workgroups share their steps: as many as there
-// are tiles, each a whole one, or up to one per compute unit, with equal shares that end inside tiles (of 64 or 128: larger tiles'
-// sums take longer to hand over than that saves).  The cut of the least time by what its parts take, in us as measured: a step of 32
-// columns where few compute units are at work and where all are (power is what the large ones run out of), a tile's end, and,
-// where tiles are shared, handing over one worker's sums.  us a launch, model / measured:
+// How a product is cut: tiles of 32 (gp_ns_product_small), 64, 128, 128 x 256, 192 or 256, and how many workgroups sum up a tile of 64 or 128,
+// a part of the columns each (larger tiles' sums take longer to hand over than that saves).  The cut of the least time by what
+// its parts take, in us as measured: a step of 32 columns where few compute units are at work and where all are (power is what
+// the large ones run out of), a tile's end, and handing over one workgroup's sums.  us a launch, model / measured:
 //     m x n, K                  64          128          192          256
 //   1024 x 1024, 1024       14 / 16      26 / 26      44 / 48      61 / 79
 //   2048 x 2048, 2048       71 / 72      59 / 60      88 / 87     121 / 138
@@ -761,42 +746,42 @@ int exponent_for(double bound)
 //   4096 x 4096, 4096      537 / 500    442 / 396    394 / 400    345 / 350
 //   the same, X X^T        311 / 275    287 / 259    196 / 198    273 / 262
 struct Cut {
-    int side;
-    int64_t workers;
-    bool split;
+    int bm, bn;
+    int64_t tiles;  // of all matrices
+    int parts;
     double us;
 };
 constexpr int kUnits = 256;  // compute units
 Cut choose_cut(int64_t m, int64_t n, int64_t k, bool symmetric, int64_t count)
 {
     const int64_t steps = k / 32;
-    auto tiles = [&](int64_t side) { return tile_numbers((m + side - 1) / side, (n + side - 1) / side, symmetric) * count; };
-    Cut best{32, tiles(32), false, 1e30};
-    if (best.workers <= 4 * kUnits) best.us = (double)((best.workers + kUnits - 1) / kUnits) * (2.5 + 0.22 * steps);
+    auto tiles = [&](int64_t bm, int64_t bn) { return tile_numbers((m + bm - 1) / bm, (n + bn - 1) / bn, symmetric) * count; };
+    Cut best{32, 32, tiles(32, 32), 1, 1e30};
+    if (best.tiles <= 4 * kUnits) best.us = (double)((best.tiles + kUnits - 1) / kUnits) * (2.5 + 0.22 * steps);
     struct Kind {
-        int side;
+        int bm, bn;
         double few, all, finish, hand_over;
     };
-    static const Kind kinds[] = {{256, 1.4, 2.6, 12.0, 0.0}, {192, 1.0, 1.46, 10.0, 0.0}, {128, 0.5, 0.8, 8.0, 0.9}, {64, 0.3, 0.36, 4.0, 0.5}};
+    static const Kind kinds[] = {{256, 256, 1.4, 2.6, 12.0, 0.0}, {192, 192, 1.0, 1.46, 10.0, 0.0}, {128, 256, 0.85, 1.4, 10.0, 0.0},
+                                 {128, 128, 0.5, 0.8, 8.0, 1.2}, {64, 64, 0.3, 0.36, 4.0, 0.5}};
     for (const Kind& c : kinds) {
-        const int64_t T = tiles(c.side);
+        if (symmetric && c.bm != c.bn) continue;
+        const int64_t T = tiles(c.bm, c.bn);
         auto step = [&](int64_t units) { return c.few + (c.all - c.few) * (double)units / kUnits; };
         // rounds of workgroups; two of those with tiles of 64 share a compute unit
-        const int64_t full = c.side == 64 ? 2 * kUnits : kUnits, rest = T % full;
-        double us = (double)(T / full) * (steps * (c.side == 64 ? 0.52 : c.all) + c.finish);
+        const int64_t full = c.bm == 64 ? 2 * kUnits : kUnits, rest = T % full;
+        double us = (double)(T / full) * (steps * (c.bm == 64 ? 0.52 : c.all) + c.finish);
         if (rest) us += steps * (rest > kUnits ? 0.52 : step(rest)) + c.finish;
-        if (us < best.us) best = {c.side, T, false, us};
-        if (c.hand_over == 0.0 || T > kMaxShared) continue;
-        for (int64_t W = kUnits; W >= 16; W /= 2) {
-            const double share = (double)T * steps / W;
-            if (share < 2.0 || T % W == 0) continue;
-            us = share * step(W) + c.finish * (std::ceil(share / steps) + 1.0) + c.hand_over * (std::min((double)W, steps / share) + 2.0);
-            if (us < best.us) best = {c.side, W, true, us};
+        if (us < best.us) best = {c.bm, c.bn, T, 1, us};
+        if (c.hand_over == 0.0) continue;
+        for (int64_t parts = 2; parts * T <= kUnits && 2 * parts <= steps; ++parts) {
+            us = (double)((steps + parts - 1) / parts) * step(parts * T) + c.finish + 4.0 + c.hand_over * (double)parts;
+            if (us < best.us) best = {c.bm, c.bn, T, (int)parts, us};
         }
     }
     return best;
 }
-int64_t cut_bytes(const Cut& c) { return c.split ? c.workers * 2 * c.side * c.side * 4 : 0; }
+int64_t cut_bytes(const Cut& c) { return c.parts > 1 ? c.tiles * c.parts * c.bm * c.bn * 4 : 0; }
 
 struct NsLayout {
     int64_t m, n;               // shorter and longer side, of whole tiles
@@ -843,16 +828,16 @@ gp_status check_shape(int64_t rows, int64_t cols, int64_t count)
     return GP_OK;
 }
 
-template <int SIDE, int WM, int WN, int STAGES, typename TO, bool LAST>
-gp_status launch_tiles(const Product& a, int64_t count, hipStream_t stream)
+template <int BM, int BN, int WM, int WN, int STAGES, typename TO, bool LAST>
+gp_status launch_tiles(const Product& a, hipStream_t stream)
 {
-    constexpr size_t lds = STAGES * 2 * SIDE * 128;
+    constexpr size_t lds = STAGES * (BM + BN) * 128;
     if constexpr (lds > 65536) {
-        gp_status st = raise_lds<&gp_ns_product<SIDE, SIDE, WM, WN, STAGES, TO, LAST>>(lds);
+        gp_status st = raise_lds<&gp_ns_product<BM, BN, WM, WN, STAGES, TO, LAST>>(lds);
         if (st != GP_OK) return st;
     }
     profile_begin("gp_ns_product", stream);
-    hipLaunchKernelGGL((gp_ns_product<SIDE, SIDE, WM, WN, STAGES, TO, LAST>), dim3((unsigned)((a.workers + 7) / 8 * 8)), dim3(64 * WM * WN), lds, stream, a);
+    hipLaunchKernelGGL((gp_ns_product<BM, BN, WM, WN, STAGES, TO, LAST>), dim3((unsigned)((a.all_tiles * a.parts + 7) / 8 * 8)), dim3(64 * WM * WN), lds, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     return GP_OK;
@@ -861,13 +846,19 @@ gp_status launch_tiles(const Product& a, int64_t count, hipStream_t stream)
 template <typename TO, bool LAST>
 gp_status launch_product(Product a, const Cut& cut, int64_t count, hipStream_t stream)
 {
-    a.tiles_m = (a.M + cut.side - 1) / cut.side, a.tiles_n = (a.N + cut.side - 1) / cut.side;
+    // (the last product of a tall matrix is the transpose of the one that the cut was made for)
+    const bool turned = a.M != a.N && (a.M > a.N);
+    const int bm = turned ? cut.bn : cut.bm, bn = turned ? cut.bm : cut.bn;
+    a.tiles_m = (a.M + bm - 1) / bm, a.tiles_n = (a.N + bn - 1) / bn;
     a.tile_count = (int)tile_numbers(a.tiles_m, a.tiles_n, a.symmetric);
-    a.workers = cut.workers, a.split = cut.split, a.units = a.tile_count * count * (a.K / 32);
-    if (cut.side == 256) return launch_tiles<256, 2, 2, 2, TO, LAST>(a, count, stream);
-    if (cut.side == 192) return launch_tiles<192, 2, 2, 3, TO, LAST>(a, count, stream);
-    if (cut.side == 128) return launch_tiles<128, 2, 4, 4, TO, LAST>(a, count, stream);
-    if (cut.side == 64) return launch_tiles<64, 2, 2, 4, TO, LAST>(a, count, stream);
+    a.all_tiles = a.tile_count * count, a.parts = cut.parts;
+    if (bm == 256 && bn == 256) return launch_tiles<256, 256, 2, 2, 2, TO, LAST>(a, stream);
+    if (bm == 192) return launch_tiles<192, 192, 2, 2, 3, TO, LAST>(a, stream);
+    if (bm == 128 && bn == 256) return launch_tiles<128, 256, 2, 4, 3, TO, LAST>(a, stream);
+    if constexpr (LAST)
+        if (bm == 256) return launch_tiles<256, 128, 4, 2, 3, TO, LAST>(a, stream);
+    if (bm == 128) return launch_tiles<128, 128, 2, 4, 4, TO, LAST>(a, stream);
+    if (bm == 64) return launch_tiles<64, 64, 2, 2, 4, TO, LAST>(a, stream);
     profile_begin("gp_ns_product", stream);
     hipLaunchKernelGGL((gp_ns_product_small<TO, LAST>), dim3((unsigned)((a.tile_count + 7) / 8 * 8), 1, (unsigned)count), dim3(64 * kSmallWaves), 0, stream, a);
     profile_end(stream);
