@@ -156,6 +156,7 @@ struct SortArgs {
     int64_t tiles;
     uint32_t* table;       // [tile][digit]
     uint32_t* totals;      // [digit]
+    int own_table;         // no totals: the scatter adds up the table
 };
 
 __device__ __forceinline__ uint64_t entry_of(int64_t token, int64_t i, int64_t V)
@@ -172,10 +173,12 @@ __device__ __forceinline__ uint64_t entry_at(const SortArgs& a, int64_t i)
 }
 
 // lanes of the wavefront that are valid and hold the same digit
-__device__ __forceinline__ unsigned long long peers_of(unsigned digit, int bits, bool valid)
+template <int BITS>
+__device__ __forceinline__ unsigned long long peers_of(unsigned digit, bool valid)
 {
     unsigned long long peers = __ballot(valid);
-    for (int b = 0; b < bits; ++b) {
+#pragma unroll
+    for (int b = 0; b < BITS; ++b) {
         const bool bit = (digit >> b) & 1u;
         const unsigned long long with = __ballot(bit);
         peers &= bit ? with : ~with;
@@ -185,9 +188,10 @@ __device__ __forceinline__ unsigned long long peers_of(unsigned digit, int bits,
 
 // Ranks a wavefront's next 64 entries among its own; count: the wavefront's digit counts in LDS (volatile: its lanes hand them on
 // without a barrier).
-__device__ __forceinline__ uint32_t rank_in_wave(volatile uint16_t* count, unsigned digit, int bits, bool valid, int lane)
+template <int BITS>
+__device__ __forceinline__ uint32_t rank_in_wave(volatile uint16_t* count, unsigned digit, bool valid, int lane)
 {
-    const unsigned long long peers = peers_of(digit, bits, valid);
+    const unsigned long long peers = peers_of<BITS>(digit, valid);
     const uint32_t before = (uint32_t)__popcll(peers & ((1ull << lane) - 1ull));
     uint32_t r = 0;
     if (valid) {
@@ -221,17 +225,21 @@ __global__ __launch_bounds__(kSortThreads) void gp_token_count(SortArgs a)
 {
     __shared__ uint32_t h[kMaxDigits];
     const int digits = 1 << a.bits;
+    const int64_t t0 = (int64_t)blockIdx.x * (ITEMS * kSortThreads) + threadIdx.x;
+    unsigned digit[ITEMS];
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) digit[j] = t0 + j * kSortThreads < a.N ? (unsigned)(entry_at<FIRST>(a, t0 + j * kSortThreads) >> a.shift) & (digits - 1) : ~0u;
     for (int i = threadIdx.x; i < digits; i += kSortThreads) h[i] = 0;
     __syncthreads();
-    const int64_t t0 = (int64_t)blockIdx.x * (ITEMS * kSortThreads);
 #pragma unroll
-    for (int j = 0; j < ITEMS; ++j) {
-        const int64_t i = t0 + j * kSortThreads + threadIdx.x;
-        if (i < a.N) atomicAdd(&h[(unsigned)(entry_at<FIRST>(a, i) >> a.shift) & (digits - 1)], 1u);
-    }
+    for (int j = 0; j < ITEMS; ++j)
+        if (digit[j] != ~0u) atomicAdd(&h[digit[j]], 1u);
     __syncthreads();
     for (int i = threadIdx.x; i < digits; i += kSortThreads) a.table[(int64_t)blockIdx.x * digits + i] = h[i];
 }
+
+// Where the table is small (kOwnTable), every scatter adds it up itself: 256 KB from an L2 cost it less than a launch.
+constexpr int64_t kOwnTable = 1 << 16;
 
 // A workgroup looks after kPrefixDigits digits: its threads stand side by side over them, and each row of threads over a range of tiles.
 constexpr int kPrefixDigits = 32, kPrefixRows = kSortThreads / kPrefixDigits;
@@ -269,42 +277,65 @@ __global__ __launch_bounds__(kSortThreads) void gp_token_prefix(SortArgs a)
 // workgroup's entries in the new order: neighbours there are neighbours in the list, and their stores share lines.
 constexpr size_t scatter_lds(int digits, int items)
 {
-    return kSortWaves * 4 + (size_t)digits * 4 + std::max((size_t)digits * 2 * kSortWaves, (size_t)items * kSortThreads * 8);
+    const size_t counts = (size_t)digits * 2 * kSortWaves, entries = (size_t)items * kSortThreads * 8;
+    return kSortWaves * 4 + (size_t)digits * 4 + (counts > entries ? counts : entries);
 }
 
-template <int ITEMS, bool FIRST>
+template <int BITS, int ITEMS, bool FIRST>
 __global__ __launch_bounds__(kSortThreads) void gp_token_scatter(SortArgs a)
 {
     extern __shared__ __align__(16) uint32_t sort_lds[];
-    const int digits = 1 << a.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int digits = 1 << BITS;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t *const part = sort_lds, *const lead = part + kSortWaves;
     uint16_t* const count = (uint16_t*)(lead + digits);
     uint64_t* const list = (uint64_t*)count;
-    for (int i = threadIdx.x; i < kSortWaves / 2 * digits; i += kSortThreads) ((uint32_t*)count)[i] = 0;
-    // where each digit begins: thread t looks after digits per t .. per t + per - 1
-    const int per = (digits + kSortThreads - 1) / kSortThreads, d0 = threadIdx.x * per;
-    uint32_t mine = 0;
-    for (int j = 0; j < per; ++j)
-        if (d0 + j < digits) mine += a.totals[d0 + j];
-    uint32_t begin = exclusive_1024(mine, part);
-    for (int j = 0; j < per; ++j)
-        if (d0 + j < digits) lead[d0 + j] = begin + a.table[(int64_t)blockIdx.x * digits + d0 + j], begin += a.totals[d0 + j];
-    __syncthreads();
     uint64_t key[ITEMS];
     uint32_t rank[ITEMS];
     const int64_t t0 = (int64_t)blockIdx.x * (ITEMS * kSortThreads), w0 = t0 + wave * (ITEMS * 64) + lane;
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) key[j] = w0 + j * 64 < a.N ? entry_at<FIRST>(a, w0 + j * 64) : 0;
+    // thread t looks after digits per t .. per t + per - 1: how many entries have them, and how many of those in the tiles before this one
+    constexpr int per = (digits + kSortThreads - 1) / kSortThreads;
+    const int d0 = threadIdx.x * per;
+    uint32_t all[2] = {0, 0}, before[2] = {0, 0};
+    static_assert(kMaxDigits == 2 * kSortThreads, "at most two digits per thread");
+    if (per == 1 && a.own_table) {
+        uint32_t(*const sums)[2] = (uint32_t(*)[2])list;
+        const int d = threadIdx.x & (digits - 1), row = threadIdx.x / digits, rows = max(kSortThreads / digits, 1);
+        uint32_t n = 0, b = 0;
+#pragma unroll 8
+        for (int t = row; t < (int)a.tiles; t += rows) {
+            const uint32_t v = a.table[(int64_t)t * digits + d];
+            n += v, b += t < (int)blockIdx.x ? v : 0;
+        }
+        sums[threadIdx.x][0] = n, sums[threadIdx.x][1] = b;
+        __syncthreads();
+        if (d0 < digits)
+            for (int r = 0; r < rows; ++r) all[0] += sums[r * digits + d0][0], before[0] += sums[r * digits + d0][1];
+        __syncthreads();
+    } else {
+#pragma unroll
+        for (int j = 0; j < per; ++j)
+            if (d0 + j < digits) all[j] = a.totals[d0 + j], before[j] = a.table[(int64_t)blockIdx.x * digits + d0 + j];
+    }
+    for (int i = threadIdx.x; i < kSortWaves / 2 * digits; i += kSortThreads) ((uint32_t*)count)[i] = 0;
+    uint32_t begin = exclusive_1024(all[0] + all[1], part);
+    if (d0 < digits) lead[d0] = begin + before[0];
+    if (per > 1 && d0 + 1 < digits) lead[d0 + 1] = begin + all[0] + before[1];
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j)
-        rank[j] = rank_in_wave(count + wave * digits, (unsigned)(key[j] >> a.shift) & (digits - 1), a.bits, w0 + j * 64 < a.N, lane);
+        rank[j] = rank_in_wave<BITS>(count + wave * digits, (unsigned)(key[j] >> a.shift) & (digits - 1), w0 + j * 64 < a.N, lane);
     __syncthreads();
-    mine = 0;
+    uint32_t mine = 0;
+#pragma unroll
     for (int j = 0; j < per; ++j)
         if (d0 + j < digits)
 #pragma unroll
             for (int w = 0; w < kSortWaves; ++w) mine += count[w * digits + d0 + j];
     begin = exclusive_1024(mine, part);
+#pragma unroll
     for (int j = 0; j < per; ++j) {
         const int d = d0 + j;
         if (d >= digits) break;
@@ -717,7 +748,9 @@ SortPlan sort_plan(int64_t N, int64_t V)
 {
     SortPlan p;
     const int all = bits_of(V);
-    p.passes = (all + 10) / 11, p.bits = (all + p.passes - 1) / p.passes;
+    p.passes = (all + 10) / 11;
+    const int least = (all + p.passes - 1) / p.passes;
+    p.bits = least <= 6 ? 6 : least <= 8 ? 8 : least == 9 ? 9 : 11;  // (those that the scatter is built for)
     p.items = N <= (1 << 20) ? 4 : 8;
     p.tiles = (N + p.items * kSortThreads - 1) / (p.items * kSortThreads);
     return p;
@@ -740,23 +773,36 @@ GradLayout grad_layout(int64_t N, int64_t V, int32_t d)
     return l;
 }
 
-template <int ITEMS, bool FIRST>
-gp_status launch_pass(const SortArgs& a, hipStream_t stream)
+template <int BITS, int ITEMS, bool FIRST>
+gp_status launch_scatter(const SortArgs& a, hipStream_t stream)
 {
-    const size_t lds = scatter_lds(1 << a.bits, ITEMS);
-    gp_status st = raise_lds<&gp_token_scatter<ITEMS, FIRST>>(scatter_lds(kMaxDigits, ITEMS));
+    constexpr size_t lds = scatter_lds(1 << BITS, ITEMS);
+    gp_status st = raise_lds<&gp_token_scatter<BITS, ITEMS, FIRST>>(lds);
     if (st != GP_OK) return st;
-    profile_begin("gp_token_count", stream);
-    hipLaunchKernelGGL((gp_token_count<ITEMS, FIRST>), dim3((unsigned)a.tiles), dim3(kSortThreads), 0, stream, a);
-    profile_end(stream);
-    profile_begin("gp_token_prefix", stream);
-    hipLaunchKernelGGL(gp_token_prefix, dim3((unsigned)(((1 << a.bits) + kPrefixDigits - 1) / kPrefixDigits)), dim3(kSortThreads), 0, stream, a);
-    profile_end(stream);
     profile_begin("gp_token_scatter", stream);
-    hipLaunchKernelGGL((gp_token_scatter<ITEMS, FIRST>), dim3((unsigned)a.tiles), dim3(kSortThreads), lds, stream, a);
+    hipLaunchKernelGGL((gp_token_scatter<BITS, ITEMS, FIRST>), dim3((unsigned)a.tiles), dim3(kSortThreads), lds, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     return GP_OK;
+}
+template <int ITEMS, bool FIRST>
+gp_status launch_pass(const SortArgs& a, hipStream_t stream)
+{
+    profile_begin("gp_token_count", stream);
+    hipLaunchKernelGGL((gp_token_count<ITEMS, FIRST>), dim3((unsigned)a.tiles), dim3(kSortThreads), 0, stream, a);
+    profile_end(stream);
+    if (!a.own_table) {
+        profile_begin("gp_token_prefix", stream);
+        hipLaunchKernelGGL(gp_token_prefix, dim3((unsigned)(((1 << a.bits) + kPrefixDigits - 1) / kPrefixDigits)), dim3(kSortThreads), 0, stream, a);
+        profile_end(stream);
+    }
+    GP_HIP(hipGetLastError());
+    switch (a.bits) {
+    case 6: return launch_scatter<6, ITEMS, FIRST>(a, stream);
+    case 8: return launch_scatter<8, ITEMS, FIRST>(a, stream);
+    case 9: return launch_scatter<9, ITEMS, FIRST>(a, stream);
+    default: return launch_scatter<11, ITEMS, FIRST>(a, stream);
+    }
 }
 
 // *sorted: whichever of the two lists of the workspace holds the result
@@ -766,7 +812,7 @@ gp_status sort_tokens(const void* tokens, int wide, int64_t N, int64_t V, char* 
     SortArgs a{};
     a.tokens = tokens, a.wide = wide, a.N = N, a.V = V, a.bits = p.bits, a.tiles = p.tiles;
     a.table = (uint32_t*)(ws + l.table), a.totals = (uint32_t*)(ws + l.totals);
-    a.shift = 32;
+    a.own_table = p.bits <= 10 && p.tiles << p.bits <= kOwnTable;
     if (N <= kShortList) {
         a.out = (uint64_t*)ws;
         profile_begin("gp_token_rank", stream);
