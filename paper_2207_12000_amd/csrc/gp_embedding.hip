@@ -751,7 +751,7 @@ SortPlan sort_plan(int64_t N, int64_t V)
     p.passes = (all + 10) / 11;
     const int least = (all + p.passes - 1) / p.passes;
     p.bits = least <= 6 ? 6 : least <= 8 ? 8 : least == 9 ? 9 : 11;  // (those that the scatter is built for)
-    p.items = N <= (1 << 20) ? 4 : 8;
+    p.items = N <= (1 << 20) ? 4 : 16;
     p.tiles = (N + p.items * kSortThreads - 1) / (p.items * kSortThreads);
     return p;
 }
@@ -826,7 +826,7 @@ gp_status sort_tokens(const void* tokens, int wide, int64_t N, int64_t V, char* 
     for (int pass = 0; pass < p.passes; ++pass) {
         a.shift = 32 + pass * p.bits, a.keys = lists[(pass + 1) & 1], a.out = lists[pass & 1];
         gp_status st = p.items == 4 ? (pass == 0 ? launch_pass<4, true>(a, stream) : launch_pass<4, false>(a, stream))
-                                    : (pass == 0 ? launch_pass<8, true>(a, stream) : launch_pass<8, false>(a, stream));
+                                    : (pass == 0 ? launch_pass<16, true>(a, stream) : launch_pass<16, false>(a, stream));
         if (st != GP_OK) return st;
     }
     *sorted = a.out;
