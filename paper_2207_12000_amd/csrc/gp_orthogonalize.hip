@@ -38,6 +38,7 @@ typedef unsigned short bf16_t;
 typedef _Float16 f16;
 typedef f16 v4h __attribute__((ext_vector_type(4)));
 typedef f16 v8h __attribute__((ext_vector_type(8)));
+typedef int v2i __attribute__((ext_vector_type(2)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
@@ -291,13 +292,17 @@ __device__ __forceinline__ void tile_at(const Product& a, int t, int& bi, int& b
 }
 __device__ __forceinline__ int64_t stretched_block() { return (int64_t)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3); }
 template <typename TO>
-__device__ __forceinline__ void write_out(const Product& a, int64_t o, float v)
+__device__ __forceinline__ void store_out(const Product& a, int64_t o, float v)
 {
-    if (a.W) v = a.keep * a.W[o] - a.lr * v;
     if constexpr (sizeof(TO) == 4)
         ((float*)a.out)[o] = v;
     else
         ((bf16_t*)a.out)[o] = __builtin_bit_cast(bf16_t, (__bf16)v);
+}
+template <typename TO>
+__device__ __forceinline__ void write_out(const Product& a, int64_t o, float v)
+{
+    store_out<TO>(a, o, a.W ? a.keep * a.W[o] - a.lr * v : v);
 }
 // the first `count` of sixteen neighbours of a row, from any element's boundary
 typedef bf16_t v8b_any __attribute__((ext_vector_type(8), aligned(2)));
@@ -697,6 +702,195 @@ __global__ __launch_bounds__(4 * M) void gp_ns_panel(Panel a)
     }
 }
 
+// The whole of it for matrices of up to 64 x 256: one workgroup each, one launch.  A wavefront owns 16 columns of X, whose values stay in
+// its registers in fp32 from first to last; LDS holds X's parts in rows (for A = X X^T, one 16 x 16 block per wavefront) and in
+// columns (for the panel's own Y = A X, then, in the same place, for A Y), and A's parts.
+struct Tiny {
+    Update u;
+    float eps;
+    int steps, tall;
+    float scale;                     // of the first X
+    float alpha[kMaxSteps];          // A's scale over X's, squared
+    float y_scale[kMaxSteps], fa[kMaxSteps], fb[kMaxSteps], fc[kMaxSteps];  // as in Panel
+    Product last;
+};
+constexpr int kTinyRows = 64, kTinyCols = 256;
+constexpr int kRowLd = 2 * kTinyCols + 8, kColLd = 2 * kTinyRows + 8;  // halves: rows and columns start on different banks
+constexpr size_t kTinyLds = (size_t)(kTinyRows * kRowLd + kTinyCols * kColLd + kTinyRows * kColLd) * 2;
+
+template <int BLOCKS, typename T, typename TO>  // blocks of 16 rows
+__global__ __launch_bounds__(1024) void gp_ns_tiny(Tiny a)
+{
+    extern __shared__ __align__(128) f16 tiny[];
+    __shared__ double part[16];
+    f16 *const rows = tiny, *const cols = rows + kTinyRows * kRowLd, *const gram = cols + kTinyCols * kColLd;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, kg = lane >> 4;
+    const int64_t z = blockIdx.x;
+    const int m = (int)(a.tall ? a.u.cols : a.u.rows), n = (int)(a.tall ? a.u.rows : a.u.cols);  // X is m x n
+    const int c = wave * 16 + r16;      // the lane's column; its elements v[g][i]: row 16 g + 4 kg + i
+    const int panels = (n + 31) / 32 * 2;  // (whole lines of columns)
+    const bool active = wave < panels;
+    constexpr int kLines = (BLOCKS + 1) / 2;
+    // U, element by element, and the new momentum
+    const T* const G = (const T*)a.u.G + z * a.u.stride_g;
+    float v[BLOCKS][4], mo[BLOCKS][4];
+    double sum = 0.0;
+#pragma unroll
+    for (int g = 0; g < BLOCKS; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 16 * g + 4 * kg + i;
+            const int64_t ur = a.tall ? c : r, uc = a.tall ? r : c;
+            v[g][i] = r < m && c < n ? widen(G[ur * a.u.ldg + uc]) : 0.0f;
+            mo[g][i] = a.u.M && r < m && c < n ? a.u.M[z * a.u.stride_m + ur * a.u.ldm + uc] : 0.0f;
+        }
+    if (a.u.M)
+#pragma unroll
+        for (int g = 0; g < BLOCKS; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 16 * g + 4 * kg + i;
+                const float x = a.u.mu * mo[g][i] + v[g][i];
+                if (r < m && c < n) a.u.M_out[z * a.u.stride_m + (a.tall ? c : r) * a.u.ldm + (a.tall ? r : c)] = x;
+                v[g][i] = a.u.nesterov ? v[g][i] + a.u.mu * x : x;
+            }
+#pragma unroll
+    for (int g = 0; g < BLOCKS; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += (double)v[g][i] * v[g][i];
+    const float factor = (float)((double)a.scale / (sqrt(block_sum<1024>(sum, part)) + (double)a.eps));
+#pragma unroll
+    for (int g = 0; g < BLOCKS; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[g][i] *= 16 * g + 4 * kg + i < m && c < n ? factor : 0.0f;
+    if constexpr (BLOCKS % 2 == 1) {  // the last line's other half: zero from first to last
+        const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (active) store_parts(cols + c * kColLd + place(16 * BLOCKS + 4 * kg), zero);
+        if (threadIdx.x < kTinyRows * 4) store_parts(gram + threadIdx.x / 4 * kColLd + place(16 * BLOCKS + threadIdx.x % 4 * 4), zero);
+    }
+    for (int k = 0;; ++k) {
+        // X into LDS, both ways
+        if (active)
+#pragma unroll
+            for (int g = 0; g < BLOCKS; ++g) {
+                // four rows of this column; and, with the neighbouring lane's, two rows of both columns
+                v4h hi, lo;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f16 x, y;
+                    split(v[g][i], x, y);
+                    hi[i] = x, lo[i] = y;
+                }
+                f16* const d = cols + c * kColLd + place(16 * g + 4 * kg);
+                *(v4h*)d = hi, *(v4h*)(d + kParts) = lo;
+                const bool odd = lane & 1;
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    const v2i own = __builtin_bit_cast(v2i, part ? lo : hi);  // rows 0 and 1, rows 2 and 3
+                    const int other = __builtin_amdgcn_mov_dpp(odd ? own[0] : own[1], 0xB1, 0xF, 0xF, true);  // of the lane beside it, the rows it keeps
+                    const unsigned mine = (unsigned)(odd ? own[1] : own[0]);
+                    const unsigned left = odd ? (unsigned)other : mine, right = odd ? mine : (unsigned)other;
+                    f16* const at = rows + (16 * g + 4 * kg + (odd ? 2 : 0)) * kRowLd + place(c & ~1) + part * kParts;
+                    *(unsigned*)at = (left & 0xFFFFu) | right << 16;
+                    *(unsigned*)(at + kRowLd) = left >> 16 | (right & 0xFFFF0000u);
+                }
+            }
+        __syncthreads();
+        if (wave < BLOCKS * (BLOCKS + 1) / 2) {  // A: a block on or above the diagonal, column by column
+            const int bj = wave < 1 ? 0 : wave < 3 ? 1 : wave < 6 ? 2 : 3, bi = wave - bj * (bj + 1) / 2;
+            const f16 *const p = rows + (bi * 16 + r16) * kRowLd + kg * 8, *const q = rows + (bj * 16 + r16) * kRowLd + kg * 8;
+            v4f acc[3] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
+            for (int s = 0; s < panels / 2; ++s) {
+                const v8h ph = *(const v8h*)(p + s * 64), pl = *(const v8h*)(p + s * 64 + kParts);
+                const v8h qh = *(const v8h*)(q + s * 64), ql = *(const v8h*)(q + s * 64 + kParts);
+                acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, qh, acc[0], 0, 0, 0);
+                acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, qh, acc[1], 0, 0, 0);
+                acc[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, ql, acc[2], 0, 0, 0);
+            }
+            // element i: row 16 bi + 4 kg + i, column 16 bj + r16; and its mirror image
+            const v4f x = acc[0] + (acc[1] + acc[2]);
+            const float t[4] = {x[0] * a.alpha[k], x[1] * a.alpha[k], x[2] * a.alpha[k], x[3] * a.alpha[k]};
+            store_parts(gram + (bj * 16 + r16) * kColLd + place(bi * 16 + 4 * kg), t);
+            if (bi != bj)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f16 hi, lo;
+                    split(t[i], hi, lo);
+                    f16* const d = gram + (bi * 16 + 4 * kg + i) * kColLd + place(bj * 16 + r16);
+                    d[0] = hi, d[kParts] = lo;
+                }
+        }
+        __syncthreads();
+        if (active) {
+            constexpr bool kKeep = BLOCKS < 4;  // A in registers, where these hold it
+            v8h av[BLOCKS][kLines][2];
+#pragma unroll
+            for (int g = 0; g < BLOCKS; ++g)
+#pragma unroll
+                for (int s = 0; s < kLines; ++s)
+#pragma unroll
+                    for (int part = 0; part < 2; ++part)
+                        if (kKeep) av[g][s][part] = *(const v8h*)(gram + (16 * g + r16) * kColLd + s * 64 + part * kParts + kg * 8);
+            auto product = [&](v4f(&y)[BLOCKS]) {  // A times the wavefront's columns in LDS
+                v8h q[kLines][2];
+#pragma unroll
+                for (int s = 0; s < kLines; ++s)
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) q[s][part] = *(const v8h*)(cols + c * kColLd + s * 64 + part * kParts + kg * 8);
+#pragma unroll
+                for (int g = 0; g < BLOCKS; ++g) {
+                    v4f acc[3] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+                    for (int s = 0; s < kLines; ++s) {
+                        const f16* const p = gram + (16 * g + r16) * kColLd + s * 64 + kg * 8;
+                        const v8h hi = kKeep ? av[g][s][0] : *(const v8h*)p, lo = kKeep ? av[g][s][1] : *(const v8h*)(p + kParts);
+                        acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, q[s][0], acc[0], 0, 0, 0);
+                        acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, q[s][0], acc[1], 0, 0, 0);
+                        acc[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, q[s][1], acc[2], 0, 0, 0);
+                    }
+                    y[g] = acc[0] + (acc[1] + acc[2]);
+                }
+            };
+            v4f y[BLOCKS], w[BLOCKS];
+            product(y);
+#pragma unroll
+            for (int g = 0; g < BLOCKS; ++g) {  // (the columns' X is not needed again)
+                const float t[4] = {y[g][0] * a.y_scale[k], y[g][1] * a.y_scale[k], y[g][2] * a.y_scale[k], y[g][3] * a.y_scale[k]};
+                store_parts(cols + c * kColLd + place(16 * g + 4 * kg), t);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (a wavefront's own columns: no barrier)
+            product(w);
+#pragma unroll
+            for (int g = 0; g < BLOCKS; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[g][i] = a.fa[k] * v[g][i] + (a.fb[k] * y[g][i] + a.fc[k] * w[g][i]);
+        }
+        if (k + 1 == a.steps) break;
+        __syncthreads();  // (A and X's rows are read to their ends)
+    }
+    const Product& p = a.last;
+    if (p.W) {  // (all requests before the first use)
+#pragma unroll
+        for (int g = 0; g < BLOCKS; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 16 * g + 4 * kg + i;
+                mo[g][i] = r < m && c < n ? p.W[z * p.stride_o + (a.tall ? c : r) * p.ldo + (a.tall ? r : c)] : 0.0f;
+            }
+#pragma unroll
+        for (int g = 0; g < BLOCKS; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[g][i] = p.keep * mo[g][i] - p.lr * v[g][i];
+    }
+#pragma unroll
+    for (int g = 0; g < BLOCKS; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 16 * g + 4 * kg + i;
+            if (r < m && c < n) store_out<TO>(p, z * p.stride_o + (a.tall ? c : r) * p.ldo + (a.tall ? r : c), v[g][i]);
+        }
+}
+
 // ---- ranges ------------------------------------------------------------------------------------------
 
 // the largest |a s + b s^3 + c s^5| over 0 <= s <= top
@@ -809,6 +1003,8 @@ NsLayout ns_layout(int64_t rows, int64_t cols, int64_t count)
     return l;
 }
 
+bool tiny_shape(int64_t rows, int64_t cols) { return std::min(rows, cols) <= kTinyRows && std::max(rows, cols) <= kTinyCols; }
+
 constexpr int64_t kMaxSide = 1 << 20;
 constexpr float kDefaultCoeff[3] = {3.4445f, -4.7750f, 2.0315f};
 
@@ -880,6 +1076,24 @@ gp_status launch_panels(const Panel& a, int64_t count, hipStream_t stream)
     return GP_OK;
 }
 
+template <int BLOCKS, typename T, typename TO>
+gp_status launch_tiny(const Tiny& a, int64_t count, hipStream_t stream)
+{
+    gp_status st = raise_lds<&gp_ns_tiny<BLOCKS, T, TO>>(kTinyLds);
+    if (st != GP_OK) return st;
+    profile_begin("gp_ns_tiny", stream);
+    hipLaunchKernelGGL((gp_ns_tiny<BLOCKS, T, TO>), dim3((unsigned)count), dim3(1024), kTinyLds, stream, a);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    return GP_OK;
+}
+template <typename T, typename TO>
+gp_status launch_tiny(const Tiny& a, int64_t count, hipStream_t stream)
+{
+    const int64_t m = std::min(a.u.rows, a.u.cols);
+    return m <= 32 ? launch_tiny<2, T, TO>(a, count, stream) : m <= 48 ? launch_tiny<3, T, TO>(a, count, stream) : launch_tiny<4, T, TO>(a, count, stream);
+}
+
 // out: the direction itself (W null, of dtype out_dtype), or the stepped weights
 gp_status newton_schulz(const Update& u, gp_dtype dtype, int64_t count, int32_t steps, const float* coeff, float eps, const float* W, float keep,
                         float lr, void* out, int64_t ldo, int64_t stride_o, gp_dtype out_dtype, void* workspace, int64_t bytes, hipStream_t stream)
@@ -898,6 +1112,19 @@ gp_status newton_schulz(const Update& u, gp_dtype dtype, int64_t count, int32_t 
     const NsLayout l = ns_layout(u.rows, u.cols, count);
     if (!workspace || bytes < l.total || (uintptr_t)workspace % 256 != 0)
         return fail(GP_ERR_INVALID_ARG, "need a workspace of %lld bytes on a 256-byte boundary", (long long)l.total);
+    if (tiny_shape(u.rows, u.cols)) {
+        Tiny t{};
+        t.u = u, t.eps = eps, t.steps = steps, t.tall = u.rows > u.cols, t.scale = std::ldexp(1.0f, ex[0]);
+        for (int k = 0; k < steps; ++k) {
+            const float* const p = coeff ? coeff + 3 * k : kDefaultCoeff;
+            const int next = k + 1 < steps ? ex[k + 1] : 0;
+            t.alpha[k] = std::ldexp(1.0f, ea[k] - 2 * ex[k]), t.y_scale[k] = std::ldexp(1.0f, ey[k] - ea[k] - ex[k]);
+            t.fa[k] = std::ldexp(p[0], next - ex[k]), t.fb[k] = std::ldexp(p[1], next - ea[k] - ex[k]), t.fc[k] = std::ldexp(p[2], next - ea[k] - ey[k]);
+        }
+        t.last.out = out, t.last.ldo = ldo, t.last.stride_o = stride_o, t.last.W = W, t.last.keep = keep, t.last.lr = lr;
+        if (dtype == GP_F32) return launch_tiny<float, float>(t, count, stream);
+        return out_dtype == GP_F32 ? launch_tiny<bf16_t, float>(t, count, stream) : launch_tiny<bf16_t, bf16_t>(t, count, stream);
+    }
     double* const partial = (double*)workspace;
     f16* const ws = (f16*)((char*)workspace + l.planes);
     int* const arrived = (int*)((char*)workspace + l.arrived);
