@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -527,26 +528,30 @@ def _on_stream(tensor, stream):
     return _other_stream(handle, tensor.device)
 
 
-def _float_type(t):
+@functools.lru_cache(maxsize=None)
+def _types():
     import torch
-    kinds = {torch.float32: GP_F32, torch.bfloat16: GP_BF16}
-    dtype = t if isinstance(t, torch.dtype) else t.dtype
-    if dtype not in kinds:
+    return {torch.float32: GP_F32, torch.bfloat16: GP_BF16}, {torch.int32: GP_I32, torch.int64: GP_I64}
+
+
+def _float_type(t):
+    kind = _types()[0].get(t.dtype)
+    if kind is None:
         raise ValueError("values must be float32 or bfloat16")
-    return kinds[dtype]
+    return kind
 
 
 def _index_type(tokens):
-    import torch
-    kinds = {torch.int32: GP_I32, torch.int64: GP_I64}
-    if tokens.dtype not in kinds or not tokens.is_contiguous():
+    kind = _types()[1].get(tokens.dtype)
+    if kind is None or not tokens.is_contiguous():
         raise ValueError("tokens must be a contiguous int32 or int64 tensor")
-    return kinds[tokens.dtype]
+    return kind
 
 
-def _one_device(*tensors):
-    if len({t.device for t in tensors if t is not None}) > 1:
-        raise ValueError("tensors must be on one device")
+def _one_device(first, *others):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("tensors must be on one device")
 
 
 def _row_stride(t, what):
