@@ -425,7 +425,7 @@ gp_status gp_embedding(const void *table, int64_t ldt, gp_dtype dtype, int64_t V
  *     table_grad[v, :] = scale * (sum of grad[i, :] over all i with token[i] = v)     (accumulate = 0: all V rows written)
  *     table_grad[v, :] += the same                    (accumulate = 1: rows without a token are neither read nor written)
  *  tokens      DEVICE, N row numbers; those outside [0, V) take no part.
- *  grad        DEVICE, N x d of `dtype`, rows ldg elements apart.
+ *  grad        DEVICE, N x d of `dtype`, rows ldg elements apart (ldg >= d, or 0: one row stands for all N).
  *  table_grad  DEVICE, V x d of `out_dtype`, rows ldt elements apart; must not overlap the inputs.
  * Sums are held in fp32 and rounded once.  The tokens are sorted, so a token's rows are added in an order that depends on
  * the tokens alone.  N and V at most 2^31 - 1 (else UNSUPPORTED).  Enqueued on hip_stream.
@@ -458,7 +458,7 @@ gp_status gp_orthogonalize(const void *G, int64_t ldg, int64_t stride_g, gp_dtyp
  *     M_out = momentum * M + G,   U = nesterov ? G + momentum * M_out : M_out,
  *     W_out = (1 - lr * weight_decay) * W - lr * orthogonalize(U)
  *  W, W_out  DEVICE fp32, rows ldw, matrices stride_w elements apart; W_out may be W.   M, M_out  the same with ldm, stride_m.
- *  G         DEVICE, of `dtype`.  Everything else, the workspace too (gp_orthogonalize_workspace), as gp_orthogonalize. */
+ *  G         DEVICE, of `dtype`; must not overlap what is written.  Everything else, the workspace too (gp_orthogonalize_workspace), as gp_orthogonalize. */
 gp_status gp_muon_step(const float *W, float *W_out, int64_t ldw, int64_t stride_w, const float *M, float *M_out, int64_t ldm,
                        int64_t stride_m, const void *G, int64_t ldg, int64_t stride_g, gp_dtype dtype, int64_t rows,
                        int64_t cols, int64_t count, float lr, float momentum, float weight_decay, int32_t nesterov,

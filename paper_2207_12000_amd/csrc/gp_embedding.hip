@@ -859,7 +859,8 @@ gp_status embedding_grad(const void* tokens, gp_index index, int64_t N, const vo
     if ((dtype != GP_F32 && dtype != GP_BF16) || (out_dtype != GP_F32 && out_dtype != GP_BF16))
         return fail(GP_ERR_INVALID_ARG, "unknown dtype %d, %d", (int)dtype, (int)out_dtype);
     if (index != GP_I32 && index != GP_I64) return fail(GP_ERR_INVALID_ARG, "unknown index type %d", (int)index);
-    if (N < 0 || V < 1 || d < 1 || ldg < d || ldt < d) return fail(GP_ERR_INVALID_ARG, "need N >= 0, V >= 1, d >= 1, ldg >= d, ldt >= d");
+    if (N < 0 || V < 1 || d < 1 || (ldg < d && ldg != 0) || ldt < d)
+        return fail(GP_ERR_INVALID_ARG, "need N >= 0, V >= 1, d >= 1, ldg >= d or 0, ldt >= d");
     if (N > kMaxCount || V > kMaxCount) return fail(GP_ERR_UNSUPPORTED, "more than 2^31 - 1 tokens or rows");
     if (!out || (N > 0 && (!tokens || !up))) return fail(GP_ERR_INVALID_ARG, "NULL argument");
     const GradLayout l = grad_layout(N, V, d);

@@ -215,11 +215,11 @@ __global__ __launch_bounds__(kThreads) void gp_ns_start(Update u, const double* 
         }
     static_assert(kNormBlocks == kThreads, "one partial sum per thread");
     const double norm = sqrt(block_sum<kThreads>(partial[z * kNormBlocks + threadIdx.x], part));
-    const float factor = (float)((double)scale / (norm + (double)eps));
+    const double factor = (double)scale / (norm + (double)eps);  // (it, or its inverse, may be beyond fp32)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[i][j] *= r0 + i < u.rows && c0 + j < u.cols ? factor : 0.0f;
+        for (int j = 0; j < 4; ++j) v[i][j] = r0 + i < u.rows && c0 + j < u.cols ? (float)((double)v[i][j] * factor) : 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float t[4] = {v[0][i], v[1][i], v[2][i], v[3][i]};
@@ -758,11 +758,11 @@ __global__ __launch_bounds__(1024) void gp_ns_tiny(Tiny a)
     for (int g = 0; g < BLOCKS; ++g)
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum += (double)v[g][i] * v[g][i];
-    const float factor = (float)((double)a.scale / (sqrt(block_sum<1024>(sum, part)) + (double)a.eps));
+    const double factor = (double)a.scale / (sqrt(block_sum<1024>(sum, part)) + (double)a.eps);
 #pragma unroll
     for (int g = 0; g < BLOCKS; ++g)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[g][i] *= 16 * g + 4 * kg + i < m && c < n ? factor : 0.0f;
+        for (int i = 0; i < 4; ++i) v[g][i] = 16 * g + 4 * kg + i < m && c < n ? (float)((double)v[g][i] * factor) : 0.0f;
     if constexpr (BLOCKS % 2 == 1) {  // the last line's other half: zero from first to last
         const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (active) store_parts(cols + c * kColLd + place(16 * BLOCKS + 4 * kg), zero);

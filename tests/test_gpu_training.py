@@ -445,3 +445,22 @@ def test_orthogonalize_large(shape, count):
         want = X if shape[0] <= shape[1] else X.t()
         tol = 4 * 2.0 ** -22 * sum(slope ** (5 - k) * norms[k] for k in range(6)) / norms[-1]
         assert float((got[i].double() - want).norm()) <= tol * norms[-1]
+
+
+@pytest.mark.parametrize("shape", [(40, 64), (70, 200)])
+@pytest.mark.parametrize("power", [-36, 36])
+def test_magnitudes_at_the_ends_of_fp32(power, shape):
+    """The norm's inverse, or the norm itself, lies beyond fp32's normal numbers."""
+    import torch
+    G = torch.from_numpy(np.random.default_rng(14).normal(size=shape) * 10.0 ** power).float().cuda()
+    check_direction(gp.orthogonalize_tensors(G, eps=0.0), G, eps=0.0)
+
+
+def test_one_gradient_row_for_all_tokens():
+    """A gradient that was expanded from one row (rows 0 elements apart), as that of a sum is."""
+    import torch
+    rng = np.random.default_rng(15)
+    tokens = torch.from_numpy(rng.integers(-1, 20, 500)).cuda()
+    row = torch.from_numpy(rng.normal(size=(1, 37))).float().cuda()
+    up = row.expand(500, 37)
+    check_gradient(gp.embedding_grad_tensors(tokens, up, 20), tokens, up, 20, 1.0)
