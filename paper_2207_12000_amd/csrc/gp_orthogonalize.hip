@@ -547,35 +547,38 @@ template <typename TO, bool LAST>
 __global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product a)
 {
     __shared__ __align__(16) float part[kSmallWaves][32][36];
-    int bi, bj;
-    const int64_t t = stretched_block();
-    if (t >= a.tile_count) return;
-    tile_at(a, (int)t, bi, bj);
+    const int bi = blockIdx.y, bj = blockIdx.x;
+    if (a.symmetric && bi > bj) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t base = (int64_t)blockIdx.z * a.stride;
     const int r0 = bi * 32, c0 = bj * 32;
-    const f16* const p = a.P + base + (int64_t)(r0 + (lane & 31)) * a.ldp + (lane >> 5) * 8;
-    const f16* const q = a.Q + base + (int64_t)(c0 + (lane & 31)) * a.ldq + (lane >> 5) * 8;
-    v16f acc[3];
+    // 16 x 16 x 32 instructions: four lanes read 64 bytes of a row (two lanes and 32 bytes, as the 32 x 32 x 16 ones have it, keep the
+    // address unit busy for twice as long)
+    const int r16 = lane & 15, kg = lane >> 4;
+    const f16* const p = a.P + base + (int64_t)(r0 + r16) * a.ldp + kg * 8;
+    const f16* const q = a.Q + base + (int64_t)(c0 + r16) * a.ldq + kg * 8;
+    v4f acc[2][2];
 #pragma unroll
-    for (int x = 0; x < 3; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[x][i] = 0.0f;
+    for (int x = 0; x < 4; ++x) acc[x / 2][x % 2] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
     const int steps = a.K / 32;
-    v8h pv[2][4], qv[2][4];  // [line][16 columns' first parts, the next 16's, second parts of both]
+    v8h pv[2][2][2], qv[2][2][2];  // [line][16 rows][part]
     auto load = [&](int b, int step) {
         if (step >= steps) return;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) pv[b][i] = *(const v8h*)(p + (int64_t)step * 64 + i * 16), qv[b][i] = *(const v8h*)(q + (int64_t)step * 64 + i * 16);
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                pv[b][h][part] = *(const v8h*)(p + (int64_t)h * 16 * a.ldp + (int64_t)step * 64 + part * kParts);
+                qv[b][h][part] = *(const v8h*)(q + (int64_t)h * 16 * a.ldq + (int64_t)step * 64 + part * kParts);
+            }
     };
     auto multiply = [&](int b, int step) {
         if (step >= steps) return;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[b][i], qv[b][i], acc[0], 0, 0, 0);
-            acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[b][i + 2], qv[b][i], acc[1], 0, 0, 0);
-            acc[2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[b][i], qv[b][i + 2], acc[2], 0, 0, 0);
-        }
+        for (int x = 0; x < 3; ++x)
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+                acc[h / 2][h % 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pv[b][h / 2][x == 0], qv[b][h % 2][x == 1], acc[h / 2][h % 2], 0, 0, 0);
     };
     load(0, wave), load(1, wave + kSmallWaves);
     const bool mine = threadIdx.x < 256;  // four neighbours of a row each, at the end
@@ -592,7 +595,9 @@ __global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product 
         load(1, k + 3 * kSmallWaves);
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) part[wave][(i >> 2) * 8 + (lane >> 5) * 4 + (i & 3)][lane & 31] = acc[0][i] + (acc[1][i] + acc[2][i]);
+    for (int h = 0; h < 4; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[wave][h / 2 * 16 + kg * 4 + i][h % 2 * 16 + r16] = acc[h / 2][h % 2][i];
     __syncthreads();
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (mine) {
@@ -1056,7 +1061,7 @@ gp_status launch_product(Product a, const Cut& cut, int64_t count, hipStream_t s
     if (bm == 128) return launch_tiles<128, 128, 2, 4, 4, TO, LAST>(a, stream);
     if (bm == 64) return launch_tiles<64, 64, 2, 2, 4, TO, LAST>(a, stream);
     profile_begin("gp_ns_product", stream);
-    hipLaunchKernelGGL((gp_ns_product_small<TO, LAST>), dim3((unsigned)((a.tile_count + 7) / 8 * 8), 1, (unsigned)count), dim3(64 * kSmallWaves), 0, stream, a);
+    hipLaunchKernelGGL((gp_ns_product_small<TO, LAST>), dim3((unsigned)a.tiles_n, (unsigned)a.tiles_m, (unsigned)count), dim3(64 * kSmallWaves), 0, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     return GP_OK;
