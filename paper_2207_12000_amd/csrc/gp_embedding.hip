@@ -37,6 +37,19 @@ template <typename T, int N>
 struct Vec {
     typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
 };
+template <typename T>
+struct Vec<T, 1> {
+    typedef T type;
+};
+// element i of one, widened
+template <typename T, int N>
+__device__ __forceinline__ float element(const typename Vec<T, N>::type& x, int i)
+{
+    if constexpr (N == 1)
+        return widen(x);
+    else
+        return widen(x[i]);
+}
 template <typename T, int N>
 __device__ __forceinline__ void load_vec(const T* p, float (&v)[N])
 {
@@ -488,17 +501,19 @@ __global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
             came_in = before == cur;
             if (!came_in) fill_gap(before, cur);
         }
-        for (int64_t p = lo; p < hi; p += U) {
-            uint64_t key[U];
-            float v[U][VEC];
+        uint64_t key[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) key[u] = p + u < hi ? a.keys[p + u] : ~UINT64_C(0);
+        for (int u = 0; u < U; ++u) key[u] = lo + u < hi ? a.keys[lo + u] : ~UINT64_C(0);
+        for (int64_t p = lo; p < hi; p += U) {
+            typename Vec<TG, VEC>::type v[U];  // (widened when they are added: registers decide how many wavefronts there are)
+            uint64_t next[U];                  // (asked for beside this step's rows, not behind them)
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) v[u][i] = 0.0f;
-                if ((int64_t)(key[u] >> 32) < a.V) load_vec<TG, VEC>(up + (int64_t)(key[u] & 0xFFFFFFFFu) * a.ldg, v[u]);
+                v[u] = 0;
+                if ((int64_t)(key[u] >> 32) < a.V) v[u] = *reinterpret_cast<const typename Vec<TG, VEC>::type*>(up + (int64_t)(key[u] & 0xFFFFFFFFu) * a.ldg);
             }
+#pragma unroll
+            for (int u = 0; u < U; ++u) next[u] = p + U + u < hi ? a.keys[p + U + u] : ~UINT64_C(0);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (p + u >= hi) break;
@@ -516,8 +531,10 @@ __global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
                     cur = tok, came_in = false;
                 }
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) acc[i] += v[u][i];
+                for (int i = 0; i < VEC; ++i) acc[i] += element<TG, VEC>(v[u], i);
             }
+#pragma unroll
+            for (int u = 0; u < U; ++u) key[u] = next[u];
         }
         open = cur < a.V && hi < a.N && (int64_t)(a.keys[hi] >> 32) == cur;
         if (came_in && g > 0) {
