@@ -16,7 +16,16 @@
 // and lo above its subnormal numbers where it counts.
 //
 // Every product is taken as rows times rows (both operands consecutive along the summed dimension): A and B are symmetric,
-// and X is kept in both orientations.
+// and X is kept in both orientations.  (Iterating on A alone and multiplying X once at the end would take fewer products for long matrices, but
+// its roundings grow by a^2 a step: NaN after five on most matrices tried, in 22 bits.)
+//
+// What bounds it, and us measured (five steps).  Large matrices: power.  The third product of 4096 x 4096 takes 355 us, 1.16 PFLOP/s of f16 products,
+// with the matrix cores 60 % busy at 1.9 GHz; the same launch on operands that are all one number takes 210.  The whole, 3.7 - 3.9 ms, of which
+// the symmetric products, half of whose tiles are computed, take 198 each; a library's fp32 products take 14.7.  Middle sizes: how evenly tiles fill
+// the chip, and the planes' traffic (two 1024 x 4096 steps with bf16 gradients 651: X X^T 48, A A 20, the update 64, the start 32,
+// norms and momentum 21).  Small ones: the chain of 17 launches, 5 us each, of which a launch on its own would take 1.6 and lines
+// that the launch before has sent past the L2s another 2 (two 256 x 256 81, 602 x 256 96).  Up to 64 x 256 one launch: 12 (16 x 16),
+// 18 (64 x 64), 32 (256 x 40), 35 (64 x 256); 45 to 62 for 256 x 40 in several.
 #include <algorithm>
 #include <cmath>
 #include <exception>
@@ -340,9 +349,12 @@ __device__ __forceinline__ void write_row(const Product& a, int64_t o, int count
     }
 }
 
-// BM x BN tiles of D by WM x WN waves.  A step sums over 32 columns: BM + BN lines of 128 bytes, which go straight from memory to one
-// half of LDS while the matrix cores work on the other half.  A line's 16-byte pieces lie in LDS in the order
-// piece ^ (row / 2 mod 8), with which the 16 lanes that LDS serves together read different banks.
+// BM x BN tiles of D by WM x WN waves.  A step sums over 32 columns: BM + BN lines of 128 bytes, which go straight from memory to one of
+// STAGES parts of LDS while the matrix cores work on another.  A line's 16-byte pieces lie in LDS in the order
+// piece ^ (row / 2 mod 8), with which the 16 lanes that LDS serves together read different banks (no conflicts counted).
+// What the shape owes to measurement: large tiles, since every product reads its operands from LDS (us for a 4096 x 4096 update in tiles of 64, 128 and
+// 256: 500, 396, 350); loads one at a time among the products (256 x 256 tiles, operands of one number, so that power does not hide it: 232
+// us, 270 where a step's loads go out together, and 204 without any).
 // A wave's registers hold its BM / WM x BN / WN sums as 32 x 32 blocks: lane l has column l mod 32, rows 8 (i / 4) + 4 (l / 32) + i mod 4.
 template <int BM, int BN, int WM, int WN, int STAGES, typename TO, bool LAST>
 __global__ __launch_bounds__(64 * WM * WN) void gp_ns_product(Product a)
@@ -708,8 +720,9 @@ __global__ __launch_bounds__(4 * M) void gp_ns_panel(Panel a)
 }
 
 // The whole of it for matrices of up to 64 x 256: one workgroup each, one launch.  A wavefront owns 16 columns of X, whose values stay in
-// its registers in fp32 from first to last; LDS holds X's parts in rows (for A = X X^T, one 16 x 16 block per wavefront) and in
-// columns (for the panel's own Y = A X, then, in the same place, for A Y), and A's parts.
+// its registers in fp32 from first to last; LDS holds X's parts in rows (for A = X X^T, a 16 x 16 block on or above the diagonal per
+// wavefront, and its mirror image) and in columns (for the panel's own Y = A X, then, in the same place, for A Y), and A's parts: 150 of
+// the 160 KB.  A step takes 3 to 6 us: three barriers, LDS reads and 24 to 72 products per wavefront, one after the other.
 struct Tiny {
     Update u;
     float eps;
@@ -938,12 +951,13 @@ int exponent_for(double bound)
 // a part of the columns each (larger tiles' sums take longer to hand over than that saves).  The cut of the least time by what
 // its parts take, in us as measured: a step of 32 columns where few compute units are at work and where all are (power is what
 // the large ones run out of), a tile's end, and handing over one workgroup's sums.  us a launch, model / measured:
-//     m x n, K                  64          128          192          256
-//   1024 x 1024, 1024       14 / 16      26 / 26      44 / 48      61 / 79
-//   2048 x 2048, 2048       71 / 72      59 / 60      88 / 87     121 / 138
-//   the same, X X^T         53 / 54      50 / 50      82 / 78     112 / 131
-//   4096 x 4096, 4096      537 / 500    442 / 396    394 / 400    345 / 350
-//   the same, X X^T        311 / 275    287 / 259    196 / 198    273 / 262
+//     m x n, K                  64          128      128 x 256       192          256
+//   1024 x 1024, 1024       16 / 16      26 / 26                   44 / 48      59 / 79
+//   2048 x 2048, 2048       75 / 72      59 / 60                   88 / 87     121 / 138
+//   the same, X X^T         61 / 54      50 / 50                   82 / 78     112 / 131
+//   4096 x 4096, 4096      564 / 500    442 / 396                 387 / 400    345 / 350
+//   the same, X X^T        326 / 275    295 / 259                 196 / 198    273 / 262
+//   2 of 1024 x 4096, 1024  83 / 87      67 / 80      55 / 61      99 / 107     76 / 84
 struct Cut {
     int bm, bn;
     int64_t tiles;  // of all matrices
