@@ -464,3 +464,41 @@ def test_one_gradient_row_for_all_tokens():
     row = torch.from_numpy(rng.normal(size=(1, 37))).float().cuda()
     up = row.expand(500, 37)
     check_gradient(gp.embedding_grad_tensors(tokens, up, 20), tokens, up, 20, 1.0)
+
+
+@pytest.mark.parametrize("N,V,d,tokens_kind", [(9000, 63, 5, "uniform"), (9000, 64, 5, "hot"), (20_000, 255, 3, "uniform"), (20_000, 256, 3, "uniform"),
+                                               (30_000, 511, 2, "hot"), (30_000, 512, 2, "uniform"), (50_000, 2047, 1, "uniform"),
+                                               (50_000, 2048, 1, "hot"), (8192, 4_300_000, 2, "uniform"), (8193, 4_194_304, 2, "uniform"),
+                                               (40_000, 9_000_001, 1, "hot"), (1_300_000, 3_000_000, 3, "hot"), (1_048_577, 300, 4, "uniform")])
+def test_gradient_at_the_sort_s_boundaries(N, V, d, tokens_kind):
+    """Digits of 6, 8, 9 and 11 bits, one to three passes, short and long lists, small and large tiles of them."""
+    import torch
+    rng = np.random.default_rng(N + V)
+    tokens = torch.from_numpy(tokens_of(tokens_kind, N, V, rng)).to(torch.int32).cuda()
+    up = torch.from_numpy(rng.normal(size=(N, d)).astype(np.float32)).cuda()
+    out = torch.full((V, d), float("nan"), device="cuda")
+    gp.embedding_grad_tensors(tokens, up, V, out=out)
+    check_gradient(out, tokens, up, V, 1.0)
+
+
+@pytest.mark.parametrize("kind", ["low", "high", "ends", "middle"])
+def test_long_gaps_between_tokens_are_zero(kind):
+    """Gaps of up to 256 rows, of more, before the first token and behind the last, around every multiple of 256."""
+    import torch
+    V, d = 3000, 5
+    places = {"low": [0, 1, 255, 256, 257], "high": [2739, 2996, 2998, 2999], "ends": [0, 2999], "middle": [1500]}[kind]
+    for shift in (0, 1):
+        tokens = torch.tensor([p + shift for p in places if p + shift < V], dtype=torch.int32, device="cuda").repeat(3)
+        up = torch.ones(tokens.numel(), d, device="cuda")
+        out = torch.full((V, d), float("nan"), device="cuda")
+        gp.embedding_grad_tensors(tokens, up, V, out=out)
+        want = torch.zeros(V, d, device="cuda")
+        want[tokens.long()] = 3.0
+        assert torch.equal(out, want)
+    for gap in (255, 256, 257, 258, 511, 513):
+        tokens = torch.arange(0, V, gap, dtype=torch.int32, device="cuda")
+        out = torch.full((V, d), float("nan"), device="cuda")
+        gp.embedding_grad_tensors(tokens, torch.ones(tokens.numel(), d, device="cuda"), V, out=out)
+        want = torch.zeros(V, d, device="cuda")
+        want[tokens.long()] = 1.0
+        assert torch.equal(out, want)
