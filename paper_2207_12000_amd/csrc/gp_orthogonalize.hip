@@ -722,7 +722,9 @@ __global__ __launch_bounds__(4 * M) void gp_ns_panel(Panel a)
 // The whole of it for matrices of up to 64 x 256: one workgroup each, one launch.  A wavefront owns 16 columns of X, whose values stay in
 // its registers in fp32 from first to last; LDS holds X's parts in rows (for A = X X^T, a 16 x 16 block on or above the diagonal per
 // wavefront, and its mirror image) and in columns (for the panel's own Y = A X, then, in the same place, for A Y), and A's parts: 150 of
-// the 160 KB.  A step takes 3 to 6 us: three barriers, LDS reads and 24 to 72 products per wavefront, one after the other.
+// the 160 KB.  A step takes 3 to 6 us: three barriers, LDS reads and 24 to 72 products per wavefront, one after the other.  The matrices
+themselves take the rest: an update of 256 x 40 takes 26 us, 43 where a tall matrix's elements, whose neighbours a lane has in a row, are
+asked for and written one by one; of 40 x 256, 27 us.
 struct Tiny {
     Update u;
     float eps;
@@ -749,29 +751,46 @@ __global__ __launch_bounds__(1024) void gp_ns_tiny(Tiny a)
     const int panels = (n + 31) / 32 * 2;  // (whole lines of columns)
     const bool active = wave < panels;
     constexpr int kLines = (BLOCKS + 1) / 2;
-    // U, element by element, and the new momentum
+    // U, element by element, and the new momentum.  The lane's four elements of a block are neighbours in a tall matrix's rows
     const T* const G = (const T*)a.u.G + z * a.u.stride_g;
     float v[BLOCKS][4], mo[BLOCKS][4];
     double sum = 0.0;
+    auto first_row = [&](int g) { return 16 * g + 4 * kg; };
+    auto held = [&](int g) { return c < n ? max(0, min(4, m - first_row(g))) : 0; };  // of the four, those that the matrix has
+    auto read = [&](const auto* from, int64_t ld, int g, float(&x)[4]) {
+        const int count = held(g);
+        if (a.tall) {
+            load_some(from + (count ? c * ld + first_row(g) : 0), count, x);
+        } else {
 #pragma unroll
-    for (int g = 0; g < BLOCKS; ++g)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = 16 * g + 4 * kg + i;
-            const int64_t ur = a.tall ? c : r, uc = a.tall ? r : c;
-            v[g][i] = r < m && c < n ? widen(G[ur * a.u.ldg + uc]) : 0.0f;
-            mo[g][i] = a.u.M && r < m && c < n ? a.u.M[z * a.u.stride_m + ur * a.u.ldm + uc] : 0.0f;
+            for (int i = 0; i < 4; ++i) x[i] = i < count ? widen(from[(first_row(g) + i) * ld + c]) : 0.0f;
         }
-    if (a.u.M)
+    };
+    auto write = [&](float* to, int64_t ld, int g, const float(&x)[4]) {
+        const int count = held(g);
+        if (a.tall) {
+            if (count) store_some(to + c * ld + first_row(g), count, x);
+        } else {
 #pragma unroll
-        for (int g = 0; g < BLOCKS; ++g)
+            for (int i = 0; i < 4; ++i)
+                if (i < count) to[(first_row(g) + i) * ld + c] = x[i];
+        }
+    };
+#pragma unroll
+    for (int g = 0; g < BLOCKS; ++g) read(G, a.u.ldg, g, v[g]);
+    if (a.u.M) {
+#pragma unroll
+        for (int g = 0; g < BLOCKS; ++g) read(a.u.M + z * a.u.stride_m, a.u.ldm, g, mo[g]);
+#pragma unroll
+        for (int g = 0; g < BLOCKS; ++g) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int r = 16 * g + 4 * kg + i;
-                const float x = a.u.mu * mo[g][i] + v[g][i];
-                if (r < m && c < n) a.u.M_out[z * a.u.stride_m + (a.tall ? c : r) * a.u.ldm + (a.tall ? r : c)] = x;
-                v[g][i] = a.u.nesterov ? v[g][i] + a.u.mu * x : x;
+                mo[g][i] = a.u.mu * mo[g][i] + v[g][i];
+                v[g][i] = a.u.nesterov ? v[g][i] + a.u.mu * mo[g][i] : mo[g][i];
             }
+            write(a.u.M_out + z * a.u.stride_m, a.u.ldm, g, mo[g]);
+        }
+    }
 #pragma unroll
     for (int g = 0; g < BLOCKS; ++g)
 #pragma unroll
@@ -889,24 +908,22 @@ __global__ __launch_bounds__(1024) void gp_ns_tiny(Tiny a)
     const Product& p = a.last;
     if (p.W) {  // (all requests before the first use)
 #pragma unroll
-        for (int g = 0; g < BLOCKS; ++g)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 16 * g + 4 * kg + i;
-                mo[g][i] = r < m && c < n ? p.W[z * p.stride_o + (a.tall ? c : r) * p.ldo + (a.tall ? r : c)] : 0.0f;
-            }
+        for (int g = 0; g < BLOCKS; ++g) read(p.W + z * p.stride_o, p.ldo, g, mo[g]);
 #pragma unroll
         for (int g = 0; g < BLOCKS; ++g)
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[g][i] = p.keep * mo[g][i] - p.lr * v[g][i];
     }
 #pragma unroll
-    for (int g = 0; g < BLOCKS; ++g)
+    for (int g = 0; g < BLOCKS; ++g) {
+        if constexpr (sizeof(TO) == 4) {
+            write((float*)p.out + z * p.stride_o, p.ldo, g, v[g]);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = 16 * g + 4 * kg + i;
-            if (r < m && c < n) store_out<TO>(p, z * p.stride_o + (a.tall ? c : r) * p.ldo + (a.tall ? r : c), v[g][i]);
+            for (int i = 0; i < 4; ++i)
+                if (i < held(g)) store_out<TO>(p, z * p.stride_o + (a.tall ? c : first_row(g) + i) * p.ldo + (a.tall ? first_row(g) + i : c), v[g][i]);
         }
+    }
 }
 
 // ---- ranges ------------------------------------------------------------------------------------------
