@@ -723,8 +723,8 @@ __global__ __launch_bounds__(4 * M) void gp_ns_panel(Panel a)
 // its registers in fp32 from first to last; LDS holds X's parts in rows (for A = X X^T, a 16 x 16 block on or above the diagonal per
 // wavefront, and its mirror image) and in columns (for the panel's own Y = A X, then, in the same place, for A Y), and A's parts: 150 of
 // the 160 KB.  A step takes 3 to 6 us: three barriers, LDS reads and 24 to 72 products per wavefront, one after the other.  The matrices
-themselves take the rest: an update of 256 x 40 takes 26 us, 43 where a tall matrix's elements, whose neighbours a lane has in a row, are
-asked for and written one by one; of 40 x 256, 27 us.
+// themselves take the rest: an update of 256 x 40 takes 26 us, 43 where a tall matrix's elements, whose neighbours a lane has in a row, are
+// asked for and written one by one; of 40 x 256, 27 us.
 struct Tiny {
     Update u;
     float eps;
