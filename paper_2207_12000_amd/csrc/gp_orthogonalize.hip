@@ -313,7 +313,26 @@ __device__ __forceinline__ void write_out(const Product& a, int64_t o, float v)
 {
     store_out<TO>(a, o, a.W ? a.keep * a.W[o] - a.lr * v : v);
 }
-// the first `count` of sixteen neighbours of a row, from any element's boundary
+// the first `count` of four and of sixteen neighbours of a row, from any element's boundary
+template <typename TO>
+__device__ __forceinline__ void write_some(const Product& a, int64_t o, int count, const float (&v)[4])
+{
+    float x[4] = {v[0], v[1], v[2], v[3]};
+    if (count <= 0) return;
+    if (a.W) {
+        float w[4];
+        load_some(a.W + o, count, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = a.keep * w[i] - a.lr * v[i];
+    }
+    if constexpr (sizeof(TO) == 4) {
+        store_some((float*)a.out + o, count, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < count) store_out<TO>(a, o + i, x[i]);
+    }
+}
 typedef bf16_t v8b_any __attribute__((ext_vector_type(8), aligned(2)));
 template <typename TO>
 __device__ __forceinline__ void write_row(const Product& a, int64_t o, int count, const float (&v)[16])
@@ -623,11 +642,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product 
     }
     if constexpr (LAST) {
         if (!mine || r >= a.rows) return;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (c + i >= a.cols) continue;
-            write_out<TO>(a, blockIdx.z * a.stride_o + (int64_t)r * a.ldo + c + i, v[i]);
-        }
+        write_some<TO>(a, blockIdx.z * a.stride_o + (int64_t)r * a.ldo + c, (int)min(a.cols - c, (int64_t)4), v);
     } else {
         if (mine) store_parts(a.D + base + (int64_t)r * a.ldd + place(c), v);
         if (a.symmetric && bi == bj) return;  // (the tile holds both halves)
@@ -702,10 +717,13 @@ __global__ __launch_bounds__(4 * M) void gp_ns_panel(Panel a)
     const int c = c0 + r16;
     if constexpr (LAST) {
         const Product& p = a.last;
+        const int64_t o = blockIdx.z * p.stride_o;
+        if (a.tall) {  // (the lane's elements are neighbours)
+            if (c < p.rows) write_some<TO>(p, o + c * p.ldo + r, (int)min(p.cols - r, (int64_t)4), v);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t row = a.tall ? c : r + i, col = a.tall ? r + i : c;
-            if (row < p.rows && col < p.cols) write_out<TO>(p, blockIdx.z * p.stride_o + row * p.ldo + col, v[i]);
+            for (int i = 0; i < 4; ++i)
+                if (r + i < p.rows && c < p.cols) write_out<TO>(p, o + (r + i) * p.ldo + c, v[i]);
         }
     } else {
         store_parts(a.Xt_out + base + (int64_t)c * (2 * M) + place(r), v);
