@@ -578,8 +578,12 @@ template <typename TO, bool LAST>
 __global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product a)
 {
     __shared__ __align__(16) float part[kSmallWaves][32][36];
-    const int bi = blockIdx.y, bj = blockIdx.x;
-    if (a.symmetric && bi > bj) return;
+    int bi = blockIdx.y, bj = blockIdx.x;
+    if (a.symmetric) {  // rows of the triangle from both ends fill one row of the grid (workgroups that end at once leave units idle: X X^T
+        const int n = a.tiles_n, even = n % 2 == 0;  // of 704 x 2000 took 30 us, 17 so, and A A of 704 x 704 12.7, 8.4 so)
+        const bool upper = bj >= bi + even;
+        bj = upper ? bj - even : n - 1 - bj, bi = upper ? bi : n - even - bi;
+    }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t base = (int64_t)blockIdx.z * a.stride;
     const int r0 = bi * 32, c0 = bj * 32;
@@ -1110,7 +1114,9 @@ gp_status launch_product(Product a, const Cut& cut, int64_t count, hipStream_t s
     if (bm == 128) return launch_tiles<128, 128, 2, 4, 4, TO, LAST>(a, stream);
     if (bm == 64) return launch_tiles<64, 64, 2, 2, 4, TO, LAST>(a, stream);
     profile_begin("gp_ns_product", stream);
-    hipLaunchKernelGGL((gp_ns_product_small<TO, LAST>), dim3((unsigned)a.tiles_n, (unsigned)a.tiles_m, (unsigned)count), dim3(64 * kSmallWaves), 0, stream, a);
+    const int even = a.tiles_n % 2 == 0;
+    const dim3 grid(a.tiles_n + (a.symmetric ? even : 0), a.symmetric ? (a.tiles_n + 1) / 2 : a.tiles_m, (unsigned)count);
+    hipLaunchKernelGGL((gp_ns_product_small<TO, LAST>), grid, dim3(64 * kSmallWaves), 0, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     return GP_OK;
