@@ -989,14 +989,22 @@ int exponent_for(double bound)
 // How a product is cut: tiles of 32 (gp_ns_product_small), 64, 128, 128 x 256, 192 or 256, and how many workgroups sum up a tile of 64 or 128,
 // a part of the columns each (larger tiles' sums take longer to hand over than that saves).  The cut of the least time by what
 // its parts take, in us as measured: a step of 32 columns where few compute units are at work and where all are (power is what
-// the large ones run out of), a tile's end, and handing over one workgroup's sums.  us a launch, model / measured:
-//     m x n, K                  64          128      128 x 256       192          256
-//   1024 x 1024, 1024       16 / 16      26 / 26                   44 / 48      59 / 79
-//   2048 x 2048, 2048       75 / 72      59 / 60                   88 / 87     121 / 138
-//   the same, X X^T         61 / 54      50 / 50                   82 / 78     112 / 131
-//   4096 x 4096, 4096      564 / 500    442 / 396                 387 / 400    345 / 350
-//   the same, X X^T        326 / 275    295 / 259                 196 / 198    273 / 262
-//   2 of 1024 x 4096, 1024  83 / 87      67 / 80      55 / 61      99 / 107     76 / 84
+// the large ones run out of), a tile's end, and for shared tiles the hand-over and its share of every workgroup's.  us a launch,
+// model / measured (and workgroups to a tile):
+//     m x n, K                    32             64               128         128 x 256     192          256
+//    256 x 256, 256            4.9 / 4.9      6.2 / 6.5        11 / 10
+//    640 x 640, 640 (A A)      7.5 / 8.0      9.0 / 9.9        15 / 18
+//    256 x 4096, X X^T          31 / 30       14 / 13 (8)      25 / 24 (8)
+//    704 x 2048, X X^T          17 / 17       14 / 13 (3)      22 / 22 (4)
+//    704 x 4096, update                       27 / 26          24 / 24
+//   1024 x 1024, 1024           31 / 32       15 / 15          19 / 24                    44 / 48      59 / 79
+//   1024 x 4096, X X^T          82            41 / 39          32 / 33 (4)
+//   1536 x 1536, X X^T                        24 / 25          24 / 27 (3)
+//   2048 x 2048, 2048                         75 / 72          61 / 60                    88 / 87     121 / 138
+//   the same, X X^T                           57 / 54          50 / 50                    82 / 78     112 / 131
+//   4096 x 4096, 4096                        566 / 500        458 / 396                  387 / 400    345 / 350
+//   the same, X X^T                          319 / 275        300 / 259                  196 / 198    273 / 262
+//   2 of 1024 x 4096, 1024                    83 / 87          68 / 80       55 / 61      99 / 107     76 / 84
 struct Cut {
     int bm, bn;
     int64_t tiles;  // of all matrices
@@ -1009,25 +1017,28 @@ Cut choose_cut(int64_t m, int64_t n, int64_t k, bool symmetric, int64_t count)
     const int64_t steps = k / 32;
     auto tiles = [&](int64_t bm, int64_t bn) { return tile_numbers((m + bm - 1) / bm, (n + bn - 1) / bn, symmetric) * count; };
     Cut best{32, 32, tiles(32, 32), 1, 1e30};
-    if (best.tiles <= 4 * kUnits) best.us = (double)((best.tiles + kUnits - 1) / kUnits) * (2.5 + 0.22 * steps);
+    const int64_t rounds = (best.tiles + kUnits - 1) / kUnits;  // workgroups that share a compute unit
+    if (rounds <= 4) best.us = 2.4 + 0.8 * (double)rounds + (0.02 + 0.195 * (double)rounds) * (double)steps;
     struct Kind {
         int bm, bn;
-        double few, all, finish, hand_over;
+        double few, all, finish, hand_over, share;
     };
-    static const Kind kinds[] = {{256, 256, 1.4, 2.6, 12.0, 0.0}, {192, 192, 1.0, 1.46, 10.0, 0.0}, {128, 256, 0.85, 1.4, 10.0, 0.0},
-                                 {128, 128, 0.5, 0.8, 8.0, 1.2}, {64, 64, 0.3, 0.36, 4.0, 0.5}};
+    static const Kind kinds[] = {{256, 256, 1.4, 2.6, 12.0, 0.0, 0.0}, {192, 192, 1.0, 1.46, 10.0, 0.0, 0.0}, {128, 256, 0.85, 1.4, 10.0, 0.0, 0.0},
+                                 {128, 128, 0.48, 0.84, 7.0, 1.5, 1.0}, {64, 64, 0.24, 0.33, 4.2, 1.4, 0.45}};
     for (const Kind& c : kinds) {
         if (symmetric && c.bm != c.bn) continue;
         const int64_t T = tiles(c.bm, c.bn);
-        auto step = [&](int64_t units) { return c.few + (c.all - c.few) * (double)units / kUnits; };
-        // rounds of workgroups; two of those with tiles of 64 share a compute unit
+        // (beyond one per unit: two workgroups with tiles of 64 share one)
+        auto step = [&](int64_t units) {
+            return units <= kUnits ? c.few + (c.all - c.few) * (double)units / kUnits : std::min(0.52, 0.35 + 0.0015 * (double)(units - kUnits));
+        };
         const int64_t full = c.bm == 64 ? 2 * kUnits : kUnits, rest = T % full;
-        double us = (double)(T / full) * (steps * (c.bm == 64 ? 0.52 : c.all) + c.finish);
-        if (rest) us += steps * (rest > kUnits ? 0.52 : step(rest)) + c.finish;
+        double us = (double)(T / full) * ((double)steps * step(full) + c.finish);
+        if (rest) us += (double)steps * step(rest) + c.finish;
         if (us < best.us) best = {c.bm, c.bn, T, 1, us};
-        if (c.hand_over == 0.0) continue;
+        if (c.share == 0.0) continue;
         for (int64_t parts = 2; parts * T <= kUnits && 2 * parts <= steps; ++parts) {
-            us = (double)((steps + parts - 1) / parts) * step(parts * T) + c.finish + 4.0 + c.hand_over * (double)parts;
+            us = (double)((steps + parts - 1) / parts) * step(parts * T) + c.finish + c.hand_over + c.share * (double)parts;
             if (us < best.us) best = {c.bm, c.bn, T, (int)parts, us};
         }
     }
