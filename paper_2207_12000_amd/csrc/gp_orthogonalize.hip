@@ -574,10 +574,11 @@ __global__ __launch_bounds__(64 * WM * WN) void gp_ns_product(Product a)
 // their sums in LDS.
 constexpr int kSmallWaves = 8;
 
-template <typename TO, bool LAST>
+template <typename TO, bool LAST, bool SHARED>
 __global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product a)
 {
     __shared__ __align__(16) float part[kSmallWaves][32][36];
+    [[maybe_unused]] __shared__ int arrivals;
     int bi = blockIdx.y, bj = blockIdx.x;
     if (a.symmetric) {  // rows of the triangle from both ends fill one row of the grid (workgroups that end at once leave units idle: X X^T
         const int n = a.tiles_n, even = n % 2 == 0;  // of 704 x 2000 took 30 us, 17 so, and A A of 704 x 704 12.7, 8.4 so)
@@ -585,7 +586,8 @@ __global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product 
         bj = upper ? bj - even : n - 1 - bj, bi = upper ? bi : n - even - bi;
     }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t base = (int64_t)blockIdx.z * a.stride;
+    const int matrix = SHARED ? blockIdx.z / a.parts : blockIdx.z, share = SHARED ? blockIdx.z - matrix * a.parts : 0;  // (of the columns)
+    const int64_t base = matrix * a.stride;
     const int r0 = bi * 32, c0 = bj * 32;
     // 16 x 16 x 32 instructions: four lanes read 64 bytes of a row (two lanes and 32 bytes, as the 32 x 32 x 16 ones have it, keep the
     // address unit busy for twice as long)
@@ -595,10 +597,10 @@ __global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product 
     v4f acc[2][2];
 #pragma unroll
     for (int x = 0; x < 4; ++x) acc[x / 2][x % 2] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
-    const int steps = a.K / 32;
+    const int steps = a.K / 32, begin = SHARED ? steps * share / a.parts : 0, end = SHARED ? steps * (share + 1) / a.parts : steps;
     v8h pv[2][2][2], qv[2][2][2];  // [line][16 rows][part]
     auto load = [&](int b, int step) {
-        if (step >= steps) return;
+        if (step >= end) return;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -608,14 +610,14 @@ __global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product 
             }
     };
     auto multiply = [&](int b, int step) {
-        if (step >= steps) return;
+        if (step >= end) return;
 #pragma unroll
         for (int x = 0; x < 3; ++x)
 #pragma unroll
             for (int h = 0; h < 4; ++h)
                 acc[h / 2][h % 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pv[b][h / 2][x == 0], qv[b][h % 2][x == 1], acc[h / 2][h % 2], 0, 0, 0);
     };
-    load(0, wave), load(1, wave + kSmallWaves);
+    load(0, begin + wave), load(1, begin + wave + kSmallWaves);
     const bool mine = threadIdx.x < 256;  // four neighbours of a row each, at the end
     const int lr = (threadIdx.x >> 3) & 31, lc = (threadIdx.x & 7) * 4, r = r0 + lr, c = c0 + lc;
     v4h eh = {0, 0, 0, 0}, el = {0, 0, 0, 0};
@@ -623,7 +625,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product 
         const f16* const e = a.E + base + (int64_t)r * a.lde + place(c);
         eh = *(const v4h*)e, el = *(const v4h*)(e + kParts);
     }
-    for (int k = wave; k < steps; k += 2 * kSmallWaves) {
+    for (int k = begin + wave; k < end; k += 2 * kSmallWaves) {
         multiply(0, k);
         load(0, k + 2 * kSmallWaves);
         multiply(1, k + kSmallWaves);
@@ -641,12 +643,52 @@ __global__ __launch_bounds__(64 * kSmallWaves) void gp_ns_product_small(Product 
             const float4 x = *(const float4*)&part[w][lr][lc];
             v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
         }
+    }
+    if constexpr (SHARED) {  // handed over as gp_ns_product does it
+        constexpr int kTogether = 4;
+        const int64_t tile = ((int64_t)matrix * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
+        uint64_t* const sums = (uint64_t*)a.partial + tile * a.parts * 512 + (threadIdx.x & 255);
+        if (mine)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const v2f x = {v[2 * q], v[2 * q + 1]};
+                __hip_atomic_store(sums + share * 512 + q * 256, __builtin_bit_cast(uint64_t, x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+        wait_and_meet<0>();
+        if (threadIdx.x == 0) arrivals = __hip_atomic_fetch_add(a.arrived + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
+        __syncthreads();
+        if (arrivals < a.parts) return;
+        if (threadIdx.x == 0) __hip_atomic_store(a.arrived + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = 0.0f;
+            for (int w = 0; w < a.parts; w += kTogether) {
+                uint64_t x[kTogether][2];
+#pragma unroll
+                for (int t = 0; t < kTogether; ++t)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        x[t][q] = __hip_atomic_load(sums + min(w + t, a.parts - 1) * 512 + q * 256, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int t = 0; t < kTogether; ++t) {
+                    if (w + t >= a.parts) break;
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const v2f y = __builtin_bit_cast(v2f, x[t][q]);
+                        v[2 * q] += y[0], v[2 * q + 1] += y[1];
+                    }
+                }
+            }
+        }
+    }
+    if (mine) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = v[i] * a.alpha + a.beta * ((float)eh[i] + (float)el[i]);
     }
     if constexpr (LAST) {
         if (!mine || r >= a.rows) return;
-        write_some<TO>(a, blockIdx.z * a.stride_o + (int64_t)r * a.ldo + c, (int)min(a.cols - c, (int64_t)4), v);
+        write_some<TO>(a, matrix * a.stride_o + (int64_t)r * a.ldo + c, (int)min(a.cols - c, (int64_t)4), v);
     } else {
         if (mine) store_parts(a.D + base + (int64_t)r * a.ldd + place(c), v);
         if (a.symmetric && bi == bj) return;  // (the tile holds both halves)
@@ -986,7 +1028,7 @@ int exponent_for(double bound)
 
 // ---- the call ----------------------------------------------------------------------------------------
 
-// How a product is cut: tiles of 32 (gp_ns_product_small), 64, 128, 128 x 256, 192 or 256, and how many workgroups sum up a tile of 64 or 128,
+// How a product is cut: tiles of 32 (gp_ns_product_small), 64, 128, 128 x 256, 192 or 256, and how many workgroups sum up a tile of 32 to 128,
 // a part of the columns each (larger tiles' sums take longer to hand over than that saves).  The cut of the least time by what
 // its parts take, in us as measured: a step of 32 columns where few compute units are at work and where all are (power is what
 // the large ones run out of), a tile's end, and for shared tiles the hand-over and its share of every workgroup's.  us a launch,
@@ -994,7 +1036,8 @@ int exponent_for(double bound)
 //     m x n, K                    32             64               128         128 x 256     192          256
 //    256 x 256, 256            4.9 / 4.9      6.2 / 6.5        11 / 10
 //    640 x 640, 640 (A A)      7.5 / 8.0      9.0 / 9.9        15 / 18
-//    256 x 4096, X X^T          31 / 30       14 / 13 (8)      25 / 24 (8)
+//    256 x 4096, X X^T          31 / 30       34 / 35          67 / 67
+//    the same, shared         11 / 11 (6)     14 / 13 (8)      25 / 24 (8)
 //    704 x 2048, X X^T          17 / 17       14 / 13 (3)      22 / 22 (4)
 //    704 x 4096, update                       27 / 26          24 / 24
 //   1024 x 1024, 1024           31 / 32       15 / 15          19 / 24                    44 / 48      59 / 79
@@ -1019,6 +1062,10 @@ Cut choose_cut(int64_t m, int64_t n, int64_t k, bool symmetric, int64_t count)
     Cut best{32, 32, tiles(32, 32), 1, 1e30};
     const int64_t rounds = (best.tiles + kUnits - 1) / kUnits;  // workgroups that share a compute unit
     if (rounds <= 4) best.us = 2.4 + 0.8 * (double)rounds + (0.02 + 0.195 * (double)rounds) * (double)steps;
+    for (int64_t parts = 2; parts * best.tiles <= kUnits && 8 * parts <= steps; ++parts) {
+        const double us = 3.2 + 0.215 * (double)((steps + parts - 1) / parts) + 1.5 + 0.18 * (double)parts;
+        if (us < best.us) best.parts = (int)parts, best.us = us;
+    }
     struct Kind {
         int bm, bn;
         double few, all, finish, hand_over, share;
@@ -1126,8 +1173,10 @@ gp_status launch_product(Product a, const Cut& cut, int64_t count, hipStream_t s
     if (bm == 64) return launch_tiles<64, 64, 2, 2, 4, TO, LAST>(a, stream);
     profile_begin("gp_ns_product", stream);
     const int even = a.tiles_n % 2 == 0;
-    const dim3 grid(a.tiles_n + (a.symmetric ? even : 0), a.symmetric ? (a.tiles_n + 1) / 2 : a.tiles_m, (unsigned)count);
-    hipLaunchKernelGGL((gp_ns_product_small<TO, LAST>), grid, dim3(64 * kSmallWaves), 0, stream, a);
+    const dim3 grid(a.tiles_n + (a.symmetric ? even : 0), a.symmetric ? (a.tiles_n + 1) / 2 : a.tiles_m, (unsigned)(count * a.parts));
+    if constexpr (!LAST)  // (the last product has too few columns for its tiles to be shared)
+        if (a.parts > 1) hipLaunchKernelGGL((gp_ns_product_small<TO, false, true>), grid, dim3(64 * kSmallWaves), 0, stream, a);
+    if (LAST || a.parts == 1) hipLaunchKernelGGL((gp_ns_product_small<TO, LAST, false>), grid, dim3(64 * kSmallWaves), 0, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     return GP_OK;
