@@ -210,25 +210,28 @@ __global__ __launch_bounds__(kThreads) void gp_ns_start(Update u, const double* 
     const int64_t z = blockIdx.z;
     const T* const G = (const T*)u.G + z * u.stride_g;
     const int64_t r0 = (int64_t)blockIdx.y * kTile + (threadIdx.x >> 4) * 4, c0 = (int64_t)blockIdx.x * kTile + (threadIdx.x & 15) * 4;
-    float v[4][4];
+    float v[4][4], m[4][4];
+    int count[4];
+    const double mine = partial[z * kNormBlocks + threadIdx.x];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+        const int64_t r = r0 + i;
+        count[i] = r < u.rows ? (int)max((int64_t)0, min(u.cols - c0, (int64_t)4)) : 0;
+        load_some(G + (count[i] ? r * u.ldg + c0 : 0), u.M && !u.nesterov ? 0 : count[i], v[i]);
+        if (u.M) load_some(u.M_out + (count[i] ? z * u.stride_m + r * u.ldm + c0 : 0), count[i], m[i]);
+    }
+    if (u.M)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t r = r0 + i, c = c0 + j;
-            v[i][j] = r < u.rows && c < u.cols ? (!u.M || u.nesterov ? widen(G[r * u.ldg + c]) : 0.0f) : 0.0f;
-            if (u.M && r < u.rows && c < u.cols) {
-                const float m = u.M_out[z * u.stride_m + r * u.ldm + c];
-                v[i][j] = u.nesterov ? v[i][j] + u.mu * m : m;
-            }
-        }
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i][j] = u.nesterov ? v[i][j] + u.mu * m[i][j] : m[i][j];
     static_assert(kNormBlocks == kThreads, "one partial sum per thread");
-    const double norm = sqrt(block_sum<kThreads>(partial[z * kNormBlocks + threadIdx.x], part));
+    const double norm = sqrt(block_sum<kThreads>(mine, part));
     const double factor = (double)scale / (norm + (double)eps);  // (it, or its inverse, may be beyond fp32)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[i][j] = r0 + i < u.rows && c0 + j < u.cols ? (float)((double)v[i][j] * factor) : 0.0f;
+        for (int j = 0; j < 4; ++j) v[i][j] = j < count[i] ? (float)((double)v[i][j] * factor) : 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float t[4] = {v[0][i], v[1][i], v[2][i], v[3][i]};
