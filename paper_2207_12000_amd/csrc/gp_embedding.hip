@@ -448,6 +448,7 @@ struct GradArgs {
     int64_t ldt;
     int accumulate;
     float* carry;  // two partial rows of nvec vectors per tile: of the run that came in, of the run that goes on
+    int64_t gap;   // rows (gap_rows)
 };
 
 // the finished sums of one vector of one row
@@ -474,8 +475,11 @@ __device__ __forceinline__ void finish(const GradArgs& a, int64_t v, int c, cons
     }
 }
 
-// rows of zeros: those of a gap in the tokens that is at most kGap rows long are written beside the run behind it, others by gp_join_tiles
-constexpr int64_t kGap = 256;
+// Rows of zeros: those of a gap in the tokens that is at most `gap` rows long are written beside the run behind it, others by gp_join_tiles.
+// A lane that writes a gap does so row after row, so that long ones are left to the others where there are many (gaps of up to 256 and up to
+// 32 rows, us: 921 tokens in 193 k rows of 64 39 / 24, 751 in 391 k 48 / 28, 10 k in 1 M rows of 100 133 / 119, 100 k in 2.4 M rows of
+// 64 185 / 177); where the mean gap is shorter than 16 rows, looking for them costs as much or more (100 k in 1 M 146 / 156).
+int64_t gap_rows(int64_t N, int64_t V) { return V > 16 * N ? 32 : 256; }
 
 // G lanes walk one stretch of a.tile / kGroups places, a lane holds one vector of the sums; the workgroup's stretches are one tile.  A run
 // that goes on from stretch to stretch is put together by the lanes in whose stretch it begins (or, where it came into the tile, by
@@ -496,7 +500,7 @@ __global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
 #pragma unroll
     for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
     auto fill_gap = [&](int64_t before, int64_t token) {
-        if (a.accumulate || token >= a.V || token - before > kGap + 1) return;
+        if (a.accumulate || token >= a.V || token - before > a.gap + 1) return;
         float zero[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) zero[i] = 0.0f;
@@ -611,19 +615,19 @@ __global__ __launch_bounds__(kThreads) void gp_zero_table(GradArgs a)
     zero_rows<TO>(a, min(r0, a.V), min(r0 + per, a.V), threadIdx.x & 63);
 }
 
-// Wavefronts behind the tiles' workgroups look after kGap rows each: a gap of more than kGap rows, or one before the first token or behind
+// Wavefronts behind the tiles' workgroups look after a.gap rows each: a gap of more rows than that, or one before the first token or behind
 // the last, covers at most the rows up to the first token among them and those behind the last.
 template <typename TO>
 __device__ __forceinline__ void fill_long_gaps(const GradArgs& a, int64_t chunk, int lane)
 {
-    const int64_t r0 = chunk * kGap, r1 = min(r0 + kGap, a.V);
+    const int64_t r0 = chunk * a.gap, r1 = min(r0 + a.gap, a.V);
     if (r0 >= a.V) return;
     const int64_t p = first_not_below(a.keys, a.N, r0, lane), q = first_not_below(a.keys, a.N, r1, lane);
     const int64_t before = p > 0 ? (int64_t)(a.keys[p - 1] >> 32) : -1, first = p < a.N ? min((int64_t)(a.keys[p] >> 32), a.V) : a.V;
-    if (p == 0 || first == a.V || first - before > kGap + 1) zero_rows<TO>(a, r0, min(first, r1), lane);
+    if (p == 0 || first == a.V || first - before > a.gap + 1) zero_rows<TO>(a, r0, min(first, r1), lane);
     if (first >= r1) return;
     const int64_t last = (int64_t)(a.keys[q - 1] >> 32), next = q < a.N ? min((int64_t)(a.keys[q] >> 32), a.V) : a.V;
-    if (next == a.V || next - last > kGap + 1) zero_rows<TO>(a, last + 1, r1, lane);
+    if (next == a.V || next - last > a.gap + 1) zero_rows<TO>(a, last + 1, r1, lane);
 }
 
 // Runs that go on into other tiles.  G lanes look at one tile: where such a run begins in it, its partial rows are added up in tile order;
@@ -729,7 +733,7 @@ gp_status launch_sums(GradArgs a, hipStream_t stream)
     hipLaunchKernelGGL((gp_sum_tiles<TG, TO, VEC, G>), dim3((unsigned)a.tiles, ny), dim3(kThreads), 0, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
-    const int64_t fills = a.accumulate ? 0 : ((a.V + kGap - 1) / kGap + kThreads / 64 - 1) / (kThreads / 64);
+    const int64_t fills = a.accumulate ? 0 : ((a.V + a.gap - 1) / a.gap + kThreads / 64 - 1) / (kThreads / 64);
     if (a.tiles > 1 || fills > 0) {
         profile_begin("gp_join_tiles", stream);
         const int64_t tile_blocks = (a.tiles + per - 1) / per;
@@ -914,7 +918,7 @@ gp_status embedding_grad(const void* tokens, gp_index index, int64_t N, const vo
     if (st != GP_OK) return st;
     GradArgs a{};
     a.keys = sorted, a.N = N, a.V = V, a.tile = stretch_length(N), a.up = up, a.ldg = ldg, a.d = d,
-    a.scale = scale, a.out = out, a.ldt = ldt, a.accumulate = accumulate != 0, a.carry = (float*)(ws + l.carry);
+    a.scale = scale, a.out = out, a.ldt = ldt, a.accumulate = accumulate != 0, a.carry = (float*)(ws + l.carry), a.gap = gap_rows(N, V);
     if (dtype == GP_F32) return out_dtype == GP_F32 ? launch_sums<float, float>(a, stream) : launch_sums<float, bf16_t>(a, stream);
     return out_dtype == GP_F32 ? launch_sums<bf16_t, float>(a, stream) : launch_sums<bf16_t, bf16_t>(a, stream);
 }

@@ -502,3 +502,21 @@ def test_long_gaps_between_tokens_are_zero(kind):
         want = torch.zeros(V, d, device="cuda")
         want[tokens.long()] = 1.0
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("gap", [15, 16, 17, 31, 32, 33, 34, 63, 65, 255, 256, 257, 258])
+@pytest.mark.parametrize("often", [1, 20])
+def test_gaps_around_their_limits_are_zero(gap, often):
+    """Few tokens for the table's rows and, each 20 times over, many: gaps of 32 and of 256 rows go either way."""
+    import torch
+    V, d = 2000, 6
+    for first in (0, 1, gap):
+        named = torch.arange(first, V, gap + 1)
+        tokens = named.to(torch.int32).repeat(often).cuda()
+        up = torch.ones(tokens.numel(), d, device="cuda")
+        for out_dtype in (torch.float32, torch.bfloat16):
+            out = torch.full((V, d), float("nan"), device="cuda", dtype=out_dtype)
+            gp.embedding_grad_tensors(tokens, up, V, out=out)
+            want = torch.zeros(V, d, device="cuda", dtype=out_dtype)
+            want[named.cuda()] = float(often)
+            assert torch.equal(out, want)
