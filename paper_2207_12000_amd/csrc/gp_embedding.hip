@@ -484,18 +484,16 @@ int64_t gap_rows(int64_t N, int64_t V) { return V > 16 * N ? 32 : 256; }
 // G lanes walk one stretch of a.tile / kGroups places, a lane holds one vector of the sums; the workgroup's stretches are one tile.  A run
 // that goes on from stretch to stretch is put together by the lanes in whose stretch it begins (or, where it came into the tile, by
 // the first ones), from what the others leave in LDS; only what leaves the tile goes through memory.
-template <typename TG, typename TO, int VEC, int G>
-__global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
+template <typename TG, typename TO, int VEC, int G, int THREADS>
+__device__ __forceinline__ void sum_tile(const GradArgs& a, const uint64_t* keys, int64_t tile, float (*head)[VEC], int* passes)
 {
-    constexpr int U = 8, kGroups = kThreads / G;
-    __shared__ float head[kThreads][VEC];   // what a stretch adds to the run that comes into it
-    __shared__ int passes[kGroups];         // that run goes on behind the stretch
+    constexpr int U = 8, kGroups = THREADS / G;
     const int g = threadIdx.x / G, c = blockIdx.y * G + threadIdx.x % G;
-    const int64_t stretch = a.tile / kGroups, lo = blockIdx.x * a.tile + g * stretch, hi = min(lo + stretch, a.N);
+    const int64_t stretch = a.tile / kGroups, lo = tile * a.tile + g * stretch, hi = min(lo + stretch, a.N);
     const bool active = c < a.nvec;
     const int col = min(min(c, a.nvec - 1) * VEC, a.d - VEC);
     const TG* const up = (const TG*)a.up + col;
-    float* const carry = a.carry + (2 * (int64_t)blockIdx.x * a.nvec + c) * VEC;  // of the run that came in; the other's is one row on
+    float* const carry = a.carry + (2 * tile * a.nvec + c) * VEC;  // of the run that came in; the other's is one row on
     float acc[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
@@ -509,15 +507,15 @@ __global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
     int64_t cur = a.V;
     bool came_in = false, open = false;
     if (lo < a.N && active) {
-        cur = (int64_t)(a.keys[lo] >> 32);
+        cur = (int64_t)(keys[lo] >> 32);
         if (lo > 0) {
-            const int64_t before = (int64_t)(a.keys[lo - 1] >> 32);
+            const int64_t before = (int64_t)(keys[lo - 1] >> 32);
             came_in = before == cur;
             if (!came_in) fill_gap(before, cur);
         }
         uint64_t key[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) key[u] = lo + u < hi ? a.keys[lo + u] : ~UINT64_C(0);
+        for (int u = 0; u < U; ++u) key[u] = lo + u < hi ? keys[lo + u] : ~UINT64_C(0);
         for (int64_t p = lo; p < hi; p += U) {
             typename Vec<TG, VEC>::type v[U];  // (widened when they are added: registers decide how many wavefronts there are)
             uint64_t next[U];                  // (asked for beside this step's rows, not behind them)
@@ -527,7 +525,7 @@ __global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
                 if ((int64_t)(key[u] >> 32) < a.V) v[u] = *reinterpret_cast<const typename Vec<TG, VEC>::type*>(up + (int64_t)(key[u] & 0xFFFFFFFFu) * a.ldg);
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u) next[u] = p + U + u < hi ? a.keys[p + U + u] : ~UINT64_C(0);
+            for (int u = 0; u < U; ++u) next[u] = p + U + u < hi ? keys[p + U + u] : ~UINT64_C(0);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (p + u >= hi) break;
@@ -550,7 +548,7 @@ __global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
 #pragma unroll
             for (int u = 0; u < U; ++u) key[u] = next[u];
         }
-        open = cur < a.V && hi < a.N && (int64_t)(a.keys[hi] >> 32) == cur;
+        open = cur < a.V && hi < a.N && (int64_t)(keys[hi] >> 32) == cur;
         if (came_in && g > 0) {
             store_vec<float, VEC>(head[threadIdx.x], acc);
             if (threadIdx.x % G == 0) passes[g] = open;
@@ -575,6 +573,14 @@ __global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
         store_vec<float, VEC>(carry + (int64_t)a.nvec * VEC, acc);
     else
         finish<TO, VEC>(a, cur, c, acc);
+}
+
+template <typename TG, typename TO, int VEC, int G>
+__global__ __launch_bounds__(kThreads) void gp_sum_tiles(GradArgs a)
+{
+    __shared__ float head[kThreads][VEC];    // what a stretch adds to the run that comes into it
+    __shared__ int passes[kThreads / G];     // that run goes on behind the stretch
+    sum_tile<TG, TO, VEC, G, kThreads>(a, a.keys, blockIdx.x, head, passes);
 }
 
 // the first place of the sorted list whose token is not below v, by all lanes of a wavefront (64 probes a round)
@@ -613,6 +619,116 @@ __global__ __launch_bounds__(kThreads) void gp_zero_table(GradArgs a)
     constexpr int kWaves = kThreads / 64;
     const int64_t per = (a.V + gridDim.x * kWaves - 1) / (gridDim.x * kWaves), r0 = ((int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6)) * per;
     zero_rows<TO>(a, min(r0, a.V), min(r0 + per, a.V), threadIdx.x & 63);
+}
+
+// Short lists in one launch: a workgroup has a range of the table's rows.  It reads all tokens, keeps those of its rows in LDS in their order,
+// sorts them there by row, writes zeros to its rows without a token and sums up the others as one tile.
+// Three dependent launches (places by counting, sums, joins) take longer the shorter the list is: us on the GPU, three launches / one,
+// 500 x 64 into 300 rows 11.0 / 5.9, 4096 x 128 into 1000 16.6 / 7.4, the same by Zipf's law 17.7 / 16.2, into 60 rows 16.2 / 9.0, into
+// 100 k 24.6 / 14.2.  But a token's rows are one workgroup's: 4096 x 128 of one token take 19 / 33, so lists of more than 128 tokens per
+// row of the table, or of more than a million elements (4096 x 602: 17 / 17, of one token 36 / 84), go the other way.
+constexpr int kShortThreads = 1024, kShortBlocks = 256;
+constexpr int64_t kShortest = 4096, kShortElements = 1 << 20, kShortPerRow = 128;
+constexpr int kCounted = 128;  // tokens of a workgroup up to which each one's place is counted; beyond, they are sorted bit by bit of the row
+
+template <typename TG, typename TO, int VEC, int G>
+__global__ __launch_bounds__(kShortThreads) void gp_sum_short(GradArgs a, const void* tokens, int wide)
+{
+    constexpr int kGroups = kShortThreads / G, kLoads = kShortest / kShortThreads, kWaves = kShortThreads / 64;
+    static_assert(kLoads * kWaves <= 64, "a lane has one count");
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int passes[kGroups];
+    __shared__ int counts[2][kLoads * kWaves];
+    float(*const head)[VEC] = (float(*)[VEC])lds;
+    uint64_t* const keys = (uint64_t*)(lds + sizeof(float) * VEC * kShortThreads);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t r0 = a.V * blockIdx.x / gridDim.x, r1 = a.V * (blockIdx.x + 1) / gridDim.x;
+    int64_t token[kLoads];
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+        const int64_t i = threadIdx.x + k * kShortThreads;
+        token[k] = i >= a.N ? -1 : wide ? ((const int64_t*)tokens)[i] : (int64_t)((const int32_t*)tokens)[i];
+    }
+    // `members` of the items (one per thread and k, their order) to the front, the others behind them, both in order; returns how many
+    auto divide = [&](const bool (&member)[kLoads], const bool (&other)[kLoads], const uint64_t (&item)[kLoads], int loads) {
+        uint64_t in[kLoads], out[kLoads];
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k)
+            if (k < loads) {
+                in[k] = __ballot(member[k]), out[k] = __ballot(other[k]);
+                if (lane == 0) counts[0][k * kWaves + wave] = __popcll(in[k]), counts[1][k * kWaves + wave] = __popcll(out[k]);
+            }
+        __syncthreads();  // (and every item has been read)
+        const int slots = loads * kWaves;
+        int x = lane < slots ? counts[0][lane] : 0, y = lane < slots ? counts[1][lane] : 0;
+#pragma unroll
+        for (int step = 1; step < 64; step *= 2) {
+            const int xs = __shfl_up(x, step), ys = __shfl_up(y, step);
+            if (lane >= step) x += xs, y += ys;
+        }
+        const int members = __shfl(x, 63);
+        const uint64_t below = (UINT64_C(1) << lane) - 1;
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k)
+            if (k < loads) {
+                const int slot = k * kWaves + wave;
+                const int x0 = __shfl(x, slot) - __popcll(in[k]), y0 = members + __shfl(y, slot) - __popcll(out[k]);
+                if (member[k]) keys[x0 + __popcll(in[k] & below)] = item[k];
+                if (other[k]) keys[y0 + __popcll(out[k] & below)] = item[k];
+            }
+        __syncthreads();
+        return members;
+    };
+    bool member[kLoads], other[kLoads];
+    uint64_t item[kLoads];
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+        member[k] = token[k] >= r0 && token[k] < r1, other[k] = false;
+        item[k] = (uint64_t)token[k] << 32 | (uint64_t)(threadIdx.x + k * kShortThreads);
+    }
+    const int count = divide(member, other, item, (int)((a.N + kShortThreads - 1) / kShortThreads));
+    if (count <= kCounted) {  // an item's place: how many are smaller
+        int place = 0;
+        const uint64_t x = threadIdx.x < count ? keys[threadIdx.x] : 0;
+        if (threadIdx.x < count)
+            for (int i = 0; i < count; ++i) place += keys[i] < x;
+        __syncthreads();
+        if (threadIdx.x < count) keys[place] = x;
+        __syncthreads();
+    } else {  // bit by bit of the row
+        for (int bit = 0; (r1 - r0 - 1) >> bit; ++bit) {
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) {
+                const int i = threadIdx.x + k * kShortThreads;
+                const bool here = i < count;
+                item[k] = here ? keys[i] : 0;
+                const bool one = (((int64_t)(item[k] >> 32) - r0) >> bit) & 1;
+                member[k] = here && !one, other[k] = here && one;
+            }
+            divide(member, other, item, (count + kShortThreads - 1) / kShortThreads);
+        }
+    }
+    if (!a.accumulate && blockIdx.y == 0)
+        for (int64_t r = r0 + wave * 64; r < r1; r += kShortThreads) {
+            int at = 0, n = count;  // the first place whose token is not below this lane's row
+            while (n > 0) {
+                const int half = n / 2;
+                const bool below = (int64_t)(keys[at + half] >> 32) < r + lane;
+                at = below ? at + half + 1 : at, n = below ? n - half - 1 : half;
+            }
+            uint64_t empty = __ballot(r + lane < r1 && !(at < count && (int64_t)(keys[at] >> 32) == r + lane));
+            while (empty) {
+                const int first = __builtin_ctzll(empty);
+                const uint64_t rest = ~(empty >> first);
+                const int rows = rest ? __builtin_ctzll(rest) : 64;  // (all 64: nothing is shifted in)
+                zero_rows<TO>(a, r + first, r + first + rows, lane);
+                empty = first + rows >= 64 ? 0 : empty >> (first + rows) << (first + rows);
+            }
+        }
+    if (count == 0) return;
+    GradArgs mine = a;  // (no gap is left to be filled beside a run)
+    mine.N = count, mine.tile = (count + kGroups - 1) / kGroups * kGroups, mine.gap = 0;
+    sum_tile<TG, TO, VEC, G, kShortThreads>(mine, keys, 0, head, passes);
 }
 
 // Wavefronts behind the tiles' workgroups look after a.gap rows each: a gap of more rows than that, or one before the first token or behind
@@ -724,9 +840,19 @@ __global__ __launch_bounds__(kThreads) void gp_join_tiles(GradArgs a, int64_t ti
 }
 
 template <typename TG, typename TO, int VEC, int G>
-gp_status launch_sums(GradArgs a, hipStream_t stream)
+gp_status launch_sums(GradArgs a, const void* tokens, int wide, hipStream_t stream)
 {
     const unsigned ny = (unsigned)((a.nvec + G - 1) / G);
+    if (tokens) {
+        const size_t lds = sizeof(float) * VEC * kShortThreads + 8 * (size_t)a.N;
+        gp_status st = raise_lds<&gp_sum_short<TG, TO, VEC, G>>(sizeof(float) * VEC * kShortThreads + 8 * kShortest);
+        if (st != GP_OK) return st;
+        profile_begin("gp_sum_short", stream);
+        hipLaunchKernelGGL((gp_sum_short<TG, TO, VEC, G>), dim3((unsigned)std::min<int64_t>(a.V, kShortBlocks), ny), dim3(kShortThreads), lds, stream, a, tokens, wide);
+        profile_end(stream);
+        GP_HIP(hipGetLastError());
+        return GP_OK;
+    }
     constexpr int per = kThreads / G;
     a.tile *= per, a.tiles = (a.N + a.tile - 1) / a.tile;
     profile_begin("gp_sum_tiles", stream);
@@ -744,19 +870,19 @@ gp_status launch_sums(GradArgs a, hipStream_t stream)
     return GP_OK;
 }
 template <typename TG, typename TO, int VEC>
-gp_status launch_sums(GradArgs a, hipStream_t stream)
+gp_status launch_sums(GradArgs a, const void* tokens, int wide, hipStream_t stream)
 {
     a.nvec = (a.d + VEC - 1) / VEC;
-    if (a.nvec <= 8) return launch_sums<TG, TO, VEC, 8>(a, stream);
-    if (a.nvec <= 16) return launch_sums<TG, TO, VEC, 16>(a, stream);
-    if (a.nvec <= 32) return launch_sums<TG, TO, VEC, 32>(a, stream);
-    return launch_sums<TG, TO, VEC, 64>(a, stream);
+    if (a.nvec <= 8) return launch_sums<TG, TO, VEC, 8>(a, tokens, wide, stream);
+    if (a.nvec <= 16) return launch_sums<TG, TO, VEC, 16>(a, tokens, wide, stream);
+    if (a.nvec <= 32) return launch_sums<TG, TO, VEC, 32>(a, tokens, wide, stream);
+    return launch_sums<TG, TO, VEC, 64>(a, tokens, wide, stream);
 }
 template <typename TG, typename TO>
-gp_status launch_sums(const GradArgs& a, hipStream_t stream)
+gp_status launch_sums(const GradArgs& a, const void* tokens, int wide, hipStream_t stream)
 {
     constexpr int VEC = sizeof(TG) == 2 ? 8 : 4;
-    return a.d >= VEC ? launch_sums<TG, TO, VEC>(a, stream) : launch_sums<TG, TO, 1>(a, stream);
+    return a.d >= VEC ? launch_sums<TG, TO, VEC>(a, tokens, wide, stream) : launch_sums<TG, TO, 1>(a, tokens, wide, stream);
 }
 
 // Stretches: equal lengths; enough of them to fill the chip, few enough that the partial rows of one token are added up fast.
@@ -913,14 +1039,18 @@ gp_status embedding_grad(const void* tokens, gp_index index, int64_t N, const vo
         return GP_OK;
     }
     char* const ws = (char*)workspace;
-    const uint64_t* sorted = nullptr;
-    gp_status st = sort_tokens(tokens, (int)(index == GP_I64), N, V, ws, l, stream, &sorted);
-    if (st != GP_OK) return st;
     GradArgs a{};
-    a.keys = sorted, a.N = N, a.V = V, a.tile = stretch_length(N), a.up = up, a.ldg = ldg, a.d = d,
-    a.scale = scale, a.out = out, a.ldt = ldt, a.accumulate = accumulate != 0, a.carry = (float*)(ws + l.carry), a.gap = gap_rows(N, V);
-    if (dtype == GP_F32) return out_dtype == GP_F32 ? launch_sums<float, float>(a, stream) : launch_sums<float, bf16_t>(a, stream);
-    return out_dtype == GP_F32 ? launch_sums<bf16_t, float>(a, stream) : launch_sums<bf16_t, bf16_t>(a, stream);
+    a.N = N, a.V = V, a.tile = stretch_length(N), a.up = up, a.ldg = ldg, a.d = d, a.scale = scale, a.out = out, a.ldt = ldt,
+    a.accumulate = accumulate != 0, a.carry = (float*)(ws + l.carry), a.gap = gap_rows(N, V);
+    const int wide = index == GP_I64;
+    const bool in_one = N <= kShortest && N * d <= kShortElements && N <= kShortPerRow * V;
+    if (!in_one) {
+        gp_status st = sort_tokens(tokens, wide, N, V, ws, l, stream, &a.keys);
+        if (st != GP_OK) return st;
+    }
+    const void* const unsorted = in_one ? tokens : nullptr;
+    if (dtype == GP_F32) return out_dtype == GP_F32 ? launch_sums<float, float>(a, unsorted, wide, stream) : launch_sums<float, bf16_t>(a, unsorted, wide, stream);
+    return out_dtype == GP_F32 ? launch_sums<bf16_t, float>(a, unsorted, wide, stream) : launch_sums<bf16_t, bf16_t>(a, unsorted, wide, stream);
 }
 
 }  // namespace

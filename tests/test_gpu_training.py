@@ -520,3 +520,33 @@ def test_gaps_around_their_limits_are_zero(gap, often):
             want = torch.zeros(V, d, device="cuda", dtype=out_dtype)
             want[named.cuda()] = float(often)
             assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("N,V,d,low,high", [(4096, 1000, 7, 0, 1000), (4096, 32, 33, 0, 32), (4096, 31, 33, 0, 31), (4096, 1000, 3, 7, 8),
+                                            (4000, 1_000_000, 4, 3906, 7812), (4000, 1_000_000, 4, 0, 3000), (129, 1000, 5, 8, 12),
+                                            (128, 1000, 5, 8, 12), (1, 1, 1, 0, 1), (1, 300_000, 16, 299_999, 300_000), (3, 5, 602, 0, 5),
+                                            (4096, 700, 256, 0, 700), (4096, 700, 257, 0, 700), (4097, 700, 9, 0, 700), (1025, 257, 8, 0, 257)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_gradient_of_short_lists(N, V, d, low, high, dtype):
+    """Around the limits of what goes in one launch, spread over the table or all in one part of it, with tokens of no row among them."""
+    import torch
+    rng = np.random.default_rng(N * 31 + V + d)
+    named = rng.integers(low, high, size=N)
+    up = torch.from_numpy(rng.normal(size=(N, d)).astype(np.float32)).to(getattr(torch, dtype)).cuda()
+    for index in (torch.int32, torch.int64):
+        for absent in (0.0, 0.2):
+            tokens = torch.from_numpy(np.where(rng.random(N) < absent, rng.choice([-1, V, -(2 ** 31), 2 ** 31 - 1], size=N), named)).to(index).cuda()
+            out = torch.full((V, d), float("nan"), device="cuda")
+            gp.embedding_grad_tensors(tokens, up, V, out=out)
+            check_gradient(out, tokens, up, V, 1.0)
+            again = torch.empty_like(out)
+            gp.embedding_grad_tensors(tokens, up, V, out=again)
+            assert torch.equal(out, again)
+            start = torch.from_numpy(rng.integers(-4, 5, size=(V, d)).astype(np.float32)).cuda()
+            kept = start.clone()
+            gp.embedding_grad_tensors(tokens, up, V, out=kept, accumulate=True)
+            known = (tokens >= 0) & (tokens < V)
+            rows = torch.zeros(V, dtype=torch.bool, device="cuda")
+            rows[tokens[known].long()] = True
+            assert torch.equal(kept[~rows], start[~rows])
+            assert torch.equal(kept[rows], start[rows] + out[rows])
