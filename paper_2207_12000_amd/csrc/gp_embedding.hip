@@ -8,14 +8,15 @@
 // length whatever the tokens are, so a token that half of the positions name costs no more than any other; a token's
 // run that a tile boundary cuts leaves one partial row in every tile it touches, and a second launch adds these up in
 // tile order.  Every row of the gradient is written once: rows without a token get their zeros beside their neighbours.  Sums are held in
-// fp32 and rounded once; what atomics there are count whole numbers, so the same inputs give the same bits.
+// fp32 and rounded once; what atomics there are count whole numbers, so the same inputs give the same bits.  Short lists take one launch
+// instead, in which a workgroup has a range of the table's rows and all tokens that name them.
 //
 // What bounds it, and us measured.  Lookups of many rows: memory (2.45 M rows of 256 bf16 out of as many, 465 us, 1.25 GB written
 // and as much asked for; 507,001 fp32 rows of 100 to bf16, 28 us); of few rows the launch (4,096 rows of 128, 4 us on the GPU).  Gradients of
 // many rows: the gathered rows, each of which touches up to a 128-byte line more than it fills (2.45 M fp32 rows of 100 into as many,
 // 563 - 590 us: sums 446 - 475, sort 106, joins and long gaps 17); of half a million the sort's four launches and the sums alike
-// (bf16 rows of 100 into 32,768 rows by Zipf's law, 76 us: sort 37, sums 30, joins 9); of few the chain of three launches (4,096
-// rows of 128 into 10,000, 18 us: ranks 8, sums 5, joins 4).
+// (bf16 rows of 100 into 32,768 rows by Zipf's law, 76 us: sort 37, sums 30, joins 9); of a few thousand one launch's chain of loads, places and
+// sums, and the call (4,096 rows of 128 into 10,000, 12 us, 10 of them on the GPU; gp_sum_short).
 #include <algorithm>
 #include <type_traits>
 
