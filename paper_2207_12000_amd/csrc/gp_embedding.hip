@@ -709,15 +709,16 @@ __global__ __launch_bounds__(kShortThreads) void gp_sum_short(GradArgs a, const 
             divide(member, other, item, (count + kShortThreads - 1) / kShortThreads);
         }
     }
+    const int share = (int)min((r1 - r0 + kWaves - 1) / kWaves, (int64_t)64);  // rows that a wavefront looks after at a time
     if (!a.accumulate && blockIdx.y == 0)
-        for (int64_t r = r0 + wave * 64; r < r1; r += kShortThreads) {
+        for (int64_t r = r0 + wave * share; r < r1; r += kWaves * share) {
             int at = 0, n = count;  // the first place whose token is not below this lane's row
             while (n > 0) {
                 const int half = n / 2;
                 const bool below = (int64_t)(keys[at + half] >> 32) < r + lane;
                 at = below ? at + half + 1 : at, n = below ? n - half - 1 : half;
             }
-            uint64_t empty = __ballot(r + lane < r1 && !(at < count && (int64_t)(keys[at] >> 32) == r + lane));
+            uint64_t empty = __ballot(lane < share && r + lane < r1 && !(at < count && (int64_t)(keys[at] >> 32) == r + lane));
             while (empty) {
                 const int first = __builtin_ctzll(empty);
                 const uint64_t rest = ~(empty >> first);
