@@ -16,7 +16,7 @@
 // many rows: the gathered rows, each of which touches up to a 128-byte line more than it fills (2.45 M fp32 rows of 100 into as many,
 // 563 - 590 us: sums 446 - 475, sort 106, joins and long gaps 17); of half a million the sort's four launches and the sums alike
 // (bf16 rows of 100 into 32,768 rows by Zipf's law, 76 us: sort 37, sums 30, joins 9); of a few thousand one launch's chain of loads, places and
-// sums, and the call (4,096 rows of 128 into 10,000, 12 us, 10 of them on the GPU; gp_sum_short).
+// sums, and the call (4,096 rows of 128 into 10,000, 12 us, 8.5 of them on the GPU; gp_sum_short).
 #include <algorithm>
 #include <type_traits>
 
