@@ -141,13 +141,16 @@ __global__ __launch_bounds__(kThreads) void gp_embedding_rows(LookupArgs a)
     }
 }
 
+// A launch takes fewer than 2^32 threads; workgroups beyond these walk on through the rest.
+constexpr int64_t kMaxBlocks = 1 << 20;
+
 template <typename TI, typename TO, int VEC>
 gp_status launch_lookup(LookupArgs a, hipStream_t stream)
 {
     a.nvec = (a.d + VEC - 1) / VEC;
     const int64_t blocks = (a.N * a.nvec + 4 * kThreads - 1) / (4 * kThreads);
     profile_begin("gp_embedding_rows", stream);
-    hipLaunchKernelGGL((gp_embedding_rows<TI, TO, VEC>), dim3((unsigned)std::min<int64_t>(blocks, 1 << 30)), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((gp_embedding_rows<TI, TO, VEC>), dim3((unsigned)std::min(blocks, kMaxBlocks)), dim3(kThreads), 0, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     return GP_OK;

@@ -1,0 +1,34 @@
+"""What the training operators launch, seen without a GPU (tests/launches.py): sizes that the runtime takes, kernels that shapes reach."""
+import re
+import shutil
+
+import pytest
+
+import paper_2207_12000_amd as gp
+from launches import launches
+
+pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not found")
+
+P = 4096  # stands for an address
+
+
+def lookup(**kw):
+    a = dict(table_ptr=P, ldt=8, dtype=gp.GP_F32, V=10, d=8, tokens_ptr=P, index=gp.GP_I32, N=4, scale=1.0, out_ptr=P, ldo=8,
+             out_dtype=gp.GP_F32)
+    return "gp_embedding", {**a, **kw}
+
+
+def check_sizes(result):
+    """hipLaunchKernel takes fewer than 2^32 threads in each dimension, and 65535 workgroups in the second and third."""
+    assert result["status"] == gp.GP_OK and result["launches"]
+    for l in result["launches"]:
+        assert all(0 < g * b < 1 << 32 for g, b in zip(l["grid"], l["block"])), l
+        assert l["grid"][1] <= 65535 and l["grid"][2] <= 65535, l
+        assert l["block"][0] * l["block"][1] * l["block"][2] <= 1024, l
+
+
+@pytest.mark.parametrize("N", [1, 2 ** 30, 2 ** 34 - 1024, 2 ** 34 + 5, 2 ** 45])
+@pytest.mark.parametrize("d", [1, 8])
+def test_lookups_of_any_length_can_be_launched(N, d):
+    for dtype in (gp.GP_F32, gp.GP_BF16):
+        check_sizes(launches([lookup(N=N, d=d, dtype=dtype, out_dtype=dtype)])[0])
