@@ -736,13 +736,12 @@ __global__ __launch_bounds__(kShortThreads) void gp_sum_short(GradArgs a, const 
     sum_tile<TG, TO, VEC, G, kShortThreads>(mine, keys, 0, head, passes);
 }
 
-// Wavefronts behind the tiles' workgroups look after a.gap rows each: a gap of more rows than that, or one before the first token or behind
+// Wavefronts behind the tiles' workgroups look after a.gap rows each and walk on through the table: a gap of more rows than that, or one before the first token or behind
 // the last, covers at most the rows up to the first token among them and those behind the last.
 template <typename TO>
 __device__ __forceinline__ void fill_long_gaps(const GradArgs& a, int64_t chunk, int lane)
 {
     const int64_t r0 = chunk * a.gap, r1 = min(r0 + a.gap, a.V);
-    if (r0 >= a.V) return;
     const int64_t p = first_not_below(a.keys, a.N, r0, lane), q = first_not_below(a.keys, a.N, r1, lane);
     const int64_t before = p > 0 ? (int64_t)(a.keys[p - 1] >> 32) : -1, first = p < a.N ? min((int64_t)(a.keys[p] >> 32), a.V) : a.V;
     if (p == 0 || first == a.V || first - before > a.gap + 1) zero_rows<TO>(a, r0, min(first, r1), lane);
@@ -763,7 +762,10 @@ __global__ __launch_bounds__(kThreads) void gp_join_tiles(GradArgs a, int64_t ti
     __shared__ int64_t longer[kGroups];
     __shared__ int longer_count;
     if (blockIdx.x >= tile_blocks) {
-        if (blockIdx.y == 0) fill_long_gaps<TO>(a, (blockIdx.x - tile_blocks) * (kThreads / 64) + (threadIdx.x >> 6), threadIdx.x & 63);
+        constexpr int kWaves = kThreads / 64;
+        if (blockIdx.y > 0) return;
+        for (int64_t chunk = (blockIdx.x - tile_blocks) * kWaves + (threadIdx.x >> 6); chunk * a.gap < a.V; chunk += (gridDim.x - tile_blocks) * kWaves)
+            fill_long_gaps<TO>(a, chunk, threadIdx.x & 63);
         return;
     }
     if (threadIdx.x == 0) longer_count = 0;
@@ -864,7 +866,7 @@ gp_status launch_sums(GradArgs a, const void* tokens, int wide, hipStream_t stre
     hipLaunchKernelGGL((gp_sum_tiles<TG, TO, VEC, G>), dim3((unsigned)a.tiles, ny), dim3(kThreads), 0, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
-    const int64_t fills = a.accumulate ? 0 : ((a.V + a.gap - 1) / a.gap + kThreads / 64 - 1) / (kThreads / 64);
+    const int64_t fills = a.accumulate ? 0 : std::min(((a.V + a.gap - 1) / a.gap + kThreads / 64 - 1) / (kThreads / 64), kMaxBlocks);
     if (a.tiles > 1 || fills > 0) {
         profile_begin("gp_join_tiles", stream);
         const int64_t tile_blocks = (a.tiles + per - 1) / per;

@@ -22,3 +22,20 @@ def test_lookup_of_more_rows_than_the_workgroups_take_at_once():
     rows = torch.cat([table, torch.zeros(1, 1, dtype=torch.bfloat16, device="cuda")]).flatten()
     for first in range(0, N, 1 << 27):
         assert torch.equal(out[first:first + (1 << 27), 0], rows[tokens[first:first + (1 << 27)].long()])
+
+
+@pytest.mark.parametrize("N", [5000, 9000])
+def test_gaps_of_a_table_longer_than_the_workgroups_take_at_once(N):
+    """2^20 workgroups of four wavefronts of 32 rows, and some: every row of the gradient is written, those behind in a second round."""
+    import torch
+    V = 2 ** 27 + 1_000_003
+    place = torch.randint(0, V, (N,), device="cuda")
+    place[:4] = torch.tensor([0, 2 ** 27 - 1, 2 ** 27 + 40, V - 500_000], device="cuda")
+    place = place.unique()
+    tokens = place[torch.randint(0, place.numel(), (N,), device="cuda")]
+    up = torch.ones(N, 1, dtype=torch.bfloat16, device="cuda")
+    out = torch.full((V, 1), float("nan"), dtype=torch.bfloat16, device="cuda")
+    gp.embedding_grad_tensors(tokens.to(torch.int32), up, V, out=out)
+    named, count = tokens.unique(return_counts=True)
+    assert torch.equal(out[named, 0], count.bfloat16())
+    assert int(torch.count_nonzero(out)) == named.numel()      # (NaN would count)

@@ -18,6 +18,12 @@ def lookup(**kw):
     return "gp_embedding", {**a, **kw}
 
 
+def grad(**kw):
+    a = dict(tokens_ptr=P, index=gp.GP_I32, N=4, grad_ptr=P, ldg=8, dtype=gp.GP_F32, d=8, scale=1.0, V=10, table_grad_ptr=P, ldt=8,
+             out_dtype=gp.GP_F32, accumulate=False, workspace_ptr=P, workspace_bytes=1 << 50)
+    return "gp_embedding_grad", {**a, **kw}
+
+
 def check_sizes(result):
     """hipLaunchKernel takes fewer than 2^32 threads in each dimension, and 65535 workgroups in the second and third."""
     assert result["status"] == gp.GP_OK and result["launches"]
@@ -32,3 +38,10 @@ def check_sizes(result):
 def test_lookups_of_any_length_can_be_launched(N, d):
     for dtype in (gp.GP_F32, gp.GP_BF16):
         check_sizes(launches([lookup(N=N, d=d, dtype=dtype, out_dtype=dtype)])[0])
+
+
+@pytest.mark.parametrize("N", [0, 4097, 100_000, 2 ** 27, 2 ** 31 - 1])
+@pytest.mark.parametrize("V", [1, 2 ** 28, 2 ** 31 - 4000, 2 ** 31 - 1])
+def test_gradients_of_any_table_can_be_launched(N, V):
+    for dtype in (gp.GP_F32, gp.GP_BF16):
+        check_sizes(launches([grad(N=N, V=V, d=1, dtype=dtype, out_dtype=dtype)])[0])
