@@ -600,11 +600,9 @@ def embedding_grad_tensors(tokens, grad, V, scale=1.0, out=None, out_dtype=None,
     bytes or more, kept by the caller; without one the call takes its memory from torch."""
     import torch
     N, index, dtype = tokens.numel(), _index_type(tokens), _float_type(grad)
-    if grad.dim() < 2:
-        raise ValueError("grad must hold one row per token")
-    if grad.dim() > 2:
-        if tuple(grad.shape[:-1]) != tuple(tokens.shape) or not grad.is_contiguous():
-            raise ValueError("grad of more than two dimensions must be contiguous, of shape tokens.shape + (d,)")
+    if grad.dim() != 2:
+        if grad.dim() == 0 or tuple(grad.shape[:-1]) != tuple(tokens.shape) or not grad.is_contiguous():
+            raise ValueError("grad of other than two dimensions must be contiguous, of shape tokens.shape + (d,)")
         grad = grad.view(N, grad.shape[-1])
     if grad.shape[0] != N:
         raise ValueError("grad must hold one row per token")

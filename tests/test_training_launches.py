@@ -25,11 +25,10 @@ def grad(**kw):
 
 
 def check_sizes(result):
-    """hipLaunchKernel takes fewer than 2^32 threads in each dimension, and 65535 workgroups in the second and third."""
+    """hipLaunchKernel takes fewer than 2^32 threads in each dimension, 1024 to a workgroup."""
     assert result["status"] == gp.GP_OK and result["launches"]
     for l in result["launches"]:
         assert all(0 < g * b < 1 << 32 for g, b in zip(l["grid"], l["block"])), l
-        assert l["grid"][1] <= 65535 and l["grid"][2] <= 65535, l
         assert l["block"][0] * l["block"][1] * l["block"][2] <= 1024, l
 
 
