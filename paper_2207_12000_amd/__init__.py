@@ -570,6 +570,12 @@ def _workspace(workspace, need, device):
     return workspace
 
 
+def _written(*tensors):
+    """Tells torch that a call writes these in place, so that a backward pass that kept what they held is an error."""
+    from torch.autograd.graph import increment_version
+    increment_version(tensors)
+
+
 def embedding_tensors(table, tokens, scale=1.0, out=None, out_dtype=None, stream=None):
     """Convenience for torch tensors: table is a (V, d) float32 / bfloat16 GPU tensor, tokens an int32 / int64 GPU tensor of
     any shape.  Returns scale * table[tokens], of shape tokens.shape + (d,), in out_dtype (the table's unless given); a
@@ -588,6 +594,8 @@ def embedding_tensors(table, tokens, scale=1.0, out=None, out_dtype=None, stream
         if out is None:
             result = torch.empty(tuple(tokens.shape) + (d,), dtype=out_dtype or table.dtype, device=table.device)
             out = result.view(N, d)
+        else:
+            _written(out)
         gp_embedding(table.data_ptr(), ldt, dtype, V, d, tokens.data_ptr(), index, N, scale, out.data_ptr(), _row_stride(out, "out"),
                      _float_type(out), handle)
     return result
@@ -615,6 +623,8 @@ def embedding_grad_tensors(tokens, grad, V, scale=1.0, out=None, out_dtype=None,
     with _on_stream(grad, stream) as handle:
         if out is None:
             out = torch.empty((V, d), dtype=out_dtype or grad.dtype, device=grad.device)
+        else:
+            _written(out)
         ws = _workspace(workspace, gp_embedding_grad_workspace(N, V, d), grad.device)
         gp_embedding_grad(tokens.data_ptr(), index, N, grad.data_ptr(), _row_stride(grad, "grad"), dtype, d, scale, V, out.data_ptr(),
                           _row_stride(out, "out"), _float_type(out), accumulate, ws.data_ptr(), ws.numel(), handle)
@@ -642,6 +652,8 @@ def orthogonalize_tensors(G, steps=5, coeff=None, eps=1e-7, out=None, workspace=
     with _on_stream(G, stream) as handle:
         if out is None:
             out = torch.empty(G.shape, dtype=G.dtype, device=G.device)
+        else:
+            _written(out)
         _, _, _, ldo, so = _matrices(out, G.shape, G.dtype, "out")
         ws = _workspace(workspace, gp_orthogonalize_workspace(rows, cols, count), G.device)
         gp_orthogonalize(G.data_ptr(), ldg, sg, dtype, rows, cols, count, steps, coeff, eps, out.data_ptr(), ldo, so, ws.data_ptr(),
@@ -653,7 +665,7 @@ def muon_step_tensors(W, M, G, lr, momentum=0.95, weight_decay=0.0, nesterov=Tru
                       M_out=None, workspace=None, stream=None):
     """Convenience for torch tensors: one step of weight matrices W (float32) with momentum M (float32) and gradient G (float32 /
     bfloat16), all (rows, cols) or (count, rows, cols).  W and M are stepped in place unless W_out, M_out are given (of the
-    same strides).  Returns (W_out, M_out).  coeff, workspace: as orthogonalize_tensors."""
+    same strides; torch's version counters see it).  Returns (W_out, M_out).  coeff, workspace: as orthogonalize_tensors."""
     import torch
     rows, cols, count, ldg, sg = _matrices(G, None, None, "G")
     dtype = _float_type(G)
@@ -664,6 +676,7 @@ def muon_step_tensors(W, M, G, lr, momentum=0.95, weight_decay=0.0, nesterov=Tru
         raise ValueError("W_out and M_out must have the strides of W and M")
     _one_device(G, W, M, W_out, M_out, workspace)
     with _on_stream(G, stream) as handle:
+        _written(W_out, M_out)
         ws = _workspace(workspace, gp_orthogonalize_workspace(rows, cols, count), G.device)
         gp_muon_step(W.data_ptr(), W_out.data_ptr(), ldw, sw, M.data_ptr(), M_out.data_ptr(), ldm, sm, G.data_ptr(), ldg, sg, dtype, rows,
                      cols, count, lr, momentum, weight_decay, nesterov, steps, coeff, eps, ws.data_ptr(), ws.numel(), handle)

@@ -24,3 +24,26 @@ def test_gradient_takes_what_the_lookup_returns(shape):
     for bad in (torch.ones(shape + (3, 3), device="cuda"), torch.ones((), device="cuda"), torch.ones((8, 3), device="cuda")):
         with pytest.raises(ValueError):
             gp.embedding_grad_tensors(tokens, bad, 7)
+
+
+def test_what_is_written_in_place_is_seen_by_automatic_differentiation():
+    """A backward pass that kept a matrix which a call has written since is an error, not a wrong gradient."""
+    import torch
+    def square(n=6):
+        return torch.randn(n, n, device="cuda")
+    W, M, out, grad = (square().requires_grad_() for _ in range(4))
+    tokens = torch.randint(0, 6, (6,), device="cuda")
+    spare = square(), square()
+    for kept, write in ((W, lambda: gp.muon_step_tensors(W, M, square(), 0.1)), (M, lambda: gp.muon_step_tensors(W, M, square(), 0.1)),
+                        (out, lambda: gp.muon_step_tensors(*spare, square(), 0.1, W_out=out, M_out=grad)),
+                        (out, lambda: gp.orthogonalize_tensors(square(), out=out)), (out, lambda: gp.embedding_tensors(square(), tokens, out=out)),
+                        (grad, lambda: gp.embedding_grad_tensors(tokens, square(), 6, out=grad)),
+                        (grad, lambda: gp.embedding_grad_tensors(tokens, square(), 6, out=grad, accumulate=True))):
+        y = square().requires_grad_() @ kept
+        write()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+    before = [t._version for t in (W, M, out, grad, *spare)]
+    gp.embedding_tensors(out.detach(), tokens), gp.embedding_grad_tensors(tokens, grad.detach(), 6), gp.orthogonalize_tensors(out.detach())
+    gp.muon_step_tensors(*spare, square(), 0.1, W_out=square(), M_out=square())
+    assert [t._version for t in (W, M, out, grad, *spare)] == before   # what is only read keeps its version
