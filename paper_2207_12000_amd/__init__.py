@@ -556,7 +556,7 @@ def _one_device(first, *others):
 
 def _row_stride(t, what):
     """The distance of a matrix's rows, in elements (that of a single row, or of none, is whatever its width asks for)."""
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.shape[-1] > 1 and t.stride(-1) != 1 and t.numel() > 0:
         raise ValueError(f"{what} must have unit column stride")
     return max(t.shape[-1], 1) if t.shape[-2] <= 1 else t.stride(-2)
 
@@ -576,11 +576,39 @@ def _written(*tensors):
     increment_version(tensors)
 
 
+@functools.lru_cache(maxsize=None)
+def _differentiable_lookup():
+    import torch
+
+    class Lookup(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, table, tokens, scale, out_dtype, stream):
+            ctx.save_for_backward(tokens)
+            ctx.scale, ctx.shape, ctx.dtype = scale, table.shape, table.dtype
+            return embedding_tensors(table, tokens, scale, out_dtype=out_dtype, stream=stream)
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, grad):
+            tokens, = ctx.saved_tensors
+            V, d = ctx.shape
+            grad = grad.reshape(tokens.numel(), d)
+            if (d > 1 and grad.stride(1) != 1) or 0 < grad.stride(0) < d:  # (a sum's gradient is one number, expanded)
+                grad = grad.contiguous()
+            return embedding_grad_tensors(tokens, grad, V, ctx.scale, out_dtype=ctx.dtype), None, None, None, None
+
+    return Lookup
+
+
 def embedding_tensors(table, tokens, scale=1.0, out=None, out_dtype=None, stream=None):
     """Convenience for torch tensors: table is a (V, d) float32 / bfloat16 GPU tensor, tokens an int32 / int64 GPU tensor of
     any shape.  Returns scale * table[tokens], of shape tokens.shape + (d,), in out_dtype (the table's unless given); a
-    token outside the table gives zeros.  out: a (tokens.numel(), d) tensor with unit column stride, filled and returned."""
+    token outside the table gives zeros.  out: a (tokens.numel(), d) tensor with unit column stride, filled and returned.
+    Where the table requires a gradient, the result does too: backward() takes it by embedding_grad_tensors, on the stream that was
+    current here.  What is filled into out is a plain copy that automatic differentiation does not follow."""
     import torch
+    if out is None and table.requires_grad and torch.is_grad_enabled():
+        return _differentiable_lookup().apply(table, tokens, scale, out_dtype, stream)
     if table.dim() != 2:
         raise ValueError("table must be a (V, d) tensor")
     V, d = table.shape
@@ -604,7 +632,7 @@ def embedding_tensors(table, tokens, scale=1.0, out=None, out_dtype=None, stream
 def embedding_grad_tensors(tokens, grad, V, scale=1.0, out=None, out_dtype=None, accumulate=False, workspace=None, stream=None):
     """Convenience for torch tensors: the gradient of embedding_tensors with respect to its table of V rows, from grad, the
     gradient of what it returned ((N, d), or tokens.shape + (d,) contiguous).  Returns a (V, d) tensor of out_dtype (grad's
-    unless given), or adds to out (accumulate=True).  workspace: a uint8 GPU tensor of gp_embedding_grad_workspace(N, V, d)
+    unless given; automatic differentiation does not follow it), or adds to out (accumulate=True).  workspace: a uint8 GPU tensor of gp_embedding_grad_workspace(N, V, d)
     bytes or more, kept by the caller; without one the call takes its memory from torch."""
     import torch
     N, index, dtype = tokens.numel(), _index_type(tokens), _float_type(grad)
@@ -642,7 +670,7 @@ def _matrices(t, shape, dtype, what):
 def orthogonalize_tensors(G, steps=5, coeff=None, eps=1e-7, out=None, workspace=None, stream=None):
     """Convenience for torch tensors: Newton-Schulz steps on G, a (rows, cols) or (count, rows, cols) float32 / bfloat16 GPU
     tensor.  coeff: (a, b, c), or three for every step, or None (3.4445, -4.7750, 2.0315).  Returns out (made if not given;
-    G itself will do).  workspace: a uint8 GPU tensor of gp_orthogonalize_workspace(rows, cols, count) bytes or more."""
+    G itself will do); automatic differentiation does not follow it.  workspace: a uint8 GPU tensor of gp_orthogonalize_workspace(rows, cols, count) bytes or more."""
     import torch
     rows, cols, count, ldg, sg = _matrices(G, None, None, "G")
     dtype = _float_type(G)
