@@ -1147,7 +1147,7 @@ template <int BM, int BN, int WM, int WN, int STAGES, typename TO, bool LAST>
 gp_status launch_tiles(const Product& a, hipStream_t stream)
 {
     constexpr size_t lds = STAGES * (BM + BN) * 128;
-    if constexpr (lds > 65536) {
+    if constexpr (lds >= 65536) {  // (there are a few bytes of its own beside it)
         gp_status st = raise_lds<&gp_ns_product<BM, BN, WM, WN, STAGES, TO, LAST>>(lds);
         if (st != GP_OK) return st;
     }

@@ -1,11 +1,14 @@
 """What the training operators launch, seen without a GPU (tests/launches.py): sizes that the runtime takes, kernels that shapes reach."""
+import os
 import re
 import shutil
+import subprocess
 
 import pytest
 
 import paper_2207_12000_amd as gp
 from launches import launches
+from test_kernel_registers import READELF, code_objects
 
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not found")
 
@@ -22,6 +25,12 @@ def grad(**kw):
     a = dict(tokens_ptr=P, index=gp.GP_I32, N=4, grad_ptr=P, ldg=8, dtype=gp.GP_F32, d=8, scale=1.0, V=10, table_grad_ptr=P, ldt=8,
              out_dtype=gp.GP_F32, accumulate=False, workspace_ptr=P, workspace_bytes=1 << 50)
     return "gp_embedding_grad", {**a, **kw}
+
+
+def orth(rows, cols, count=1, **kw):
+    a = dict(G_ptr=P, ldg=cols, stride_g=rows * cols, dtype=gp.GP_F32, rows=rows, cols=cols, count=count, steps=2, coeff=None, eps=1e-7, out_ptr=P,
+             ldo=cols, stride_o=rows * cols, workspace_ptr=P, workspace_bytes=1 << 60)
+    return "gp_orthogonalize", {**a, **kw}
 
 
 def check_sizes(result):
@@ -44,3 +53,34 @@ def test_lookups_of_any_length_can_be_launched(N, d):
 def test_gradients_of_any_table_can_be_launched(N, V):
     for dtype in (gp.GP_F32, gp.GP_BF16):
         check_sizes(launches([grad(N=N, V=V, d=1, dtype=dtype, out_dtype=dtype)])[0])
+
+
+@pytest.fixture(scope="module")
+def own_lds(tmp_path_factory):
+    """The LDS that a kernel has by itself, in bytes, by its name."""
+    if not os.path.exists(READELF):
+        pytest.skip("llvm-readelf not found")
+    found = {}
+    for i, code in enumerate(code_objects()):
+        path = tmp_path_factory.mktemp("co") / f"{i}.co"
+        path.write_bytes(code)
+        notes = subprocess.run([READELF, "--notes", str(path)], capture_output=True, text=True, check=True).stdout
+        for entry in re.split(r"\n  - \.agpr_count", notes)[1:]:
+            found[re.search(r"\.name:\s+(\S+)", entry).group(1)] = int(re.search(r"\.group_segment_fixed_size:\s+(\d+)", entry).group(1))
+    return found
+
+
+def test_lds_beyond_64_kb_is_asked_for(own_lds):
+    """A kernel has 64 KB, its own and what the launch adds together; the launch's part of more than that needs the runtime's leave."""
+    calls = [orth(*shape) for shape in ((16, 16), (40, 256), (64, 64), (100, 1000), (300, 300), (704, 2000), (768, 768), (1024, 1024), (1536, 1536),
+                                        (2048, 2048), (4096, 4096), (4096, 1024))] + [orth(1024, 4096, 2), orth(4096, 1024, 2)]
+    calls += [grad(N=N, V=V, d=d, ldg=d, ldt=d, dtype=dtype) for N, V, d in ((4096, 1000, 128), (4096, 1000, 3), (9000, 60, 16), (20_000, 100_000, 16), (2_000_000, 3_000_000, 16))
+              for dtype in (gp.GP_F32, gp.GP_BF16)]
+    large = 0
+    for result in launches(calls):
+        check_sizes(result)
+        for l in result["launches"]:
+            total = own_lds[l["kernel"]] + l["lds"]
+            assert total <= 160 * 1024 and (total <= 64 * 1024 or l["lds_asked"] >= l["lds"]), (l, own_lds[l["kernel"]])
+            large += total > 64 * 1024
+    assert large
