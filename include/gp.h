@@ -417,7 +417,7 @@ typedef enum { GP_I32 = 0, GP_I64 = 1 } gp_index;
  *  table   DEVICE, V x d of `dtype`, rows ldt elements apart (ldt >= d >= 1, V >= 1).
  *  tokens  DEVICE, N row numbers of type `index` (N >= 0).  A number outside [0, V) is not an error: its row of out is zero.
  *  out     DEVICE, N x d of `out_dtype`, rows ldo elements apart (ldo >= d); may be a slab of a hop stack; must not overlap the inputs.
- * Rows may start on any element.  Enqueued on hip_stream.  Errors: INVALID_ARG, OVERFLOW, DEVICE. */
+ * Rows may start on any element.  Enqueued on hip_stream.  Errors: INVALID_ARG, OVERFLOW, OOM_HOST, DEVICE. */
 gp_status gp_embedding(const void *table, int64_t ldt, gp_dtype dtype, int64_t V, int32_t d, const void *tokens,
                        gp_index index, int64_t N, float scale, void *out, int64_t ldo, gp_dtype out_dtype, void *hip_stream);
 
@@ -429,7 +429,7 @@ gp_status gp_embedding(const void *table, int64_t ldt, gp_dtype dtype, int64_t V
  *  table_grad  DEVICE, V x d of `out_dtype`, rows ldt elements apart; must not overlap the inputs.
  * Sums are held in fp32 and rounded once.  The tokens are sorted, so a token's rows are added in an order that depends on
  * the tokens alone.  N and V at most 2^31 - 1 (else UNSUPPORTED).  Enqueued on hip_stream.
- * Errors: INVALID_ARG, UNSUPPORTED, DEVICE.  gp_embedding_grad_workspace: bytes; -1 for sizes that the call rejects. */
+ * Errors: INVALID_ARG, UNSUPPORTED, OOM_HOST, DEVICE.  gp_embedding_grad_workspace: bytes; -1 for sizes that the call rejects. */
 int64_t gp_embedding_grad_workspace(int64_t N, int64_t V, int32_t d);
 gp_status gp_embedding_grad(const void *tokens, gp_index index, int64_t N, const void *grad, int64_t ldg, gp_dtype dtype,
                             int32_t d, float scale, int64_t V, void *table_grad, int64_t ldt, gp_dtype out_dtype,
@@ -448,7 +448,7 @@ gp_status gp_embedding_grad(const void *tokens, gp_index index, int64_t N, const
  * Products are taken in about 22 bits with fp32 accumulation whatever `dtype` is, X is held in as many; bf16 results are rounded once.  The
  * sum of squares is held in fp64.  rows, cols <= 2^20, count <= 65535 (else UNSUPPORTED); nothing is done where one of them is 0.
  * A matrix with an infinity or NaN gives NaN, and leaves the others alone.  Enqueued on hip_stream.
- * Errors: INVALID_ARG, UNSUPPORTED, DEVICE.  gp_orthogonalize_workspace: bytes; -1 for sizes that the call rejects. */
+ * Errors: INVALID_ARG, UNSUPPORTED, OOM_HOST, DEVICE.  gp_orthogonalize_workspace: bytes; -1 for sizes that the call rejects. */
 int64_t gp_orthogonalize_workspace(int64_t rows, int64_t cols, int64_t count);
 gp_status gp_orthogonalize(const void *G, int64_t ldg, int64_t stride_g, gp_dtype dtype, int64_t rows, int64_t cols,
                            int64_t count, int32_t steps, const float *coeff, float eps, void *out, int64_t ldo,

@@ -18,6 +18,7 @@
 // (bf16 rows of 100 into 32,768 rows by Zipf's law, 76 us: sort 37, sums 30, joins 9); of a few thousand one launch's chain of loads, places and
 // sums, and the call (4,096 rows of 128 into 10,000, 12 us, 8.5 of them on the GPU; gp_sum_short).
 #include <algorithm>
+#include <exception>
 #include <type_traits>
 
 #include "gp_internal.h"
@@ -1067,7 +1068,11 @@ gp_status embedding_grad(const void* tokens, gp_index index, int64_t N, const vo
 extern "C" gp_status gp_embedding(const void* table, int64_t ldt, gp_dtype dtype, int64_t V, int32_t d, const void* tokens, gp_index index,
                                   int64_t N, float scale, void* out, int64_t ldo, gp_dtype out_dtype, void* hip_stream)
 {
-    return gp::embedding(table, ldt, dtype, V, d, tokens, index, N, scale, out, ldo, out_dtype, (hipStream_t)hip_stream);
+    try {
+        return gp::embedding(table, ldt, dtype, V, d, tokens, index, N, scale, out, ldo, out_dtype, (hipStream_t)hip_stream);
+    } catch (const std::exception& e) {
+        return gp::fail(GP_ERR_OOM_HOST, "gp_embedding: %s", e.what());
+    }
 }
 
 extern "C" int64_t gp_embedding_grad_workspace(int64_t N, int64_t V, int32_t d)
@@ -1080,6 +1085,10 @@ extern "C" gp_status gp_embedding_grad(const void* tokens, gp_index index, int64
                                        float scale, int64_t V, void* table_grad, int64_t ldt, gp_dtype out_dtype, int32_t accumulate,
                                        void* workspace, int64_t workspace_bytes, void* hip_stream)
 {
-    return gp::embedding_grad(tokens, index, N, grad, ldg, dtype, d, scale, V, table_grad, ldt, out_dtype, accumulate, workspace,
-                              workspace_bytes, (hipStream_t)hip_stream);
+    try {
+        return gp::embedding_grad(tokens, index, N, grad, ldg, dtype, d, scale, V, table_grad, ldt, out_dtype, accumulate, workspace,
+                                  workspace_bytes, (hipStream_t)hip_stream);
+    } catch (const std::exception& e) {
+        return gp::fail(GP_ERR_OOM_HOST, "gp_embedding_grad: %s", e.what());
+    }
 }

@@ -84,3 +84,13 @@ def test_lds_beyond_64_kb_is_asked_for(own_lds):
             assert total <= 160 * 1024 and (total <= 64 * 1024 or l["lds_asked"] >= l["lds"]), (l, own_lds[l["kernel"]])
             large += total > 64 * 1024
     assert large
+
+
+def test_an_allocation_that_fails_is_an_error_of_the_call():
+    """Timed launches are noted in memory of the library's own; without any, a call says so, and the process lives on."""
+    W = dict(W_ptr=P, W_out_ptr=P, ldw=8, stride_w=80, M_ptr=P, M_out_ptr=P, ldm=8, stride_m=80, G_ptr=P, ldg=8, stride_g=80, dtype=gp.GP_F32, rows=10,
+             cols=8, count=2, lr=0.1, momentum=0.9, weight_decay=0.0, nesterov=True, steps=5, coeff=None, eps=1e-7, workspace_ptr=P, workspace_bytes=1 << 30)
+    calls = [lookup(), grad(), grad(N=0), grad(N=5000), orth(8, 8), ("gp_muon_step", W)]
+    for name, kw in calls:
+        failed, after = launches([(name, {**kw, "no_memory": True}), (name, kw)])
+        assert failed["status"] == gp.GP_ERR_OOM_HOST and after["status"] == gp.GP_OK, name
