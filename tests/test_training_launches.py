@@ -94,3 +94,20 @@ def test_an_allocation_that_fails_is_an_error_of_the_call():
     for name, kw in calls:
         failed, after = launches([(name, {**kw, "no_memory": True}), (name, kw)])
         assert failed["status"] == gp.GP_ERR_OOM_HOST and after["status"] == gp.GP_OK, name
+
+
+def kernels(result):
+    """The names of what was launched, in order."""
+    assert result["status"] == gp.GP_OK
+    return [re.search(r"gp_(?:token|sum|join|zero|ns|embedding)\w*?(?=I[A-Z]|E[A-Z]|I[ft]|E[v]|ENS)", l["kernel"]).group(0) for l in result["launches"]]
+
+
+def test_shapes_of_long_lists_reach_what_they_are_for():
+    from test_gpu_training_long import SHAPES
+    ways = set()
+    for (N, V, d, _, _), result in zip(SHAPES, launches([grad(N=N, V=V, d=d, ldg=d, ldt=d) for N, V, d, _, _ in SHAPES])):
+        seen = kernels(result)
+        assert seen[-2:] == ["gp_sum_tiles", "gp_join_tiles"] and "gp_sum_short" not in seen, (N, V, seen)
+        items = {int(m) for l in result["launches"] for m in re.findall(r"gp_token_countILi(\d+)E", l["kernel"])}
+        ways.add(("rank",) if "gp_token_rank" in seen else (seen.count("gp_token_scatter"), *items))
+    assert {("rank",), (1, 4), (2, 4), (3, 4), (2, 16)} <= ways
