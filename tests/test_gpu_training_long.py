@@ -104,3 +104,40 @@ def test_a_row_with_infinity_or_nan_stays_alone():
     want = torch.bincount(tokens.long(), minlength=V + 1)[:V].float()[:, None].repeat(1, d)
     want[3, 2], want[5, 4] = float("inf"), float("nan")
     assert torch.allclose(gp.embedding_grad_tensors(tokens, up, V), want, rtol=0, atol=0, equal_nan=True)
+
+
+def gaps_of(limit, first, last, seed):
+    """Named rows with gaps of around `limit` rows between them, some of none and some far longer, so that they begin and end on every side of the
+    multiples of `limit`; `first` rows before and `last` rows behind.  Tokens (more than 4,096 of them) and V: for gaps of 32, a table of more than 16 rows
+    per token, for 256 of fewer."""
+    rng = np.random.default_rng(seed)
+    count, often = (4500, 1) if limit == 32 else (3000, 30)
+    usual = [limit - 2, limit - 1, limit, limit + 1, limit + 2, 2 * limit - 1, 2 * limit, 2 * limit + 1]
+    gaps = rng.choice(usual + [0, 1, 7 * limit + 5], size=count - 1, p=[0.11] * 8 + [0.04] * 3)
+    named = first + np.concatenate([[0], np.cumsum(gaps + 1)])
+    V = int(named[-1]) + 1 + last
+    tokens = rng.permutation(np.repeat(named, often))
+    assert len(tokens) > 4096 and (V > 16 * len(tokens)) == (limit == 32)
+    return named, tokens, V, float(often)
+
+
+GAPS = [(limit, first, last) for limit in (32, 256) for first in (0, 1, limit - 1, limit, limit + 1, 3 * limit + 2) for last in (0, 1, limit, limit + 1, 5 * limit)]
+
+
+@pytest.mark.parametrize("limit,first,last", GAPS)
+def test_rows_in_gaps_around_their_limits_are_zero(limit, first, last):
+    """Gaps of up to 32 rows, or 256 where the table has at most 16 rows per token, are written beside the run behind them, longer ones by wavefronts
+    of another launch."""
+    import torch
+    named, tokens, V, often = gaps_of(limit, first, last, 64 * limit + first + 7 * last)
+    d = 5
+    tokens = torch.from_numpy(tokens).to(torch.int32).cuda()
+    for dtype, pad, skew in ((torch.float32, 0, 0), (torch.bfloat16, 2, 1), (torch.float32, 3, 3)):
+        flat, out = padded(V, d, d + pad, dtype, skew, fill=0.25)
+        out.fill_(float("nan"))
+        gp.embedding_grad_tensors(tokens, torch.ones(tokens.numel(), d, device="cuda", dtype=dtype), V, out=out)
+        want = torch.zeros(V, d, device="cuda", dtype=dtype)
+        want[torch.from_numpy(named).cuda()] = often
+        assert torch.equal(out, want)
+        out.fill_(0.25)
+        assert bool((flat == 0.25).all())

@@ -111,3 +111,16 @@ def test_shapes_of_long_lists_reach_what_they_are_for():
         items = {int(m) for l in result["launches"] for m in re.findall(r"gp_token_countILi(\d+)E", l["kernel"])}
         ways.add(("rank",) if "gp_token_rank" in seen else (seen.count("gp_token_scatter"), *items))
     assert {("rank",), (1, 4), (2, 4), (3, 4), (2, 16)} <= ways
+
+
+def test_gaps_of_long_lists_reach_both_ways_of_writing_them():
+    from test_gpu_training_long import GAPS, gaps_of
+    sizes = []
+    for limit, first, last in GAPS:
+        named, tokens, V, _ = gaps_of(limit, first, last, 64 * limit + first + 7 * last)
+        inside = named[1:] - named[:-1] - 1
+        assert (inside > limit).any() and ((inside <= limit) & (inside >= limit - 2)).any()
+        assert {int(x) % limit for x in named} == set(range(limit))   # (first rows of gaps on all sides of a wavefront's rows)
+        sizes.append((len(tokens), V))
+    for result in launches([grad(N=N, V=V, d=5) for N, V in sizes]):
+        assert kernels(result)[-2:] == ["gp_sum_tiles", "gp_join_tiles"]
