@@ -124,3 +124,22 @@ def test_gaps_of_long_lists_reach_both_ways_of_writing_them():
         sizes.append((len(tokens), V))
     for result in launches([grad(N=N, V=V, d=5) for N, V in sizes]):
         assert kernels(result)[-2:] == ["gp_sum_tiles", "gp_join_tiles"]
+
+
+def test_newton_schulz_shapes_reach_every_kernel():
+    from test_gpu_newton_schulz import PANELS, SHAPES, SMALL, THIRTY_TWOS, TILES
+
+    def seen(shapes, name):
+        return {re.search(name, l["kernel"]).group(1) for result in launches([orth(*s, dtype=d) for s in shapes for d in (gp.GP_F32, gp.GP_BF16)])
+                for l in result["launches"] if re.search(name, l["kernel"])}
+
+    types = ("f", "t")
+    assert seen(SMALL, r"gp_ns_(tiny)") == {"tiny"} and seen(SHAPES[len(SMALL):], r"gp_ns_(tiny)") == set()
+    assert seen(SMALL, r"gp_ns_tinyILi(.*)EEvNS") == {f"{b}E{t}{o}" for b in (2, 3, 4) for t, o in (("f", "f"), ("t", "t"))}
+    assert seen(PANELS, r"gp_ns_panelILi(.*)EEEvNS") == {f"{m}E{t}Lb{last}" for m in (64, 128) for t, last in (("f", 0), ("f", 1), ("t", 1))}
+    assert seen(THIRTY_TWOS, r"gp_ns_product_smallI(.*)EEEvNS") == {"fLb0ELb0", "fLb0ELb1", "fLb1ELb0", "tLb1ELb0"}
+    wide, tall = {(64, 64), (128, 128), (128, 256), (192, 192), (256, 256)}, {(256, 128)}
+    last = {f"{m}ELi{n}E{t}" for m, n in wide | tall for t in types}
+    assert {re.sub(r"E(Li\dE){3}", "E", x) for x in seen(TILES, r"gp_ns_productILi(\S*)Lb1EEEvNS")} == last
+    assert {re.sub(r"E(Li\dE){3}", "E", x) for x in seen(TILES, r"gp_ns_productILi(\S*)Lb0EEEvNS")} == {f"{m}ELi{n}Ef" for m, n in wide}
+    assert seen(SHAPES, r"gp_ns_normsILi(\d+)") == {"256", "1024"}
