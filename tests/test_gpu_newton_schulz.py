@@ -1,4 +1,4 @@
-"""Newton-Schulz directions on the GPU, at every kernel and tile: as near to 64 bits as operands of 22 bits allow.
+"""Newton-Schulz directions and the Muon step on the GPU, at every kernel and tile: as near to 64 bits as operands of 22 bits allow.
 
 The bar is that of tests/test_newton_schulz_bits.py: four times the error that fp32 steps leave on the same matrices (the median over a batch), which a
 kernel that has lost one of its part products does not meet.  tests/test_training_launches.py checks, without a GPU, that the shapes reach what they are for.
@@ -8,7 +8,7 @@ import pytest
 
 import paper_2207_12000_amd as gp
 from oracle import training
-from test_gpu_training import same_bits
+from test_gpu_training import padded, same_bits, types
 from test_newton_schulz_bits import TIMES_FP32, matrices
 
 pytestmark = pytest.mark.gpu
@@ -61,3 +61,45 @@ def test_directions_are_as_near_as_22_bits_allow(rows, cols, count, kind):
     got = gp.orthogonalize_tensors(G)
     assert float(errors(got, exact).median()) <= TIMES_FP32 * float(errors(steps(G), exact).median())
     assert same_bits(got, gp.orthogonalize_tensors(G))
+
+
+@pytest.mark.parametrize("rows,cols,count", SHAPES)
+def test_a_bf16_direction_is_the_fp32_one_rounded_once(rows, cols, count):
+    G = inputs((rows, cols), count, "gradient").bfloat16()
+    assert same_bits(gp.orthogonalize_tensors(G), gp.orthogonalize_tensors(G.float()).bfloat16())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("rows,cols,count", SHAPES)
+def test_muon_steps(rows, cols, count, nesterov, dtype):
+    """M: two roundings.  W: the direction's bar (the fp32 steps start from their own U), times lr, and three roundings."""
+    import torch
+    lr, mu, wd = (float(np.float32(x)) for x in (0.02, 0.95, 0.1))
+    G = inputs((rows, cols), count, "gradient").to(types()[dtype])
+    M0 = 5 * inputs((rows, cols), count, "gradient", 1)
+    W0 = inputs((rows, cols), count, "normal", 2) / rows ** 0.5
+
+    def strided(values, pad, skew):   # matrices in rows of their own length, from an odd address; NaN beside them
+        flat, all_rows = padded(count * rows, cols, cols + pad, torch.float32, skew)
+        view = all_rows.unflatten(0, (count, rows))
+        view.copy_(values)
+        return flat, view
+
+    w_flat, W = strided(W0, 3, 1)
+    m_flat, M = strided(M0, 5, 2)
+    gp.muon_step_tensors(W, M, G, lr, mu, wd, nesterov)
+    assert int(w_flat.isnan().sum()) == w_flat.numel() - W.numel() and int(m_flat.isnan().sum()) == m_flat.numel() - M.numel()
+    W2, M2 = gp.muon_step_tensors(W0, M0, G, lr, mu, wd, nesterov, W_out=torch.empty_like(W0), M_out=torch.empty_like(M0))
+    assert same_bits(W, W2) and same_bits(M, M2)
+
+    m, g = M0.double(), G.double()
+    want_M = mu * m + g
+    assert bool(((M2.double() - want_M).abs() <= 2.0 ** -23 * ((mu * m).abs() + g.abs())).all())
+    exact = steps(g + mu * want_M if nesterov else want_M)
+    M32 = mu * M0 + G.float()
+    near = TIMES_FP32 * float(errors(steps(G.float() + mu * M32 if nesterov else M32), exact).median())
+    want_W = (1 - lr * wd) * W0.double() - lr * exact
+    norm = lambda x: x.flatten(1).norm(dim=1)  # noqa: E731
+    over = norm(W2.double() - want_W) - 3 * 2.0 ** -24 * (norm(W0.double()) + lr * norm(exact))
+    assert float((over / (lr * norm(exact))).median()) <= near

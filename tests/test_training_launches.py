@@ -143,3 +143,17 @@ def test_newton_schulz_shapes_reach_every_kernel():
     assert {re.sub(r"E(Li\dE){3}", "E", x) for x in seen(TILES, r"gp_ns_productILi(\S*)Lb1EEEvNS")} == last
     assert {re.sub(r"E(Li\dE){3}", "E", x) for x in seen(TILES, r"gp_ns_productILi(\S*)Lb0EEEvNS")} == {f"{m}ELi{n}Ef" for m, n in wide}
     assert seen(SHAPES, r"gp_ns_normsILi(\d+)") == {"256", "1024"}
+
+
+def test_muon_shapes_reach_every_kernel_that_writes_weights():
+    """The same cuts, whatever U is made of."""
+    from test_gpu_newton_schulz import SHAPES
+    calls = []
+    for rows, cols, count in SHAPES:
+        calls.append(("gp_muon_step", dict(W_ptr=P, W_out_ptr=P, ldw=cols, stride_w=rows * cols, M_ptr=P, M_out_ptr=P, ldm=cols, stride_m=rows * cols, G_ptr=P,
+                                           ldg=cols, stride_g=rows * cols, dtype=gp.GP_BF16, rows=rows, cols=cols, count=count, lr=0.1, momentum=0.9,
+                                           weight_decay=0.0, nesterov=True, steps=2, coeff=None, eps=1e-7, workspace_ptr=P, workspace_bytes=1 << 60)))
+    with_weights = launches(calls)
+    plain = launches([orth(*s) for s in SHAPES])
+    products = lambda result: [l["kernel"] for l in result["launches"] if "gp_ns_product" in l["kernel"] or "gp_ns_panel" in l["kernel"]]  # noqa: E731
+    assert [products(a) for a in with_weights] == [products(b) for b in plain]
