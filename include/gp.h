@@ -445,8 +445,9 @@ gp_status gp_embedding_grad(const void *tokens, gp_index index, int64_t N, const
  *         INVALID_ARG.  1 <= steps <= 32.
  *  out    DEVICE, the same shape and dtype, rows ldo, matrices stride_o elements apart; may be G itself (same strides).  Matrices
  *         of out must not overlap (INVALID_ARG).
- * Products are taken in about 22 bits with fp32 accumulation whatever `dtype` is, X is held in as many; bf16 results are rounded once.  The
- * sum of squares is held in fp64.  rows, cols <= 2^20, count <= 65535 (else UNSUPPORTED); nothing is done where one of them is 0.
+ * Products are taken in about 22 bits with fp32 accumulation whatever `dtype` is, X is held in as many (33 where the shorter side is at most 16 and
+ * the longer at most 256); bf16 results are rounded once.  Errors are those of fp32 products or smaller (about 1e-6), but up to 1.7 times these where the
+ * shorter side is below 32 and the longer beyond 256.  The sum of squares is held in fp64.  rows, cols <= 2^20, count <= 65535 (else UNSUPPORTED); nothing is done where one of them is 0.
  * A matrix with an infinity or NaN gives NaN, and leaves the others alone.  Enqueued on hip_stream.
  * Errors: INVALID_ARG, UNSUPPORTED, OOM_HOST, DEVICE.  gp_orthogonalize_workspace: bytes; -1 for sizes that the call rejects. */
 int64_t gp_orthogonalize_workspace(int64_t rows, int64_t cols, int64_t count);

@@ -11,7 +11,8 @@
 // 0.35 off (relative error in the Frobenius norm) for gradients of low rank over a floor of noise; with single f16
 // operands 1.3e-3 and 2.8e-2.  So every matrix is held as two f16 parts, x = hi + lo with 22 bits between them, and a product is three
 // f16 products with fp32 accumulation, hi hi + hi lo + lo hi: 3.7e-7 and 9e-6, where fp32 arithmetic itself left 1.6e-6 and
-// 1.7e-5.  A singular value after any number of steps is at most what the polynomial makes of [0, 1], and no element exceeds
+// 1.7e-5.  (Of matrices with a shorter side of up to 16, whose sums have few terms, fp32 left less; where these go in one launch they have
+// three parts, TinyParts.)  A singular value after any number of steps is at most what the polynomial makes of [0, 1], and no element exceeds
 // the largest singular value: a power of two per matrix and step, known beforehand, keeps every part inside f16's range
 // and lo above its subnormal numbers where it counts.
 //
@@ -166,6 +167,14 @@ __device__ __forceinline__ void split(float v, f16& hi, f16& lo)
     asm("" : "+v"(v));
     hi = (f16)v;
     lo = (f16)(v - (float)hi);
+}
+
+// a third part: what two leave of a number, 33 bits in all
+__device__ __forceinline__ void split(float v, f16& hi, f16& lo, f16& rest)
+{
+    asm("" : "+v"(v));
+    split(v, hi, lo);
+    rest = (f16)(v - (float)hi - (float)lo);
 }
 
 constexpr int kParts = 32;  // from a first part to its second
@@ -789,7 +798,7 @@ __global__ __launch_bounds__(4 * M) void gp_ns_panel(Panel a)
 // The whole of it for matrices of up to 64 x 256: one workgroup each, one launch.  A wavefront owns 16 columns of X, whose values stay in
 // its registers in fp32 from first to last; LDS holds X's parts in rows (for A = X X^T, a 16 x 16 block on or above the diagonal per
 // wavefront, and its mirror image) and in columns (for the panel's own Y = A X, then, in the same place, for A Y), and A's parts: 150 of
-// the 160 KB.  A step takes 3 to 6 us: three barriers, LDS reads and 24 to 72 products per wavefront, one after the other.  The matrices
+// the 160 KB.  A step takes 1 to 6 us: three barriers, LDS reads and 18 to 72 products per wavefront, one after the other.  The matrices
 // themselves take the rest: an update of 256 x 40 takes 26 us, 43 where a tall matrix's elements, whose neighbours a lane has in a row, are
 // asked for and written one by one; of 40 x 256, 27 us.
 struct Tiny {
@@ -805,6 +814,58 @@ constexpr int kTinyRows = 64, kTinyCols = 256;
 constexpr int kRowLd = 2 * kTinyCols + 8, kColLd = 2 * kTinyRows + 8;  // halves: rows and columns start on different banks
 constexpr size_t kTinyLds = (size_t)(kTinyRows * kRowLd + kTinyCols * kColLd + kTinyRows * kColLd) * 2;
 
+// A shorter side of up to 16 leaves half of LDS free, and there numbers have three parts and products six part products (those of 2^-33 are left
+// out): with so few singular values and terms to a sum, what two parts drop does not average out.  Error over that of fp32 steps on the same matrices (geometric mean over 128
+// of them, normal ones / of low rank), two parts, three parts: 1 x 16 1.74 / 1.43, 0.82 / 0.78; 4 x 4 1.47 / 1.35, 0.84 / 0.91; 8 x 256 1.21 / 1.18,
+// 0.81 / 0.89; 16 x 16 1.07 / 1.07, 0.72 / 0.90; from 24 on two parts are within 1.06 (24 x 24 0.92 / 1.06, 64 x 64 0.69 / 0.93).  us a call of one matrix:
+// 8 x 8 7.8, 16 x 256 14.8 (8.9 and 15.4 with 32 rows in two parts).
+template <int PARTS>
+struct TinyParts {
+    // where a column of X or of A, or a row of X, has its third parts, in halves from its first ones
+    static constexpr int kColThird = 2 * kParts, kRowThird = kTinyRows / 2 * kRowLd;
+    // the parts of four neighbours of a column
+    static __device__ __forceinline__ void take(const float (&v)[4], v4h (&h)[PARTS])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f16 hi, lo, rest;
+            if constexpr (PARTS == 3)
+                split(v[i], hi, lo, rest), h[2][i] = rest;
+            else
+                split(v[i], hi, lo);
+            h[0][i] = hi, h[1][i] = lo;
+        }
+    }
+    static __device__ __forceinline__ void store(f16* d, const v4h (&h)[PARTS])
+    {
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) *(v4h*)(d + part * kParts) = h[part];
+    }
+    static __device__ __forceinline__ void store(f16* d, const float (&v)[4])
+    {
+        v4h h[PARTS];
+        take(v, h);
+        store(d, h);
+    }
+    // eight neighbours of a line; third: where its third parts are
+    static __device__ __forceinline__ void load(v8h (&x)[PARTS], const f16* p, int third)
+    {
+        x[0] = *(const v8h*)p, x[1] = *(const v8h*)(p + kParts);
+        if constexpr (PARTS == 3) x[2] = *(const v8h*)(p + third);
+    }
+    static __device__ __forceinline__ void multiply(v4f (&acc)[3], const v8h (&p)[PARTS], const v8h (&q)[PARTS])
+    {
+        acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[0], q[0], acc[0], 0, 0, 0);
+        acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[1], q[0], acc[1], 0, 0, 0);
+        acc[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[0], q[1], acc[2], 0, 0, 0);
+        if constexpr (PARTS == 3) {
+            acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[2], q[0], acc[1], 0, 0, 0);
+            acc[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[0], q[2], acc[2], 0, 0, 0);
+            acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[1], q[1], acc[1], 0, 0, 0);
+        }
+    }
+};
+
 template <int BLOCKS, typename T, typename TO>  // blocks of 16 rows
 __global__ __launch_bounds__(1024) void gp_ns_tiny(Tiny a)
 {
@@ -817,7 +878,8 @@ __global__ __launch_bounds__(1024) void gp_ns_tiny(Tiny a)
     const int c = wave * 16 + r16;      // the lane's column; its elements v[g][i]: row 16 g + 4 kg + i
     const int panels = (n + 31) / 32 * 2;  // (whole lines of columns)
     const bool active = wave < panels;
-    constexpr int kLines = (BLOCKS + 1) / 2;
+    constexpr int kLines = (BLOCKS + 1) / 2, PARTS = BLOCKS == 1 ? 3 : 2;
+    using Parts = TinyParts<PARTS>;
     // U, element by element, and the new momentum.  The lane's four elements of a block are neighbours in a tall matrix's rows
     const T* const G = (const T*)a.u.G + z * a.u.stride_g;
     float v[BLOCKS][4], mo[BLOCKS][4];
@@ -869,8 +931,8 @@ __global__ __launch_bounds__(1024) void gp_ns_tiny(Tiny a)
         for (int i = 0; i < 4; ++i) v[g][i] = 16 * g + 4 * kg + i < m && c < n ? (float)((double)v[g][i] * factor) : 0.0f;
     if constexpr (BLOCKS % 2 == 1) {  // the last line's other half: zero from first to last
         const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (active) store_parts(cols + c * kColLd + place(16 * BLOCKS + 4 * kg), zero);
-        if (threadIdx.x < kTinyRows * 4) store_parts(gram + threadIdx.x / 4 * kColLd + place(16 * BLOCKS + threadIdx.x % 4 * 4), zero);
+        if (active) Parts::store(cols + c * kColLd + place(16 * BLOCKS + 4 * kg), zero);
+        if (threadIdx.x < kTinyRows * 4) Parts::store(gram + threadIdx.x / 4 * kColLd + place(16 * BLOCKS + threadIdx.x % 4 * 4), zero);
     }
     for (int k = 0;; ++k) {
         // X into LDS, both ways
@@ -878,23 +940,17 @@ __global__ __launch_bounds__(1024) void gp_ns_tiny(Tiny a)
 #pragma unroll
             for (int g = 0; g < BLOCKS; ++g) {
                 // four rows of this column; and, with the neighbouring lane's, two rows of both columns
-                v4h hi, lo;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    f16 x, y;
-                    split(v[g][i], x, y);
-                    hi[i] = x, lo[i] = y;
-                }
-                f16* const d = cols + c * kColLd + place(16 * g + 4 * kg);
-                *(v4h*)d = hi, *(v4h*)(d + kParts) = lo;
+                v4h h[PARTS];
+                Parts::take(v[g], h);
+                Parts::store(cols + c * kColLd + place(16 * g + 4 * kg), h);
                 const bool odd = lane & 1;
 #pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    const v2i own = __builtin_bit_cast(v2i, part ? lo : hi);  // rows 0 and 1, rows 2 and 3
+                for (int part = 0; part < PARTS; ++part) {
+                    const v2i own = __builtin_bit_cast(v2i, h[part]);  // rows 0 and 1, rows 2 and 3
                     const int other = __builtin_amdgcn_mov_dpp(odd ? own[0] : own[1], 0xB1, 0xF, 0xF, true);  // of the lane beside it, the rows it keeps
                     const unsigned mine = (unsigned)(odd ? own[1] : own[0]);
                     const unsigned left = odd ? (unsigned)other : mine, right = odd ? mine : (unsigned)other;
-                    f16* const at = rows + (16 * g + 4 * kg + (odd ? 2 : 0)) * kRowLd + place(c & ~1) + part * kParts;
+                    f16* const at = rows + (16 * g + 4 * kg + (odd ? 2 : 0)) * kRowLd + place(c & ~1) + (part == 2 ? Parts::kRowThird : part * kParts);
                     *(unsigned*)at = (left & 0xFFFFu) | right << 16;
                     *(unsigned*)(at + kRowLd) = left >> 16 | (right & 0xFFFF0000u);
                 }
@@ -905,52 +961,45 @@ __global__ __launch_bounds__(1024) void gp_ns_tiny(Tiny a)
             const f16 *const p = rows + (bi * 16 + r16) * kRowLd + kg * 8, *const q = rows + (bj * 16 + r16) * kRowLd + kg * 8;
             v4f acc[3] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
             for (int s = 0; s < panels / 2; ++s) {
-                const v8h ph = *(const v8h*)(p + s * 64), pl = *(const v8h*)(p + s * 64 + kParts);
-                const v8h qh = *(const v8h*)(q + s * 64), ql = *(const v8h*)(q + s * 64 + kParts);
-                acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, qh, acc[0], 0, 0, 0);
-                acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, qh, acc[1], 0, 0, 0);
-                acc[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, ql, acc[2], 0, 0, 0);
+                v8h pv[PARTS], qv[PARTS];
+                Parts::load(pv, p + s * 64, Parts::kRowThird);
+                Parts::load(qv, q + s * 64, Parts::kRowThird);
+                Parts::multiply(acc, pv, qv);
             }
             // element i: row 16 bi + 4 kg + i, column 16 bj + r16; and its mirror image
             const v4f x = acc[0] + (acc[1] + acc[2]);
             const float t[4] = {x[0] * a.alpha[k], x[1] * a.alpha[k], x[2] * a.alpha[k], x[3] * a.alpha[k]};
-            store_parts(gram + (bj * 16 + r16) * kColLd + place(bi * 16 + 4 * kg), t);
+            v4h h[PARTS];
+            Parts::take(t, h);
+            Parts::store(gram + (bj * 16 + r16) * kColLd + place(bi * 16 + 4 * kg), h);
             if (bi != bj)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    f16 hi, lo;
-                    split(t[i], hi, lo);
                     f16* const d = gram + (bi * 16 + 4 * kg + i) * kColLd + place(bj * 16 + r16);
-                    d[0] = hi, d[kParts] = lo;
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) d[part * kParts] = h[part][i];
                 }
         }
         __syncthreads();
         if (active) {
             constexpr bool kKeep = BLOCKS < 4;  // A in registers, where these hold it
-            v8h av[BLOCKS][kLines][2];
+            v8h av[BLOCKS][kLines][PARTS];
 #pragma unroll
             for (int g = 0; g < BLOCKS; ++g)
 #pragma unroll
                 for (int s = 0; s < kLines; ++s)
-#pragma unroll
-                    for (int part = 0; part < 2; ++part)
-                        if (kKeep) av[g][s][part] = *(const v8h*)(gram + (16 * g + r16) * kColLd + s * 64 + part * kParts + kg * 8);
+                    if (kKeep) Parts::load(av[g][s], gram + (16 * g + r16) * kColLd + s * 64 + kg * 8, Parts::kColThird);
             auto product = [&](v4f(&y)[BLOCKS]) {  // A times the wavefront's columns in LDS
-                v8h q[kLines][2];
+                v8h q[kLines][PARTS];
 #pragma unroll
-                for (int s = 0; s < kLines; ++s)
-#pragma unroll
-                    for (int part = 0; part < 2; ++part) q[s][part] = *(const v8h*)(cols + c * kColLd + s * 64 + part * kParts + kg * 8);
+                for (int s = 0; s < kLines; ++s) Parts::load(q[s], cols + c * kColLd + s * 64 + kg * 8, Parts::kColThird);
 #pragma unroll
                 for (int g = 0; g < BLOCKS; ++g) {
                     v4f acc[3] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
                     for (int s = 0; s < kLines; ++s) {
-                        const f16* const p = gram + (16 * g + r16) * kColLd + s * 64 + kg * 8;
-                        const v8h hi = kKeep ? av[g][s][0] : *(const v8h*)p, lo = kKeep ? av[g][s][1] : *(const v8h*)(p + kParts);
-                        acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, q[s][0], acc[0], 0, 0, 0);
-                        acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, q[s][0], acc[1], 0, 0, 0);
-                        acc[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, q[s][1], acc[2], 0, 0, 0);
+                        if (!kKeep) Parts::load(av[g][s], gram + (16 * g + r16) * kColLd + s * 64 + kg * 8, Parts::kColThird);
+                        Parts::multiply(acc, av[g][s], q[s]);
                     }
                     y[g] = acc[0] + (acc[1] + acc[2]);
                 }
@@ -960,7 +1009,7 @@ __global__ __launch_bounds__(1024) void gp_ns_tiny(Tiny a)
 #pragma unroll
             for (int g = 0; g < BLOCKS; ++g) {  // (the columns' X is not needed again)
                 const float t[4] = {y[g][0] * a.y_scale[k], y[g][1] * a.y_scale[k], y[g][2] * a.y_scale[k], y[g][3] * a.y_scale[k]};
-                store_parts(cols + c * kColLd + place(16 * g + 4 * kg), t);
+                Parts::store(cols + c * kColLd + place(16 * g + 4 * kg), t);
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (a wavefront's own columns: no barrier)
             product(w);
@@ -1214,7 +1263,7 @@ template <typename T, typename TO>
 gp_status launch_tiny(const Tiny& a, int64_t count, hipStream_t stream)
 {
     const int64_t m = std::min(a.u.rows, a.u.cols);
-    return m <= 32 ? launch_tiny<2, T, TO>(a, count, stream) : m <= 48 ? launch_tiny<3, T, TO>(a, count, stream) : launch_tiny<4, T, TO>(a, count, stream);
+    return m <= 16 ? launch_tiny<1, T, TO>(a, count, stream) : m <= 32 ? launch_tiny<2, T, TO>(a, count, stream) : m <= 48 ? launch_tiny<3, T, TO>(a, count, stream) : launch_tiny<4, T, TO>(a, count, stream);
 }
 
 // out: the direction itself (W null, of dtype out_dtype), or the stepped weights

@@ -135,7 +135,7 @@ def test_newton_schulz_shapes_reach_every_kernel():
 
     types = ("f", "t")
     assert seen(SMALL, r"gp_ns_(tiny)") == {"tiny"} and seen(SHAPES[len(SMALL):], r"gp_ns_(tiny)") == set()
-    assert seen(SMALL, r"gp_ns_tinyILi(.*)EEvNS") == {f"{b}E{t}{o}" for b in (2, 3, 4) for t, o in (("f", "f"), ("t", "t"))}
+    assert seen(SMALL, r"gp_ns_tinyILi(.*)EEvNS") == {f"{b}E{t}{o}" for b in (1, 2, 3, 4) for t, o in (("f", "f"), ("t", "t"))}
     assert seen(PANELS, r"gp_ns_panelILi(.*)EEEvNS") == {f"{m}E{t}Lb{last}" for m in (64, 128) for t, last in (("f", 0), ("f", 1), ("t", 1))}
     assert seen(THIRTY_TWOS, r"gp_ns_product_smallI(.*)EEEvNS") == {"fLb0ELb0", "fLb0ELb1", "fLb1ELb0", "tLb1ELb0"}
     wide, tall = {(64, 64), (128, 128), (128, 256), (192, 192), (256, 256)}, {(256, 128)}
