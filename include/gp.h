@@ -447,7 +447,8 @@ gp_status gp_embedding_grad(const void *tokens, gp_index index, int64_t N, const
  *         of out must not overlap (INVALID_ARG).
  * Products are taken in about 22 bits with fp32 accumulation whatever `dtype` is, X is held in as many (33 where the shorter side is at most 16 and
  * the longer at most 256); bf16 results are rounded once.  Errors are those of fp32 products or smaller (about 1e-6), but up to 1.7 times these where the
- * shorter side is below 32 and the longer beyond 256.  The sum of squares is held in fp64.  rows, cols <= 2^20, count <= 65535 (else UNSUPPORTED); nothing is done where one of them is 0.
+ * shorter side is below 32 and the longer beyond 256.  The sum of squares is held in fp64.
+ * rows, cols <= 2^20, count <= 65535 (else UNSUPPORTED); nothing is done where one of them is 0.
  * A matrix with an infinity or NaN gives NaN, and leaves the others alone.  Enqueued on hip_stream.
  * Errors: INVALID_ARG, UNSUPPORTED, OOM_HOST, DEVICE.  gp_orthogonalize_workspace: bytes; -1 for sizes that the call rejects. */
 int64_t gp_orthogonalize_workspace(int64_t rows, int64_t cols, int64_t count);
@@ -458,6 +459,8 @@ gp_status gp_orthogonalize(const void *G, int64_t ldg, int64_t stride_g, gp_dtyp
 /* gp_muon_step -- a step of weight matrices along such directions:
  *     M_out = momentum * M + G,   U = nesterov ? G + momentum * M_out : M_out,
  *     W_out = (1 - lr * weight_decay) * W - lr * orthogonalize(U)
+ * One lr is the decay's and the direction's.  Recipes that scale a direction by its shape, by r = sqrt(max(1, rows / cols)) say, pass lr * r and
+ * weight_decay / r.
  *  W, W_out  DEVICE fp32, rows ldw, matrices stride_w elements apart; W_out may be W.   M, M_out  the same with ldm, stride_m.
  *  G         DEVICE, of `dtype`; must not overlap what is written.  Everything else, the workspace too (gp_orthogonalize_workspace), as gp_orthogonalize. */
 gp_status gp_muon_step(const float *W, float *W_out, int64_t ldw, int64_t stride_w, const float *M, float *M_out, int64_t ldm,

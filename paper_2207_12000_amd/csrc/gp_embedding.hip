@@ -170,6 +170,9 @@ gp_status launch_lookup(const LookupArgs& a, hipStream_t stream)
 // the digits of its tile of consecutive entries, (2) for every digit the tiles before each tile are added up, (3) every workgroup
 // ranks its tile's entries -- a wavefront takes 64 at a time, finds the lanes with its own digit by one ballot per bit, and
 // keeps counts of its own in LDS, so that no barrier stands between its steps -- and writes each to its place.
+// (The sort that plans use, gp_device_sort.hip, is for long lists of keys that are there already: five launches a pass of 8 bits, tiles of 16,384
+// keys, three barriers for every 256 of them.  507,001 tokens of 16 bits would take ten launches of up to 31 workgroups, and one to make the keys; here
+// they take four launches, of 124.)
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMaxDigits = 2048;
 
 struct SortArgs {
@@ -482,8 +485,8 @@ __device__ __forceinline__ void finish(const GradArgs& a, int64_t v, int c, cons
 
 // Rows of zeros: those of a gap in the tokens that is at most `gap` rows long are written beside the run behind it, others by gp_join_tiles.
 // A lane that writes a gap does so row after row, so that long ones are left to the others where there are many (gaps of up to 256 and up to
-// 32 rows, us: 921 tokens in 193 k rows of 64 39 / 24, 751 in 391 k 48 / 28, 10 k in 1 M rows of 100 133 / 119, 100 k in 2.4 M rows of
-// 64 185 / 177); where the mean gap is shorter than 16 rows, looking for them costs as much or more (100 k in 1 M 146 / 156).
+// 32 rows, us: 5 k tokens in 200 k rows of 64 36 / 28, 10 k in 1 M rows of 100 131 / 117, 100 k in 2.4 M rows of 64 186 / 172); where the mean
+// gap is shorter than 16 rows, looking for them costs as much or more (100 k in 1.7 M 146 / 147, in 1 M 98 / 109).
 int64_t gap_rows(int64_t N, int64_t V) { return V > 16 * N ? 32 : 256; }
 
 // G lanes walk one stretch of a.tile / kGroups places, a lane holds one vector of the sums; the workgroup's stretches are one tile.  A run
@@ -629,9 +632,10 @@ __global__ __launch_bounds__(kThreads) void gp_zero_table(GradArgs a)
 // Short lists in one launch: a workgroup has a range of the table's rows.  It reads all tokens, keeps those of its rows in LDS in their order,
 // sorts them there by row, writes zeros to its rows without a token and sums up the others as one tile.
 // Three dependent launches (places by counting, sums, joins) take longer the shorter the list is: us on the GPU, three launches / one,
-// 500 x 64 into 300 rows 11.0 / 5.9, 4096 x 128 into 1000 16.6 / 7.4, the same by Zipf's law 17.7 / 16.2, into 60 rows 16.2 / 9.0, into
-// 100 k 24.6 / 14.2.  But a token's rows are one workgroup's: 4096 x 128 of one token take 19 / 33, so lists of more than 128 tokens per
-// row of the table, or of more than a million elements (4096 x 602: 17 / 17, of one token 36 / 84), go the other way.
+// 500 x 64 into 300 rows 10.8 / 5.9, 4096 x 128 into 1000 16.3 / 7.4, the same by Zipf's law 17.7 / 16.3, into 60 rows 16.7 / 9.6, into
+// 100 k 24.5 / 13.6.  But a token's rows are one workgroup's: 4096 x 128 of one token take 18 / 29 with 32 rows, 18 / 33 with 1000, 19 / 42 with 10,000, so
+// lists of more than 128 tokens per row of the table, or of more than a million elements (4096 x 602: 17 / 17, of one token 36 / 84), go the
+// other way.  4,096 tokens are what one count per lane of a wavefront holds (divide below), no limit of the method: 4,097 take 17.5, 8,192 22.4.
 constexpr int kShortThreads = 1024, kShortBlocks = 256;
 constexpr int64_t kShortest = 4096, kShortElements = 1 << 20, kShortPerRow = 128;
 constexpr int kCounted = 128;  // tokens of a workgroup up to which each one's place is counted; beyond, they are sorted bit by bit of the row

@@ -23,10 +23,12 @@
 // What bounds it, and us measured (five steps).  Large matrices: power.  The third product of 4096 x 4096 takes 355 us, 1.16 PFLOP/s of f16 products,
 // with the matrix cores 60 % busy at 1.9 GHz; the same launch on operands that are all one number takes 210.  The whole, 3.7 - 3.9 ms, of which
 // the symmetric products, half of whose tiles are computed, take 198 each; a library's fp32 products take 14.7.  Middle sizes: how evenly tiles fill
-// the chip, and the planes' traffic (two 1024 x 4096 steps with bf16 gradients 651: X X^T 48, A A 20, the update 64, the start 32,
-// norms and momentum 21).  Small ones: the chain of 17 launches, 5 us each, of which a launch on its own would take 1.6 and lines
-// that the launch before has sent past the L2s another 2 (two 256 x 256 81, 602 x 256 96).  Up to 64 x 256 one launch: 12 (16 x 16),
-// 18 (64 x 64), 32 (256 x 40), 35 (64 x 256); 45 to 62 for 256 x 40 in several.
+// the chip, and the planes' traffic (two 1024 x 4096 steps with bf16 gradients 646: as traced, X X^T 49, whose 72 tiles of 128 by three workgroups each
+// leave 40 of 256 compute units idle, A A 21, 272 tiles of 64, the update 66 a step, the start 24, norms and momentum 21).  Small ones: the
+// chain of 17 launches, 5 us each, of which a launch on its own would take 1.6 and lines that the launch before has sent past the L2s another 2
+// (two 256 x 256 79, 602 x 256 in bf16 92; a barrier among 64 workgroups inside a launch takes 1.4, 2.2 where they hand on what they have by
+// device-wide atomics, 20 by fences).  Up to 64 x 256 one launch: 8 (16 x 16), 16 (64 x 64), 24 (256 x 40), 34 (64 x 256); 45 to 62 for
+// 256 x 40 in several.
 #include <algorithm>
 #include <cmath>
 #include <exception>
