@@ -6,9 +6,11 @@ allocations fail during the call, with every kernel timed (gp_profile_enable), s
 """
 from __future__ import annotations
 
+import atexit
 import functools
 import json
 import os
+import shutil
 import subprocess
 import sys
 import tempfile
@@ -19,6 +21,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 @functools.lru_cache(maxsize=None)
 def _recorder():
     folder = tempfile.mkdtemp(prefix="launches")
+    atexit.register(shutil.rmtree, folder, ignore_errors=True)
     path = os.path.join(folder, "recorder.so")
     subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-fvisibility=default", os.path.join(HERE, "launch_recorder.cpp"), "-o", path], check=True)
     return path
