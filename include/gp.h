@@ -470,6 +470,90 @@ gp_status gp_muon_step(const float *W, float *W_out, int64_t ldw, int64_t stride
                        void *hip_stream);
 
 /* ---------------------------------------------------------------------------
+ * What stands between those weights and a loss: layer norm, log probabilities of classes or words with what else might have been answered, and
+ * learning from a teacher's best answers.  As above: nothing is kept between calls or allocated, scratch is the caller's (256-byte boundary, one for
+ * each of the calls that overlap in time), all may be captured in a HIP graph, the same inputs give the same bits.  Sums are held in fp32 or more,
+ * rounded once to the type of what is written.  Rows may start on any element.
+ */
+
+/* gp_layer_norm -- row by row  m = mean(x),  r = 1 / sqrt(mean((x - m)^2) + eps),  y = (x - m) r weight + bias.
+ *  x       DEVICE, N x d of `dtype`, rows ldx elements apart (ldx >= d >= 1, N >= 0).
+ *  weight, bias  DEVICE, d of `weight_dtype` each; NULL: all 1, all 0.   eps: above 0, at most 1e30.
+ *  y       DEVICE, N x d of `out_dtype`, rows ldy elements apart; may be x itself (same type and ldy), else must not overlap the inputs.
+ *  stats   DEVICE, N x 2 fp32: (m, r) of every row, what the gradient needs; NULL: not wanted.
+ * A row with an infinity or NaN gives NaN and leaves the others alone.  Enqueued on hip_stream.  Errors: INVALID_ARG, OOM_HOST, DEVICE. */
+gp_status gp_layer_norm(const void *x, int64_t ldx, gp_dtype dtype, int64_t N, int32_t d, const void *weight, const void *bias,
+                        gp_dtype weight_dtype, float eps, void *y, int64_t ldy, gp_dtype out_dtype, float *stats, void *hip_stream);
+
+/* gp_layer_norm_grad -- its gradients, with h = (x - m) r and u = weight grad:
+ *     x_grad = r (u - mean(u) - h mean(u h)),   weight_grad = sum over rows of grad h,   bias_grad = sum over rows of grad
+ *  grad    DEVICE, N x d of `grad_dtype`, rows ldg elements apart (ldg >= d, or 0: one row stands for all N).
+ *  x, stats, weight  as gp_layer_norm had and left them.
+ *  x_grad  DEVICE, N x d of `dtype`, rows ldxg elements apart; may be x or grad itself (same type and distance of rows); NULL: not wanted.
+ *  weight_grad, bias_grad  DEVICE, d of `weight_dtype` each; NULL: not wanted.  accumulate = 1: added to what they hold.
+ *  workspace  gp_layer_norm_grad_workspace bytes; not needed where neither weight_grad nor bias_grad is wanted and d <= 16384.
+ * Sums over rows are taken in an order that depends on N, d and the types alone.  N at most 2^40 (else UNSUPPORTED).  Enqueued on hip_stream.
+ * Errors: INVALID_ARG, UNSUPPORTED, OOM_HOST, DEVICE.  gp_layer_norm_grad_workspace: -1 for sizes that the call rejects. */
+int64_t gp_layer_norm_grad_workspace(int64_t N, int32_t d);
+gp_status gp_layer_norm_grad(const void *grad, int64_t ldg, gp_dtype grad_dtype, const void *x, int64_t ldx, gp_dtype dtype, int64_t N, int32_t d,
+                             const float *stats, const void *weight, gp_dtype weight_dtype, void *x_grad, int64_t ldxg, void *weight_grad,
+                             void *bias_grad, int32_t accumulate, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/* gp_log_probs -- what rows of logits say.  With z = scale * logits and log p = z - log(sum over the row of exp z):
+ *     logp[i] = log p of class token[i] (0 where it names none),   entropy[i] = - sum p log p,
+ *     (top_index, top_logp)[i, 0 .. k-1] = the k largest logits' classes and log p, largest first, lower classes first among equal ones
+ *  logits  DEVICE, N x C of `dtype`, rows ld elements apart (ld >= C >= 1).  A class of -inf is ruled out: p = 0, and it is no alternative
+ *          (places that no class is left for hold -1 and -inf).  A row without any other has log p = -inf throughout and entropy 0.  +inf or NaN
+ *          make a row's logp, entropy and top_logp NaN; in the order of alternatives NaN stands above +inf.
+ *  tokens  DEVICE, N class numbers of type `index`; one outside [0, C) is not an error.  Needed for logp alone.   scale: within 1e-30 .. 1e30.
+ *  logp, entropy  DEVICE, N fp32 each;  top_index  DEVICE, N x k int32;  top_logp  DEVICE, N x k fp32 (0 <= k <= 64, else UNSUPPORTED; k may
+ *          be above C);  stats  DEVICE, N x 2 fp32: (largest logit, log of the sum of exp behind it), what the gradient needs.
+ *          NULL: not wanted (top_*: where k = 0).
+ *  workspace  gp_log_probs_workspace bytes (0 for most sizes: rows that few workgroups would have to themselves are cut into parts).
+ * N at most 2^40, C at most 2^28 (else UNSUPPORTED).  Enqueued on hip_stream.
+ * Errors: INVALID_ARG, UNSUPPORTED, OOM_HOST, DEVICE.  gp_log_probs_workspace: -1 for sizes that the call rejects. */
+int64_t gp_log_probs_workspace(int64_t N, int32_t C, int32_t k);
+gp_status gp_log_probs(const void *logits, int64_t ld, gp_dtype dtype, int64_t N, int32_t C, const void *tokens, gp_index index, float scale,
+                       float *logp, float *entropy, int32_t k, int32_t *top_index, float *top_logp, float *stats, void *workspace,
+                       int64_t workspace_bytes, void *hip_stream);
+
+/* gp_log_probs_grad -- the gradient with respect to the logits of  sum_i grad_logp[i] logp[i] + grad_entropy[i] entropy[i]:
+ *     grad[i, j] = scale * (grad_logp[i] ([j = token[i]] - p_j) - grad_entropy[i] p_j (log p_j + entropy[i]))
+ *  (grad_logp = -1 / N is the mean cross entropy's; a row whose token names no class has no part of it).
+ *  logits, tokens, scale, stats, entropy  as gp_log_probs had and left them (tokens for grad_logp, entropy for grad_entropy).
+ *  grad_logp, grad_entropy  DEVICE, fp32, elements stride_* apart: 1, or 0 (one stands for all rows); NULL: 0.
+ *  grad    DEVICE, N x C of `dtype`, rows ldg elements apart; must not overlap the inputs.
+ * N x C below 2^62 (else OVERFLOW).  Enqueued on hip_stream.  Errors: INVALID_ARG, UNSUPPORTED, OVERFLOW, OOM_HOST, DEVICE. */
+gp_status gp_log_probs_grad(const void *logits, int64_t ld, gp_dtype dtype, int64_t N, int32_t C, const void *tokens, gp_index index,
+                            float scale, const float *stats, const float *entropy, const float *grad_logp, int64_t stride_logp,
+                            const float *grad_entropy, int64_t stride_entropy, void *grad, int64_t ldg, void *hip_stream);
+
+/* gp_distill -- a student's loss against its teacher's K best logits, and its gradient.  With T the temperature,
+ *     q = softmax over the row's entries of teacher_logits / T,   p = softmax over all C classes of logits / T:
+ *     loss[i] = T^2 sum over entries of q (log q - log p[class of the entry])
+ *     grad[i, j] = grad_loss[i] T (p_j - sum of q over the entries that name class j)
+ *  logits  DEVICE, N x C of `dtype`, rows ld elements apart.  Classes of -inf have p = 0 (a loss of +inf where the teacher names one).
+ *  teacher_index   DEVICE, N x K class numbers of type `index`, rows ldi elements apart; one outside [0, C) makes its entry none (-1 ends a
+ *                  shorter list).  A class may be named more than once.   teacher_logits  DEVICE, N x K of teacher_dtype, rows ldt elements apart
+ *                  (logits or log probabilities: a row's common offset does not matter); -inf makes its entry none.  1 <= K <= 64.
+ *  A row without an entry has loss and gradient 0.   temperature: within 1e-30 .. 1e30.
+ *  loss    DEVICE, N fp32;  stats  DEVICE, N x 2 fp32, what gp_distill_grad needs.  NULL: not wanted.
+ *  grad    DEVICE, N x C of `dtype`, rows ldg elements apart, made in the same pass from grad_loss (DEVICE, fp32, elements stride_loss apart: 1, or 0);
+ *          must not overlap the inputs; NULL: not wanted.
+ *  workspace  gp_distill_workspace bytes (0 for most sizes).
+ * gp_distill_grad makes the gradient alone, from the stats that gp_distill left.
+ * N at most 2^40, C at most 2^28, K at most 64 (else UNSUPPORTED).  Enqueued on hip_stream.
+ * Errors: INVALID_ARG, UNSUPPORTED, OOM_HOST, DEVICE.  gp_distill_workspace: -1 for sizes that the call rejects. */
+int64_t gp_distill_workspace(int64_t N, int32_t C);
+gp_status gp_distill(const void *logits, int64_t ld, gp_dtype dtype, int64_t N, int32_t C, const void *teacher_index, int64_t ldi,
+                     gp_index index, const void *teacher_logits, int64_t ldt, gp_dtype teacher_dtype, int32_t K, float temperature, float *loss,
+                     float *stats, const float *grad_loss, int64_t stride_loss, void *grad, int64_t ldg, void *workspace,
+                     int64_t workspace_bytes, void *hip_stream);
+gp_status gp_distill_grad(const void *logits, int64_t ld, gp_dtype dtype, int64_t N, int32_t C, const void *teacher_index, int64_t ldi,
+                          gp_index index, const void *teacher_logits, int64_t ldt, gp_dtype teacher_dtype, int32_t K, float temperature,
+                          const float *stats, const float *grad_loss, int64_t stride_loss, void *grad, int64_t ldg, void *hip_stream);
+
+/* ---------------------------------------------------------------------------
  * Optimal graph decomposition (Section 3.2, Eq. 11 and Eq. 12): block counts
  * from byte volumes, the available GPU volume and the environment's coefficients
  * (all in the same unit, e.g. bytes or GB; coefficients are measured by watching

@@ -9,7 +9,7 @@ import contextlib
 import ctypes
 import functools
 import os
-from typing import Optional
+from typing import Any, NamedTuple, Optional
 
 import numpy as np
 
@@ -78,6 +78,24 @@ _SIGNATURES = {
                                 _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_float,
                                 _c.c_float, _c.c_float, _c.c_int32, _c.c_int32, _c.c_void_p, _c.c_float, _c.c_void_p, _c.c_int64,
                                 _c.c_void_p]),
+    "gp_layer_norm": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int, _c.c_int64, _c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_int, _c.c_float,
+                                 _c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_void_p]),
+    "gp_layer_norm_grad_workspace": (_c.c_int64, [_c.c_int64, _c.c_int32]),
+    "gp_layer_norm_grad": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_int64, _c.c_int, _c.c_int64, _c.c_int32, _c.c_void_p,
+                                      _c.c_void_p, _c.c_int, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_void_p,
+                                      _c.c_int64, _c.c_void_p]),
+    "gp_log_probs_workspace": (_c.c_int64, [_c.c_int64, _c.c_int32, _c.c_int32]),
+    "gp_log_probs": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int, _c.c_int64, _c.c_int32, _c.c_void_p, _c.c_int, _c.c_float, _c.c_void_p,
+                                _c.c_void_p, _c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p]),
+    "gp_log_probs_grad": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int, _c.c_int64, _c.c_int32, _c.c_void_p, _c.c_int, _c.c_float, _c.c_void_p,
+                                     _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_void_p]),
+    "gp_distill_workspace": (_c.c_int64, [_c.c_int64, _c.c_int32]),
+    "gp_distill": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int, _c.c_int64, _c.c_int32, _c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p,
+                              _c.c_int64, _c.c_int, _c.c_int32, _c.c_float, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p,
+                              _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_void_p]),
+    "gp_distill_grad": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int, _c.c_int64, _c.c_int32, _c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p,
+                                   _c.c_int64, _c.c_int, _c.c_int32, _c.c_float, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p,
+                                   _c.c_int64, _c.c_void_p]),
     "gp_solve_normalisation_blocks": (_c.c_int, [_c.c_double] * 7 + [_c.POINTER(_c.c_int64)]),
     "gp_solve_aggregation_blocks": (_c.c_int, [_c.c_double] * 5 + [_c.c_int64, _c.POINTER(_c.c_int64),
                                                                   _c.POINTER(_c.c_int64)]),
@@ -709,6 +727,451 @@ def muon_step_tensors(W, M, G, lr, momentum=0.95, weight_decay=0.0, nesterov=Tru
         gp_muon_step(W.data_ptr(), W_out.data_ptr(), ldw, sw, M.data_ptr(), M_out.data_ptr(), ldm, sm, G.data_ptr(), ldg, sg, dtype, rows,
                      cols, count, lr, momentum, weight_decay, nesterov, steps, coeff, eps, ws.data_ptr(), ws.numel(), handle)
     return W_out, M_out
+
+
+def gp_layer_norm(x_ptr: int, ldx: int, dtype: int, N: int, d: int, weight_ptr: Optional[int], bias_ptr: Optional[int], weight_dtype: int,
+                  eps: float, y_ptr: int, ldy: int, out_dtype: int, stats_ptr: Optional[int] = None, stream: Optional[int] = None):
+    """Raw-pointer form: y = (x - mean) / sqrt(variance + eps) * weight + bias row by row; all addresses are device addresses."""
+    st = lib().gp_layer_norm(x_ptr or None, ldx, dtype, N, d, weight_ptr or None, bias_ptr or None, weight_dtype, eps, y_ptr or None, ldy,
+                             out_dtype, stats_ptr or None, stream or None)
+    _check(st, "gp_layer_norm")
+
+
+def gp_layer_norm_grad_workspace(N: int, d: int) -> int:
+    return lib().gp_layer_norm_grad_workspace(N, d)
+
+
+def gp_layer_norm_grad(grad_ptr: int, ldg: int, grad_dtype: int, x_ptr: int, ldx: int, dtype: int, N: int, d: int, stats_ptr: int,
+                       weight_ptr: Optional[int], weight_dtype: int, x_grad_ptr: Optional[int], ldxg: int, weight_grad_ptr: Optional[int],
+                       bias_grad_ptr: Optional[int], accumulate: bool, workspace_ptr: int, workspace_bytes: int, stream: Optional[int] = None):
+    """Raw-pointer form of the gradients of gp_layer_norm; all addresses are device addresses."""
+    st = lib().gp_layer_norm_grad(grad_ptr or None, ldg, grad_dtype, x_ptr or None, ldx, dtype, N, d, stats_ptr or None, weight_ptr or None,
+                                  weight_dtype, x_grad_ptr or None, ldxg, weight_grad_ptr or None, bias_grad_ptr or None, int(accumulate),
+                                  workspace_ptr or None, workspace_bytes, stream or None)
+    _check(st, "gp_layer_norm_grad")
+
+
+def gp_log_probs_workspace(N: int, C: int, k: int = 0) -> int:
+    return lib().gp_log_probs_workspace(N, C, k)
+
+
+def gp_log_probs(logits_ptr: int, ld: int, dtype: int, N: int, C: int, tokens_ptr: Optional[int], index: int, scale: float,
+                 logp_ptr: Optional[int], entropy_ptr: Optional[int], k: int, top_index_ptr: Optional[int], top_logp_ptr: Optional[int],
+                 stats_ptr: Optional[int], workspace_ptr: Optional[int], workspace_bytes: int, stream: Optional[int] = None):
+    """Raw-pointer form; all addresses are device addresses."""
+    st = lib().gp_log_probs(logits_ptr or None, ld, dtype, N, C, tokens_ptr or None, index, scale, logp_ptr or None, entropy_ptr or None, k,
+                            top_index_ptr or None, top_logp_ptr or None, stats_ptr or None, workspace_ptr or None, workspace_bytes,
+                            stream or None)
+    _check(st, "gp_log_probs")
+
+
+def gp_log_probs_grad(logits_ptr: int, ld: int, dtype: int, N: int, C: int, tokens_ptr: Optional[int], index: int, scale: float,
+                      stats_ptr: int, entropy_ptr: Optional[int], grad_logp_ptr: Optional[int], stride_logp: int,
+                      grad_entropy_ptr: Optional[int], stride_entropy: int, grad_ptr: int, ldg: int, stream: Optional[int] = None):
+    """Raw-pointer form of the gradient of gp_log_probs; all addresses are device addresses."""
+    st = lib().gp_log_probs_grad(logits_ptr or None, ld, dtype, N, C, tokens_ptr or None, index, scale, stats_ptr or None, entropy_ptr or None,
+                                 grad_logp_ptr or None, stride_logp, grad_entropy_ptr or None, stride_entropy, grad_ptr or None, ldg,
+                                 stream or None)
+    _check(st, "gp_log_probs_grad")
+
+
+def gp_distill_workspace(N: int, C: int) -> int:
+    return lib().gp_distill_workspace(N, C)
+
+
+def gp_distill(logits_ptr: int, ld: int, dtype: int, N: int, C: int, teacher_index_ptr: int, ldi: int, index: int, teacher_logits_ptr: int,
+               ldt: int, teacher_dtype: int, K: int, temperature: float, loss_ptr: Optional[int], stats_ptr: Optional[int],
+               grad_loss_ptr: Optional[int], stride_loss: int, grad_ptr: Optional[int], ldg: int, workspace_ptr: Optional[int],
+               workspace_bytes: int, stream: Optional[int] = None):
+    """Raw-pointer form; all addresses are device addresses."""
+    st = lib().gp_distill(logits_ptr or None, ld, dtype, N, C, teacher_index_ptr or None, ldi, index, teacher_logits_ptr or None, ldt,
+                          teacher_dtype, K, temperature, loss_ptr or None, stats_ptr or None, grad_loss_ptr or None, stride_loss,
+                          grad_ptr or None, ldg, workspace_ptr or None, workspace_bytes, stream or None)
+    _check(st, "gp_distill")
+
+
+def gp_distill_grad(logits_ptr: int, ld: int, dtype: int, N: int, C: int, teacher_index_ptr: int, ldi: int, index: int,
+                    teacher_logits_ptr: int, ldt: int, teacher_dtype: int, K: int, temperature: float, stats_ptr: int, grad_loss_ptr: int,
+                    stride_loss: int, grad_ptr: int, ldg: int, stream: Optional[int] = None):
+    """Raw-pointer form of the gradient of gp_distill from the stats that it left; all addresses are device addresses."""
+    st = lib().gp_distill_grad(logits_ptr or None, ld, dtype, N, C, teacher_index_ptr or None, ldi, index, teacher_logits_ptr or None, ldt,
+                               teacher_dtype, K, temperature, stats_ptr or None, grad_loss_ptr or None, stride_loss, grad_ptr or None, ldg,
+                               stream or None)
+    _check(st, "gp_distill_grad")
+
+
+def _followed(t, stream):
+    """Whether automatic differentiation is to follow a call on t.  Its backward pass runs on the stream that is current at the call, and may meet
+    leaves that a graph outside a capture has as well, which ends the process: so neither another stream nor a capture goes with it."""
+    import torch
+    if t is None or not (t.requires_grad and torch.is_grad_enabled()):
+        return False
+    if stream is not None:
+        raise ValueError("a call that automatic differentiation follows runs on the current stream: set that one")
+    if torch.cuda.is_current_stream_capturing():
+        raise ValueError("a call that automatic differentiation follows is not captured: capture it under torch.no_grad(), and the gradient's own call")
+    return True
+
+
+def _as_rows(t, what):
+    """A (rows, width) view of a tensor whose last dimension is a row: any distance of rows in two dimensions, contiguous in others."""
+    if t.dim() == 2:
+        return t
+    if t.dim() == 0 or not t.is_contiguous() or t.shape[-1] == 0:
+        raise ValueError(f"{what} of other than two dimensions must be contiguous, its last dimension a row")
+    return t.view(-1, t.shape[-1])
+
+
+def _rows_for(t, shape, dtype, what):
+    """(view, distance of rows) of a tensor that rows are written to: of `shape`, or two-dimensional with as many rows."""
+    N = 1
+    for n in shape[:-1]:
+        N *= n
+    if (tuple(t.shape) != tuple(shape) and tuple(t.shape) != (N, shape[-1])) or t.dtype != dtype:
+        raise ValueError(f"{what} must be of the rows' shape and of the right type")
+    t = _as_rows(t, what)
+    return t, _row_stride(t, what)
+
+
+def _vector(t, n, what):
+    if t is not None and (t.dim() != 1 or t.shape[0] != n or not t.is_contiguous()):
+        raise ValueError(f"{what} must be a contiguous vector, one value per column")
+
+
+def _row_stats(stats, N):
+    import torch
+    if stats is not None and (stats.dtype != torch.float32 or tuple(stats.shape) != (N, 2) or not stats.is_contiguous()):
+        raise ValueError("stats must be a contiguous (rows, 2) float32 tensor")
+
+
+def _per_row(t, N, what):
+    """(tensor, distance of its elements) of a float32 value per row, or of one that stands for all rows."""
+    import torch
+    if t is None:
+        return None, 0
+    if t.dtype != torch.float32:
+        raise ValueError(f"{what} must be float32")
+    if t.numel() == 1 or (t.numel() == N and not any(t.stride()) and N > 0):
+        return t, 0
+    if t.numel() != N or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous, one value per row, or one for all")
+    return t, 1
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+@functools.lru_cache(maxsize=None)
+def _differentiable_norm():
+    import torch
+
+    class Norm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, eps, out_dtype):
+            stats = torch.empty((x.numel() // max(x.shape[-1], 1), 2), dtype=torch.float32, device=x.device)
+            y = layer_norm_tensors(x, weight, bias, eps, out_dtype=out_dtype, stats=stats)
+            ctx.save_for_backward(x, weight, stats)
+            ctx.weight_dtype = None if weight is None and bias is None else (bias if weight is None else weight).dtype
+            return y
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, grad):
+            x, weight, stats = ctx.saved_tensors
+            want = ctx.needs_input_grad
+            rows = grad.reshape(-1, x.shape[-1])
+            if (rows.shape[1] > 1 and rows.stride(1) != 1) or 0 < rows.stride(0) < rows.shape[1]:  # (a sum's gradient is one number, expanded)
+                rows = rows.contiguous()
+            x_grad, weight_grad, bias_grad = layer_norm_grad_tensors(rows, _as_rows(x, "x"), stats, weight, x_grad=None if want[0] else False,
+                                                                     weight_grad=None if want[1] else False, bias_grad=None if want[2] else False,
+                                                                     weight_dtype=ctx.weight_dtype)
+            return None if x_grad is None else x_grad.view(x.shape), weight_grad, bias_grad, None, None
+
+    return Norm
+
+
+def layer_norm_tensors(x, weight=None, bias=None, eps=1e-5, out=None, out_dtype=None, stats=None, stream=None):
+    """Convenience for torch tensors: x is a float32 / bfloat16 GPU tensor whose last dimension is normalised (any distance of rows in two dimensions,
+    contiguous in others), weight and bias vectors of float32 or bfloat16 (both of one type) or None.  Returns the normalised rows, of x's shape,
+    in out_dtype (x's unless given); out: a tensor of that shape, filled and returned (x itself will do).  stats: a (rows, 2) float32 tensor that
+    receives what layer_norm_grad_tensors needs.  Where x, weight or bias require a gradient, the result does too (not with out, stats or a stream of
+    its own, nor in a capture)."""
+    import torch
+    if out is None and stats is None and (_followed(x, stream) or _followed(weight, stream) or _followed(bias, stream)):
+        return _differentiable_norm().apply(x, weight, bias, eps, out_dtype)
+    dtype, rows = _float_type(x), _as_rows(x, "x")
+    N, d = rows.shape
+    ldx = _row_stride(rows, "x")
+    _vector(weight, d, "weight")
+    _vector(bias, d, "bias")
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise ValueError("weight and bias must be of one type")
+    kind = weight if weight is not None else bias
+    weight_dtype = GP_F32 if kind is None else _float_type(kind)
+    _row_stats(stats, N)
+    if out is not None:
+        to, ldy = _rows_for(out, x.shape, out_dtype or out.dtype, "out")
+    _one_device(x, weight, bias, out, stats)
+    with _on_stream(x, stream) as handle:
+        if out is None:
+            out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
+            to, ldy = out, d
+        else:
+            _written(out)
+        if stats is not None:
+            _written(stats)
+        gp_layer_norm(x.data_ptr(), ldx, dtype, N, d, _ptr(weight), _ptr(bias), weight_dtype, eps, to.data_ptr(), ldy, _float_type(out), _ptr(stats),
+                      handle)
+    return out
+
+
+def layer_norm_grad_tensors(grad, x, stats, weight=None, x_grad=None, weight_grad=None, bias_grad=None, accumulate=False, weight_dtype=None,
+                            workspace=None, stream=None):
+    """Convenience for torch tensors: the gradients of layer_norm_tensors from grad, the gradient of what it returned, and the stats it left.  Returns
+    (x_grad, weight_grad, bias_grad): each is made where None is given, filled where a tensor is, left out (None) where False is.  accumulate: weight_grad
+    and bias_grad are added to (both given, or False).  weight_dtype: of the gradients that are made (weight's; float32 without one).  workspace: a uint8
+    GPU tensor of gp_layer_norm_grad_workspace(rows, d) bytes or more, kept by the caller; without one the call takes its memory from torch."""
+    import torch
+    dtype, grad_dtype = _float_type(x), _float_type(grad)
+    rows, up = _as_rows(x, "x"), _as_rows(grad, "grad")
+    if rows.shape != up.shape:
+        raise ValueError("grad must be of x's shape")
+    N, d = rows.shape
+    ldx = _row_stride(rows, "x")
+    ldg = _row_stride(up, "grad")
+    _row_stats(stats, N)
+    if stats is None:
+        raise ValueError("stats are needed")
+    _vector(weight, d, "weight")
+    given = [t for t in (weight, weight_grad, bias_grad) if t is not None and t is not False]
+    weight_dtype = weight_dtype or (given[0].dtype if given else torch.float32)
+    if any(t.dtype != weight_dtype for t in given):
+        raise ValueError("weight and the gradients of weight and bias must be of one type")
+    if accumulate and (weight_grad is None or bias_grad is None):
+        raise ValueError("accumulate needs tensors to add to")
+    for t, what in ((weight_grad, "weight_grad"), (bias_grad, "bias_grad")):
+        if t is not False:
+            _vector(t, d, what)
+    if x_grad is not None and x_grad is not False:
+        to, ldxg = _rows_for(x_grad, x.shape, x.dtype, "x_grad")
+    outs = [None if t is False else t for t in (x_grad, weight_grad, bias_grad)]
+    _one_device(x, grad, stats, weight, workspace, *outs)
+    with _on_stream(x, stream) as handle:
+        written = [t for t in outs if t is not None]
+        if written:
+            _written(*written)
+        if x_grad is None:
+            x_grad = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            to, ldxg = x_grad, d
+        elif x_grad is False:
+            x_grad, to, ldxg = None, None, d
+        weight_grad, bias_grad = (torch.empty(d, dtype=weight_dtype, device=x.device) if t is None else None if t is False else t
+                                  for t in (weight_grad, bias_grad))
+        ws = _workspace(workspace, gp_layer_norm_grad_workspace(N, d), x.device)
+        kind = _types()[0].get(weight_dtype, -1)
+        gp_layer_norm_grad(up.data_ptr(), ldg, grad_dtype, rows.data_ptr(), ldx, dtype, N, d, stats.data_ptr(), _ptr(weight), kind, _ptr(to), ldxg,
+                           _ptr(weight_grad), _ptr(bias_grad), accumulate, ws.data_ptr(), ws.numel(), handle)
+    return x_grad, weight_grad, bias_grad
+
+
+class LogProbs(NamedTuple):
+    """What log_probs_tensors returns; None in the place of what was not asked for."""
+    logp: Any
+    entropy: Any
+    top_index: Any
+    top_logp: Any
+
+
+def _rows_of_logits(logits, tokens):
+    rows = _as_rows(logits, "logits")
+    if tokens is not None and tuple(tokens.shape) != tuple(logits.shape[:-1]):
+        raise ValueError("tokens must hold one class per row")
+    return rows, _row_stride(rows, "logits")
+
+
+@functools.lru_cache(maxsize=None)
+def _differentiable_log_probs():
+    import torch
+
+    class Answers(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, logits, tokens, scale, top, entropy):
+            stats = torch.empty((logits.numel() // max(logits.shape[-1], 1), 2), dtype=torch.float32, device=logits.device)
+            a = log_probs_tensors(logits, tokens, scale, top, entropy, stats=stats)
+            ctx.save_for_backward(logits, tokens, stats, a.entropy)
+            ctx.scale = scale
+            if top:
+                ctx.mark_non_differentiable(a.top_index, a.top_logp)
+            ctx.set_materialize_grads(False)
+            return tuple(a)
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, grad_logp, grad_entropy, _index, _top):
+            logits, tokens, stats, entropy = ctx.saved_tensors
+            grads = [None if g is None else g if g.is_contiguous() or not any(g.stride()) else g.contiguous() for g in (grad_logp, grad_entropy)]
+            return log_probs_grad_tensors(logits, tokens, stats, ctx.scale, entropy, *grads), None, None, None, None
+
+    return Answers
+
+
+def log_probs_tensors(logits, tokens=None, scale=1.0, top=0, entropy=True, stats=None, workspace=None, stream=None):
+    """Convenience for torch tensors: logits is a float32 / bfloat16 GPU tensor whose last dimension holds the classes (any distance of rows in two
+    dimensions, contiguous in others), tokens an int32 / int64 GPU tensor of one class per row.  Returns LogProbs(logp, entropy, top_index, top_logp)
+    of scale * logits: the tokens' log probabilities (0 where a token is outside the classes), the rows' entropies, and the `top` (up to 64) best
+    classes (int32) with their log probabilities; ties go to the lower class.  stats: a (rows, 2) float32 tensor that receives what
+    log_probs_grad_tensors needs.  workspace: a uint8 GPU tensor of gp_log_probs_workspace(rows, classes, top) bytes or more, kept by the caller.  Where
+    logits require a gradient, logp and entropy do too (not with stats or a stream of its own, nor in a capture)."""
+    import torch
+    if stats is None and _followed(logits, stream):
+        return LogProbs(*_differentiable_log_probs().apply(logits, tokens, scale, top, entropy))
+    dtype, index = _float_type(logits), GP_I32 if tokens is None else _index_type(tokens)
+    rows, ld = _rows_of_logits(logits, tokens)
+    N, C = rows.shape
+    _row_stats(stats, N)
+    if top < 0:
+        raise ValueError("top must be 0 or more")
+    _one_device(logits, tokens, stats, workspace)
+    with _on_stream(logits, stream) as handle:
+        if stats is not None:
+            _written(stats)
+        shape = tuple(logits.shape[:-1])
+        logp = None if tokens is None else torch.empty(shape, dtype=torch.float32, device=logits.device)
+        spread = torch.empty(shape, dtype=torch.float32, device=logits.device) if entropy else None
+        best = torch.empty(shape + (top,), dtype=torch.int32, device=logits.device) if top else None
+        best_logp = torch.empty(shape + (top,), dtype=torch.float32, device=logits.device) if top else None
+        need = gp_log_probs_workspace(N, C, top)
+        ws = _workspace(workspace, need, logits.device) if need > 0 else None
+        gp_log_probs(rows.data_ptr(), ld, dtype, N, C, _ptr(tokens), index, scale, _ptr(logp), _ptr(spread), top, _ptr(best), _ptr(best_logp),
+                     _ptr(stats), _ptr(ws), 0 if ws is None else ws.numel(), handle)
+    return LogProbs(logp, spread, best, best_logp)
+
+
+def log_probs_grad_tensors(logits, tokens, stats, scale=1.0, entropy=None, grad_logp=None, grad_entropy=None, out=None, stream=None):
+    """Convenience for torch tensors: the gradient of log_probs_tensors with respect to its logits, from the stats (and, for grad_entropy, the entropy) it left.
+    grad_logp, grad_entropy: float32, one value per row or one for all, or None.  Returns out, of logits' shape and type (made if not given)."""
+    import torch
+    dtype, index = _float_type(logits), GP_I32 if tokens is None else _index_type(tokens)
+    rows, ld = _rows_of_logits(logits, tokens)
+    N, C = rows.shape
+    if stats is None:
+        raise ValueError("stats are needed")
+    _row_stats(stats, N)
+    grad_logp, s1 = _per_row(grad_logp, N, "grad_logp")
+    grad_entropy, s2 = _per_row(grad_entropy, N, "grad_entropy")
+    if grad_entropy is not None and (entropy is None or _per_row(entropy, N, "entropy")[1] != (1 if N != 1 else 0)):
+        raise ValueError("the entropies are needed, one per row")
+    if grad_logp is not None and tokens is None:
+        raise ValueError("tokens are needed")
+    if out is not None:
+        to, ldg = _rows_for(out, logits.shape, logits.dtype, "out")
+    _one_device(logits, tokens, stats, entropy, grad_logp, grad_entropy, out)
+    with _on_stream(logits, stream) as handle:
+        if out is None:
+            out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+            to, ldg = out, C
+        else:
+            _written(out)
+        gp_log_probs_grad(rows.data_ptr(), ld, dtype, N, C, _ptr(tokens), index, scale, stats.data_ptr(), _ptr(entropy), _ptr(grad_logp), s1,
+                          _ptr(grad_entropy), s2, to.data_ptr(), ldg, handle)
+    return out
+
+
+def _teacher(logits, teacher_index, teacher_logits):
+    """(address, distance of rows, type) of a teacher's classes and of their logits, and the entries of a row."""
+    if tuple(teacher_index.shape[:-1]) != tuple(logits.shape[:-1]) or teacher_index.shape != teacher_logits.shape:
+        raise ValueError("teacher_index and teacher_logits must be of one shape, with a row for every row of logits")
+    index = _types()[1].get(teacher_index.dtype)
+    if index is None:
+        raise ValueError("teacher_index must be int32 or int64")
+    at, values = _as_rows(teacher_index, "teacher_index"), _as_rows(teacher_logits, "teacher_logits")
+    return (at.data_ptr(), _row_stride(at, "teacher_index"), index, values.data_ptr(), _row_stride(values, "teacher_logits"),
+            _float_type(teacher_logits), at.shape[1])
+
+
+@functools.lru_cache(maxsize=None)
+def _differentiable_distill():
+    import torch
+
+    class Distill(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, logits, teacher_index, teacher_logits, temperature):
+            stats = torch.empty((logits.numel() // max(logits.shape[-1], 1), 2), dtype=torch.float32, device=logits.device)
+            loss = distill_tensors(logits, teacher_index, teacher_logits, temperature, stats=stats)
+            ctx.save_for_backward(logits, teacher_index, teacher_logits, stats)
+            ctx.temperature = temperature
+            return loss
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, grad):
+            logits, teacher_index, teacher_logits, stats = ctx.saved_tensors
+            grad = grad if grad.is_contiguous() or not any(grad.stride()) else grad.contiguous()
+            return distill_grad_tensors(logits, teacher_index, teacher_logits, stats, grad, ctx.temperature), None, None, None
+
+    return Distill
+
+
+def distill_tensors(logits, teacher_index, teacher_logits, temperature=1.0, grad_loss=None, out=None, stats=None, workspace=None, stream=None):
+    """Convenience for torch tensors: the loss of every row of logits (as log_probs_tensors takes them) against a teacher's best classes and their logits, each
+    one row of up to 64 per row of logits (int32 / int64, -1 for none, and float32 / bfloat16: log_probs_tensors' top_index and top_logp will do).  Returns the
+    float32 losses, of logits.shape[:-1]; with grad_loss (float32, one value per row or one for all) the gradient of the logits is made in the same
+    pass and (loss, gradient) returned, the gradient in out where that is given.  stats: a (rows, 2) float32 tensor that receives what
+    distill_grad_tensors needs.  workspace: a uint8 GPU tensor of gp_distill_workspace(rows, classes) bytes or more, kept by the caller.  Where logits
+    require a gradient, the loss does too (not with grad_loss, stats or a stream of its own, nor in a capture); the teacher gets none."""
+    import torch
+    if stats is None and grad_loss is None and _followed(logits, stream):
+        return _differentiable_distill().apply(logits, teacher_index, teacher_logits, temperature)
+    dtype = _float_type(logits)
+    rows, ld = _rows_of_logits(logits, None)
+    N, C = rows.shape
+    at, ldi, index, values, ldt, teacher_dtype, K = _teacher(logits, teacher_index, teacher_logits)
+    _row_stats(stats, N)
+    if out is not None and grad_loss is None:
+        raise ValueError("out takes a gradient, which needs grad_loss")
+    grad_loss, stride = _per_row(grad_loss, N, "grad_loss")
+    to, ldg = (None, C) if out is None else _rows_for(out, logits.shape, logits.dtype, "out")
+    _one_device(logits, teacher_index, teacher_logits, grad_loss, out, stats, workspace)
+    with _on_stream(logits, stream) as handle:
+        loss = torch.empty(tuple(logits.shape[:-1]), dtype=torch.float32, device=logits.device)
+        if out is not None:
+            _written(out)
+        elif grad_loss is not None:
+            to = out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        if stats is not None:
+            _written(stats)
+        need = gp_distill_workspace(N, C)
+        ws = _workspace(workspace, need, logits.device) if need > 0 else None
+        gp_distill(rows.data_ptr(), ld, dtype, N, C, at, ldi, index, values, ldt, teacher_dtype, K, temperature, loss.data_ptr(), _ptr(stats),
+                   _ptr(grad_loss), stride, _ptr(to), ldg, _ptr(ws), 0 if ws is None else ws.numel(), handle)
+    return loss if grad_loss is None else (loss, out)
+
+
+def distill_grad_tensors(logits, teacher_index, teacher_logits, stats, grad_loss, temperature=1.0, out=None, stream=None):
+    """Convenience for torch tensors: the gradient of distill_tensors with respect to its logits, from the stats it left and grad_loss, the gradient of the
+    losses (float32, one value per row or one for all).  Returns out, of logits' shape and type (made if not given)."""
+    import torch
+    dtype = _float_type(logits)
+    rows, ld = _rows_of_logits(logits, None)
+    N, C = rows.shape
+    at, ldi, index, values, ldt, teacher_dtype, K = _teacher(logits, teacher_index, teacher_logits)
+    if stats is None or grad_loss is None:
+        raise ValueError("stats and grad_loss are needed")
+    _row_stats(stats, N)
+    grad_loss, stride = _per_row(grad_loss, N, "grad_loss")
+    if out is not None:
+        to, ldg = _rows_for(out, logits.shape, logits.dtype, "out")
+    _one_device(logits, teacher_index, teacher_logits, stats, grad_loss, out)
+    with _on_stream(logits, stream) as handle:
+        if out is None:
+            out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+            to, ldg = out, C
+        else:
+            _written(out)
+        gp_distill_grad(rows.data_ptr(), ld, dtype, N, C, at, ldi, index, values, ldt, teacher_dtype, K, temperature, stats.data_ptr(),
+                        grad_loss.data_ptr(), stride, to.data_ptr(), ldg, handle)
+    return out
 
 
 def gp_solve_normalisation_blocks(B_A, B_S, B_D, B_GPU, alpha_A=1.0, alpha_S=1.0, alpha_D=1.0) -> int:

@@ -19,70 +19,15 @@
 // sums, and the call (4,096 rows of 128 into 10,000, 12 us, 8.5 of them on the GPU; gp_sum_short).
 #include <algorithm>
 #include <exception>
-#include <type_traits>
 
 #include "gp_internal.h"
+#include "gp_rows.h"
 
 namespace gp {
 
 namespace {
 
 constexpr int kThreads = 256;
-
-typedef unsigned short bf16_t;
-
-__device__ __forceinline__ float widen(float v) { return v; }
-__device__ __forceinline__ float widen(bf16_t v) { return __uint_as_float((unsigned)v << 16); }
-template <typename T>
-__device__ __forceinline__ T narrow(float v)
-{
-    if constexpr (std::is_same<T, float>::value)
-        return v;
-    else
-        return __builtin_bit_cast(bf16_t, (__bf16)v);  // to nearest even
-}
-
-// N elements from or to any element's boundary: gfx950 loads and stores vectors from there in one request
-template <typename T, int N>
-struct Vec {
-    typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-};
-template <typename T>
-struct Vec<T, 1> {
-    typedef T type;
-};
-// element i of one, widened
-template <typename T, int N>
-__device__ __forceinline__ float element(const typename Vec<T, N>::type& x, int i)
-{
-    if constexpr (N == 1)
-        return widen(x);
-    else
-        return widen(x[i]);
-}
-template <typename T, int N>
-__device__ __forceinline__ void load_vec(const T* p, float (&v)[N])
-{
-    if constexpr (N == 1) {
-        v[0] = widen(*p);
-    } else {
-        const typename Vec<T, N>::type x = *reinterpret_cast<const typename Vec<T, N>::type*>(p);
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = widen(x[i]);
-    }
-}
-template <typename T, int N>
-__device__ __forceinline__ void store_vec(T* p, const float (&v)[N])
-{
-    if constexpr (N == 1) {
-        *p = narrow<T>(v[0]);
-    } else {
-        typename Vec<T, N>::type x;
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = narrow<T>(v[i]);
-        *reinterpret_cast<typename Vec<T, N>::type*>(p) = x;
-    }
-}
 
 // ---- lookup -----------------------------------------------------------------------------------------
 
@@ -97,11 +42,6 @@ struct LookupArgs {
     void* out;
     int64_t ldo;
 };
-
-__device__ __forceinline__ int64_t token_at(const void* tokens, int wide, int64_t i)
-{
-    return wide ? ((const int64_t*)tokens)[i] : (int64_t)((const int32_t*)tokens)[i];
-}
 
 // One vector per thread and step, four steps' requests at once.  A row's last vector is moved back to end with the row (what
 // it repeats is written twice, identically).

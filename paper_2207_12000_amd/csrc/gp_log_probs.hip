@@ -1,0 +1,1248 @@
+// What rows of logits say, and what they learn from: log probabilities with entropies and alternatives, and a teacher's best logits, with their gradients.
+//
+//   answers   z = s x,  log p_j = z_j - log(sum exp z),  entropy = -sum p log p,  the k largest x
+//   gradient  dx_j = s (g1 ([j = token] - p_j) - g2 p_j (log p_j + entropy))
+//   distill   q = softmax(v / T) over a teacher's entries,  loss = T^2 sum q (log q - log p),  dx_j = g T (p_j - sum of q over entries that name j)
+//
+// With m the row's largest logit everything is a function of (x_j - m): sums are of exp(s (x_j - m)), which are at most 1, and log p_j is
+// s (x_j - m) - log(sum), so that large logits cost no bits.  (m, log(sum)) are what a row's gradient needs.  A row whose logits are all -inf
+// keeps (0, 0): every p is 0 and every log p is -inf, without a case of its own.
+//
+// All are bound by memory: a row is read once, into the registers of a team of lanes, and where the gradient is asked for along with the
+// loss it is written from there.  Rows that 1,024 lanes cannot hold, and few long rows, are cut into parts, a workgroup each, whose
+// results a second launch joins.
+//
+// Alternatives.  A logit and its class make one whole number (key_of), larger logits and then lower classes first, so no two are equal.  Teams of part of a
+// wavefront keep sorted lists in registers, into which every key is sorted by maxima and minima, and merge them.  Teams of a wavefront or more
+// compare with a bound instead: the k-th largest of 64 groups' maxima is no larger than the k-th largest logit, and few others
+// reach it (8.5 for 8, 44 for 32, 300 for 64, in any order that does not follow the groups); these are listed in LDS and ranked by counting.
+// Where more reach it than the list has room for, as in rows of equal logits, the largest key below the last is looked for k times.
+#include <algorithm>
+#include <exception>
+
+#include "gp_internal.h"
+#include "gp_rows.h"
+
+namespace gp {
+
+namespace {
+
+constexpr int kMostTop = 64;      // alternatives, and entries of a teacher: one to a lane of a wavefront
+constexpr int kIndexBits = 28;    // of a class in a key
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr int kRoom = 1024;       // keys that a workgroup's list has room for (a wavefront's: a quarter)
+
+struct AnswerArgs {
+    const void* x;
+    int64_t ld, N;
+    int C, nvec;
+    const void* tokens;
+    int wide;
+    float scale;
+    float *logp, *entropy, *stats;
+    int k;
+    int32_t* top_index;
+    float* top_logp;
+    int parts;      // of a row; more than one: results go to `partial`
+    float* partial;  // [N][parts][4]: largest, sum of exp, sum of z exp; then [N][parts][k] keys
+    uint64_t* keys;
+};
+
+__device__ __forceinline__ float infinity() { return __builtin_inff(); }
+
+// max of floats that are no NaN's business: what is larger by the instruction (NaN is passed over)
+__device__ __forceinline__ float larger(float a, float b)
+{
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+template <int W>
+__device__ __forceinline__ float team_largest(float v)
+{
+    return team<W>(v, [](float a, float b) { return larger(a, b); });
+}
+
+// Larger logits first (NaN above infinity, 0 and -0 the same), lower classes among equals.  60 bits: as a double a positive number, whose order is theirs.
+__device__ __forceinline__ uint64_t key_of(float x, int j)
+{
+    const unsigned b = __float_as_uint(x + 0.0f);
+    const unsigned o = x != x ? 0xFFFFFFFFu : b ^ ((unsigned)((int)b >> 31) | 0x80000000u);
+    return ((uint64_t)o << kIndexBits) | (uint64_t)((1u << kIndexBits) - 1 - j);
+}
+__device__ __forceinline__ float logit_of(uint64_t key)
+{
+    const unsigned o = (unsigned)(key >> kIndexBits);
+    return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);  // (NaN gives NaN)
+}
+__device__ __forceinline__ int class_of(uint64_t key) { return (int)((1u << kIndexBits) - 1 - (unsigned)(key & ((1u << kIndexBits) - 1))); }
+__device__ __forceinline__ uint64_t key_max(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t key_min(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t shuffled(uint64_t v, int mask)
+{
+    return ((uint64_t)(unsigned)__shfl_xor((int)(v >> 32), mask, 64) << 32) | (unsigned)__shfl_xor((int)v, mask, 64);
+}
+template <int CTRL>
+__device__ __forceinline__ uint64_t moved_key(uint64_t v)
+{
+    return ((uint64_t)moved<CTRL>((unsigned)(v >> 32)) << 32) | moved<CTRL>((unsigned)v);
+}
+
+// What a row's numbers come to.  m: the largest logit, total: the sum of exp(s (x - m)), weighted: the sum of s (x - m) times that.
+struct RowSums {
+    float m, total, weighted;
+    __device__ __forceinline__ bool none() const { return total == 0.0f; }  // (every logit is -inf)
+    __device__ __forceinline__ float log_total() const { return none() ? 0.0f : logf(total); }
+    __device__ __forceinline__ float entropy() const { return none() ? 0.0f : logf(total) - weighted / total; }
+};
+__device__ __forceinline__ float base_of(float m) { return m == -infinity() ? 0.0f : m; }
+
+__device__ __forceinline__ void write_top(const AnswerArgs& a, int64_t row, int place, uint64_t key, float base, float log_total)
+{
+    const float x = key ? logit_of(key) : -infinity();
+    const bool none = x == -infinity();
+    a.top_index[row * a.k + place] = none ? -1 : class_of(key);
+    a.top_logp[row * a.k + place] = none ? -infinity() : (x - base) * a.scale - log_total;
+}
+__device__ __forceinline__ void write_row(const AnswerArgs& a, int64_t row, int64_t token, float logit, float base, const RowSums& s)
+{
+    const float l = s.log_total();
+    if (a.logp) a.logp[row] = token >= 0 && token < a.C ? (logit - base) * a.scale - l : 0.0f;
+    if (a.entropy) a.entropy[row] = s.entropy();
+    if (a.stats) a.stats[2 * row] = base, a.stats[2 * row + 1] = l;
+}
+
+// A row's part in a team's registers: vector t = v * TPR + lane starts at column t * VEC, the last one is moved back to end with the part; what
+// it repeats and what no vector holds is -inf.  (Teams within a wavefront take as few vectors as hold a row, so only the last can be such.)
+template <typename T, int VEC, int NV, int TPR>
+__device__ __forceinline__ void load_row(const T* x, int len, int nvec, int lane, float (&e)[NV][VEC], int (&col)[NV])
+{
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int t = v * TPR + lane;
+        col[v] = min(t, nvec - 1) * VEC;
+        col[v] = min(col[v], len - VEC);
+        load_vec<T, VEC>(x + col[v], e[v]);
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        if (TPR < 64 && v < NV - 1) continue;
+        if (TPR >= 64 && __builtin_amdgcn_readfirstlane(v * TPR + (int)(lane & ~63)) + 64 < nvec) continue;
+        const int t = v * TPR + lane;
+        const int first = t < nvec ? t * VEC - col[v] : VEC;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (i < first) e[v][i] = -infinity();
+    }
+}
+
+// A list of K keys, largest first, and one more
+template <int K>
+__device__ __forceinline__ void sort_in(uint64_t (&list)[K], uint64_t key)
+{
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        const uint64_t low = key_min(list[i], key);
+        list[i] = key_max(list[i], key);
+        key = low;
+    }
+}
+// The K largest of two lists, sorted: their maxima crosswise, put in order by neighbours.
+template <int K>
+__device__ __forceinline__ void merge(uint64_t (&list)[K], const uint64_t (&other)[K])
+{
+#pragma unroll
+    for (int i = 0; i < K; ++i) list[i] = key_max(list[i], other[K - 1 - i]);
+#pragma unroll
+    for (int n = 0; n < K * (K - 1); ++n) {
+        const int round = n / (K - 1), i = n % (K - 1);
+        if ((i ^ round) & 1) continue;
+        const uint64_t hi = key_max(list[i], list[i + 1]);
+        list[i + 1] = key_min(list[i], list[i + 1]);
+        list[i] = hi;
+    }
+}
+template <int W, int K>
+__device__ __forceinline__ void team_merge(uint64_t (&list)[K])
+{
+    uint64_t other[K];
+    if constexpr (W >= 2) {
+#pragma unroll
+        for (int i = 0; i < K; ++i) other[i] = moved_key<0xB1>(list[i]);
+        merge<K>(list, other);
+    }
+    if constexpr (W >= 4) {
+#pragma unroll
+        for (int i = 0; i < K; ++i) other[i] = moved_key<0x4E>(list[i]);
+        merge<K>(list, other);
+    }
+    if constexpr (W >= 8) {
+#pragma unroll
+        for (int i = 0; i < K; ++i) other[i] = moved_key<0x141>(list[i]);
+        merge<K>(list, other);
+    }
+    if constexpr (W >= 16) {
+#pragma unroll
+        for (int i = 0; i < K; ++i) other[i] = moved_key<0x140>(list[i]);
+        merge<K>(list, other);
+    }
+    if constexpr (W >= 32) {
+#pragma unroll
+        for (int i = 0; i < K; ++i) other[i] = shuffled(list[i], 16);
+        merge<K>(list, other);
+    }
+}
+
+// ---- answers, rows of part of a wavefront ------------------------------------------------------------------------
+
+// KT: places of a lane's list, k or more (0: no alternatives)
+template <typename T, int VEC, int NV, int TPR, int KT>
+__global__ __launch_bounds__(256) void gp_answer_short(AnswerArgs a)
+{
+    constexpr int TEAMS = 256 / TPR;
+    const int lane = threadIdx.x % TPR;
+    for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR; row < a.N; row += (int64_t)gridDim.x * TEAMS) {
+        const T* const x = (const T*)a.x + row * a.ld;
+        const int64_t token = a.logp ? token_at(a.tokens, a.wide, row) : -1;
+        float e[NV][VEC];
+        int col[NV];
+        load_row<T, VEC, NV, TPR>(x, a.C, a.nvec, lane, e, col);
+        const float logit = token >= 0 && token < a.C ? widen(x[token]) : 0.0f;
+        float m = -infinity();
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) m = larger(m, e[v][i]);
+        RowSums s;
+        s.m = base_of(team_largest<TPR>(m));
+        float total = 0.0f, weighted = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float z = (e[v][i] - s.m) * a.scale, p = __builtin_amdgcn_exp2f(z * kLog2e);
+                total += p;
+                weighted += p * larger(z, -1e4f);  // (p is 0 there)
+            }
+        s.total = team_sum<TPR>(total), s.weighted = team_sum<TPR>(weighted);
+        if (lane == 0) write_row(a, row, token, logit, s.m, s);
+        if constexpr (KT > 0) {
+            uint64_t list[KT] = {};
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sort_in<KT>(list, key_of(e[v][i], col[v] + i));
+            team_merge<TPR, KT>(list);
+            const float l = s.log_total();
+            constexpr int MINE = (KT + TPR - 1) / TPR;
+            uint64_t key[MINE] = {};
+#pragma unroll
+            for (int i = 0; i < KT; ++i) key[i / TPR] = lane == i % TPR ? list[i] : key[i / TPR];
+#pragma unroll
+            for (int i = 0; i < MINE; ++i)
+                if (i * TPR + lane < a.k) write_top(a, row, i * TPR + lane, key[i], s.m, l);
+        }
+    }
+}
+
+// ---- answers, rows of a wavefront or a workgroup ----------------------------------------------------------------
+
+template <int TPR>
+__device__ __forceinline__ void team_barrier()
+{
+    if constexpr (TPR > 64) {
+        __syncthreads();
+    } else {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    }
+}
+
+// What a team shares in LDS.
+template <int TPR>
+struct TeamLds {
+    static constexpr int WAVES = TPR / 64, ROOM = TPR > 64 ? kRoom : kRoom / 4;
+    float m[WAVES], total[WAVES], weighted[WAVES];
+    float group[64];
+    float bound;
+    int count;
+    uint64_t best[WAVES];
+    uint64_t list[ROOM];
+};
+
+// The k-th largest of a wavefront's 64 values (k <= 64), in every lane: few by taking the largest away, many by counting.
+__device__ __forceinline__ float kth_largest(float v, int k)
+{
+    if (k <= 16) {
+        float last = infinity();
+        for (int r = 0; r < k; ++r) {
+            last = team_largest<64>(v);
+            const uint64_t with = __ballot(v == last);
+            if ((int)(threadIdx.x & 63) == __ffsll((unsigned long long)with) - 1) v = -infinity();
+        }
+        return last;
+    }
+    int above = 0;
+    for (int l = 0; l < 64; ++l) above += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), l)) > v;
+    return -team_largest<64>(above < k ? -v : -infinity());
+}
+
+// Where the largest key of all is in `best` of every lane.
+template <int TPR>
+__device__ __forceinline__ uint64_t team_best(uint64_t best, TeamLds<TPR>& lds)
+{
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) best = key_max(best, shuffled(best, w));
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) lds.best[threadIdx.x >> 6] = best;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < TPR / 64; ++w) best = key_max(best, lds.best[w]);
+        __syncthreads();
+    }
+    return best;
+}
+
+// One team to a row, or to a row's part.  TPR 64: four rows to a workgroup.
+template <typename T, int VEC, int NV, int TPR>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_answer_rows(AnswerArgs a)
+{
+    constexpr int BLOCK = TPR < 256 ? 256 : TPR, TEAMS = BLOCK / TPR;
+    __shared__ TeamLds<TPR> all_lds[TEAMS];
+    TeamLds<TPR>& lds = all_lds[threadIdx.x / TPR];
+    const int lane = threadIdx.x % TPR, wave = lane >> 6;
+    const int64_t items = a.N * a.parts;
+    for (int64_t item = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR; item < items; item += (int64_t)gridDim.x * TEAMS) {
+        const int64_t row = a.parts == 1 ? item : item / a.parts;
+        const int part = a.parts == 1 ? 0 : (int)(item - row * a.parts);
+        const int lo = (int)((int64_t)a.nvec * part / a.parts), hi = (int)((int64_t)a.nvec * (part + 1) / a.parts);
+        const int off = lo * VEC, len = min(hi * VEC, a.C) - off;
+        const T* const x = (const T*)a.x + row * a.ld;
+        const int64_t token = a.logp && a.parts == 1 ? token_at(a.tokens, a.wide, row) : -1;
+        float e[NV][VEC];
+        int col[NV];
+        load_row<T, VEC, NV, TPR>(x + off, len, hi - lo, lane, e, col);
+        const float logit = token >= 0 && token < a.C ? widen(x[token]) : 0.0f;
+        float mine = -infinity();
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) mine = larger(mine, e[v][i]);
+        float m, group = mine;
+        if constexpr (TPR > 64) {
+            group = team_largest<TPR / 64>(mine);
+            if ((lane & (TPR / 64 - 1)) == 0) lds.group[lane / (TPR / 64)] = group;
+            m = team_largest<64>(group);
+            if ((lane & 63) == 0) lds.m[wave] = m;
+            if (lane == 0) lds.count = 0;
+            __syncthreads();
+            m = team_largest<TPR / 64>(lds.m[lane & (TPR / 64 - 1)]);
+        } else {
+            m = team_largest<64>(mine);
+            if (lane == 0) lds.count = 0;
+        }
+        RowSums s;
+        s.m = base_of(m);
+        float total = 0.0f, weighted = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float z = (e[v][i] - s.m) * a.scale, p = __builtin_amdgcn_exp2f(z * kLog2e);
+                total += p;
+                weighted += p * larger(z, -1e4f);
+            }
+        total = team_sum<64>(total), weighted = team_sum<64>(weighted);
+        float bound = -infinity();
+        if constexpr (TPR > 64) {
+            if ((lane & 63) == 0) lds.total[wave] = total, lds.weighted[wave] = weighted;
+            if (a.k > 0 && wave == 0) {
+                bound = kth_largest(lds.group[lane], a.k);
+                if (lane == 0) lds.bound = bound;
+            }
+            __syncthreads();
+            total = team_sum<TPR / 64>(lds.total[lane & (TPR / 64 - 1)]), weighted = team_sum<TPR / 64>(lds.weighted[lane & (TPR / 64 - 1)]);
+            if (a.k > 0) bound = lds.bound;
+        } else if (a.k > 0) {
+            bound = kth_largest(group, a.k);
+        }
+        s.total = total, s.weighted = weighted;
+        if (lane == 0) {
+            if (a.parts == 1) {
+                write_row(a, row, token, logit, s.m, s);
+            } else {
+                float* const to = a.partial + 4 * item;
+                to[0] = m, to[1] = total, to[2] = weighted;
+            }
+        }
+        if (a.k > 0) {
+            // whatever is not below the bound; -inf is no alternative, NaN above all
+            if (!(mine < bound) || m != m || total != total) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i)
+                        if (!(e[v][i] < bound) && e[v][i] != -infinity()) {
+                            const int at = atomicAdd(&lds.count, 1);
+                            if (at < TeamLds<TPR>::ROOM) lds.list[at] = key_of(e[v][i], off + col[v] + i);
+                        }
+            }
+            team_barrier<TPR>();
+            const int count = lds.count;
+            const float l = s.log_total();
+            uint64_t* const keys = a.parts == 1 ? nullptr : a.keys + item * a.k;
+            if (count <= TeamLds<TPR>::ROOM) {
+                for (int c = lane; c < count; c += TPR) {
+                    const uint64_t key = lds.list[c];
+                    int rank = 0;
+                    for (int j = 0; j < count; ++j) rank += lds.list[j] > key;
+                    if (rank < a.k) {
+                        if (keys)
+                            keys[rank] = key;
+                        else
+                            write_top(a, row, rank, key, s.m, l);
+                    }
+                }
+                for (int place = count + lane; place < a.k; place += TPR) {
+                    if (keys)
+                        keys[place] = 0;
+                    else
+                        write_top(a, row, place, 0, s.m, l);
+                }
+            } else {
+                uint64_t last = UINT64_C(1) << 60;  // (above every key)
+                for (int place = 0; place < a.k; ++place) {
+                    uint64_t best = 0;
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) {
+                            const uint64_t key = e[v][i] != -infinity() ? key_of(e[v][i], off + col[v] + i) : 0;
+                            if (key < last && key > best) best = key;
+                        }
+                    last = team_best<TPR>(best, lds);
+                    if (lane == 0) {
+                        if (keys)
+                            keys[place] = last;
+                        else
+                            write_top(a, row, place, last, s.m, l);
+                    }
+                }
+            }
+            team_barrier<TPR>();
+        }
+        if constexpr (TPR > 64) __syncthreads();  // (the next row's numbers go where this one's were)
+    }
+}
+
+// The sums of a row's parts, in every lane of a wavefront.
+__device__ __forceinline__ RowSums join_parts(const float* partial, int parts, float scale, float* largest = nullptr)
+{
+    const int lane = threadIdx.x & 63;
+    float m = -infinity();
+    for (int p = lane; p < parts; p += 64) m = larger(m, partial[4 * p]);
+    m = team_largest<64>(m);
+    RowSums s;
+    s.m = base_of(m);
+    float total = 0.0f, weighted = 0.0f;
+    for (int p = lane; p < parts; p += 64) {
+        // a part's sums are of exp(z - its own largest): z = (its largest - m) s + its own
+        const float own = partial[4 * p], t = partial[4 * p + 1];
+        const float z = (base_of(own) - s.m) * scale, f = own == -infinity() && t == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(z * kLog2e);
+        total += f * t;
+        weighted += f * (partial[4 * p + 2] + larger(z, -1e4f) * t);
+    }
+    s.total = team_sum<64>(total), s.weighted = team_sum<64>(weighted);
+    return s;
+}
+
+// Joins the parts of a row: its sums, and the largest of the parts' keys by the same bound as above.
+template <typename T>
+__global__ __launch_bounds__(256) void gp_answer_join(AnswerArgs a)
+{
+    __shared__ uint64_t list[kRoom], group[64], bound_at, best_at[4];
+    __shared__ int count;
+    for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
+        const int64_t token = a.logp ? token_at(a.tokens, a.wide, row) : -1;
+        const RowSums s = join_parts(a.partial + 4 * row * a.parts, a.parts, a.scale);
+        if (threadIdx.x == 0) {
+            write_row(a, row, token, token >= 0 && token < a.C ? widen(((const T*)a.x)[row * a.ld + token]) : 0.0f, s.m, s);
+            count = 0;
+        }
+        if (a.k == 0) continue;
+        const uint64_t* const keys = a.keys + row * a.parts * a.k;
+        const int all = a.parts * a.k;
+        uint64_t mine = 0;
+        for (int j = threadIdx.x; j < all; j += 256) mine = key_max(mine, keys[j]);
+        uint64_t best = key_max(mine, shuffled(mine, 1));
+        best = key_max(best, shuffled(best, 2));
+        if ((threadIdx.x & 3) == 0) group[threadIdx.x >> 2] = best;
+        __syncthreads();
+        if (threadIdx.x < 64) {
+            const uint64_t g = group[threadIdx.x];
+            int above = 0;
+            for (int j = 0; j < 64; ++j) above += group[j] > g || (group[j] == g && j < (int)threadIdx.x);
+            if (above == a.k - 1) bound_at = g;
+        }
+        __syncthreads();
+        const uint64_t bound = bound_at;
+        for (int j = threadIdx.x; j < all; j += 256) {
+            const uint64_t key = keys[j];
+            if (key >= bound && key > 0) {
+                const int at = atomicAdd(&count, 1);
+                if (at < kRoom) list[at] = key;
+            }
+        }
+        __syncthreads();
+        const float l = s.log_total();
+        const int found = count;
+        if (found <= kRoom) {
+            for (int c = threadIdx.x; c < found; c += 256) {
+                const uint64_t key = list[c];
+                int rank = 0;
+                for (int j = 0; j < found; ++j) rank += list[j] > key;
+                if (rank < a.k) write_top(a, row, rank, key, s.m, l);
+            }
+            for (int place = found + threadIdx.x; place < a.k; place += 256) write_top(a, row, place, 0, s.m, l);
+        } else {
+            uint64_t last = UINT64_C(1) << 60;  // (above every key)
+            for (int place = 0; place < a.k; ++place) {
+                best = 0;
+                for (int j = threadIdx.x; j < all; j += 256) {
+                    const uint64_t key = keys[j];
+                    if (key < last && key > best) best = key;
+                }
+#pragma unroll
+                for (int w = 1; w < 64; w *= 2) best = key_max(best, shuffled(best, w));
+                if ((threadIdx.x & 63) == 0) best_at[threadIdx.x >> 6] = best;
+                __syncthreads();
+                last = key_max(key_max(best_at[0], best_at[1]), key_max(best_at[2], best_at[3]));
+                if (threadIdx.x == 0) write_top(a, row, place, last, s.m, l);
+                __syncthreads();
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ---- gradient of answers -----------------------------------------------------------------------------------------
+
+struct AnswerGradArgs {
+    const void* x;
+    int64_t ld, N;
+    int C, nvec;
+    const void* tokens;
+    int wide;
+    float scale;
+    const float *stats, *entropy, *g1, *g2;
+    int64_t s1, s2;  // distances of g1's and g2's elements: 0 or 1
+    void* grad;
+    int64_t ldg;
+};
+
+// One vector per thread and step.  A row's last vector is moved back to end with the row (what it repeats is written twice, identically).
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void gp_answer_grad(AnswerGradArgs a)
+{
+    constexpr int U = 2;
+    const int64_t total = a.N * a.nvec;
+    for (int64_t b0 = (int64_t)blockIdx.x * (U * 256); b0 < total; b0 += (int64_t)gridDim.x * (U * 256)) {
+        const int64_t r0 = b0 / a.nvec;
+        const unsigned rem = (unsigned)(b0 - r0 * a.nvec);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const unsigned place = rem + u * 256 + threadIdx.x, q = place / (unsigned)a.nvec;
+            const int64_t row = r0 + q;
+            if (row >= a.N) continue;
+            const int col = min((int)(place - q * a.nvec) * VEC, a.C - VEC);
+            float v[VEC];
+            load_vec<T, VEC>((const T*)a.x + row * a.ld + col, v);
+            const int64_t token = a.g1 ? token_at(a.tokens, a.wide, row) : -1;
+            const bool named = token >= 0 && token < a.C;
+            const float base = a.stats[2 * row], l = a.stats[2 * row + 1];
+            const float g1 = named ? a.g1[row * a.s1] * a.scale : 0.0f, g2 = a.g2 ? a.g2[row * a.s2] * a.scale : 0.0f, h = a.g2 ? a.entropy[row] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float logp = (v[i] - base) * a.scale - l, p = __builtin_amdgcn_exp2f(logp * kLog2e);
+                v[i] = (named && token == col + i ? g1 : 0.0f) - p * (g1 + g2 * (larger(logp, -1e4f) + h));
+            }
+            store_vec<T, VEC>((T*)a.grad + row * a.ldg + col, v);
+        }
+    }
+}
+
+// ---- distillation ----------------------------------------------------------------------------------------------------
+
+struct DistillArgs {
+    const void* x;
+    int64_t ld, N;
+    int C, nvec;
+    const void* index;
+    int wide;
+    int64_t ldi;
+    const void* teacher;
+    int64_t ldv;
+    int wide_teacher;  // fp32
+    int K;
+    float T;
+    float *loss, *stats;
+    const float* from;  // stats that an earlier pass left: no loss, the gradient alone
+    const float* g;
+    int64_t sg;
+    void* grad;
+    int64_t ldg;
+    int parts;
+    float* partial;
+};
+
+__device__ __forceinline__ int64_t entry_index(const DistillArgs& a, int64_t row, int k)
+{
+    return token_at(a.index, a.wide, row * a.ldi + k);
+}
+__device__ __forceinline__ float entry_logit(const DistillArgs& a, int64_t row, int k)
+{
+    return a.wide_teacher ? ((const float*)a.teacher)[row * a.ldv + k] : widen(((const bf16_t*)a.teacher)[row * a.ldv + k]);
+}
+
+// Entries of a row's teacher, PER of them in a lane of a team of W: k = i * W + lane.
+template <int W, int PER>
+struct Teacher {
+    int at[PER];    // the class, -1: none
+    float q[PER], logq[PER], logit[PER];  // its probability, the log of it, the student's logit
+    bool some;      // the row has an entry that counts
+
+    template <typename T>
+    __device__ __forceinline__ void load(const DistillArgs& a, int64_t row, const T* x, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int k = i * W + lane;
+            const int64_t j = k < a.K ? entry_index(a, row, k) : -1;
+            at[i] = j >= 0 && j < a.C ? (int)j : -1;
+            q[i] = k < a.K && at[i] >= 0 ? entry_logit(a, row, k) : -infinity();
+            logit[i] = at[i] >= 0 ? widen(x[at[i]]) : 0.0f;
+        }
+    }
+    __device__ __forceinline__ void weigh(float T)
+    {
+        float m = -infinity(), total = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) m = larger(m, q[i]);
+        m = base_of(team_largest<W>(m));
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            logq[i] = (q[i] - m) / T;
+            q[i] = __builtin_amdgcn_exp2f(logq[i] * kLog2e);
+            total += q[i];
+        }
+        total = team_sum<W>(total);
+        some = !(total == 0.0f);
+        const float l = some ? logf(total) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            logq[i] -= l;
+            q[i] = some ? q[i] / total : 0.0f;
+        }
+    }
+    __device__ __forceinline__ float loss(float T, float base, float log_total) const
+    {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (!(q[i] == 0.0f)) sum += q[i] * (logq[i] - ((logit[i] - base) / T - log_total));
+        return T * T * team_sum<W>(sum);
+    }
+};
+
+// Rows of part of a wavefront: the gradient goes through LDS, where the entries' shares are taken off, one after another.
+template <typename T, int VEC, int NV, int TPR, int PER>
+__global__ __launch_bounds__(256) void gp_distill_short(DistillArgs a)
+{
+    constexpr int TEAMS = 256 / TPR, CELLS = NV * VEC * TPR;
+    __shared__ __attribute__((aligned(16))) float cells[TEAMS][CELLS];
+    const int lane = threadIdx.x % TPR;
+    float* const mine = cells[threadIdx.x / TPR];
+    const float s = 1.0f / a.T;
+    for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR; row < a.N; row += (int64_t)gridDim.x * TEAMS) {
+        const T* const x = (const T*)a.x + row * a.ld;
+        float e[NV][VEC];
+        int col[NV];
+        load_row<T, VEC, NV, TPR>(x, a.C, a.nvec, lane, e, col);
+        Teacher<TPR, PER> t;
+        t.load(a, row, x, lane);
+        float base, log_total;
+        if (a.from) {
+            base = a.from[2 * row], log_total = a.from[2 * row + 1];
+        } else {
+            float m = -infinity(), total = 0.0f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) m = larger(m, e[v][i]);
+            base = base_of(team_largest<TPR>(m));
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) total += __builtin_amdgcn_exp2f((e[v][i] - base) * s * kLog2e);
+            total = team_sum<TPR>(total);
+            log_total = total == 0.0f ? 0.0f : logf(total);
+        }
+        t.weigh(a.T);
+        if (!a.from) {
+            const float loss = t.some ? t.loss(a.T, base, log_total) : 0.0f;
+            if (lane == 0) {
+                if (a.loss) a.loss[row] = loss;
+                if (a.stats) a.stats[2 * row] = base, a.stats[2 * row + 1] = log_total;
+            }
+        }
+        if (!a.grad) continue;
+        const float f = a.g[row * a.sg] * a.T;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float p = __builtin_amdgcn_exp2f(((e[v][i] - base) * s - log_total) * kLog2e);
+                mine[(v * TPR + lane) * VEC + i] = t.some ? f * p : 0.0f;
+            }
+        }
+        team_barrier<64>();
+        // (the last vector was moved back to end with the row; one lane of a team at a time, so that entries of one class go in their order)
+        for (int i = 0; i < PER; ++i)
+            for (int j = 0; j < min(TPR, a.K - i * TPR); ++j) {
+                if (lane != j || t.at[i] < 0) continue;
+                const int c = t.at[i];
+                atomicAdd(c / VEC < a.nvec - 1 ? mine + c : mine + (a.nvec - 1) * VEC + (c - (a.C - VEC)), -f * t.q[i]);
+            }
+        team_barrier<64>();
+        T* const out = (T*)a.grad + row * a.ldg;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int at = v * TPR + lane;
+            if (at >= a.nvec) continue;
+            const int first = at * VEC - col[v];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) e[v][i] = mine[at * VEC + i];
+            if (first == 0) {
+                store_vec<T, VEC>(out + col[v], e[v]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (i >= first) out[col[v] + i] = narrow<T>(e[v][i]);
+            }
+        }
+    }
+}
+
+// Rows of a wavefront or a workgroup, or parts of them where `from` has their sums: the gradient is written from the registers, then the entries' classes once more.
+template <typename T, int VEC, int NV, int TPR>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_distill_rows(DistillArgs a)
+{
+    constexpr int BLOCK = TPR < 256 ? 256 : TPR, TEAMS = BLOCK / TPR, WAVES = TPR / 64;
+    __shared__ float lds[3][16];
+    const int lane = threadIdx.x % TPR, wave = lane >> 6;
+    const int64_t items = a.N * a.parts;
+    const float s = 1.0f / a.T;
+    for (int64_t item = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR; item < items; item += (int64_t)gridDim.x * TEAMS) {
+        const int64_t row = a.parts == 1 ? item : item / a.parts;
+        const int part = a.parts == 1 ? 0 : (int)(item - row * a.parts);
+        const int lo = (int)((int64_t)a.nvec * part / a.parts), hi = (int)((int64_t)a.nvec * (part + 1) / a.parts);
+        const int off = lo * VEC, len = min(hi * VEC, a.C) - off;
+        const T* const x = (const T*)a.x + row * a.ld;
+        float e[NV][VEC];
+        int col[NV];
+        load_row<T, VEC, NV, TPR>(x + off, len, hi - lo, lane, e, col);
+        Teacher<64, 1> t;
+        t.some = true;
+        if (wave == 0) t.load(a, row, x, lane);
+        float base, log_total;
+        if (a.from) {
+            base = a.from[2 * row], log_total = a.from[2 * row + 1];
+        } else {
+            float m = -infinity(), total = 0.0f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) m = larger(m, e[v][i]);
+            m = team_largest<64>(m);
+            if constexpr (TPR > 64) {
+                if ((lane & 63) == 0) lds[0][wave] = m;
+                __syncthreads();
+                m = team_largest<WAVES>(lds[0][lane & (WAVES - 1)]);
+            }
+            base = base_of(m);
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) total += __builtin_amdgcn_exp2f((e[v][i] - base) * s * kLog2e);
+            total = team_sum<64>(total);
+            if constexpr (TPR > 64) {
+                if ((lane & 63) == 0) lds[1][wave] = total;
+                __syncthreads();
+                total = team_sum<WAVES>(lds[1][lane & (WAVES - 1)]);
+            }
+            log_total = total == 0.0f ? 0.0f : logf(total);
+        }
+        if (wave == 0) {
+            t.weigh(a.T);
+            if (!a.from) {
+                const float loss = t.some ? t.loss(a.T, base, log_total) : 0.0f;
+                if (lane == 0) {
+                    if (a.loss) a.loss[row] = loss;
+                    if (a.stats) a.stats[2 * row] = base, a.stats[2 * row + 1] = log_total;
+                }
+            }
+        }
+        if (!a.grad) {
+            if constexpr (TPR > 64) __syncthreads();
+            continue;
+        }
+        if constexpr (TPR > 64) {
+            if (lane == 0) lds[2][0] = t.some ? 1.0f : 0.0f;
+            __syncthreads();
+            t.some = lds[2][0] != 0.0f;
+        }
+        const float f = a.g[row * a.sg] * a.T;
+        T* const out = (T*)a.grad + row * a.ldg;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int at = v * TPR + lane;
+            if (at >= hi - lo) continue;
+            const int first = at * VEC - col[v];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float p = __builtin_amdgcn_exp2f(((e[v][i] - base) * s - log_total) * kLog2e);
+                e[v][i] = t.some ? f * p : 0.0f;
+            }
+            if (first == 0) {
+                store_vec<T, VEC>(out + off + col[v], e[v]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (i >= first) out[off + col[v] + i] = narrow<T>(e[v][i]);
+            }
+        }
+        team_barrier<TPR>();  // (a workgroup's stores to one place are seen in their order)
+        if (wave == 0) {
+            float taken = 0.0f;
+            for (int k = 0; k < a.K; ++k) {
+                const int c = __builtin_amdgcn_readlane(t.at[0], k);
+                const float q = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(t.q[0]), k));
+                if (c == t.at[0]) taken += q;
+            }
+            if (t.some && t.at[0] >= off && t.at[0] < off + len) {
+                const float p = __builtin_amdgcn_exp2f(((t.logit[0] - base) * s - log_total) * kLog2e);
+                out[t.at[0]] = narrow<T>(f * (p - taken));
+            }
+        }
+        if constexpr (TPR > 64) __syncthreads();
+    }
+}
+
+// Joins the parts of a row: its sums, and the loss.
+template <typename T>
+__global__ __launch_bounds__(256) void gp_distill_join(DistillArgs a)
+{
+    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < a.N; row += (int64_t)gridDim.x * 4) {
+        const int lane = threadIdx.x & 63;
+        Teacher<64, 1> t;
+        t.load(a, row, (const T*)a.x + row * a.ld, lane);
+        const RowSums s = join_parts(a.partial + 4 * row * a.parts, a.parts, 1.0f / a.T);
+        t.weigh(a.T);
+        const float l = s.log_total(), loss = t.some ? t.loss(a.T, s.m, l) : 0.0f;
+        if (lane == 0) {
+            if (a.loss) a.loss[row] = loss;
+            if (a.stats) a.stats[2 * row] = s.m, a.stats[2 * row + 1] = l;
+        }
+    }
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------
+
+constexpr int64_t kMaxBlocks = 1 << 20;  // of a launch; workgroups walk on through the rest
+constexpr int64_t kFull = 256 * 16;      // wavefronts below which a row is spread over more lanes
+constexpr int64_t kMostRows = INT64_C(1) << 40;
+constexpr int kMostClasses = 1 << kIndexBits;
+constexpr int64_t kFillParts = 512;      // workgroups that few long rows are cut into, at least
+constexpr int64_t kPartVectors = 512;    // vectors of such a part, at least
+constexpr int kLongestRow = 1024 * 32;   // elements that a workgroup holds
+
+template <typename T>
+constexpr int kVec = 16 / sizeof(T);
+
+int64_t row_parts(int64_t N, int64_t C, int vec)
+{
+    const int64_t nvec = (C + vec - 1) / vec, parts = (C + kLongestRow - 1) / kLongestRow;
+    if (N * parts >= kFillParts || nvec < 8 * kPartVectors) return parts;
+    return std::max(parts, std::min(nvec / kPartVectors, (kFillParts + N - 1) / N));
+}
+
+// Lanes of a row's team: as few as hold it in four vectors each; more, up to `most`, where the rows make too few wavefronts.
+int team_lanes(int64_t N, int64_t nvec, int most)
+{
+    int lanes = 4;
+    while (lanes < most && nvec > lanes * 4) lanes *= 2;
+    while (lanes < most && nvec > lanes && N * lanes / 64 < kFull) lanes *= 2;
+    return lanes;
+}
+
+template <typename T, int VEC, int NV, int TPR, int KT>
+gp_status launch_short(const AnswerArgs& a, hipStream_t stream)
+{
+    constexpr int TEAMS = 256 / TPR;
+    profile_begin("gp_answer_short", stream);
+    hipLaunchKernelGGL((gp_answer_short<T, VEC, NV, TPR, KT>), dim3((unsigned)std::min((a.N + TEAMS - 1) / TEAMS, kMaxBlocks)), dim3(256), 0, stream, a);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    return GP_OK;
+}
+template <typename T, int VEC, int NV, int TPR>
+gp_status launch_short(const AnswerArgs& a, hipStream_t stream)
+{
+    if (a.k == 0) return launch_short<T, VEC, NV, TPR, 0>(a, stream);
+    if (a.k <= 2) return launch_short<T, VEC, NV, TPR, 2>(a, stream);
+    if (a.k <= 5) return launch_short<T, VEC, NV, TPR, 5>(a, stream);
+    return launch_short<T, VEC, NV, TPR, 8>(a, stream);
+}
+template <typename T, int VEC, int TPR>
+gp_status launch_short(const AnswerArgs& a, hipStream_t stream)
+{
+    switch ((a.nvec + TPR - 1) / TPR) {
+    case 1: return launch_short<T, VEC, 1, TPR>(a, stream);
+    case 2: return launch_short<T, VEC, 2, TPR>(a, stream);
+    case 3: return launch_short<T, VEC, 3, TPR>(a, stream);
+    default: return launch_short<T, VEC, 4, TPR>(a, stream);
+    }
+}
+template <typename T, int VEC, int NV, int TPR>
+gp_status launch_rows(const AnswerArgs& a, hipStream_t stream)
+{
+    constexpr int BLOCK = TPR < 256 ? 256 : TPR, TEAMS = BLOCK / TPR;
+    const int64_t items = a.N * a.parts;
+    profile_begin("gp_answer_rows", stream);
+    hipLaunchKernelGGL((gp_answer_rows<T, VEC, NV, TPR>), dim3((unsigned)std::min((items + TEAMS - 1) / TEAMS, kMaxBlocks)), dim3(BLOCK), 0, stream, a);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    return GP_OK;
+}
+template <typename T, int VEC, int TPR>
+gp_status launch_rows(const AnswerArgs& a, int64_t longest, hipStream_t stream)
+{
+    if (longest <= TPR) return launch_rows<T, VEC, 1, TPR>(a, stream);
+    if (longest <= 2 * TPR) return launch_rows<T, VEC, 2, TPR>(a, stream);
+    if constexpr (TPR == 1024 && VEC * 4 < kLongestRow / 1024)
+        if (longest > 4 * TPR) return launch_rows<T, VEC, 8, TPR>(a, stream);
+    return launch_rows<T, VEC, 4, TPR>(a, stream);
+}
+// Rows of a wavefront or more, or parts of them
+template <typename T>
+gp_status launch_rows(const AnswerArgs& a, hipStream_t stream)
+{
+    const int64_t longest = (a.nvec + a.parts - 1) / a.parts;
+    if (longest <= 256) return launch_rows<T, kVec<T>, 64>(a, longest, stream);
+    if (longest <= 1024) return launch_rows<T, kVec<T>, 256>(a, longest, stream);
+    return launch_rows<T, kVec<T>, 1024>(a, longest, stream);
+}
+
+template <typename T>
+gp_status launch_answer(AnswerArgs a, char* workspace, hipStream_t stream)
+{
+    constexpr int VEC = kVec<T>;
+    if (a.C < VEC) {
+        a.nvec = a.C;
+        return a.k <= 8 ? launch_short<T, 1, 1, 8>(a, stream) : launch_rows<T, 1, 1, 64>(a, stream);
+    }
+    a.nvec = (a.C + VEC - 1) / VEC;
+    if (a.nvec <= 128 && a.k <= 8) {
+        switch (team_lanes(a.N, a.nvec, 32)) {
+        case 4: return launch_short<T, VEC, 4>(a, stream);
+        case 8: return launch_short<T, VEC, 8>(a, stream);
+        case 16: return launch_short<T, VEC, 16>(a, stream);
+        default: return launch_short<T, VEC, 32>(a, stream);
+        }
+    }
+    a.parts = (int)row_parts(a.N, a.C, VEC);
+    a.partial = (float*)workspace;
+    a.keys = (uint64_t*)(workspace + 16 * a.N * a.parts);
+    gp_status st = launch_rows<T>(a, stream);
+    if (st != GP_OK || a.parts == 1) return st;
+    profile_begin("gp_answer_join", stream);
+    hipLaunchKernelGGL(gp_answer_join<T>, dim3((unsigned)std::min(a.N, kMaxBlocks)), dim3(256), 0, stream, a);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    return GP_OK;
+}
+
+template <typename T, int VEC, int NV, int TPR>
+gp_status launch_distill_short(const DistillArgs& a, hipStream_t stream)
+{
+    constexpr int TEAMS = 256 / TPR;
+    const dim3 grid((unsigned)std::min((a.N + TEAMS - 1) / TEAMS, kMaxBlocks));
+    profile_begin("gp_distill_short", stream);
+    if (a.K <= 8)
+        hipLaunchKernelGGL((gp_distill_short<T, VEC, NV, TPR, (TPR < 8 ? 8 / TPR : 1)>), grid, dim3(256), 0, stream, a);
+    else
+        hipLaunchKernelGGL((gp_distill_short<T, VEC, NV, TPR, kMostTop / TPR>), grid, dim3(256), 0, stream, a);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    return GP_OK;
+}
+template <typename T, int VEC, int TPR>
+gp_status launch_distill_short(const DistillArgs& a, hipStream_t stream)
+{
+    switch ((a.nvec + TPR - 1) / TPR) {
+    case 1: return launch_distill_short<T, VEC, 1, TPR>(a, stream);
+    case 2: return launch_distill_short<T, VEC, 2, TPR>(a, stream);
+    case 3: return launch_distill_short<T, VEC, 3, TPR>(a, stream);
+    default: return launch_distill_short<T, VEC, 4, TPR>(a, stream);
+    }
+}
+template <typename T, int VEC, int NV, int TPR>
+gp_status launch_distill_rows(const DistillArgs& a, hipStream_t stream)
+{
+    constexpr int BLOCK = TPR < 256 ? 256 : TPR, TEAMS = BLOCK / TPR;
+    const int64_t items = a.N * a.parts;
+    profile_begin("gp_distill_rows", stream);
+    hipLaunchKernelGGL((gp_distill_rows<T, VEC, NV, TPR>), dim3((unsigned)std::min((items + TEAMS - 1) / TEAMS, kMaxBlocks)), dim3(BLOCK), 0, stream, a);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    return GP_OK;
+}
+template <typename T, int VEC, int TPR>
+gp_status launch_distill_rows(const DistillArgs& a, int64_t longest, hipStream_t stream)
+{
+    if (longest <= TPR) return launch_distill_rows<T, VEC, 1, TPR>(a, stream);
+    if (longest <= 2 * TPR) return launch_distill_rows<T, VEC, 2, TPR>(a, stream);
+    if constexpr (TPR == 1024 && VEC * 4 < kLongestRow / 1024)
+        if (longest > 4 * TPR) return launch_distill_rows<T, VEC, 8, TPR>(a, stream);
+    return launch_distill_rows<T, VEC, 4, TPR>(a, stream);
+}
+template <typename T>
+gp_status launch_distill_rows(const DistillArgs& a, hipStream_t stream)
+{
+    const int64_t longest = (a.nvec + a.parts - 1) / a.parts;
+    if (longest <= 256) return launch_distill_rows<T, kVec<T>, 64>(a, longest, stream);
+    if (longest <= 1024) return launch_distill_rows<T, kVec<T>, 256>(a, longest, stream);
+    return launch_distill_rows<T, kVec<T>, 1024>(a, longest, stream);
+}
+
+template <typename T>
+gp_status launch_distill(DistillArgs a, char* workspace, hipStream_t stream)
+{
+    constexpr int VEC = kVec<T>;
+    a.parts = 1;
+    if (a.C < VEC) {
+        a.nvec = a.C;
+        return launch_distill_short<T, 1, 1, 8>(a, stream);
+    }
+    a.nvec = (a.C + VEC - 1) / VEC;
+    if (a.nvec <= 128) {
+        switch (team_lanes(a.N, a.nvec, 32)) {
+        case 4: return launch_distill_short<T, VEC, 4>(a, stream);
+        case 8: return launch_distill_short<T, VEC, 8>(a, stream);
+        case 16: return launch_distill_short<T, VEC, 16>(a, stream);
+        default: return launch_distill_short<T, VEC, 32>(a, stream);
+        }
+    }
+    a.parts = (int)row_parts(a.N, a.C, VEC);
+    if (a.parts == 1 || a.from) return launch_distill_rows<T>(a, stream);
+    AnswerArgs s{};
+    s.x = a.x, s.ld = a.ld, s.N = a.N, s.C = a.C, s.nvec = a.nvec, s.scale = 1.0f / a.T, s.parts = a.parts;
+    s.partial = a.partial = (float*)workspace;
+    gp_status st = launch_rows<T>(s, stream);
+    if (st != GP_OK) return st;
+    if (!a.stats) a.stats = (float*)(workspace + 16 * a.N * a.parts);
+    profile_begin("gp_distill_join", stream);
+    hipLaunchKernelGGL(gp_distill_join<T>, dim3((unsigned)std::min((a.N + 3) / 4, kMaxBlocks)), dim3(256), 0, stream, a);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    if (!a.grad) return GP_OK;
+    a.from = a.stats;
+    return launch_distill_rows<T>(a, stream);
+}
+
+template <typename T, int VEC>
+gp_status launch_answer_grad(AnswerGradArgs a, hipStream_t stream)
+{
+    a.nvec = (a.C + VEC - 1) / VEC;
+    const int64_t blocks = (a.N * a.nvec + 511) / 512;
+    profile_begin("gp_answer_grad", stream);
+    hipLaunchKernelGGL((gp_answer_grad<T, VEC>), dim3((unsigned)std::min(blocks, kMaxBlocks)), dim3(256), 0, stream, a);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    return GP_OK;
+}
+template <typename T>
+gp_status launch_answer_grad(const AnswerGradArgs& a, hipStream_t stream)
+{
+    return a.C >= kVec<T> ? launch_answer_grad<T, kVec<T>>(a, stream) : launch_answer_grad<T, 1>(a, stream);
+}
+
+// Bytes of the parts' results, whichever type the logits are of.
+int64_t parts_bytes(int64_t N, int32_t C, int32_t k)
+{
+    if (N == 0) return 0;
+    int64_t most = 0;
+    for (int vec : {kVec<float>, kVec<bf16_t>}) {
+        const int64_t parts = row_parts(N, C, vec);
+        if (parts > 1) most = std::max(most, N * parts * (16 + 8 * (int64_t)k));
+    }
+    return (most + 255) / 256 * 256;
+}
+
+bool known(gp_dtype t) { return t == GP_F32 || t == GP_BF16; }
+
+// What every call asks of the logits; `done` where there are none.
+gp_status check_logits(int64_t ld, gp_dtype dtype, int64_t N, int32_t C)
+{
+    if (!known(dtype)) return fail(GP_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+    if (N < 0 || C < 1 || ld < C) return fail(GP_ERR_INVALID_ARG, "need N >= 0, C >= 1, ld >= C");
+    if (N > kMostRows || C > kMostClasses) return fail(GP_ERR_UNSUPPORTED, "more than 2^40 rows or 2^28 classes");
+    return GP_OK;
+}
+gp_status check_workspace(const void* workspace, int64_t bytes, int64_t need)
+{
+    if (need > 0 && (!workspace || bytes < need || (uintptr_t)workspace % 256 != 0))
+        return fail(GP_ERR_INVALID_ARG, "need a workspace of %lld bytes on a 256-byte boundary", (long long)need);
+    return GP_OK;
+}
+bool good_scale(float s) { return s > 0.0f && s <= 1e30f && s >= 1e-30f; }
+
+gp_status log_probs(const void* x, int64_t ld, gp_dtype dtype, int64_t N, int32_t C, const void* tokens, gp_index index, float scale, float* logp, float* entropy,
+                    int32_t k, int32_t* top_index, float* top_logp, float* stats, void* workspace, int64_t bytes, hipStream_t stream)
+{
+    gp_status st = check_logits(ld, dtype, N, C);
+    if (st != GP_OK) return st;
+    if (index != GP_I32 && index != GP_I64) return fail(GP_ERR_INVALID_ARG, "unknown index type %d", (int)index);
+    if (!good_scale(scale)) return fail(GP_ERR_INVALID_ARG, "need a scale within 1e-30 .. 1e30");
+    if (k < 0) return fail(GP_ERR_INVALID_ARG, "need k >= 0");
+    if (k > kMostTop) return fail(GP_ERR_UNSUPPORTED, "more than %d alternatives", kMostTop);
+    if (N == 0) return GP_OK;
+    if (!x || (logp && !tokens) || (k > 0 && (!top_index || !top_logp))) return fail(GP_ERR_INVALID_ARG, "NULL argument");
+    if ((st = check_workspace(workspace, bytes, parts_bytes(N, C, k))) != GP_OK) return st;
+    if (!logp && !entropy && k == 0 && !stats) return GP_OK;
+    AnswerArgs a{};
+    a.x = x, a.ld = ld, a.N = N, a.C = C, a.tokens = tokens, a.wide = index == GP_I64, a.scale = scale, a.logp = logp, a.entropy = entropy, a.stats = stats,
+    a.k = k, a.top_index = top_index, a.top_logp = top_logp, a.parts = 1;
+    return dtype == GP_F32 ? launch_answer<float>(a, (char*)workspace, stream) : launch_answer<bf16_t>(a, (char*)workspace, stream);
+}
+
+gp_status log_probs_grad(const void* x, int64_t ld, gp_dtype dtype, int64_t N, int32_t C, const void* tokens, gp_index index, float scale, const float* stats,
+                         const float* entropy, const float* g1, int64_t s1, const float* g2, int64_t s2, void* grad, int64_t ldg, hipStream_t stream)
+{
+    gp_status st = check_logits(ld, dtype, N, C);
+    if (st != GP_OK) return st;
+    if (index != GP_I32 && index != GP_I64) return fail(GP_ERR_INVALID_ARG, "unknown index type %d", (int)index);
+    if (!good_scale(scale)) return fail(GP_ERR_INVALID_ARG, "need a scale within 1e-30 .. 1e30");
+    if (ldg < C || (s1 != 0 && s1 != 1) || (s2 != 0 && s2 != 1)) return fail(GP_ERR_INVALID_ARG, "need ldg >= C, distances of 0 or 1");
+    if (N == 0) return GP_OK;
+    if (!x || !stats || !grad || (g1 && !tokens) || (g2 && !entropy)) return fail(GP_ERR_INVALID_ARG, "NULL argument");
+    if (N > (INT64_C(1) << 62) / C) return fail(GP_ERR_OVERFLOW, "N x C does not fit 62 bits");
+    AnswerGradArgs a{};
+    a.x = x, a.ld = ld, a.N = N, a.C = C, a.tokens = tokens, a.wide = index == GP_I64, a.scale = scale, a.stats = stats, a.entropy = entropy, a.g1 = g1, a.s1 = s1,
+    a.g2 = g2, a.s2 = s2, a.grad = grad, a.ldg = ldg;
+    return dtype == GP_F32 ? launch_answer_grad<float>(a, stream) : launch_answer_grad<bf16_t>(a, stream);
+}
+
+int64_t distill_bytes(int64_t N, int32_t C)
+{
+    const int64_t parts = parts_bytes(N, C, 0);
+    return parts ? parts + (8 * N + 255) / 256 * 256 : 0;
+}
+
+gp_status distill(const void* x, int64_t ld, gp_dtype dtype, int64_t N, int32_t C, const void* index, int64_t ldi, gp_index index_type, const void* teacher,
+                  int64_t ldt, gp_dtype teacher_dtype, int32_t K, float T, float* loss, float* stats, const float* from, const float* g, int64_t sg, void* grad,
+                  int64_t ldg, void* workspace, int64_t bytes, hipStream_t stream)
+{
+    gp_status st = check_logits(ld, dtype, N, C);
+    if (st != GP_OK) return st;
+    if (index_type != GP_I32 && index_type != GP_I64) return fail(GP_ERR_INVALID_ARG, "unknown index type %d", (int)index_type);
+    if (!known(teacher_dtype)) return fail(GP_ERR_INVALID_ARG, "unknown dtype %d", (int)teacher_dtype);
+    if (K < 1 || ldi < K || ldt < K) return fail(GP_ERR_INVALID_ARG, "need K >= 1, ldi >= K, ldt >= K");
+    if (K > kMostTop) return fail(GP_ERR_UNSUPPORTED, "more than %d entries", kMostTop);
+    if (!good_scale(T)) return fail(GP_ERR_INVALID_ARG, "need a temperature within 1e-30 .. 1e30");
+    if (grad && (ldg < C || (sg != 0 && sg != 1))) return fail(GP_ERR_INVALID_ARG, "need ldg >= C, a distance of 0 or 1");
+    if (N == 0) return GP_OK;
+    if (!x || !index || !teacher || (grad && !g)) return fail(GP_ERR_INVALID_ARG, "NULL argument");
+    if (!from && (st = check_workspace(workspace, bytes, distill_bytes(N, C))) != GP_OK) return st;
+    if (!loss && !stats && !grad) return GP_OK;
+    DistillArgs a{};
+    a.x = x, a.ld = ld, a.N = N, a.C = C, a.index = index, a.wide = index_type == GP_I64, a.ldi = ldi, a.teacher = teacher, a.ldv = ldt,
+    a.wide_teacher = teacher_dtype == GP_F32, a.K = K, a.T = T, a.loss = loss, a.stats = stats, a.from = from, a.g = g, a.sg = sg, a.grad = grad, a.ldg = ldg;
+    return dtype == GP_F32 ? launch_distill<float>(a, (char*)workspace, stream) : launch_distill<bf16_t>(a, (char*)workspace, stream);
+}
+
+}  // namespace
+
+}  // namespace gp
+
+extern "C" int64_t gp_log_probs_workspace(int64_t N, int32_t C, int32_t k)
+{
+    if (N < 0 || N > gp::kMostRows || C < 1 || C > gp::kMostClasses || k < 0 || k > gp::kMostTop) return -1;
+    return gp::parts_bytes(N, C, k);
+}
+
+extern "C" gp_status gp_log_probs(const void* logits, int64_t ld, gp_dtype dtype, int64_t N, int32_t C, const void* tokens, gp_index index, float scale, float* logp,
+                                  float* entropy, int32_t k, int32_t* top_index, float* top_logp, float* stats, void* workspace, int64_t workspace_bytes,
+                                  void* hip_stream)
+{
+    try {
+        return gp::log_probs(logits, ld, dtype, N, C, tokens, index, scale, logp, entropy, k, top_index, top_logp, stats, workspace, workspace_bytes,
+                             (hipStream_t)hip_stream);
+    } catch (const std::exception& e) {
+        return gp::fail(GP_ERR_OOM_HOST, "gp_log_probs: %s", e.what());
+    }
+}
+
+extern "C" gp_status gp_log_probs_grad(const void* logits, int64_t ld, gp_dtype dtype, int64_t N, int32_t C, const void* tokens, gp_index index, float scale,
+                                       const float* stats, const float* entropy, const float* grad_logp, int64_t stride_logp, const float* grad_entropy,
+                                       int64_t stride_entropy, void* grad, int64_t ldg, void* hip_stream)
+{
+    try {
+        return gp::log_probs_grad(logits, ld, dtype, N, C, tokens, index, scale, stats, entropy, grad_logp, stride_logp, grad_entropy, stride_entropy, grad, ldg,
+                                  (hipStream_t)hip_stream);
+    } catch (const std::exception& e) {
+        return gp::fail(GP_ERR_OOM_HOST, "gp_log_probs_grad: %s", e.what());
+    }
+}
+
+extern "C" int64_t gp_distill_workspace(int64_t N, int32_t C)
+{
+    if (N < 0 || N > gp::kMostRows || C < 1 || C > gp::kMostClasses) return -1;
+    return gp::distill_bytes(N, C);
+}
+
+extern "C" gp_status gp_distill(const void* logits, int64_t ld, gp_dtype dtype, int64_t N, int32_t C, const void* teacher_index, int64_t ldi, gp_index index,
+                                const void* teacher_logits, int64_t ldt, gp_dtype teacher_dtype, int32_t K, float temperature, float* loss, float* stats,
+                                const float* grad_loss, int64_t stride_loss, void* grad, int64_t ldg, void* workspace, int64_t workspace_bytes, void* hip_stream)
+{
+    try {
+        return gp::distill(logits, ld, dtype, N, C, teacher_index, ldi, index, teacher_logits, ldt, teacher_dtype, K, temperature, loss, stats, nullptr, grad_loss,
+                           stride_loss, grad, ldg, workspace, workspace_bytes, (hipStream_t)hip_stream);
+    } catch (const std::exception& e) {
+        return gp::fail(GP_ERR_OOM_HOST, "gp_distill: %s", e.what());
+    }
+}
+
+extern "C" gp_status gp_distill_grad(const void* logits, int64_t ld, gp_dtype dtype, int64_t N, int32_t C, const void* teacher_index, int64_t ldi, gp_index index,
+                                     const void* teacher_logits, int64_t ldt, gp_dtype teacher_dtype, int32_t K, float temperature, const float* stats,
+                                     const float* grad_loss, int64_t stride_loss, void* grad, int64_t ldg, void* hip_stream)
+{
+    try {
+        if (N > 0 && (!stats || !grad)) return gp::fail(GP_ERR_INVALID_ARG, "NULL argument");
+        return gp::distill(logits, ld, dtype, N, C, teacher_index, ldi, index, teacher_logits, ldt, teacher_dtype, K, temperature, nullptr, nullptr, stats, grad_loss,
+                           stride_loss, grad, ldg, nullptr, 0, (hipStream_t)hip_stream);
+    } catch (const std::exception& e) {
+        return gp::fail(GP_ERR_OOM_HOST, "gp_distill_grad: %s", e.what());
+    }
+}
