@@ -29,7 +29,7 @@ namespace {
 
 constexpr int kMostTop = 64;      // alternatives, and entries of a teacher: one to a lane of a wavefront
 constexpr int kIndexBits = 28;    // of a class in a key
-constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr int kRoom = 1024;       // keys that a workgroup's list has room for (a wavefront's: a quarter)
 
 struct AnswerArgs {
@@ -107,6 +107,19 @@ struct RowSums {
 };
 __device__ __forceinline__ float base_of(float m) { return m == -infinity() ? 0.0f : m; }
 
+// The sums of a row from those of its parts, one in each lane of a team of W, in every lane.  A part's are of exp(s (x - its own largest)): with
+// z = s (its largest - the row's), exp(z) times them, and z exp(z) times the total more of the weighted one.
+template <int W>
+__device__ __forceinline__ RowSums joined(const RowSums& part, float scale)
+{
+    RowSums s;
+    s.m = team_largest<W>(part.m);
+    const float z = (base_of(part.m) - base_of(s.m)) * scale, f = part.total == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(z * kLog2e);
+    s.total = team_sum<W>(f * part.total);
+    s.weighted = team_sum<W>(f * (part.weighted + larger(z, -1e4f) * part.total));
+    return s;
+}
+
 __device__ __forceinline__ void write_top(const AnswerArgs& a, int64_t row, int place, uint64_t key, float base, float log_total)
 {
     const float x = key ? logit_of(key) : -infinity();
@@ -122,29 +135,107 @@ __device__ __forceinline__ void write_row(const AnswerArgs& a, int64_t row, int6
     if (a.stats) a.stats[2 * row] = base, a.stats[2 * row + 1] = l;
 }
 
-// A row's part in a team's registers: vector t = v * TPR + lane starts at column t * VEC, the last one is moved back to end with the part; what
-// it repeats and what no vector holds is -inf.  (Teams within a wavefront take as few vectors as hold a row, so only the last can be such.)
-template <typename T, int VEC, int NV, int TPR>
-__device__ __forceinline__ void load_row(const T* x, int len, int nvec, int lane, float (&e)[NV][VEC], int (&col)[NV])
+__device__ __forceinline__ float largest_of(float a, float b, float c)
 {
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int t = v * TPR + lane;
-        col[v] = min(t, nvec - 1) * VEC;
-        col[v] = min(col[v], len - VEC);
-        load_vec<T, VEC>(x + col[v], e[v]);
-    }
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        if (TPR < 64 && v < NV - 1) continue;
-        if (TPR >= 64 && __builtin_amdgcn_readfirstlane(v * TPR + (int)(lane & ~63)) + 64 < nvec) continue;
-        const int t = v * TPR + lane;
-        const int first = t < nvec ? t * VEC - col[v] : VEC;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i)
-            if (i < first) e[v][i] = -infinity();
-    }
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
 }
+
+// y = c (x - base) in one instruction, c x + k with k = -c base rounded: every y of a row is off by the same `shift`, which is taken off its sums.
+// (Where that rounding is no small number, x - base and then the product.)
+struct Exponent {
+    float base, c, k, shift, back;
+    bool far;
+    __device__ __forceinline__ Exponent(float base_, float c_) : base(base_), c(c_)
+    {
+        k = -(base * c);
+        far = !(fabsf(k) < 65536.0f);
+        shift = fmaf(base, c, k);
+        back = __builtin_amdgcn_exp2f(-shift);
+    }
+};
+
+// A row's part in a team's registers, as it is stored: vector t = v * TPR + lane starts at column t * VEC, the last one is moved back to end with the
+// part; what it repeats and what no vector holds is -inf.  (Teams within a wavefront take as few vectors as hold a row, so only the last can be such.)
+template <typename T, int VEC, int NV, int TPR>
+struct Row {
+    typename Vec<T, VEC>::type raw[NV];
+
+    static __device__ __forceinline__ unsigned column(int v, int lane, int len, int nvec) { return (unsigned)min(min(v * TPR + lane, nvec - 1) * VEC, len - VEC); }
+    __device__ __forceinline__ float at(int v, int i) const { return element<T, VEC>(raw[v], i); }
+    __device__ __forceinline__ void load(const T* x, int len, int nvec, int lane)
+    {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) raw[v] = *reinterpret_cast<const typename Vec<T, VEC>::type*>(x + column(v, lane, len, nvec));
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            if (TPR < 64 && v < NV - 1) continue;
+            if (TPR >= 64 && __builtin_amdgcn_readfirstlane(v * TPR + (int)(lane & ~63)) + 64 < nvec) continue;
+            const int t = v * TPR + lane, first = t < nvec ? t * VEC - column(v, lane, len, nvec) : VEC;
+            const T none = narrow<T>(-__builtin_inff());
+            if constexpr (VEC == 1) {
+                if (first > 0) raw[v] = none;
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (i < first) raw[v][i] = none;
+            }
+        }
+    }
+    // Between passes over a row in bf16: the compiler would keep its elements widened, in twice the registers.
+    __device__ __forceinline__ void as_stored()
+    {
+        if constexpr (sizeof(T) == 2 && VEC == 8) {
+            typedef unsigned Quad __attribute__((ext_vector_type(4)));
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                Quad q = __builtin_bit_cast(Quad, raw[v]);
+                asm volatile("" : "+v"(q));
+                raw[v] = __builtin_bit_cast(typename Vec<T, VEC>::type, q);
+            }
+        }
+    }
+    // The largest of this lane's elements; a row with a NaN is told by its sum.
+    __device__ __forceinline__ float largest() const
+    {
+        float m = -__builtin_inff();
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            if constexpr (VEC == 1) {
+                m = larger(m, at(v, 0));
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; i += 2) m = largest_of(m, at(v, i), at(v, i + 1));
+            }
+        }
+        return m;
+    }
+    template <typename Y>
+    __device__ __forceinline__ void add_up(Y exponent, float& total, float& weighted)
+    {
+        as_stored();
+        total = weighted = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float y = exponent(at(v, i)), p = __builtin_amdgcn_exp2f(y);
+                total += p;
+                weighted += p * larger(y, -1e4f);  // (p is 0 there)
+            }
+    }
+    // the sums of 2^y and y 2^y over this lane's elements, y = c (x - base)
+    __device__ __forceinline__ void sums(const Exponent& e, float& total, float& weighted)
+    {
+        if (!e.far) {
+            add_up([&](float x) { return fmaf(x, e.c, e.k); }, total, weighted);
+            weighted = (weighted - e.shift * total) * e.back, total *= e.back;
+        } else {
+            add_up([&](float x) { return (x - e.base) * e.c; }, total, weighted);
+        }
+    }
+};
 
 // A list of K keys, largest first, and one more
 template <int K>
@@ -214,34 +305,21 @@ __global__ __launch_bounds__(256) void gp_answer_short(AnswerArgs a)
     for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR; row < a.N; row += (int64_t)gridDim.x * TEAMS) {
         const T* const x = (const T*)a.x + row * a.ld;
         const int64_t token = a.logp ? token_at(a.tokens, a.wide, row) : -1;
-        float e[NV][VEC];
-        int col[NV];
-        load_row<T, VEC, NV, TPR>(x, a.C, a.nvec, lane, e, col);
+        Row<T, VEC, NV, TPR> e;
+        e.load(x, a.C, a.nvec, lane);
         const float logit = token >= 0 && token < a.C ? widen(x[token]) : 0.0f;
-        float m = -infinity();
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) m = larger(m, e[v][i]);
         RowSums s;
-        s.m = base_of(team_largest<TPR>(m));
-        float total = 0.0f, weighted = 0.0f;
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float z = (e[v][i] - s.m) * a.scale, p = __builtin_amdgcn_exp2f(z * kLog2e);
-                total += p;
-                weighted += p * larger(z, -1e4f);  // (p is 0 there)
-            }
-        s.total = team_sum<TPR>(total), s.weighted = team_sum<TPR>(weighted);
+        s.m = base_of(team_largest<TPR>(e.largest()));
+        float total, weighted;
+        e.sums(Exponent(s.m, a.scale * kLog2e), total, weighted);
+        s.total = team_sum<TPR>(total), s.weighted = team_sum<TPR>(weighted) * kLn2;
         if (lane == 0) write_row(a, row, token, logit, s.m, s);
         if constexpr (KT > 0) {
             uint64_t list[KT] = {};
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) sort_in<KT>(list, key_of(e[v][i], col[v] + i));
+                for (int i = 0; i < VEC; ++i) sort_in<KT>(list, key_of(e.at(v, i), e.column(v, lane, a.C, a.nvec) + i));
             team_merge<TPR, KT>(list);
             const float l = s.log_total();
             constexpr int MINE = (KT + TPR - 1) / TPR;
@@ -256,6 +334,14 @@ __global__ __launch_bounds__(256) void gp_answer_short(AnswerArgs a)
 }
 
 // ---- answers, rows of a wavefront or a workgroup ----------------------------------------------------------------
+
+// The same number, of which the compiler knows nothing: what is worked out from it stays where it is needed, and is not kept in registers from one
+// row to the next (60 instead of 99 for rows of 32,768 in bf16, so that a compute unit has four workgroups of 512 and not two).
+__device__ __forceinline__ int opaque(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
 
 template <int TPR>
 __device__ __forceinline__ void team_barrier()
@@ -273,7 +359,7 @@ __device__ __forceinline__ void team_barrier()
 template <int TPR>
 struct TeamLds {
     static constexpr int WAVES = TPR / 64, ROOM = TPR > 64 ? kRoom : kRoom / 4;
-    float m[WAVES], total[WAVES], weighted[WAVES];
+    RowSums sums[WAVES];
     float group[64];
     float bound;
     int count;
@@ -321,81 +407,65 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_answer_rows(AnswerAr
     constexpr int BLOCK = TPR < 256 ? 256 : TPR, TEAMS = BLOCK / TPR;
     __shared__ TeamLds<TPR> all_lds[TEAMS];
     TeamLds<TPR>& lds = all_lds[threadIdx.x / TPR];
-    const int lane = threadIdx.x % TPR, wave = lane >> 6;
+    const int wave = threadIdx.x % TPR >> 6;
     const int64_t items = a.N * a.parts;
-    for (int64_t item = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR; item < items; item += (int64_t)gridDim.x * TEAMS) {
+    for (int64_t item = (int64_t)blockIdx.x * TEAMS + (TEAMS > 1 ? threadIdx.x / TPR : 0); item < items; item += (int64_t)gridDim.x * TEAMS) {
+        const int lane = opaque(threadIdx.x % TPR);
         const int64_t row = a.parts == 1 ? item : item / a.parts;
         const int part = a.parts == 1 ? 0 : (int)(item - row * a.parts);
         const int lo = (int)((int64_t)a.nvec * part / a.parts), hi = (int)((int64_t)a.nvec * (part + 1) / a.parts);
         const int off = lo * VEC, len = min(hi * VEC, a.C) - off;
         const T* const x = (const T*)a.x + row * a.ld;
         const int64_t token = a.logp && a.parts == 1 ? token_at(a.tokens, a.wide, row) : -1;
-        float e[NV][VEC];
-        int col[NV];
-        load_row<T, VEC, NV, TPR>(x + off, len, hi - lo, lane, e, col);
+        Row<T, VEC, NV, TPR> e;
+        e.load(x + off, len, hi - lo, lane);
         const float logit = token >= 0 && token < a.C ? widen(x[token]) : 0.0f;
-        float mine = -infinity();
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) mine = larger(mine, e[v][i]);
-        float m, group = mine;
-        if constexpr (TPR > 64) {
-            group = team_largest<TPR / 64>(mine);
-            if ((lane & (TPR / 64 - 1)) == 0) lds.group[lane / (TPR / 64)] = group;
-            m = team_largest<64>(group);
-            if ((lane & 63) == 0) lds.m[wave] = m;
-            if (lane == 0) lds.count = 0;
-            __syncthreads();
-            m = team_largest<TPR / 64>(lds.m[lane & (TPR / 64 - 1)]);
-        } else {
-            m = team_largest<64>(mine);
-            if (lane == 0) lds.count = 0;
-        }
+        // every wavefront takes its own largest as the base of its sums, which are joined afterwards
+        const float mine = e.largest();
         RowSums s;
-        s.m = base_of(m);
-        float total = 0.0f, weighted = 0.0f;
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float z = (e[v][i] - s.m) * a.scale, p = __builtin_amdgcn_exp2f(z * kLog2e);
-                total += p;
-                weighted += p * larger(z, -1e4f);
-            }
-        total = team_sum<64>(total), weighted = team_sum<64>(weighted);
+        s.m = team_largest<64>(mine);
+        e.sums(Exponent(base_of(s.m), a.scale * kLog2e), s.total, s.weighted);
+        e.as_stored();
+        s.total = team_sum<64>(s.total), s.weighted = team_sum<64>(s.weighted) * kLn2;
         float bound = -infinity();
+        if (lane == 0) lds.count = 0;
         if constexpr (TPR > 64) {
-            if ((lane & 63) == 0) lds.total[wave] = total, lds.weighted[wave] = weighted;
-            if (a.k > 0 && wave == 0) {
-                bound = kth_largest(lds.group[lane], a.k);
-                if (lane == 0) lds.bound = bound;
-            }
+            const float group = team_largest<TPR / 64>(mine);
+            if ((lane & (TPR / 64 - 1)) == 0) lds.group[lane / (TPR / 64)] = group;
+            if ((lane & 63) == 0) lds.sums[wave] = s;
             __syncthreads();
-            total = team_sum<TPR / 64>(lds.total[lane & (TPR / 64 - 1)]), weighted = team_sum<TPR / 64>(lds.weighted[lane & (TPR / 64 - 1)]);
-            if (a.k > 0) bound = lds.bound;
+            s = joined<TPR / 64>(lds.sums[lane & (TPR / 64 - 1)], a.scale);
+            if (a.k > 0) {
+                if (wave == 0) {
+                    bound = kth_largest(lds.group[lane], a.k);
+                    if (lane == 0) lds.bound = bound;
+                }
+                __syncthreads();
+                bound = lds.bound;
+            }
         } else if (a.k > 0) {
-            bound = kth_largest(group, a.k);
+            bound = kth_largest(mine, a.k);
         }
-        s.total = total, s.weighted = weighted;
+        const float base = base_of(s.m);
         if (lane == 0) {
             if (a.parts == 1) {
-                write_row(a, row, token, logit, s.m, s);
+                write_row(a, row, token, logit, base, s);
             } else {
                 float* const to = a.partial + 4 * item;
-                to[0] = m, to[1] = total, to[2] = weighted;
+                to[0] = s.m, to[1] = s.total, to[2] = s.weighted;
             }
         }
         if (a.k > 0) {
             // whatever is not below the bound; -inf is no alternative, NaN above all
-            if (!(mine < bound) || m != m || total != total) {
+            if (!(mine < bound) || s.total != s.total) {
+                const int here = opaque(lane);
 #pragma unroll
                 for (int v = 0; v < NV; ++v)
 #pragma unroll
                     for (int i = 0; i < VEC; ++i)
-                        if (!(e[v][i] < bound) && e[v][i] != -infinity()) {
+                        if (!(e.at(v, i) < bound) && e.at(v, i) != -infinity()) {
                             const int at = atomicAdd(&lds.count, 1);
-                            if (at < TeamLds<TPR>::ROOM) lds.list[at] = key_of(e[v][i], off + col[v] + i);
+                            if (at < TeamLds<TPR>::ROOM) lds.list[at] = key_of(e.at(v, i), off + e.column(v, here, len, hi - lo) + i);
                         }
             }
             team_barrier<TPR>();
@@ -411,125 +481,135 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_answer_rows(AnswerAr
                         if (keys)
                             keys[rank] = key;
                         else
-                            write_top(a, row, rank, key, s.m, l);
+                            write_top(a, row, rank, key, base, l);
                     }
                 }
                 for (int place = count + lane; place < a.k; place += TPR) {
                     if (keys)
                         keys[place] = 0;
                     else
-                        write_top(a, row, place, 0, s.m, l);
+                        write_top(a, row, place, 0, base, l);
                 }
             } else {
                 uint64_t last = UINT64_C(1) << 60;  // (above every key)
                 for (int place = 0; place < a.k; ++place) {
                     uint64_t best = 0;
-#pragma unroll
-                    for (int v = 0; v < NV; ++v)
-#pragma unroll
-                        for (int i = 0; i < VEC; ++i) {
-                            const uint64_t key = e[v][i] != -infinity() ? key_of(e[v][i], off + col[v] + i) : 0;
-                            if (key < last && key > best) best = key;
-                        }
+                    for (int j = lane; j < len; j += TPR) {  // (as it is in memory: what is rare shall cost others no registers)
+                        const float y = widen(x[off + j]);
+                        const uint64_t key = y != -infinity() ? key_of(y, off + j) : 0;
+                        if (key < last && key > best) best = key;
+                    }
                     last = team_best<TPR>(best, lds);
                     if (lane == 0) {
                         if (keys)
                             keys[place] = last;
                         else
-                            write_top(a, row, place, last, s.m, l);
+                            write_top(a, row, place, last, base, l);
                     }
                 }
             }
-            team_barrier<TPR>();
         }
-        if constexpr (TPR > 64) __syncthreads();  // (the next row's numbers go where this one's were)
+        team_barrier<TPR>();  // (the next row's numbers go where this one's were)
     }
 }
 
 // The sums of a row's parts, in every lane of a wavefront.
-__device__ __forceinline__ RowSums join_parts(const float* partial, int parts, float scale, float* largest = nullptr)
+__device__ __forceinline__ RowSums join_parts(const float* partial, int parts, int lane, int lanes, float scale)
 {
-    const int lane = threadIdx.x & 63;
-    float m = -infinity();
-    for (int p = lane; p < parts; p += 64) m = larger(m, partial[4 * p]);
-    m = team_largest<64>(m);
-    RowSums s;
-    s.m = base_of(m);
-    float total = 0.0f, weighted = 0.0f;
-    for (int p = lane; p < parts; p += 64) {
-        // a part's sums are of exp(z - its own largest): z = (its largest - m) s + its own
-        const float own = partial[4 * p], t = partial[4 * p + 1];
-        const float z = (base_of(own) - s.m) * scale, f = own == -infinity() && t == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(z * kLog2e);
-        total += f * t;
-        weighted += f * (partial[4 * p + 2] + larger(z, -1e4f) * t);
+    RowSums s{-infinity(), 0.0f, 0.0f};
+    for (int p = lane; p < parts; p += lanes) {
+        const float4 q = *(const float4*)(partial + 4 * (int64_t)p);
+        const float m = larger(s.m, q.x), z = (base_of(s.m) - base_of(m)) * scale, y = (base_of(q.x) - base_of(m)) * scale;
+        const float f = s.total == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(z * kLog2e), g = q.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(y * kLog2e);
+        s.weighted = f * (s.weighted + larger(z, -1e4f) * s.total) + g * (q.z + larger(y, -1e4f) * q.y);
+        s.total = f * s.total + g * q.y;
+        s.m = m;
     }
-    s.total = team_sum<64>(total), s.weighted = team_sum<64>(weighted);
-    return s;
+    return joined<64>(s, scale);
 }
 
-// Joins the parts of a row: its sums, and the largest of the parts' keys by the same bound as above.
-template <typename T>
-__global__ __launch_bounds__(256) void gp_answer_join(AnswerArgs a)
+// Joins the parts of a row: its sums, and the largest of the parts' keys by the same bound as above, of 64 groups of lanes.  A wavefront for few
+// keys, a workgroup of 1,024 for many (one row of 190 parts by 20 keys 5 us; by 256 lanes 14).
+template <typename T, int LANES>
+__global__ __launch_bounds__(LANES) void gp_answer_join(AnswerArgs a)
 {
-    __shared__ uint64_t list[kRoom], group[64], bound_at, best_at[4];
+    constexpr int WAVES = LANES / 64;
+    __shared__ uint64_t list[kRoom], group[64], bound_at, best_at[WAVES];
+    __shared__ RowSums sums[WAVES];
     __shared__ int count;
+    const int lane = threadIdx.x;
     for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
-        const int64_t token = a.logp ? token_at(a.tokens, a.wide, row) : -1;
-        const RowSums s = join_parts(a.partial + 4 * row * a.parts, a.parts, a.scale);
-        if (threadIdx.x == 0) {
-            write_row(a, row, token, token >= 0 && token < a.C ? widen(((const T*)a.x)[row * a.ld + token]) : 0.0f, s.m, s);
-            count = 0;
-        }
-        if (a.k == 0) continue;
         const uint64_t* const keys = a.keys + row * a.parts * a.k;
         const int all = a.parts * a.k;
-        uint64_t mine = 0;
-        for (int j = threadIdx.x; j < all; j += 256) mine = key_max(mine, keys[j]);
-        uint64_t best = key_max(mine, shuffled(mine, 1));
-        best = key_max(best, shuffled(best, 2));
-        if ((threadIdx.x & 3) == 0) group[threadIdx.x >> 2] = best;
-        __syncthreads();
-        if (threadIdx.x < 64) {
-            const uint64_t g = group[threadIdx.x];
-            int above = 0;
-            for (int j = 0; j < 64; ++j) above += group[j] > g || (group[j] == g && j < (int)threadIdx.x);
-            if (above == a.k - 1) bound_at = g;
-        }
-        __syncthreads();
-        const uint64_t bound = bound_at;
-        for (int j = threadIdx.x; j < all; j += 256) {
-            const uint64_t key = keys[j];
-            if (key >= bound && key > 0) {
-                const int at = atomicAdd(&count, 1);
-                if (at < kRoom) list[at] = key;
-            }
-        }
-        __syncthreads();
-        const float l = s.log_total();
-        const int found = count;
-        if (found <= kRoom) {
-            for (int c = threadIdx.x; c < found; c += 256) {
-                const uint64_t key = list[c];
-                int rank = 0;
-                for (int j = 0; j < found; ++j) rank += list[j] > key;
-                if (rank < a.k) write_top(a, row, rank, key, s.m, l);
-            }
-            for (int place = found + threadIdx.x; place < a.k; place += 256) write_top(a, row, place, 0, s.m, l);
-        } else {
-            uint64_t last = UINT64_C(1) << 60;  // (above every key)
-            for (int place = 0; place < a.k; ++place) {
-                best = 0;
-                for (int j = threadIdx.x; j < all; j += 256) {
-                    const uint64_t key = keys[j];
-                    if (key < last && key > best) best = key;
-                }
+        const int64_t token = a.logp ? token_at(a.tokens, a.wide, row) : -1;
+        constexpr int OWN = 4;  // keys that a lane holds; what is beyond is read twice
+        uint64_t own[OWN], mine = 0;
 #pragma unroll
-                for (int w = 1; w < 64; w *= 2) best = key_max(best, shuffled(best, w));
-                if ((threadIdx.x & 63) == 0) best_at[threadIdx.x >> 6] = best;
-                __syncthreads();
-                last = key_max(key_max(best_at[0], best_at[1]), key_max(best_at[2], best_at[3]));
-                if (threadIdx.x == 0) write_top(a, row, place, last, s.m, l);
-                __syncthreads();
+        for (int i = 0; i < OWN; ++i) own[i] = i * LANES + lane < all ? keys[i * LANES + lane] : 0;
+        const float logit = token >= 0 && token < a.C ? widen(((const T*)a.x)[row * a.ld + token]) : 0.0f;
+        RowSums s = join_parts(a.partial + 4 * row * a.parts, a.parts, lane, LANES, a.scale);
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) mine = key_max(mine, own[i]);
+        for (int j = OWN * LANES + lane; j < all; j += LANES) mine = key_max(mine, keys[j]);
+        if constexpr (WAVES >= 2) mine = key_max(mine, moved_key<0xB1>(mine));
+        if constexpr (WAVES >= 4) mine = key_max(mine, moved_key<0x4E>(mine));
+        if constexpr (WAVES >= 8) mine = key_max(mine, moved_key<0x141>(mine));
+        if constexpr (WAVES >= 16) mine = key_max(mine, moved_key<0x140>(mine));
+        if ((lane & (WAVES - 1)) == 0) group[lane / WAVES] = mine;
+        if ((lane & 63) == 0) sums[lane >> 6] = s;
+        if (lane == 0) count = 0;
+        __syncthreads();
+        s = joined<WAVES>(sums[lane & (WAVES - 1)], a.scale);
+        const float base = base_of(s.m);
+        if (lane == 0) write_row(a, row, token, logit, base, s);
+        if (a.k > 0) {
+            if (lane < 64) {
+                const uint64_t g = group[lane];
+                int above = 0;
+#pragma unroll 16
+                for (int j = 0; j < 64; ++j) above += group[j] > g || (group[j] == g && j < lane);
+                if (above == a.k - 1) bound_at = g;
+            }
+            __syncthreads();
+            const uint64_t bound = bound_at;
+            const auto offer = [&](uint64_t key) {
+                if (key >= bound && key > 0) {
+                    const int at = atomicAdd(&count, 1);
+                    if (at < kRoom) list[at] = key;
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) offer(own[i]);
+            for (int j = OWN * LANES + lane; j < all; j += LANES) offer(keys[j]);
+            __syncthreads();
+            const float l = s.log_total();
+            const int found = count;
+            if (found <= kRoom) {
+                for (int c = lane; c < found; c += LANES) {
+                    const uint64_t key = list[c];
+                    int rank = 0;
+                    for (int j = 0; j < found; ++j) rank += list[j] > key;
+                    if (rank < a.k) write_top(a, row, rank, key, base, l);
+                }
+                for (int place = found + lane; place < a.k; place += LANES) write_top(a, row, place, 0, base, l);
+            } else {
+                uint64_t last = UINT64_C(1) << 60;  // (above every key)
+                for (int place = 0; place < a.k; ++place) {
+                    uint64_t best = 0;
+                    for (int j = lane; j < all; j += LANES) {
+                        const uint64_t key = keys[j];
+                        if (key < last && key > best) best = key;
+                    }
+#pragma unroll
+                    for (int w = 1; w < 64; w *= 2) best = key_max(best, shuffled(best, w));
+                    if ((lane & 63) == 0) best_at[lane >> 6] = best;
+                    __syncthreads();
+                    last = 0;
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) last = key_max(last, best_at[w]);
+                    if (lane == 0) write_top(a, row, place, last, base, l);
+                    __syncthreads();
+                }
             }
         }
         __syncthreads();
@@ -673,28 +753,20 @@ __global__ __launch_bounds__(256) void gp_distill_short(DistillArgs a)
     __shared__ __attribute__((aligned(16))) float cells[TEAMS][CELLS];
     const int lane = threadIdx.x % TPR;
     float* const mine = cells[threadIdx.x / TPR];
-    const float s = 1.0f / a.T;
+    const float c = kLog2e / a.T;
     for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR; row < a.N; row += (int64_t)gridDim.x * TEAMS) {
         const T* const x = (const T*)a.x + row * a.ld;
-        float e[NV][VEC];
-        int col[NV];
-        load_row<T, VEC, NV, TPR>(x, a.C, a.nvec, lane, e, col);
+        Row<T, VEC, NV, TPR> e;
+        e.load(x, a.C, a.nvec, lane);
         Teacher<TPR, PER> t;
         t.load(a, row, x, lane);
         float base, log_total;
         if (a.from) {
             base = a.from[2 * row], log_total = a.from[2 * row + 1];
         } else {
-            float m = -infinity(), total = 0.0f;
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) m = larger(m, e[v][i]);
-            base = base_of(team_largest<TPR>(m));
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) total += __builtin_amdgcn_exp2f((e[v][i] - base) * s * kLog2e);
+            float total, weighted;
+            base = base_of(team_largest<TPR>(e.largest()));
+            e.sums(Exponent(base, c), total, weighted);
             total = team_sum<TPR>(total);
             log_total = total == 0.0f ? 0.0f : logf(total);
         }
@@ -707,22 +779,22 @@ __global__ __launch_bounds__(256) void gp_distill_short(DistillArgs a)
             }
         }
         if (!a.grad) continue;
-        const float f = a.g[row * a.sg] * a.T;
+        const float f = a.g[row * a.sg] * a.T, l2 = log_total * kLog2e;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const float p = __builtin_amdgcn_exp2f(((e[v][i] - base) * s - log_total) * kLog2e);
+                const float p = __builtin_amdgcn_exp2f((e.at(v, i) - base) * c - l2);
                 mine[(v * TPR + lane) * VEC + i] = t.some ? f * p : 0.0f;
             }
         }
         team_barrier<64>();
         // (the last vector was moved back to end with the row; one lane of a team at a time, so that entries of one class go in their order)
         for (int i = 0; i < PER; ++i)
-            for (int j = 0; j < min(TPR, a.K - i * TPR); ++j) {
-                if (lane != j || t.at[i] < 0) continue;
-                const int c = t.at[i];
-                atomicAdd(c / VEC < a.nvec - 1 ? mine + c : mine + (a.nvec - 1) * VEC + (c - (a.C - VEC)), -f * t.q[i]);
+            for (int turn = 0; turn < min(TPR, a.K - i * TPR); ++turn) {
+                if (lane != turn || t.at[i] < 0) continue;
+                const int j = t.at[i];
+                atomicAdd(j / VEC < a.nvec - 1 ? mine + j : mine + (a.nvec - 1) * VEC + (j - (a.C - VEC)), -f * t.q[i]);
             }
         team_barrier<64>();
         T* const out = (T*)a.grad + row * a.ldg;
@@ -730,15 +802,16 @@ __global__ __launch_bounds__(256) void gp_distill_short(DistillArgs a)
         for (int v = 0; v < NV; ++v) {
             const int at = v * TPR + lane;
             if (at >= a.nvec) continue;
-            const int first = at * VEC - col[v];
+            const int col = e.column(v, lane, a.C, a.nvec), first = at * VEC - col;
+            float y[VEC];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) e[v][i] = mine[at * VEC + i];
+            for (int i = 0; i < VEC; ++i) y[i] = mine[at * VEC + i];
             if (first == 0) {
-                store_vec<T, VEC>(out + col[v], e[v]);
+                store_vec<T, VEC>(out + col, y);
             } else {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i)
-                    if (i >= first) out[col[v] + i] = narrow<T>(e[v][i]);
+                    if (i >= first) out[col + i] = narrow<T>(y[i]);
             }
         }
     }
@@ -749,19 +822,20 @@ template <typename T, int VEC, int NV, int TPR>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_distill_rows(DistillArgs a)
 {
     constexpr int BLOCK = TPR < 256 ? 256 : TPR, TEAMS = BLOCK / TPR, WAVES = TPR / 64;
-    __shared__ float lds[3][16];
-    const int lane = threadIdx.x % TPR, wave = lane >> 6;
+    __shared__ RowSums lds[WAVES];
+    __shared__ float some;
+    const int wave = threadIdx.x % TPR >> 6;
     const int64_t items = a.N * a.parts;
-    const float s = 1.0f / a.T;
-    for (int64_t item = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR; item < items; item += (int64_t)gridDim.x * TEAMS) {
+    const float c = kLog2e / a.T;
+    for (int64_t item = (int64_t)blockIdx.x * TEAMS + (TEAMS > 1 ? threadIdx.x / TPR : 0); item < items; item += (int64_t)gridDim.x * TEAMS) {
+        const int lane = opaque(threadIdx.x % TPR);
         const int64_t row = a.parts == 1 ? item : item / a.parts;
         const int part = a.parts == 1 ? 0 : (int)(item - row * a.parts);
         const int lo = (int)((int64_t)a.nvec * part / a.parts), hi = (int)((int64_t)a.nvec * (part + 1) / a.parts);
         const int off = lo * VEC, len = min(hi * VEC, a.C) - off;
         const T* const x = (const T*)a.x + row * a.ld;
-        float e[NV][VEC];
-        int col[NV];
-        load_row<T, VEC, NV, TPR>(x + off, len, hi - lo, lane, e, col);
+        Row<T, VEC, NV, TPR> e;
+        e.load(x + off, len, hi - lo, lane);
         Teacher<64, 1> t;
         t.some = true;
         if (wave == 0) t.load(a, row, x, lane);
@@ -769,29 +843,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_distill_rows(Distill
         if (a.from) {
             base = a.from[2 * row], log_total = a.from[2 * row + 1];
         } else {
-            float m = -infinity(), total = 0.0f;
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) m = larger(m, e[v][i]);
-            m = team_largest<64>(m);
+            RowSums sum;
+            sum.m = team_largest<64>(e.largest());
+            e.sums(Exponent(base_of(sum.m), c), sum.total, sum.weighted);
+            e.as_stored();
+            sum.total = team_sum<64>(sum.total);
+            sum.weighted = 0.0f;
             if constexpr (TPR > 64) {
-                if ((lane & 63) == 0) lds[0][wave] = m;
+                if ((lane & 63) == 0) lds[wave] = sum;
                 __syncthreads();
-                m = team_largest<WAVES>(lds[0][lane & (WAVES - 1)]);
+                sum = joined<WAVES>(lds[lane & (WAVES - 1)], 1.0f / a.T);
             }
-            base = base_of(m);
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) total += __builtin_amdgcn_exp2f((e[v][i] - base) * s * kLog2e);
-            total = team_sum<64>(total);
-            if constexpr (TPR > 64) {
-                if ((lane & 63) == 0) lds[1][wave] = total;
-                __syncthreads();
-                total = team_sum<WAVES>(lds[1][lane & (WAVES - 1)]);
-            }
-            log_total = total == 0.0f ? 0.0f : logf(total);
+            base = base_of(sum.m), log_total = sum.log_total();
         }
         if (wave == 0) {
             t.weigh(a.T);
@@ -808,40 +871,41 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_distill_rows(Distill
             continue;
         }
         if constexpr (TPR > 64) {
-            if (lane == 0) lds[2][0] = t.some ? 1.0f : 0.0f;
+            if (lane == 0) some = t.some ? 1.0f : 0.0f;
             __syncthreads();
-            t.some = lds[2][0] != 0.0f;
+            t.some = some != 0.0f;
         }
-        const float f = a.g[row * a.sg] * a.T;
+        const float f = a.g[row * a.sg] * a.T, l2 = log_total * kLog2e;
         T* const out = (T*)a.grad + row * a.ldg;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int at = v * TPR + lane;
             if (at >= hi - lo) continue;
-            const int first = at * VEC - col[v];
+            const int col = off + e.column(v, lane, len, hi - lo), first = off + at * VEC - col;
+            float y[VEC];
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const float p = __builtin_amdgcn_exp2f(((e[v][i] - base) * s - log_total) * kLog2e);
-                e[v][i] = t.some ? f * p : 0.0f;
+                const float p = __builtin_amdgcn_exp2f((e.at(v, i) - base) * c - l2);
+                y[i] = t.some ? f * p : 0.0f;
             }
             if (first == 0) {
-                store_vec<T, VEC>(out + off + col[v], e[v]);
+                store_vec<T, VEC>(out + col, y);
             } else {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i)
-                    if (i >= first) out[off + col[v] + i] = narrow<T>(e[v][i]);
+                    if (i >= first) out[col + i] = narrow<T>(y[i]);
             }
         }
         team_barrier<TPR>();  // (a workgroup's stores to one place are seen in their order)
         if (wave == 0) {
             float taken = 0.0f;
             for (int k = 0; k < a.K; ++k) {
-                const int c = __builtin_amdgcn_readlane(t.at[0], k);
+                const int at = __builtin_amdgcn_readlane(t.at[0], k);
                 const float q = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(t.q[0]), k));
-                if (c == t.at[0]) taken += q;
+                if (at == t.at[0]) taken += q;
             }
             if (t.some && t.at[0] >= off && t.at[0] < off + len) {
-                const float p = __builtin_amdgcn_exp2f(((t.logit[0] - base) * s - log_total) * kLog2e);
+                const float p = __builtin_amdgcn_exp2f((t.logit[0] - base) * c - l2);
                 out[t.at[0]] = narrow<T>(f * (p - taken));
             }
         }
@@ -857,12 +921,12 @@ __global__ __launch_bounds__(256) void gp_distill_join(DistillArgs a)
         const int lane = threadIdx.x & 63;
         Teacher<64, 1> t;
         t.load(a, row, (const T*)a.x + row * a.ld, lane);
-        const RowSums s = join_parts(a.partial + 4 * row * a.parts, a.parts, 1.0f / a.T);
+        const RowSums s = join_parts(a.partial + 4 * row * a.parts, a.parts, lane, 64, 1.0f / a.T);
         t.weigh(a.T);
-        const float l = s.log_total(), loss = t.some ? t.loss(a.T, s.m, l) : 0.0f;
+        const float base = base_of(s.m), l = s.log_total(), loss = t.some ? t.loss(a.T, base, l) : 0.0f;
         if (lane == 0) {
             if (a.loss) a.loss[row] = loss;
-            if (a.stats) a.stats[2 * row] = s.m, a.stats[2 * row + 1] = l;
+            if (a.stats) a.stats[2 * row] = base, a.stats[2 * row + 1] = l;
         }
     }
 }
@@ -940,9 +1004,9 @@ gp_status launch_rows(const AnswerArgs& a, int64_t longest, hipStream_t stream)
 {
     if (longest <= TPR) return launch_rows<T, VEC, 1, TPR>(a, stream);
     if (longest <= 2 * TPR) return launch_rows<T, VEC, 2, TPR>(a, stream);
-    if constexpr (TPR == 1024 && VEC * 4 < kLongestRow / 1024)
-        if (longest > 4 * TPR) return launch_rows<T, VEC, 8, TPR>(a, stream);
-    return launch_rows<T, VEC, 4, TPR>(a, stream);
+    if (TPR < 512 || longest <= 4 * TPR) return launch_rows<T, VEC, 4, TPR>(a, stream);
+    if constexpr (TPR >= 512) return launch_rows<T, VEC, 8, TPR>(a, stream);
+    return GP_OK;
 }
 // Rows of a wavefront or more, or parts of them
 template <typename T>
@@ -951,7 +1015,8 @@ gp_status launch_rows(const AnswerArgs& a, hipStream_t stream)
     const int64_t longest = (a.nvec + a.parts - 1) / a.parts;
     if (longest <= 256) return launch_rows<T, kVec<T>, 64>(a, longest, stream);
     if (longest <= 1024) return launch_rows<T, kVec<T>, 256>(a, longest, stream);
-    return launch_rows<T, kVec<T>, 1024>(a, longest, stream);
+    if (longest <= 4096) return launch_rows<T, kVec<T>, 512>(a, longest, stream);
+    return launch_rows<float, kVec<float>, 1024>(a, longest, stream);
 }
 
 template <typename T>
@@ -977,7 +1042,11 @@ gp_status launch_answer(AnswerArgs a, char* workspace, hipStream_t stream)
     gp_status st = launch_rows<T>(a, stream);
     if (st != GP_OK || a.parts == 1) return st;
     profile_begin("gp_answer_join", stream);
-    hipLaunchKernelGGL(gp_answer_join<T>, dim3((unsigned)std::min(a.N, kMaxBlocks)), dim3(256), 0, stream, a);
+    const dim3 grid((unsigned)std::min(a.N, kMaxBlocks));
+    if ((int64_t)a.parts * std::max(a.k, 1) <= 256)
+        hipLaunchKernelGGL((gp_answer_join<T, 64>), grid, dim3(64), 0, stream, a);
+    else
+        hipLaunchKernelGGL((gp_answer_join<T, 1024>), grid, dim3(1024), 0, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     return GP_OK;
@@ -1023,9 +1092,9 @@ gp_status launch_distill_rows(const DistillArgs& a, int64_t longest, hipStream_t
 {
     if (longest <= TPR) return launch_distill_rows<T, VEC, 1, TPR>(a, stream);
     if (longest <= 2 * TPR) return launch_distill_rows<T, VEC, 2, TPR>(a, stream);
-    if constexpr (TPR == 1024 && VEC * 4 < kLongestRow / 1024)
-        if (longest > 4 * TPR) return launch_distill_rows<T, VEC, 8, TPR>(a, stream);
-    return launch_distill_rows<T, VEC, 4, TPR>(a, stream);
+    if (TPR < 512 || longest <= 4 * TPR) return launch_distill_rows<T, VEC, 4, TPR>(a, stream);
+    if constexpr (TPR >= 512) return launch_distill_rows<T, VEC, 8, TPR>(a, stream);
+    return GP_OK;
 }
 template <typename T>
 gp_status launch_distill_rows(const DistillArgs& a, hipStream_t stream)
@@ -1033,7 +1102,8 @@ gp_status launch_distill_rows(const DistillArgs& a, hipStream_t stream)
     const int64_t longest = (a.nvec + a.parts - 1) / a.parts;
     if (longest <= 256) return launch_distill_rows<T, kVec<T>, 64>(a, longest, stream);
     if (longest <= 1024) return launch_distill_rows<T, kVec<T>, 256>(a, longest, stream);
-    return launch_distill_rows<T, kVec<T>, 1024>(a, longest, stream);
+    if (longest <= 4096) return launch_distill_rows<T, kVec<T>, 512>(a, longest, stream);
+    return launch_distill_rows<float, kVec<float>, 1024>(a, longest, stream);
 }
 
 template <typename T>

@@ -69,7 +69,7 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, int wide, int64_
     return wide ? ((const int64_t*)tokens)[i] : (int64_t)((const int32_t*)tokens)[i];
 }
 
-// All lanes of a team of W (a power of two up to 64, on a multiple of W) get the team's result.  Up to 16 lanes a step is a move inside the
+// All lanes of a team of W (a power of two up to 64, on a multiple of W) get the team's result, the same bits each.  Up to 16 lanes a step is a move inside the
 // instruction that uses it: neighbours, pairs, then mirrored halves (which hold the same by then); beyond, rows of 16 and halves of 32 change places.
 template <int CTRL>
 __device__ __forceinline__ unsigned moved(unsigned v)
@@ -102,7 +102,10 @@ __device__ __forceinline__ float team(float v, Op op)
 template <int W>
 __device__ __forceinline__ float team_sum(float v)
 {
-    return team<W>(v, [](float a, float b) { return a + b; });
+    return team<W>(v, [](float a, float b) {
+#pragma clang fp contract(off)  // (a product that one lane adds in one instruction and its neighbour in two gives them different bits)
+        return a + b;
+    });
 }
 template <int W>
 __device__ __forceinline__ float team_max(float v)

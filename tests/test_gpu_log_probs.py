@@ -145,6 +145,21 @@ def test_alternatives_that_all_lie_with_one_lane(C, period):
             check(gp.log_probs_tensors(y.bfloat16(), top=k), y.bfloat16(), None, 1.0, k)
 
 
+@pytest.mark.parametrize("C", [47, 700, 33_000])
+def test_tiny_and_negative_logits_keep_their_order(C):
+    import torch
+    gen, x, _ = logits_of(6, C, "f32")
+    x[0] *= 1e-40                     # below the type's normal numbers
+    x[1] = -x[1].abs() * 1e-40
+    x[2] = -x[2].abs() - 1
+    x[3] = -1e30 * x[3].abs() - 1e30
+    x[4] = -x[4].abs()
+    x[4, ::2] = -0.0
+    for y in (x, x.bfloat16()):
+        for k in (8, 40):
+            check(gp.log_probs_tensors(y, top=k), y, None, 1.0, k)
+
+
 def gradient(x, tokens, scale, g1, g2):
     return answers.log_probs_grad(x, tokens, scale, g1, g2)
 
