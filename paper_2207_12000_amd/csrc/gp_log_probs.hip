@@ -92,6 +92,17 @@ __device__ __forceinline__ uint64_t shuffled(uint64_t v, int mask)
 {
     return ((uint64_t)(unsigned)__shfl_xor((int)(v >> 32), mask, 64) << 32) | (unsigned)__shfl_xor((int)v, mask, 64);
 }
+// The same order for less, where NaN is 0x7FC00000: the logit's bits are a double's upper half, whose sign and magnitude order as a float's do, and the class
+// makes it larger the lower it is.
+__device__ __forceinline__ uint64_t double_of(float x, int j)
+{
+    const unsigned b = __float_as_uint(x + 0.0f);
+    return ((uint64_t)b << 32) | (unsigned)~(j ^ ((int)b >> 31));
+}
+__device__ __forceinline__ float logit_of_double(uint64_t d) { return __uint_as_float((unsigned)(d >> 32)); }
+__device__ __forceinline__ int class_of_double(uint64_t d) { return ~((int)(unsigned)d ^ ((int)(unsigned)(d >> 32) >> 31)); }
+constexpr uint64_t kBelowAll = UINT64_C(0xFFF0000000000000);  // the double -inf
+
 template <int CTRL>
 __device__ __forceinline__ uint64_t moved_key(uint64_t v)
 {
@@ -120,12 +131,15 @@ __device__ __forceinline__ RowSums joined(const RowSums& part, float scale)
     return s;
 }
 
+__device__ __forceinline__ void write_top(const AnswerArgs& a, int64_t row, int place, float x, int j, float base, float log_total)
+{
+    const bool none = x == -infinity();
+    a.top_index[row * a.k + place] = none ? -1 : j;
+    a.top_logp[row * a.k + place] = none ? -infinity() : (x - base) * a.scale - log_total;
+}
 __device__ __forceinline__ void write_top(const AnswerArgs& a, int64_t row, int place, uint64_t key, float base, float log_total)
 {
-    const float x = key ? logit_of(key) : -infinity();
-    const bool none = x == -infinity();
-    a.top_index[row * a.k + place] = none ? -1 : class_of(key);
-    a.top_logp[row * a.k + place] = none ? -infinity() : (x - base) * a.scale - log_total;
+    write_top(a, row, place, key ? logit_of(key) : -infinity(), class_of(key), base, log_total);
 }
 __device__ __forceinline__ void write_row(const AnswerArgs& a, int64_t row, int64_t token, float logit, float base, const RowSums& s)
 {
@@ -170,7 +184,7 @@ struct Row {
         for (int v = 0; v < NV; ++v) raw[v] = *reinterpret_cast<const typename Vec<T, VEC>::type*>(x + column(v, lane, len, nvec));
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            if (TPR < 64 && v < NV - 1) continue;
+            if (TPR < 64 && v < (NV <= 4 ? NV - 1 : NV - 2)) continue;
             if (TPR >= 64 && __builtin_amdgcn_readfirstlane(v * TPR + (int)(lane & ~63)) + 64 < nvec) continue;
             const int t = v * TPR + lane, first = t < nvec ? t * VEC - column(v, lane, len, nvec) : VEC;
             const T none = narrow<T>(-__builtin_inff());
@@ -193,6 +207,21 @@ struct Row {
                 Quad q = __builtin_bit_cast(Quad, raw[v]);
                 asm volatile("" : "+v"(q));
                 raw[v] = __builtin_bit_cast(typename Vec<T, VEC>::type, q);
+            }
+        }
+    }
+    // Every NaN in the one form that double_of takes.
+    __device__ __forceinline__ void one_nan()
+    {
+        const T nan = narrow<T>(__uint_as_float(0x7FC00000u));
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            if constexpr (VEC == 1) {
+                if (at(v, 0) != at(v, 0)) raw[v] = nan;
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (at(v, i) != at(v, i)) raw[v][i] = nan;
             }
         }
     }
@@ -294,6 +323,14 @@ __device__ __forceinline__ void team_merge(uint64_t (&list)[K])
     }
 }
 
+// The same number, of which the compiler knows nothing: what is worked out from it stays where it is needed, and is not kept in registers from one
+// row to the next (60 instead of 99 for rows of 32,768 in bf16, so that a compute unit has four workgroups of 512 and not two).
+__device__ __forceinline__ int opaque(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // ---- answers, rows of part of a wavefront ------------------------------------------------------------------------
 
 // KT: places of a lane's list, k or more (0: no alternatives)
@@ -301,8 +338,8 @@ template <typename T, int VEC, int NV, int TPR, int KT>
 __global__ __launch_bounds__(256) void gp_answer_short(AnswerArgs a)
 {
     constexpr int TEAMS = 256 / TPR;
-    const int lane = threadIdx.x % TPR;
     for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR; row < a.N; row += (int64_t)gridDim.x * TEAMS) {
+        const int lane = opaque(threadIdx.x % TPR);
         const T* const x = (const T*)a.x + row * a.ld;
         const int64_t token = a.logp ? token_at(a.tokens, a.wide, row) : -1;
         Row<T, VEC, NV, TPR> e;
@@ -315,33 +352,28 @@ __global__ __launch_bounds__(256) void gp_answer_short(AnswerArgs a)
         s.total = team_sum<TPR>(total), s.weighted = team_sum<TPR>(weighted) * kLn2;
         if (lane == 0) write_row(a, row, token, logit, s.m, s);
         if constexpr (KT > 0) {
-            uint64_t list[KT] = {};
+            if (s.total != s.total) e.one_nan();
+            uint64_t list[KT];  // (a team has eight elements or more: every place is taken)
+#pragma unroll
+            for (int i = 0; i < KT; ++i) list[i] = kBelowAll;
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) sort_in<KT>(list, key_of(e.at(v, i), e.column(v, lane, a.C, a.nvec) + i));
+                for (int i = 0; i < VEC; ++i) sort_in<KT>(list, double_of(e.at(v, i), e.column(v, lane, a.C, a.nvec) + i));
             team_merge<TPR, KT>(list);
             const float l = s.log_total();
             constexpr int MINE = (KT + TPR - 1) / TPR;
-            uint64_t key[MINE] = {};
+            uint64_t d[MINE] = {};
 #pragma unroll
-            for (int i = 0; i < KT; ++i) key[i / TPR] = lane == i % TPR ? list[i] : key[i / TPR];
+            for (int i = 0; i < KT; ++i) d[i / TPR] = lane == i % TPR ? list[i] : d[i / TPR];
 #pragma unroll
             for (int i = 0; i < MINE; ++i)
-                if (i * TPR + lane < a.k) write_top(a, row, i * TPR + lane, key[i], s.m, l);
+                if (i * TPR + lane < a.k) write_top(a, row, i * TPR + lane, logit_of_double(d[i]), class_of_double(d[i]), s.m, l);
         }
     }
 }
 
 // ---- answers, rows of a wavefront or a workgroup ----------------------------------------------------------------
-
-// The same number, of which the compiler knows nothing: what is worked out from it stays where it is needed, and is not kept in registers from one
-// row to the next (60 instead of 99 for rows of 32,768 in bf16, so that a compute unit has four workgroups of 512 and not two).
-__device__ __forceinline__ int opaque(int v)
-{
-    asm volatile("" : "+v"(v));
-    return v;
-}
 
 template <int TPR>
 __device__ __forceinline__ void team_barrier()
@@ -349,9 +381,9 @@ __device__ __forceinline__ void team_barrier()
     if constexpr (TPR > 64) {
         __syncthreads();
     } else {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
@@ -695,7 +727,7 @@ __device__ __forceinline__ float entry_logit(const DistillArgs& a, int64_t row, 
     return a.wide_teacher ? ((const float*)a.teacher)[row * a.ldv + k] : widen(((const bf16_t*)a.teacher)[row * a.ldv + k]);
 }
 
-// Entries of a row's teacher, PER of them in a lane of a team of W: k = i * W + lane.
+// Entries of a row's teacher, PER of them in a lane of a team of W: k = lane * PER + i.
 template <int W, int PER>
 struct Teacher {
     int at[PER];    // the class, -1: none
@@ -707,10 +739,10 @@ struct Teacher {
     {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int k = i * W + lane;
+            const int k = lane * PER + i;
             const int64_t j = k < a.K ? entry_index(a, row, k) : -1;
             at[i] = j >= 0 && j < a.C ? (int)j : -1;
-            q[i] = k < a.K && at[i] >= 0 ? entry_logit(a, row, k) : -infinity();
+            q[i] = at[i] >= 0 ? entry_logit(a, row, k) : -infinity();
             logit[i] = at[i] >= 0 ? widen(x[at[i]]) : 0.0f;
         }
     }
@@ -751,14 +783,14 @@ __global__ __launch_bounds__(256) void gp_distill_short(DistillArgs a)
 {
     constexpr int TEAMS = 256 / TPR, CELLS = NV * VEC * TPR;
     __shared__ __attribute__((aligned(16))) float cells[TEAMS][CELLS];
-    const int lane = threadIdx.x % TPR;
     float* const mine = cells[threadIdx.x / TPR];
     const float c = kLog2e / a.T;
     for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR; row < a.N; row += (int64_t)gridDim.x * TEAMS) {
+        const int lane = opaque(threadIdx.x % TPR);
         const T* const x = (const T*)a.x + row * a.ld;
         Row<T, VEC, NV, TPR> e;
-        e.load(x, a.C, a.nvec, lane);
         Teacher<TPR, PER> t;
+        e.load(x, a.C, a.nvec, lane);
         t.load(a, row, x, lane);
         float base, log_total;
         if (a.from) {
@@ -782,37 +814,40 @@ __global__ __launch_bounds__(256) void gp_distill_short(DistillArgs a)
         const float f = a.g[row * a.sg] * a.T, l2 = log_total * kLog2e;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
+            const int at = v * TPR + lane, col = e.column(v, lane, a.C, a.nvec), first = at < a.nvec ? at * VEC - col : VEC;
+            float y[VEC];
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 const float p = __builtin_amdgcn_exp2f((e.at(v, i) - base) * c - l2);
-                mine[(v * TPR + lane) * VEC + i] = t.some ? f * p : 0.0f;
+                y[i] = t.some ? f * p : 0.0f;
+            }
+            if (v < NV - 1) {  // (whole)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) mine[at * VEC + i] = y[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (i >= first) mine[col + i] = y[i];
             }
         }
         team_barrier<64>();
-        // (the last vector was moved back to end with the row; one lane of a team at a time, so that entries of one class go in their order)
-        for (int i = 0; i < PER; ++i)
-            for (int turn = 0; turn < min(TPR, a.K - i * TPR); ++turn) {
-                if (lane != turn || t.at[i] < 0) continue;
-                const int j = t.at[i];
-                atomicAdd(j / VEC < a.nvec - 1 ? mine + j : mine + (a.nvec - 1) * VEC + (j - (a.C - VEC)), -f * t.q[i]);
-            }
+        // one lane of a team at a time, so that entries of one class go in their order
+        for (int turn = 0; turn * PER < a.K; ++turn) {
+            if (lane != turn) continue;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (t.at[i] >= 0) atomicAdd(mine + t.at[i], -f * t.q[i]);
+        }
         team_barrier<64>();
         T* const out = (T*)a.grad + row * a.ldg;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int at = v * TPR + lane;
+            const int at = v * TPR + lane, col = v < NV - 1 ? at * VEC : (int)e.column(v, lane, a.C, a.nvec);
             if (at >= a.nvec) continue;
-            const int col = e.column(v, lane, a.C, a.nvec), first = at * VEC - col;
             float y[VEC];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) y[i] = mine[at * VEC + i];
-            if (first == 0) {
-                store_vec<T, VEC>(out + col, y);
-            } else {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i)
-                    if (i >= first) out[col + i] = narrow<T>(y[i]);
-            }
+            for (int i = 0; i < VEC; ++i) y[i] = mine[col + i];
+            store_vec<T, VEC>(out + col, y);
         }
     }
 }
@@ -951,12 +986,12 @@ int64_t row_parts(int64_t N, int64_t C, int vec)
     return std::max(parts, std::min(nvec / kPartVectors, (kFillParts + N - 1) / N));
 }
 
-// Lanes of a row's team: as few as hold it in four vectors each; more, up to `most`, where the rows make too few wavefronts.
-int team_lanes(int64_t N, int64_t nvec, int most)
+// Lanes of a row's team: `least`, or as few as hold it in `most` vectors each; more, up to 32, where the rows make too few wavefronts.
+int team_lanes(int64_t N, int64_t nvec, int least, int most)
 {
-    int lanes = 4;
-    while (lanes < most && nvec > lanes * 4) lanes *= 2;
-    while (lanes < most && nvec > lanes && N * lanes / 64 < kFull) lanes *= 2;
+    int lanes = least;
+    while (lanes < 32 && nvec > lanes * most) lanes *= 2;
+    while (lanes < 32 && nvec > lanes && N * lanes / 64 < kFull) lanes *= 2;
     return lanes;
 }
 
@@ -985,8 +1020,10 @@ gp_status launch_short(const AnswerArgs& a, hipStream_t stream)
     case 1: return launch_short<T, VEC, 1, TPR>(a, stream);
     case 2: return launch_short<T, VEC, 2, TPR>(a, stream);
     case 3: return launch_short<T, VEC, 3, TPR>(a, stream);
-    default: return launch_short<T, VEC, 4, TPR>(a, stream);
+    case 4: return launch_short<T, VEC, 4, TPR>(a, stream);
     }
+    if constexpr (VEC == 4) return a.nvec <= 6 * TPR ? launch_short<T, VEC, 6, TPR>(a, stream) : launch_short<T, VEC, 8, TPR>(a, stream);
+    return GP_OK;
 }
 template <typename T, int VEC, int NV, int TPR>
 gp_status launch_rows(const AnswerArgs& a, hipStream_t stream)
@@ -1029,7 +1066,8 @@ gp_status launch_answer(AnswerArgs a, char* workspace, hipStream_t stream)
     }
     a.nvec = (a.C + VEC - 1) / VEC;
     if (a.nvec <= 128 && a.k <= 8) {
-        switch (team_lanes(a.N, a.nvec, 32)) {
+        switch (team_lanes(a.N, a.nvec, 2, 32 / VEC)) {
+        case 2: return launch_short<T, VEC, 2>(a, stream);
         case 4: return launch_short<T, VEC, 4>(a, stream);
         case 8: return launch_short<T, VEC, 8>(a, stream);
         case 16: return launch_short<T, VEC, 16>(a, stream);
@@ -1058,8 +1096,10 @@ gp_status launch_distill_short(const DistillArgs& a, hipStream_t stream)
     constexpr int TEAMS = 256 / TPR;
     const dim3 grid((unsigned)std::min((a.N + TEAMS - 1) / TEAMS, kMaxBlocks));
     profile_begin("gp_distill_short", stream);
-    if (a.K <= 8)
-        hipLaunchKernelGGL((gp_distill_short<T, VEC, NV, TPR, (TPR < 8 ? 8 / TPR : 1)>), grid, dim3(256), 0, stream, a);
+    if constexpr (TPR < 8)
+        hipLaunchKernelGGL((gp_distill_short<T, VEC, NV, TPR, 8 / TPR>), grid, dim3(256), 0, stream, a);
+    else if (a.K <= 8)
+        hipLaunchKernelGGL((gp_distill_short<T, VEC, NV, TPR, 1>), grid, dim3(256), 0, stream, a);
     else
         hipLaunchKernelGGL((gp_distill_short<T, VEC, NV, TPR, kMostTop / TPR>), grid, dim3(256), 0, stream, a);
     profile_end(stream);
@@ -1117,7 +1157,7 @@ gp_status launch_distill(DistillArgs a, char* workspace, hipStream_t stream)
     }
     a.nvec = (a.C + VEC - 1) / VEC;
     if (a.nvec <= 128) {
-        switch (team_lanes(a.N, a.nvec, 32)) {
+        switch (team_lanes(a.N, a.nvec, a.K <= 8 ? 4 : 8, 4)) {  // (more entries than 8 a lane take too many registers)
         case 4: return launch_distill_short<T, VEC, 4>(a, stream);
         case 8: return launch_distill_short<T, VEC, 8>(a, stream);
         case 16: return launch_distill_short<T, VEC, 16>(a, stream);
