@@ -491,7 +491,7 @@ gp_status gp_layer_norm(const void *x, int64_t ldx, gp_dtype dtype, int64_t N, i
  *  x, stats, weight  as gp_layer_norm had and left them.
  *  x_grad  DEVICE, N x d of `dtype`, rows ldxg elements apart; may be x or grad itself (same type and distance of rows); NULL: not wanted.
  *  weight_grad, bias_grad  DEVICE, d of `weight_dtype` each; NULL: not wanted.  accumulate = 1: added to what they hold.
- *  workspace  gp_layer_norm_grad_workspace bytes; not needed where neither weight_grad nor bias_grad is wanted and d <= 16384.
+ *  workspace  gp_layer_norm_grad_workspace bytes (0 for few rows); not needed where neither weight_grad nor bias_grad is wanted and d <= 16384.
  * Sums over rows are taken in an order that depends on N, d and the types alone.  N at most 2^40 (else UNSUPPORTED).  Enqueued on hip_stream.
  * Errors: INVALID_ARG, UNSUPPORTED, OOM_HOST, DEVICE.  gp_layer_norm_grad_workspace: -1 for sizes that the call rejects. */
 int64_t gp_layer_norm_grad_workspace(int64_t N, int32_t d);

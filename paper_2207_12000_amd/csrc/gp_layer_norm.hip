@@ -46,6 +46,7 @@ struct NormGradArgs {
     float* partial;  // [workgroups][2][d]: sums of g h, sums of g
     float* means;    // long rows: [N][2], mean(u) and mean(u h)
     int64_t chunk;   // long rows: rows that one workgroup sums up
+    unsigned row_blocks;  // workgroups that have rows; those behind them have columns
 };
 
 __device__ __forceinline__ float parameter(const void* p, int wide, int i, float without)
@@ -165,6 +166,41 @@ __global__ __launch_bounds__(1024) void gp_norm_long(NormArgs a)
 
 // ---- backward -----------------------------------------------------------------------------------------------------
 
+__device__ __forceinline__ void write_sum(const NormGradArgs& a, bool of_weight, int64_t at, float sum)
+{
+    void* const to = of_weight ? a.weight_grad : a.bias_grad;
+    if (!to) return;
+    if (a.wide_weights)
+        ((float*)to)[at] = sum + (a.accumulate ? ((float*)to)[at] : 0.0f);
+    else
+        ((bf16_t*)to)[at] = narrow<bf16_t>(sum + (a.accumulate ? widen(((bf16_t*)to)[at]) : 0.0f));
+}
+
+// The sums of eight columns down all rows, by a workgroup: few rows are read once more from the caches sooner than a second launch has begun.
+template <typename TX, typename TG, int BLOCK>
+__device__ __forceinline__ void sum_columns(const NormGradArgs& a, unsigned block)
+{
+    __shared__ float sums[2][BLOCK / 64][8];
+    const int c = threadIdx.x & 7;
+    const int64_t j = (int64_t)block * 8 + c, at = min(j, (int64_t)a.d - 1);
+    float dw = 0.0f, db = 0.0f;
+#pragma unroll 4
+    for (int64_t row = threadIdx.x >> 3; row < a.N; row += BLOCK / 8) {
+        const float mean = a.stats[2 * row], r = a.stats[2 * row + 1];
+        const float g = widen(((const TG*)a.g)[row * a.ldg + at]), h = (widen(((const TX*)a.x)[row * a.ldx + at]) - mean) * r;
+        dw += g * h, db += g;
+    }
+#pragma unroll
+    for (int m = 8; m < 64; m *= 2) dw += __shfl_xor(dw, m, 64), db += __shfl_xor(db, m, 64);
+    if ((threadIdx.x & 63) < 8) sums[0][threadIdx.x >> 6][c] = dw, sums[1][threadIdx.x >> 6][c] = db;
+    __syncthreads();
+    if (threadIdx.x >= 16 || j >= a.d) return;
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < BLOCK / 64; ++w) sum += sums[threadIdx.x >> 3][w][c];
+    write_sum(a, threadIdx.x < 8, j, sum);
+}
+
 // x_grad may be x or g: a row is read before it is written.
 template <typename TX, typename TG, int VEC, int NV, int TPR>
 __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void gp_norm_grad_rows(NormGradArgs a)
@@ -174,6 +210,10 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void gp_norm_grad_rows(NormG
     constexpr int SETS = TPR < 64 ? BLOCK / 64 : TEAMS;  // sets of columns' sums that are left after a wavefront has added up its own
     __shared__ float lds[2][2][16];
     extern __shared__ float sums[];  // [SETS][2][NV * VEC][TPR] where SETS > 1
+    if (blockIdx.x >= a.row_blocks) {
+        sum_columns<TX, TG, BLOCK>(a, blockIdx.x - a.row_blocks);
+        return;
+    }
     const int lane = threadIdx.x % TPR;
     float w[NV][VEC], dw[NV][VEC] = {}, db[NV][VEC] = {};
     int col[NV], first = 0;
@@ -188,7 +228,7 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void gp_norm_grad_rows(NormG
     const float share = 1.0f / (float)a.d;
     int turn = 0;
     // (every team of a workgroup goes round as often: long ones meet at a barrier)
-    for (int64_t base = (int64_t)blockIdx.x * TEAMS; base < a.N; base += (int64_t)gridDim.x * TEAMS, turn ^= 1) {
+    for (int64_t base = (int64_t)blockIdx.x * TEAMS; base < a.N; base += (int64_t)a.row_blocks * TEAMS, turn ^= 1) {
         const int64_t row = base + threadIdx.x / TPR;
         const bool live = row < a.N;
         float h[NV][VEC], u[NV][VEC], su = 0.0f, suh = 0.0f, r = 0.0f;
@@ -290,14 +330,7 @@ __global__ __launch_bounds__(1024) void gp_norm_grad_join(NormGradArgs a, int64_
     for (int n = 16; n > 0; n /= 2)
 #pragma unroll
         for (int i = 0; i < n; ++i) part[i] += part[i + n];
-    const bool of_weight = j < a.d;
-    void* const to = of_weight ? a.weight_grad : a.bias_grad;
-    const int64_t at = of_weight ? j : j - a.d;
-    if (!to) return;
-    if (a.wide_weights)
-        ((float*)to)[at] = part[0] + (a.accumulate ? ((float*)to)[at] : 0.0f);
-    else
-        ((bf16_t*)to)[at] = narrow<bf16_t>(part[0] + (a.accumulate ? widen(((bf16_t*)to)[at]) : 0.0f));
+    write_sum(a, j < a.d, j < a.d ? j : j - a.d, part[0]);
 }
 
 // Rows too long for registers, first half: mean(u) and mean(u h) of a row.
@@ -407,6 +440,10 @@ gp_status launch_norm(NormArgs a, hipStream_t stream)
     }
 }
 
+// Few rows: their columns are summed by workgroups of their own in the same launch.  us on the GPU, one launch / rows' sums and a second one: 64 x 128
+// 3.5 / 5.8, 1000 x 256 4.9 / 6.9, 300 x 1000 5.3 / 8.6, 1000 x 1000 8.6 / 10.1, 128 x 8000 11.2 / 15.4; 2048 x 128 6.4 / 6.2, 2048 x 500 11.9 / 8.5 (fp32).
+bool few_rows(int64_t N, int64_t d) { return N <= 1024 && N * d <= (1 << 20); }
+
 // Workgroups of the backward pass, a row of sums each: two of 512 or one of 1,024 to a compute unit, fewer where rows are.
 template <int TPR>
 constexpr int kGradBlock = TPR < 512 ? 512 : TPR;
@@ -428,20 +465,39 @@ gp_status launch_join(const NormGradArgs& a, int64_t rows, hipStream_t stream)
 }
 
 template <typename TX, typename TG, int VEC, int NV, int TPR>
-gp_status launch_norm_grad(const NormGradArgs& a, hipStream_t stream)
+gp_status launch_grad_rows(const NormGradArgs& a, unsigned blocks, size_t lds, hipStream_t stream)
+{
+    profile_begin("gp_norm_grad_rows", stream);
+    hipLaunchKernelGGL((gp_norm_grad_rows<TX, TG, VEC, NV, TPR>), dim3(blocks), dim3(kGradBlock<TPR>), lds, stream, a);
+    profile_end(stream);
+    GP_HIP(hipGetLastError());
+    return GP_OK;
+}
+template <typename TX, typename TG, int VEC, int NV, int TPR>
+gp_status launch_norm_grad(NormGradArgs a, hipStream_t stream)
 {
     constexpr int BLOCK = kGradBlock<TPR>, TEAMS = BLOCK / TPR, SETS = TPR < 64 ? BLOCK / 64 : TEAMS;
     constexpr size_t lds = SETS > 1 ? (size_t)SETS * 2 * NV * VEC * TPR * 4 : 0;
+    const unsigned blocks = (unsigned)grad_blocks<TPR>(a.N), columns = a.weight_grad || a.bias_grad ? (unsigned)((a.d + 7) / 8) : 0;
+    if (few_rows(a.N, a.d)) {
+        a.partial = nullptr;
+        gp_status st = GP_OK;
+        if (columns && (a.x_grad == a.x || a.x_grad == a.g)) {  // what the columns' workgroups read, rows' would write: one after the other
+            a.row_blocks = 0;
+            st = launch_grad_rows<TX, TG, VEC, NV, TPR>(a, columns, 0, stream);
+            a.row_blocks = blocks;
+            return st == GP_OK ? launch_grad_rows<TX, TG, VEC, NV, TPR>(a, blocks, 0, stream) : st;
+        }
+        a.row_blocks = a.x_grad ? blocks : 0;
+        return launch_grad_rows<TX, TG, VEC, NV, TPR>(a, a.row_blocks + columns, 0, stream);
+    }
     if constexpr (lds > 0) {
         gp_status st = raise_lds<&gp_norm_grad_rows<TX, TG, VEC, NV, TPR>>(lds);
         if (st != GP_OK) return st;
     }
-    const int64_t blocks = grad_blocks<TPR>(a.N);
-    profile_begin("gp_norm_grad_rows", stream);
-    hipLaunchKernelGGL((gp_norm_grad_rows<TX, TG, VEC, NV, TPR>), dim3((unsigned)blocks), dim3(BLOCK), lds, stream, a);
-    profile_end(stream);
-    GP_HIP(hipGetLastError());
-    return launch_join(a, blocks, stream);
+    a.row_blocks = blocks;
+    gp_status st = launch_grad_rows<TX, TG, VEC, NV, TPR>(a, blocks, lds, stream);
+    return st == GP_OK ? launch_join(a, blocks, stream) : st;
 }
 template <typename TX, typename TG, int VEC, int TPR>
 gp_status launch_norm_grad(const NormGradArgs& a, hipStream_t stream)
@@ -516,7 +572,7 @@ NormGradLayout norm_grad_layout(int64_t N, int32_t d)
     const int64_t rows = d > kLongRow ? std::min(N, kLongChunks) : std::min(N, kUnits * 2), means = d > kLongRow ? N : 0;
     NormGradLayout l;
     l.partial = (8 * means + 255) / 256 * 256;
-    l.total = l.partial + (rows * 2 * d * 4 + 255) / 256 * 256;
+    l.total = few_rows(N, d) && d <= kLongRow ? 0 : l.partial + (rows * 2 * d * 4 + 255) / 256 * 256;
     return l;
 }
 
@@ -535,13 +591,13 @@ gp_status layer_norm_grad(const void* g, int64_t ldg, gp_dtype grad_dtype, const
     const bool sums = weight_grad || bias_grad;
     if (!x_grad && !sums) return GP_OK;
     const NormGradLayout l = norm_grad_layout(N, d);
-    if (N > 0 && (sums || d > kLongRow) && (!workspace || bytes < l.total || (uintptr_t)workspace % 256 != 0))
+    if (N > 0 && (sums || d > kLongRow) && l.total > 0 && (!workspace || bytes < l.total || (uintptr_t)workspace % 256 != 0))
         return fail(GP_ERR_INVALID_ARG, "need a workspace of %lld bytes on a 256-byte boundary", (long long)l.total);
     NormGradArgs a{};
     a.g = g, a.ldg = ldg, a.x = x, a.ldx = ldx, a.N = N, a.d = d, a.stats = stats, a.weight = weight, a.wide_weights = weight_dtype == GP_F32, a.x_grad = x_grad,
     a.ldxg = ldxg, a.weight_grad = weight_grad, a.bias_grad = bias_grad, a.accumulate = accumulate != 0;
     a.means = (float*)workspace;
-    a.partial = sums ? (float*)((char*)workspace + l.partial) : nullptr;
+    a.partial = sums && l.total > 0 ? (float*)((char*)workspace + l.partial) : nullptr;
     if (N == 0) return accumulate ? GP_OK : launch_join(a, 0, stream);  // (sums of nothing)
     if (dtype == GP_F32) return grad_dtype == GP_F32 ? launch_norm_grad<float, float>(a, stream) : launch_norm_grad<float, bf16_t>(a, stream);
     return grad_dtype == GP_F32 ? launch_norm_grad<bf16_t, float>(a, stream) : launch_norm_grad<bf16_t, bf16_t>(a, stream);

@@ -53,8 +53,8 @@ REFUSED = [
     (norm, dict(eps=NAN), BAD), (norm, dict(eps=float("inf")), BAD),
     (norm_grad, dict(grad_ptr=0), BAD), (norm_grad, dict(x_ptr=0), BAD), (norm_grad, dict(stats_ptr=0), BAD), (norm_grad, dict(dtype=9), BAD),
     (norm_grad, dict(grad_dtype=2), BAD), (norm_grad, dict(weight_dtype=2), BAD), (norm_grad, dict(N=-1), BAD), (norm_grad, dict(d=0), BAD),
-    (norm_grad, dict(ldg=7), BAD), (norm_grad, dict(ldx=7), BAD), (norm_grad, dict(ldxg=7), BAD), (norm_grad, dict(workspace_ptr=0), BAD),
-    (norm_grad, dict(workspace_ptr=P + 16), BAD), (norm_grad, dict(workspace_bytes=gp.gp_layer_norm_grad_workspace(4, 8) - 1), BAD),
+    (norm_grad, dict(ldg=7), BAD), (norm_grad, dict(ldx=7), BAD), (norm_grad, dict(ldxg=7), BAD), (norm_grad, dict(N=5000, workspace_ptr=0), BAD),
+    (norm_grad, dict(N=5000, workspace_ptr=P + 16), BAD), (norm_grad, dict(N=5000, workspace_bytes=gp.gp_layer_norm_grad_workspace(5000, 8) - 1), BAD),
     (norm_grad, dict(N=(1 << 40) + 1), NO),
     (norm_grad, dict(d=16385, ldx=16385, ldg=16385, ldxg=16385, weight_grad_ptr=0, bias_grad_ptr=0, workspace_ptr=0), BAD),
     (answer, dict(logits_ptr=0), BAD), (answer, dict(tokens_ptr=0), BAD), (answer, dict(top_index_ptr=0), BAD), (answer, dict(top_logp_ptr=0), BAD),
@@ -108,6 +108,7 @@ def test_workspace_sizes():
         assert gp.gp_log_probs_workspace(*bad) == -1
     for bad in ((-1, 8), ((1 << 40) + 1, 8), (4, 0), (4, (1 << 28) + 1)):
         assert gp.gp_distill_workspace(*bad) == -1
+    assert gp.gp_layer_norm_grad_workspace(4, 8) == 0 < gp.gp_layer_norm_grad_workspace(5000, 8) and gp.gp_layer_norm_grad_workspace(4, 17_000) > 0
     assert 0 < gp.gp_log_probs_workspace(1 << 40, 1 << 28, 64) < 1 << 63
     assert gp.gp_log_probs_workspace(1, 1 << 20, 0) < gp.gp_log_probs_workspace(1, 1 << 20, 1)
 
