@@ -54,6 +54,20 @@ __device__ __forceinline__ float parameter(const void* p, int wide, int i, float
     return !p ? without : wide ? ((const float*)p)[i] : widen(((const bf16_t*)p)[i]);
 }
 
+// VEC of them from place i on (16 bytes a request, whatever the place)
+template <int VEC>
+__device__ __forceinline__ void parameters(const void* p, int wide, int i, float without, float (&v)[VEC])
+{
+    if (!p) {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) v[k] = without;
+    } else if (wide) {
+        load_vec<float, VEC>((const float*)p + i, v);
+    } else {
+        load_vec<bf16_t, VEC>((const bf16_t*)p + i, v);
+    }
+}
+
 // The sum over a team of TPR lanes: of a part of a wavefront, or of a whole workgroup, whose `lds` (a float per wavefront) nothing else touches until
 // every wavefront has passed a later barrier.
 template <int TPR>
@@ -87,11 +101,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_norm_rows(NormArgs a
         const int t = v * TPR + lane;
         col[v] = t < a.nvec ? min(t * VEC, a.d - VEC) : 0;
         if (v == NV - 1) first = t < a.nvec ? t * VEC - col[v] : VEC;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            w[v][i] = parameter(a.weight, a.wide_weights, col[v] + i, 1.0f);
-            b[v][i] = parameter(a.bias, a.wide_weights, col[v] + i, 0.0f);
-        }
+        parameters<VEC>(a.weight, a.wide_weights, col[v], 1.0f, w[v]);
+        parameters<VEC>(a.bias, a.wide_weights, col[v], 0.0f, b[v]);
     }
     const float share = 1.0f / (float)a.d;
     for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR; row < a.N; row += (int64_t)gridDim.x * TEAMS) {
@@ -222,8 +233,7 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void gp_norm_grad_rows(NormG
         const int t = v * TPR + lane;
         col[v] = t < a.nvec ? min(t * VEC, a.d - VEC) : 0;
         if (v == NV - 1) first = t < a.nvec ? t * VEC - col[v] : VEC;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) w[v][i] = parameter(a.weight, a.wide_weights, col[v] + i, 1.0f);
+        parameters<VEC>(a.weight, a.wide_weights, col[v], 1.0f, w[v]);
     }
     const float share = 1.0f / (float)a.d;
     int turn = 0;
@@ -385,7 +395,7 @@ constexpr int64_t kLongChunks = 64;      // stretches of rows that long rows' we
 // Lanes of a row's team: as few as hold it in `most` vectors each; more, up to a wavefront, where the rows make too few wavefronts.
 int team_lanes(int64_t N, int64_t nvec, int most)
 {
-    int lanes = 8;
+    int lanes = 2;
     while (lanes < kMostLanes && nvec > (int64_t)lanes * most) lanes *= 2;
     while (lanes < 64 && nvec > lanes && N * lanes / 64 < kFull) lanes *= 2;
     return lanes;
@@ -428,7 +438,9 @@ gp_status launch_norm(NormArgs a, hipStream_t stream)
         return GP_OK;
     }
     a.nvec = (a.d + VEC - 1) / VEC;
-    switch (team_lanes(a.N, a.nvec, 4)) {
+    switch (team_lanes(a.N, a.nvec, 16 / VEC)) {
+    case 2: return launch_norm<TX, TY, VEC, 2>(a, stream);
+    case 4: return launch_norm<TX, TY, VEC, 4>(a, stream);
     case 8: return launch_norm<TX, TY, VEC, 8>(a, stream);
     case 16: return launch_norm<TX, TY, VEC, 16>(a, stream);
     case 32: return launch_norm<TX, TY, VEC, 32>(a, stream);
@@ -534,6 +546,8 @@ gp_status launch_norm_grad(NormGradArgs a, hipStream_t stream)
     }
     a.nvec = (a.d + VEC - 1) / VEC;
     switch (team_lanes(a.N, a.nvec, kGradElements / VEC)) {
+    case 2: return launch_norm_grad<TX, TG, VEC, 2>(a, stream);
+    case 4: return launch_norm_grad<TX, TG, VEC, 4>(a, stream);
     case 8: return launch_norm_grad<TX, TG, VEC, 8>(a, stream);
     case 16: return launch_norm_grad<TX, TG, VEC, 16>(a, stream);
     case 32: return launch_norm_grad<TX, TG, VEC, 32>(a, stream);

@@ -94,14 +94,15 @@ __device__ __forceinline__ uint64_t shuffled(uint64_t v, int mask)
 }
 // The same order for less, where NaN is 0x7FC00000: the logit's bits are a double's upper half, whose sign and magnitude order as a float's do, and the class
 // makes it larger the lower it is.
+constexpr uint64_t kBelowAll = UINT64_C(0xFFF0000000000000);  // the double -inf: a place that nothing took
 __device__ __forceinline__ uint64_t double_of(float x, int j)
 {
     const unsigned b = __float_as_uint(x + 0.0f);
     return ((uint64_t)b << 32) | (unsigned)~(j ^ ((int)b >> 31));
 }
-__device__ __forceinline__ float logit_of_double(uint64_t d) { return __uint_as_float((unsigned)(d >> 32)); }
+__device__ __forceinline__ float logit_of_double(uint64_t d) { return d == kBelowAll ? -infinity() : __uint_as_float((unsigned)(d >> 32)); }
 __device__ __forceinline__ int class_of_double(uint64_t d) { return ~((int)(unsigned)d ^ ((int)(unsigned)(d >> 32) >> 31)); }
-constexpr uint64_t kBelowAll = UINT64_C(0xFFF0000000000000);  // the double -inf
+constexpr int round_up(int n) { return n <= 1 ? 1 : 2 * round_up((n + 1) / 2); }  // to a power of two
 
 template <int CTRL>
 __device__ __forceinline__ uint64_t moved_key(uint64_t v)
@@ -139,7 +140,7 @@ __device__ __forceinline__ void write_top(const AnswerArgs& a, int64_t row, int 
 }
 __device__ __forceinline__ void write_top(const AnswerArgs& a, int64_t row, int place, uint64_t key, float base, float log_total)
 {
-    write_top(a, row, place, key ? logit_of(key) : -infinity(), class_of(key), base, log_total);
+    write_top(a, row, place, key ? logit_of(key) : -infinity(), key ? class_of(key) : -1, base, log_total);
 }
 __device__ __forceinline__ void write_row(const AnswerArgs& a, int64_t row, int64_t token, float logit, float base, const RowSums& s)
 {
@@ -184,7 +185,7 @@ struct Row {
         for (int v = 0; v < NV; ++v) raw[v] = *reinterpret_cast<const typename Vec<T, VEC>::type*>(x + column(v, lane, len, nvec));
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            if (TPR < 64 && v < (NV <= 4 ? NV - 1 : NV - 2)) continue;
+            if (TPR < 64 && VEC > 1 && v < (NV <= 4 ? NV - 1 : NV - 2)) continue;
             if (TPR >= 64 && __builtin_amdgcn_readfirstlane(v * TPR + (int)(lane & ~63)) + 64 < nvec) continue;
             const int t = v * TPR + lane, first = t < nvec ? t * VEC - column(v, lane, len, nvec) : VEC;
             const T none = narrow<T>(-__builtin_inff());
@@ -240,6 +241,16 @@ struct Row {
         }
         return m;
     }
+    // The largest of each fourth of this lane's elements.
+    __device__ __forceinline__ void largest_four(float (&m)[4]) const
+    {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) m[q] = -__builtin_inff();
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) m[i & 3] = larger(m[i & 3], at(v, i));
+    }
     template <typename Y>
     __device__ __forceinline__ void add_up(Y exponent, float& total, float& weighted)
     {
@@ -266,60 +277,93 @@ struct Row {
     }
 };
 
-// A list of K keys, largest first, and one more
-template <int K>
-__device__ __forceinline__ void sort_in(uint64_t (&list)[K], uint64_t key)
+// Sorted lists of keys in a lane's registers, largest first; lengths are powers of two.
+__device__ __forceinline__ void in_order(uint64_t& a, uint64_t& b)
 {
+    const uint64_t low = key_min(a, b);
+    a = key_max(a, b);
+    b = low;
+}
+// Places LO, LO + R, LO + 2 R ... of N: two sorted halves become one list (odd-even merging, K. E. Batcher 1968).
+template <int LO, int N, int R, int L>
+__device__ __forceinline__ void merge_halves(uint64_t (&list)[L])
+{
+    if constexpr (2 * R < N) {
+        merge_halves<LO, N, 2 * R>(list);
+        merge_halves<LO + R, N, 2 * R>(list);
 #pragma unroll
-    for (int i = 0; i < K; ++i) {
-        const uint64_t low = key_min(list[i], key);
-        list[i] = key_max(list[i], key);
-        key = low;
+        for (int i = LO + R; i + R < LO + N; i += 2 * R) in_order(list[i], list[i + R]);
+    } else {
+        in_order(list[LO], list[LO + R]);
     }
 }
-// The K largest of two lists, sorted: their maxima crosswise, put in order by neighbours.
-template <int K>
-__device__ __forceinline__ void merge(uint64_t (&list)[K], const uint64_t (&other)[K])
+template <int LO, int N, int L>
+__device__ __forceinline__ void sort_list(uint64_t (&list)[L])
 {
-#pragma unroll
-    for (int i = 0; i < K; ++i) list[i] = key_max(list[i], other[K - 1 - i]);
-#pragma unroll
-    for (int n = 0; n < K * (K - 1); ++n) {
-        const int round = n / (K - 1), i = n % (K - 1);
-        if ((i ^ round) & 1) continue;
-        const uint64_t hi = key_max(list[i], list[i + 1]);
-        list[i + 1] = key_min(list[i], list[i + 1]);
-        list[i] = hi;
+    if constexpr (N > 1) {
+        sort_list<LO, N / 2>(list);
+        sort_list<LO + N / 2, N / 2>(list);
+        merge_halves<LO, N, 1>(list);
     }
 }
-template <int W, int K>
-__device__ __forceinline__ void team_merge(uint64_t (&list)[K])
+// A list that first falls and then rises is put in order.
+template <int L>
+__device__ __forceinline__ void straighten(uint64_t (&list)[L])
 {
-    uint64_t other[K];
-    if constexpr (W >= 2) {
+    if constexpr (L > 1) {
 #pragma unroll
-        for (int i = 0; i < K; ++i) other[i] = moved_key<0xB1>(list[i]);
-        merge<K>(list, other);
+        for (int n = 0; n < L / 2; ++n) in_order(list[n], list[n + L / 2]);
+        if constexpr (L > 2) {
+#pragma unroll
+            for (int n = 0; n < L / 2; ++n) in_order(list[n / (L / 4) * (L / 2) + n % (L / 4)], list[n / (L / 4) * (L / 2) + n % (L / 4) + L / 4]);
+        }
+        if constexpr (L > 4) {
+#pragma unroll
+            for (int n = 0; n < L / 2; ++n) in_order(list[n / (L / 8) * (L / 4) + n % (L / 8)], list[n / (L / 8) * (L / 4) + n % (L / 8) + L / 8]);
+        }
+        if constexpr (L > 8) {
+#pragma unroll
+            for (int n = 0; n < L / 2; ++n) in_order(list[n / (L / 16) * (L / 8) + n % (L / 16)], list[n / (L / 16) * (L / 8) + n % (L / 16) + L / 16]);
+        }
+        if constexpr (L > 16) {
+#pragma unroll
+            for (int n = 0; n < L / 2; ++n) in_order(list[n / (L / 32) * (L / 16) + n % (L / 32)], list[n / (L / 32) * (L / 16) + n % (L / 32) + L / 32]);
+        }
+        if constexpr (L > 32) {
+#pragma unroll
+            for (int n = 0; n < L / 2; ++n) in_order(list[n / (L / 64) * (L / 32) + n % (L / 64)], list[n / (L / 64) * (L / 32) + n % (L / 64) + L / 64]);
+        }
     }
-    if constexpr (W >= 4) {
+}
+template <int W>
+__device__ __forceinline__ uint64_t from_other(uint64_t v)  // that of the lane W away, or of one that holds the same
+{
+    if constexpr (W == 1) return moved_key<0xB1>(v);
+    else if constexpr (W == 2) return moved_key<0x4E>(v);
+    else if constexpr (W == 4) return moved_key<0x141>(v);
+    else if constexpr (W == 8) return moved_key<0x140>(v);
+    else return shuffled(v, W);
+}
+// The K largest of a team's sorted lists of L, from lanes W away on: lists are put together until they have K places, from then on the larger of places
+// crosswise are the K largest of both.
+template <int K, int TPR, int W, int L>
+__device__ __forceinline__ void team_list(const uint64_t (&list)[L], uint64_t (&top)[K])
+{
+    if constexpr (W >= TPR) {
 #pragma unroll
-        for (int i = 0; i < K; ++i) other[i] = moved_key<0x4E>(list[i]);
-        merge<K>(list, other);
-    }
-    if constexpr (W >= 8) {
+        for (int i = 0; i < K; ++i) top[i] = i < L ? list[i] : kBelowAll;
+    } else if constexpr (2 * L <= K) {
+        uint64_t both[2 * L];
 #pragma unroll
-        for (int i = 0; i < K; ++i) other[i] = moved_key<0x141>(list[i]);
-        merge<K>(list, other);
-    }
-    if constexpr (W >= 16) {
+        for (int i = 0; i < L; ++i) both[i] = list[i], both[2 * L - 1 - i] = from_other<W>(list[i]);
+        straighten(both);
+        team_list<K, TPR, 2 * W>(both, top);
+    } else {
+        uint64_t both[L];
 #pragma unroll
-        for (int i = 0; i < K; ++i) other[i] = moved_key<0x140>(list[i]);
-        merge<K>(list, other);
-    }
-    if constexpr (W >= 32) {
-#pragma unroll
-        for (int i = 0; i < K; ++i) other[i] = shuffled(list[i], 16);
-        merge<K>(list, other);
+        for (int i = 0; i < L; ++i) both[i] = key_max(list[i], from_other<W>(list[L - 1 - i]));
+        straighten(both);
+        team_list<K, TPR, 2 * W>(both, top);
     }
 }
 
@@ -333,7 +377,7 @@ __device__ __forceinline__ int opaque(int v)
 
 // ---- answers, rows of part of a wavefront ------------------------------------------------------------------------
 
-// KT: places of a lane's list, k or more (0: no alternatives)
+// KT: places of a lane's list, as many as are asked for or as there are classes (0: no alternatives)
 template <typename T, int VEC, int NV, int TPR, int KT>
 __global__ __launch_bounds__(256) void gp_answer_short(AnswerArgs a)
 {
@@ -353,14 +397,28 @@ __global__ __launch_bounds__(256) void gp_answer_short(AnswerArgs a)
         if (lane == 0) write_row(a, row, token, logit, s.m, s);
         if constexpr (KT > 0) {
             if (s.total != s.total) e.one_nan();
-            uint64_t list[KT];  // (a team has eight elements or more: every place is taken)
+            // this lane's elements in stretches of KT or fewer, sorted and merged
+            constexpr int E = NV * VEC, L = KT < round_up(E) ? KT : round_up(E);
+            uint64_t mine[L], list[KT];
 #pragma unroll
-            for (int i = 0; i < KT; ++i) list[i] = kBelowAll;
+            for (int first = 0; first < E; first += L) {
+                uint64_t part[L];
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
+                for (int n = 0; n < L; ++n) {
+                    const int v = min(first + n, E - 1) / VEC, i = min(first + n, E - 1) % VEC;
+                    part[n] = first + n < E ? double_of(e.at(v, i), e.column(v, lane, a.C, a.nvec) + i) : kBelowAll;
+                }
+                sort_list<0, L>(part);
+                if (first == 0) {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) sort_in<KT>(list, double_of(e.at(v, i), e.column(v, lane, a.C, a.nvec) + i));
-            team_merge<TPR, KT>(list);
+                    for (int n = 0; n < L; ++n) mine[n] = part[n];
+                } else {
+#pragma unroll
+                    for (int n = 0; n < L; ++n) mine[n] = key_max(mine[n], part[L - 1 - n]);
+                    straighten(mine);
+                }
+            }
+            team_list<KT, TPR, 1>(mine, list);
             const float l = s.log_total();
             constexpr int MINE = (KT + TPR - 1) / TPR;
             uint64_t d[MINE] = {};
@@ -369,6 +427,7 @@ __global__ __launch_bounds__(256) void gp_answer_short(AnswerArgs a)
 #pragma unroll
             for (int i = 0; i < MINE; ++i)
                 if (i * TPR + lane < a.k) write_top(a, row, i * TPR + lane, logit_of_double(d[i]), class_of_double(d[i]), s.m, l);
+            for (int place = KT + lane; place < a.k; place += TPR) write_top(a, row, place, -infinity(), 0, s.m, l);  // (there are KT classes or fewer)
         }
     }
 }
@@ -392,28 +451,58 @@ template <int TPR>
 struct TeamLds {
     static constexpr int WAVES = TPR / 64, ROOM = TPR > 64 ? kRoom : kRoom / 4;
     RowSums sums[WAVES];
-    float group[64];
-    float bound;
+    unsigned group[TPR > 64 ? 256 : 1];
+    unsigned bound;
     int count;
     uint64_t best[WAVES];
-    uint64_t list[ROOM];
+    uint64_t list[ROOM + 8];
 };
 
-// The k-th largest of a wavefront's 64 values (k <= 64), in every lane: few by taking the largest away, many by counting.
-__device__ __forceinline__ float kth_largest(float v, int k)
+__device__ __forceinline__ unsigned ordered(float x)
 {
-    if (k <= 16) {
-        float last = infinity();
-        for (int r = 0; r < k; ++r) {
-            last = team_largest<64>(v);
-            const uint64_t with = __ballot(v == last);
-            if ((int)(threadIdx.x & 63) == __ffsll((unsigned long long)with) - 1) v = -infinity();
-        }
-        return last;
+    const unsigned b = __float_as_uint(x);
+    return b ^ ((unsigned)((int)b >> 31) | 0x80000000u);
+}
+// A bound that k or more of a wavefront's 256 values reach, and few others: the k-th largest to its first 16 bits, found bit by bit (0: fewer than k are there).
+__device__ __forceinline__ unsigned kth_bound(const unsigned (&v)[4], int k)
+{
+    unsigned t = 0;
+    for (int bit = 31; bit >= 16; --bit) {
+        const unsigned with = t | 1u << bit;
+        int n = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) n += __popcll(__ballot(v[q] >= with));
+        if (n >= k) t = with;
     }
-    int above = 0;
-    for (int l = 0; l < 64; ++l) above += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), l)) > v;
-    return -team_largest<64>(above < k ? -v : -infinity());
+    return t;
+}
+// As a float to compare with: what is not below it, and NaN, which is above everything, is not less.
+__device__ __forceinline__ float bound_of(unsigned t) { return __uint_as_float(t & 0x80000000u ? t & 0x7FFFFFFFu : ~t); }
+
+// Places for `mine` entries of every lane behind one another: this lane's first, and how many there are.
+__device__ __forceinline__ int places(int mine, int& all)
+{
+    int first = 0;
+    all = 0;
+    for (int bit = 0; __ballot(mine >> bit != 0) != 0; ++bit) {
+        const uint64_t with = __ballot(mine >> bit & 1);
+        first += __builtin_amdgcn_mbcnt_hi((unsigned)(with >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)with, 0)) << bit;
+        all += __popcll(with) << bit;
+    }
+    return first;
+}
+// How many of `count` keys in LDS are larger than `key`; eight reads are under way at a time, `list` has eight places more.
+__device__ __forceinline__ int rank_of(const uint64_t* list, int count, uint64_t key)
+{
+    int rank = 0;
+    for (int j = 0; j < count; j += 8) {
+        uint64_t other[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) other[u] = list[j + u];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) rank += j + u < count && other[u] > key;
+    }
+    return rank;
 }
 
 // Where the largest key of all is in `best` of every lane.
@@ -453,7 +542,13 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_answer_rows(AnswerAr
         e.load(x + off, len, hi - lo, lane);
         const float logit = token >= 0 && token < a.C ? widen(x[token]) : 0.0f;
         // every wavefront takes its own largest as the base of its sums, which are joined afterwards
-        const float mine = e.largest();
+        float four[4], mine;
+        if constexpr (TPR > 64) {
+            mine = e.largest();
+        } else {
+            e.largest_four(four);
+            mine = larger(larger(four[0], four[1]), larger(four[2], four[3]));
+        }
         RowSums s;
         s.m = team_largest<64>(mine);
         e.sums(Exponent(base_of(s.m), a.scale * kLog2e), s.total, s.weighted);
@@ -462,21 +557,24 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_answer_rows(AnswerAr
         float bound = -infinity();
         if (lane == 0) lds.count = 0;
         if constexpr (TPR > 64) {
-            const float group = team_largest<TPR / 64>(mine);
-            if ((lane & (TPR / 64 - 1)) == 0) lds.group[lane / (TPR / 64)] = group;
+            constexpr int LANES = TPR / 256;  // of one of the 256 groups
+            const unsigned group = ordered(team_largest<LANES>(mine));
+            if (lane % LANES == 0) lds.group[lane / LANES] = group;
             if ((lane & 63) == 0) lds.sums[wave] = s;
             __syncthreads();
             s = joined<TPR / 64>(lds.sums[lane & (TPR / 64 - 1)], a.scale);
             if (a.k > 0) {
                 if (wave == 0) {
-                    bound = kth_largest(lds.group[lane], a.k);
-                    if (lane == 0) lds.bound = bound;
+                    const unsigned v[4] = {lds.group[lane], lds.group[lane + 64], lds.group[lane + 128], lds.group[lane + 192]};
+                    const unsigned t = kth_bound(v, a.k);
+                    if (lane == 0) lds.bound = t;
                 }
                 __syncthreads();
-                bound = lds.bound;
+                bound = bound_of(lds.bound);
             }
         } else if (a.k > 0) {
-            bound = kth_largest(mine, a.k);
+            const unsigned v[4] = {ordered(four[0]), ordered(four[1]), ordered(four[2]), ordered(four[3])};
+            bound = bound_of(kth_bound(v, a.k));
         }
         const float base = base_of(s.m);
         if (lane == 0) {
@@ -489,36 +587,54 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_answer_rows(AnswerAr
         }
         if (a.k > 0) {
             // whatever is not below the bound; -inf is no alternative, NaN above all
-            if (!(mine < bound) || s.total != s.total) {
-                const int here = opaque(lane);
+            const int here = opaque(lane);
+            const bool look = !(mine < bound) || s.total != s.total;
+            int found = 0;
+            if (look) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) found += !(e.at(v, i) < bound) && e.at(v, i) != -infinity();
+            }
+            e.as_stored();
+            int all, at = places(found, all);
+            if constexpr (TPR > 64) {
+                if (all > 0) {
+                    int first = 0;
+                    if ((lane & 63) == 0) first = atomicAdd(&lds.count, all);
+                    at += __builtin_amdgcn_readfirstlane(first);
+                }
+            } else {
+                if (lane == 0) lds.count = all;
+            }
+            if (found > 0) {
 #pragma unroll
                 for (int v = 0; v < NV; ++v)
 #pragma unroll
                     for (int i = 0; i < VEC; ++i)
                         if (!(e.at(v, i) < bound) && e.at(v, i) != -infinity()) {
-                            const int at = atomicAdd(&lds.count, 1);
                             if (at < TeamLds<TPR>::ROOM) lds.list[at] = key_of(e.at(v, i), off + e.column(v, here, len, hi - lo) + i);
+                            ++at;
                         }
             }
             team_barrier<TPR>();
-            const int count = lds.count;
+            const int count = __builtin_amdgcn_readfirstlane(lds.count);
             const float l = s.log_total();
-            uint64_t* const keys = a.parts == 1 ? nullptr : a.keys + item * a.k;
+            uint64_t* const keys = a.parts == 1 ? nullptr : a.keys + row * a.parts * a.k + part;  // place by place, in each the parts side by side
             if (count <= TeamLds<TPR>::ROOM) {
                 for (int c = lane; c < count; c += TPR) {
                     const uint64_t key = lds.list[c];
-                    int rank = 0;
-                    for (int j = 0; j < count; ++j) rank += lds.list[j] > key;
+                    const int rank = rank_of(lds.list, count, key);
                     if (rank < a.k) {
                         if (keys)
-                            keys[rank] = key;
+                            keys[(int64_t)rank * a.parts] = key;
                         else
                             write_top(a, row, rank, key, base, l);
                     }
                 }
                 for (int place = count + lane; place < a.k; place += TPR) {
                     if (keys)
-                        keys[place] = 0;
+                        keys[(int64_t)place * a.parts] = 0;
                     else
                         write_top(a, row, place, 0, base, l);
                 }
@@ -534,7 +650,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_answer_rows(AnswerAr
                     last = team_best<TPR>(best, lds);
                     if (lane == 0) {
                         if (keys)
-                            keys[place] = last;
+                            keys[(int64_t)place * a.parts] = last;
                         else
                             write_top(a, row, place, last, base, l);
                     }
@@ -566,7 +682,8 @@ template <typename T, int LANES>
 __global__ __launch_bounds__(LANES) void gp_answer_join(AnswerArgs a)
 {
     constexpr int WAVES = LANES / 64;
-    __shared__ uint64_t list[kRoom], group[64], bound_at, best_at[WAVES];
+    __shared__ uint64_t list[kRoom + 8], best_at[WAVES];
+    __shared__ unsigned group[256], bound_at;
     __shared__ RowSums sums[WAVES];
     __shared__ int count;
     const int lane = threadIdx.x;
@@ -583,29 +700,29 @@ __global__ __launch_bounds__(LANES) void gp_answer_join(AnswerArgs a)
 #pragma unroll
         for (int i = 0; i < OWN; ++i) mine = key_max(mine, own[i]);
         for (int j = OWN * LANES + lane; j < all; j += LANES) mine = key_max(mine, keys[j]);
-        if constexpr (WAVES >= 2) mine = key_max(mine, moved_key<0xB1>(mine));
-        if constexpr (WAVES >= 4) mine = key_max(mine, moved_key<0x4E>(mine));
-        if constexpr (WAVES >= 8) mine = key_max(mine, moved_key<0x141>(mine));
-        if constexpr (WAVES >= 16) mine = key_max(mine, moved_key<0x140>(mine));
-        if ((lane & (WAVES - 1)) == 0) group[lane / WAVES] = mine;
-        if ((lane & 63) == 0) sums[lane >> 6] = s;
+        // (logits alone decide the bound: a key's upper part)
+        if constexpr (WAVES > 1) {
+            const unsigned o = (unsigned)(mine >> kIndexBits), p = max(o, moved<0xB1>(o)), q = max(p, moved<0x4E>(p));
+            if ((lane & 3) == 0) group[lane >> 2] = q;
+            if ((lane & 63) == 0) sums[lane >> 6] = s;
+        }
         if (lane == 0) count = 0;
         __syncthreads();
-        s = joined<WAVES>(sums[lane & (WAVES - 1)], a.scale);
+        if constexpr (WAVES > 1) s = joined<WAVES>(sums[lane & (WAVES - 1)], a.scale);
         const float base = base_of(s.m);
         if (lane == 0) write_row(a, row, token, logit, base, s);
         if (a.k > 0) {
             if (lane < 64) {
-                const uint64_t g = group[lane];
-                int above = 0;
-#pragma unroll 16
-                for (int j = 0; j < 64; ++j) above += group[j] > g || (group[j] == g && j < lane);
-                if (above == a.k - 1) bound_at = g;
+                unsigned v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = WAVES > 1 ? group[lane + 64 * i] : (unsigned)(own[i] >> kIndexBits);
+                const unsigned t = kth_bound(v, a.k);
+                if (lane == 0) bound_at = t;
             }
             __syncthreads();
-            const uint64_t bound = bound_at;
+            const unsigned bound = bound_at;
             const auto offer = [&](uint64_t key) {
-                if (key >= bound && key > 0) {
+                if ((unsigned)(key >> kIndexBits) >= bound && key > 0) {
                     const int at = atomicAdd(&count, 1);
                     if (at < kRoom) list[at] = key;
                 }
@@ -615,12 +732,11 @@ __global__ __launch_bounds__(LANES) void gp_answer_join(AnswerArgs a)
             for (int j = OWN * LANES + lane; j < all; j += LANES) offer(keys[j]);
             __syncthreads();
             const float l = s.log_total();
-            const int found = count;
+            const int found = __builtin_amdgcn_readfirstlane(count);
             if (found <= kRoom) {
                 for (int c = lane; c < found; c += LANES) {
                     const uint64_t key = list[c];
-                    int rank = 0;
-                    for (int j = 0; j < found; ++j) rank += list[j] > key;
+                    const int rank = rank_of(list, found, key);
                     if (rank < a.k) write_top(a, row, rank, key, base, l);
                 }
                 for (int place = found + lane; place < a.k; place += LANES) write_top(a, row, place, 0, base, l);
@@ -987,11 +1103,11 @@ int64_t row_parts(int64_t N, int64_t C, int vec)
 }
 
 // Lanes of a row's team: `least`, or as few as hold it in `most` vectors each; more, up to 32, where the rows make too few wavefronts.
-int team_lanes(int64_t N, int64_t nvec, int least, int most)
+int team_lanes(int64_t N, int64_t nvec, int least, int most, int widest = 32)
 {
     int lanes = least;
-    while (lanes < 32 && nvec > lanes * most) lanes *= 2;
-    while (lanes < 32 && nvec > lanes && N * lanes / 64 < kFull) lanes *= 2;
+    while (lanes < widest && nvec > lanes * most) lanes *= 2;
+    while (lanes < widest && nvec > lanes && N * lanes / 64 < kFull) lanes *= 2;
     return lanes;
 }
 
@@ -1005,25 +1121,36 @@ gp_status launch_short(const AnswerArgs& a, hipStream_t stream)
     GP_HIP(hipGetLastError());
     return GP_OK;
 }
+// Elements of a row that lists of more than 8 places are kept in registers for: beyond, a wavefront's or workgroup's bound finds them sooner.
+constexpr int kListRow = 256, kLongListRow = 128;
+
 template <typename T, int VEC, int NV, int TPR>
 gp_status launch_short(const AnswerArgs& a, hipStream_t stream)
 {
-    if (a.k == 0) return launch_short<T, VEC, NV, TPR, 0>(a, stream);
-    if (a.k <= 2) return launch_short<T, VEC, NV, TPR, 2>(a, stream);
-    if (a.k <= 5) return launch_short<T, VEC, NV, TPR, 5>(a, stream);
-    return launch_short<T, VEC, NV, TPR, 8>(a, stream);
+    const int places = std::min(a.k, a.C);
+    if (places == 0) return launch_short<T, VEC, NV, TPR, 0>(a, stream);
+    if (places == 1) return launch_short<T, VEC, NV, TPR, 1>(a, stream);
+    if (places <= 4) return launch_short<T, VEC, NV, TPR, 4>(a, stream);
+    if (places <= 8) return launch_short<T, VEC, NV, TPR, 8>(a, stream);
+    if constexpr (NV * VEC <= 16 && VEC > 1) {
+        if constexpr (TPR * 16 <= kListRow) {
+            if (places <= 16) return launch_short<T, VEC, NV, TPR, 16>(a, stream);
+            if (places <= 32) return launch_short<T, VEC, NV, TPR, 32>(a, stream);
+        }
+        if constexpr (TPR * 16 <= kLongListRow) return launch_short<T, VEC, NV, TPR, 64>(a, stream);
+    }
+    return fail(GP_ERR_UNSUPPORTED, "no kernel for %d alternatives of %d classes", a.k, a.C);
 }
 template <typename T, int VEC, int TPR>
 gp_status launch_short(const AnswerArgs& a, hipStream_t stream)
 {
-    switch ((a.nvec + TPR - 1) / TPR) {
-    case 1: return launch_short<T, VEC, 1, TPR>(a, stream);
-    case 2: return launch_short<T, VEC, 2, TPR>(a, stream);
-    case 3: return launch_short<T, VEC, 3, TPR>(a, stream);
-    case 4: return launch_short<T, VEC, 4, TPR>(a, stream);
-    }
-    if constexpr (VEC == 4) return a.nvec <= 6 * TPR ? launch_short<T, VEC, 6, TPR>(a, stream) : launch_short<T, VEC, 8, TPR>(a, stream);
-    return GP_OK;
+    const int need = (a.nvec + TPR - 1) / TPR;
+    if (need == 1) return launch_short<T, VEC, 1, TPR>(a, stream);
+    if (need == 2) return launch_short<T, VEC, 2, TPR>(a, stream);
+    if (need == 3) return launch_short<T, VEC, 3, TPR>(a, stream);
+    if (need == 4) return launch_short<T, VEC, 4, TPR>(a, stream);
+    if constexpr (VEC < 8) return need <= 6 ? launch_short<T, VEC, 6, TPR>(a, stream) : launch_short<T, VEC, 8, TPR>(a, stream);
+    return fail(GP_ERR_UNSUPPORTED, "no kernel for %d classes", a.C);
 }
 template <typename T, int VEC, int NV, int TPR>
 gp_status launch_rows(const AnswerArgs& a, hipStream_t stream)
@@ -1060,13 +1187,14 @@ template <typename T>
 gp_status launch_answer(AnswerArgs a, char* workspace, hipStream_t stream)
 {
     constexpr int VEC = kVec<T>;
-    if (a.C < VEC) {
+    if (a.C < VEC) {  // (a lane to a row)
         a.nvec = a.C;
-        return a.k <= 8 ? launch_short<T, 1, 1, 8>(a, stream) : launch_rows<T, 1, 1, 64>(a, stream);
+        return launch_short<T, 1, 1>(a, stream);
     }
     a.nvec = (a.C + VEC - 1) / VEC;
-    if (a.nvec <= 128 && a.k <= 8) {
-        switch (team_lanes(a.N, a.nvec, 2, 32 / VEC)) {
+    const int places = std::min(a.k, a.C);
+    if (places <= 8 ? a.nvec <= 128 : a.C <= (places <= 32 ? kListRow : kLongListRow)) {
+        switch (team_lanes(a.N, a.nvec, 2, (places <= 8 ? 32 : 16) / VEC, places <= 8 ? 32 : (places <= 32 ? kListRow : kLongListRow) / 16)) {
         case 2: return launch_short<T, VEC, 2>(a, stream);
         case 4: return launch_short<T, VEC, 4>(a, stream);
         case 8: return launch_short<T, VEC, 8>(a, stream);
@@ -1109,12 +1237,13 @@ gp_status launch_distill_short(const DistillArgs& a, hipStream_t stream)
 template <typename T, int VEC, int TPR>
 gp_status launch_distill_short(const DistillArgs& a, hipStream_t stream)
 {
-    switch ((a.nvec + TPR - 1) / TPR) {
-    case 1: return launch_distill_short<T, VEC, 1, TPR>(a, stream);
-    case 2: return launch_distill_short<T, VEC, 2, TPR>(a, stream);
-    case 3: return launch_distill_short<T, VEC, 3, TPR>(a, stream);
-    default: return launch_distill_short<T, VEC, 4, TPR>(a, stream);
-    }
+    const int need = (a.nvec + TPR - 1) / TPR;
+    if (need == 1) return launch_distill_short<T, VEC, 1, TPR>(a, stream);
+    if (need == 2) return launch_distill_short<T, VEC, 2, TPR>(a, stream);
+    if (need == 3) return launch_distill_short<T, VEC, 3, TPR>(a, stream);
+    if constexpr (VEC == 1)
+        if (need > 4) return need <= 6 ? launch_distill_short<T, VEC, 6, TPR>(a, stream) : launch_distill_short<T, VEC, 8, TPR>(a, stream);
+    return launch_distill_short<T, VEC, 4, TPR>(a, stream);
 }
 template <typename T, int VEC, int NV, int TPR>
 gp_status launch_distill_rows(const DistillArgs& a, hipStream_t stream)
@@ -1153,11 +1282,12 @@ gp_status launch_distill(DistillArgs a, char* workspace, hipStream_t stream)
     a.parts = 1;
     if (a.C < VEC) {
         a.nvec = a.C;
-        return launch_distill_short<T, 1, 1, 8>(a, stream);
+        return a.K <= 8 ? launch_distill_short<T, 1, 1>(a, stream) : launch_distill_short<T, 1, 1, 8>(a, stream);
     }
     a.nvec = (a.C + VEC - 1) / VEC;
     if (a.nvec <= 128) {
-        switch (team_lanes(a.N, a.nvec, a.K <= 8 ? 4 : 8, 4)) {  // (more entries than 8 a lane take too many registers)
+        switch (team_lanes(a.N, a.nvec, a.K > 8 ? 8 : a.nvec > 4 ? 4 : 2, 4)) {  // (more entries than 8 a lane take too many registers)
+        case 2: return launch_distill_short<T, VEC, 2>(a, stream);
         case 4: return launch_distill_short<T, VEC, 4>(a, stream);
         case 8: return launch_distill_short<T, VEC, 8>(a, stream);
         case 16: return launch_distill_short<T, VEC, 16>(a, stream);
