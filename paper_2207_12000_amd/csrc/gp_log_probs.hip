@@ -30,6 +30,7 @@ namespace {
 constexpr int kMostTop = 64;      // alternatives, and entries of a teacher: one to a lane of a wavefront
 constexpr int kIndexBits = 28;    // of a class in a key
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr int kFewTop = 32;       // alternatives up to which 64 groups bound them: 8.5 logits reach the bound for 8, 44 for 32
 constexpr int kRoom = 1024;       // keys that a workgroup's list has room for (a wavefront's: a quarter)
 
 struct AnswerArgs {
@@ -451,8 +452,8 @@ template <int TPR>
 struct TeamLds {
     static constexpr int WAVES = TPR / 64, ROOM = TPR > 64 ? kRoom : kRoom / 4;
     RowSums sums[WAVES];
-    unsigned group[TPR > 64 ? 256 : 1];
-    unsigned bound;
+    float group[TPR > 64 ? 256 : 1];
+    float bound;
     int count;
     uint64_t best[WAVES];
     uint64_t list[ROOM + 8];
@@ -462,6 +463,22 @@ __device__ __forceinline__ unsigned ordered(float x)
 {
     const unsigned b = __float_as_uint(x);
     return b ^ ((unsigned)((int)b >> 31) | 0x80000000u);
+}
+// The k-th largest of a wavefront's 64 values (k <= 64), in every lane: few by taking the largest away, many by counting.
+__device__ __forceinline__ float kth_largest(float v, int k)
+{
+    if (k <= 16) {
+        float last = infinity();
+        for (int r = 0; r < k; ++r) {
+            last = team_largest<64>(v);
+            const uint64_t with = __ballot(v == last);
+            if ((int)(threadIdx.x & 63) == __ffsll((unsigned long long)with) - 1) v = -infinity();
+        }
+        return last;
+    }
+    int above = 0;
+    for (int l = 0; l < 64; ++l) above += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), l)) > v;
+    return -team_largest<64>(above < k ? -v : -infinity());
 }
 // A bound that k or more of a wavefront's 256 values reach, and few others: the k-th largest to its first 16 bits, found bit by bit (0: fewer than k are there).
 __device__ __forceinline__ unsigned kth_bound(const unsigned (&v)[4], int k)
@@ -479,18 +496,6 @@ __device__ __forceinline__ unsigned kth_bound(const unsigned (&v)[4], int k)
 // As a float to compare with: what is not below it, and NaN, which is above everything, is not less.
 __device__ __forceinline__ float bound_of(unsigned t) { return __uint_as_float(t & 0x80000000u ? t & 0x7FFFFFFFu : ~t); }
 
-// Places for `mine` entries of every lane behind one another: this lane's first, and how many there are.
-__device__ __forceinline__ int places(int mine, int& all)
-{
-    int first = 0;
-    all = 0;
-    for (int bit = 0; __ballot(mine >> bit != 0) != 0; ++bit) {
-        const uint64_t with = __ballot(mine >> bit & 1);
-        first += __builtin_amdgcn_mbcnt_hi((unsigned)(with >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)with, 0)) << bit;
-        all += __popcll(with) << bit;
-    }
-    return first;
-}
 // How many of `count` keys in LDS are larger than `key`; eight reads are under way at a time, `list` has eight places more.
 __device__ __forceinline__ int rank_of(const uint64_t* list, int count, uint64_t key)
 {
@@ -542,13 +547,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_answer_rows(AnswerAr
         e.load(x + off, len, hi - lo, lane);
         const float logit = token >= 0 && token < a.C ? widen(x[token]) : 0.0f;
         // every wavefront takes its own largest as the base of its sums, which are joined afterwards
-        float four[4], mine;
-        if constexpr (TPR > 64) {
-            mine = e.largest();
-        } else {
-            e.largest_four(four);
-            mine = larger(larger(four[0], four[1]), larger(four[2], four[3]));
-        }
+        const float mine = e.largest();
         RowSums s;
         s.m = team_largest<64>(mine);
         e.sums(Exponent(base_of(s.m), a.scale * kLog2e), s.total, s.weighted);
@@ -557,24 +556,34 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_answer_rows(AnswerAr
         float bound = -infinity();
         if (lane == 0) lds.count = 0;
         if constexpr (TPR > 64) {
-            constexpr int LANES = TPR / 256;  // of one of the 256 groups
-            const unsigned group = ordered(team_largest<LANES>(mine));
-            if (lane % LANES == 0) lds.group[lane / LANES] = group;
+            // the largest of 64 groups of lanes, or of 256
+            const bool many = a.k > kFewTop;
+            const float pair = team_largest<TPR / 256>(mine), group = many ? pair : team_largest<TPR / 64>(mine);
+            const int lanes = many ? TPR / 256 : TPR / 64;
+            if ((lane & (lanes - 1)) == 0) lds.group[lane / lanes] = group;
             if ((lane & 63) == 0) lds.sums[wave] = s;
             __syncthreads();
             s = joined<TPR / 64>(lds.sums[lane & (TPR / 64 - 1)], a.scale);
             if (a.k > 0) {
                 if (wave == 0) {
-                    const unsigned v[4] = {lds.group[lane], lds.group[lane + 64], lds.group[lane + 128], lds.group[lane + 192]};
-                    const unsigned t = kth_bound(v, a.k);
-                    if (lane == 0) lds.bound = t;
+                    if (many) {
+                        const unsigned v[4] = {ordered(lds.group[lane]), ordered(lds.group[lane + 64]), ordered(lds.group[lane + 128]), ordered(lds.group[lane + 192])};
+                        bound = bound_of(kth_bound(v, a.k));
+                    } else {
+                        bound = kth_largest(lds.group[lane], a.k);
+                    }
+                    if (lane == 0) lds.bound = bound;
                 }
                 __syncthreads();
-                bound = bound_of(lds.bound);
+                bound = lds.bound;
             }
-        } else if (a.k > 0) {
+        } else if (a.k > kFewTop) {
+            float four[4];
+            e.largest_four(four);
             const unsigned v[4] = {ordered(four[0]), ordered(four[1]), ordered(four[2]), ordered(four[3])};
             bound = bound_of(kth_bound(v, a.k));
+        } else if (a.k > 0) {
+            bound = kth_largest(mine, a.k);
         }
         const float base = base_of(s.m);
         if (lane == 0) {
@@ -587,34 +596,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_answer_rows(AnswerAr
         }
         if (a.k > 0) {
             // whatever is not below the bound; -inf is no alternative, NaN above all
-            const int here = opaque(lane);
-            const bool look = !(mine < bound) || s.total != s.total;
-            int found = 0;
-            if (look) {
-#pragma unroll
-                for (int v = 0; v < NV; ++v)
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) found += !(e.at(v, i) < bound) && e.at(v, i) != -infinity();
-            }
-            e.as_stored();
-            int all, at = places(found, all);
-            if constexpr (TPR > 64) {
-                if (all > 0) {
-                    int first = 0;
-                    if ((lane & 63) == 0) first = atomicAdd(&lds.count, all);
-                    at += __builtin_amdgcn_readfirstlane(first);
-                }
-            } else {
-                if (lane == 0) lds.count = all;
-            }
-            if (found > 0) {
+            if (!(mine < bound) || s.total != s.total) {
+                const int here = opaque(lane);
 #pragma unroll
                 for (int v = 0; v < NV; ++v)
 #pragma unroll
                     for (int i = 0; i < VEC; ++i)
                         if (!(e.at(v, i) < bound) && e.at(v, i) != -infinity()) {
+                            const int at = atomicAdd(&lds.count, 1);
                             if (at < TeamLds<TPR>::ROOM) lds.list[at] = key_of(e.at(v, i), off + e.column(v, here, len, hi - lo) + i);
-                            ++at;
                         }
             }
             team_barrier<TPR>();
@@ -1218,21 +1208,26 @@ gp_status launch_answer(AnswerArgs a, char* workspace, hipStream_t stream)
     return GP_OK;
 }
 
-template <typename T, int VEC, int NV, int TPR>
+template <typename T, int VEC, int NV, int TPR, int PER>
 gp_status launch_distill_short(const DistillArgs& a, hipStream_t stream)
 {
     constexpr int TEAMS = 256 / TPR;
-    const dim3 grid((unsigned)std::min((a.N + TEAMS - 1) / TEAMS, kMaxBlocks));
     profile_begin("gp_distill_short", stream);
-    if constexpr (TPR < 8)
-        hipLaunchKernelGGL((gp_distill_short<T, VEC, NV, TPR, 8 / TPR>), grid, dim3(256), 0, stream, a);
-    else if (a.K <= 8)
-        hipLaunchKernelGGL((gp_distill_short<T, VEC, NV, TPR, 1>), grid, dim3(256), 0, stream, a);
-    else
-        hipLaunchKernelGGL((gp_distill_short<T, VEC, NV, TPR, kMostTop / TPR>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((gp_distill_short<T, VEC, NV, TPR, PER>), dim3((unsigned)std::min((a.N + TEAMS - 1) / TEAMS, kMaxBlocks)), dim3(256), 0, stream, a);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     return GP_OK;
+}
+template <typename T, int VEC, int NV, int TPR>
+gp_status launch_distill_short(const DistillArgs& a, hipStream_t stream)
+{
+    if (a.K <= TPR) return launch_distill_short<T, VEC, NV, TPR, 1>(a, stream);
+    if (a.K <= 2 * TPR) return launch_distill_short<T, VEC, NV, TPR, 2>(a, stream);
+    if constexpr (TPR <= 16)
+        if (a.K <= 4 * TPR) return launch_distill_short<T, VEC, NV, TPR, 4>(a, stream);
+    if constexpr (TPR <= 8)
+        if (a.K <= 8 * TPR) return launch_distill_short<T, VEC, NV, TPR, 8>(a, stream);
+    return fail(GP_ERR_UNSUPPORTED, "no kernel for %d entries of %d classes", a.K, a.C);
 }
 template <typename T, int VEC, int TPR>
 gp_status launch_distill_short(const DistillArgs& a, hipStream_t stream)
@@ -1286,7 +1281,7 @@ gp_status launch_distill(DistillArgs a, char* workspace, hipStream_t stream)
     }
     a.nvec = (a.C + VEC - 1) / VEC;
     if (a.nvec <= 128) {
-        switch (team_lanes(a.N, a.nvec, a.K > 8 ? 8 : a.nvec > 4 ? 4 : 2, 4)) {  // (more entries than 8 a lane take too many registers)
+        switch (team_lanes(a.N, a.nvec, a.K > 32 ? 8 : a.K > 16 || a.nvec > 4 ? 4 : 2, 4)) {  // (at most eight entries to a lane)
         case 2: return launch_distill_short<T, VEC, 2>(a, stream);
         case 4: return launch_distill_short<T, VEC, 4>(a, stream);
         case 8: return launch_distill_short<T, VEC, 8>(a, stream);
