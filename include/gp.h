@@ -536,7 +536,7 @@ gp_status gp_log_probs_grad(const void *logits, int64_t ld, gp_dtype dtype, int6
  *  teacher_index   DEVICE, N x K class numbers of type `index`, rows ldi elements apart; one outside [0, C) makes its entry none (-1 ends a
  *                  shorter list).  A class may be named more than once.   teacher_logits  DEVICE, N x K of teacher_dtype, rows ldt elements apart
  *                  (logits or log probabilities: a row's common offset does not matter); -inf makes its entry none.  1 <= K <= 64.
- *  A row without an entry has loss and gradient 0.   temperature: within 1e-30 .. 1e30.
+ *  A row without an entry has loss and gradient 0.   temperature: within 1e-15 .. 1e15.
  *  loss    DEVICE, N fp32;  stats  DEVICE, N x 2 fp32, what gp_distill_grad needs.  NULL: not wanted.
  *  grad    DEVICE, N x C of `dtype`, rows ldg elements apart, made in the same pass from grad_loss (DEVICE, fp32, elements stride_loss apart: 1, or 0);
  *          must not overlap the inputs; NULL: not wanted.

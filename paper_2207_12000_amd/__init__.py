@@ -831,11 +831,22 @@ def _followed(t, stream):
     import torch
     if t is None or not (t.requires_grad and torch.is_grad_enabled()):
         return False
+    if not t.is_cuda:
+        raise ValueError("tensors must be on the GPU")
     if stream is not None:
         raise ValueError("a call that automatic differentiation follows runs on the current stream: set that one")
-    if torch.cuda.is_current_stream_capturing():
+    with contextlib.nullcontext() if t.get_device() == torch.cuda.current_device() else torch.cuda.device(t.device):
+        capturing = torch.cuda.is_current_stream_capturing()
+    if capturing:
         raise ValueError("a call that automatic differentiation follows is not captured: capture it under torch.no_grad(), and the gradient's own call")
     return True
+
+
+def _not_captured():
+    """A backward pass in a capture may meet leaves that a graph outside it has as well, which ends the process: the gradient's own calls can be captured."""
+    import torch
+    if torch.cuda.is_current_stream_capturing():
+        raise ValueError("a backward pass is not captured: capture the gradient's own call")
 
 
 def _as_rows(t, what):
@@ -903,6 +914,7 @@ def _differentiable_norm():
         @staticmethod
         @torch.autograd.function.once_differentiable
         def backward(ctx, grad):
+            _not_captured()
             x, weight, stats = ctx.saved_tensors
             want = ctx.needs_input_grad
             rows = grad.reshape(-1, x.shape[-1])
@@ -956,7 +968,8 @@ def layer_norm_grad_tensors(grad, x, stats, weight=None, x_grad=None, weight_gra
     """Convenience for torch tensors: the gradients of layer_norm_tensors from grad, the gradient of what it returned, and the stats it left.  Returns
     (x_grad, weight_grad, bias_grad): each is made where None is given, filled where a tensor is, left out (None) where False is.  accumulate: weight_grad
     and bias_grad are added to (both given, or False).  weight_dtype: of the gradients that are made (weight's; float32 without one).  workspace: a uint8
-    GPU tensor of gp_layer_norm_grad_workspace(rows, d) bytes or more, kept by the caller; without one the call takes its memory from torch."""
+    GPU tensor of gp_layer_norm_grad_workspace(rows, d) bytes or more, kept by the caller; without one the call takes its memory from torch.  Automatic
+    differentiation does not follow it."""
     import torch
     dtype, grad_dtype = _float_type(x), _float_type(grad)
     rows, up = _as_rows(x, "x"), _as_rows(grad, "grad")
@@ -1014,7 +1027,7 @@ class LogProbs(NamedTuple):
 
 def _rows_of_logits(logits, tokens):
     rows = _as_rows(logits, "logits")
-    if tokens is not None and tuple(tokens.shape) != tuple(logits.shape[:-1]):
+    if tokens is not None and tokens.shape != logits.shape[:-1]:
         raise ValueError("tokens must hold one class per row")
     return rows, _row_stride(rows, "logits")
 
@@ -1038,6 +1051,7 @@ def _differentiable_log_probs():
         @staticmethod
         @torch.autograd.function.once_differentiable
         def backward(ctx, grad_logp, grad_entropy, _index, _top):
+            _not_captured()
             logits, tokens, stats, entropy = ctx.saved_tensors
             grads = [None if g is None else g if g.is_contiguous() or not any(g.stride()) else g.contiguous() for g in (grad_logp, grad_entropy)]
             return log_probs_grad_tensors(logits, tokens, stats, ctx.scale, entropy, *grads), None, None, None, None
@@ -1065,11 +1079,11 @@ def log_probs_tensors(logits, tokens=None, scale=1.0, top=0, entropy=True, stats
     with _on_stream(logits, stream) as handle:
         if stats is not None:
             _written(stats)
-        shape = tuple(logits.shape[:-1])
-        logp = None if tokens is None else torch.empty(shape, dtype=torch.float32, device=logits.device)
-        spread = torch.empty(shape, dtype=torch.float32, device=logits.device) if entropy else None
-        best = torch.empty(shape + (top,), dtype=torch.int32, device=logits.device) if top else None
-        best_logp = torch.empty(shape + (top,), dtype=torch.float32, device=logits.device) if top else None
+        shape, device = logits.shape[:-1], logits.device
+        logp = None if tokens is None else torch.empty(shape, dtype=torch.float32, device=device)
+        spread = None if not entropy else torch.empty(shape, dtype=torch.float32, device=device) if logp is None else torch.empty_like(logp)
+        best = torch.empty((*shape, top), dtype=torch.int32, device=device) if top else None
+        best_logp = torch.empty((*shape, top), dtype=torch.float32, device=device) if top else None
         need = gp_log_probs_workspace(N, C, top)
         ws = _workspace(workspace, need, logits.device) if need > 0 else None
         gp_log_probs(rows.data_ptr(), ld, dtype, N, C, _ptr(tokens), index, scale, _ptr(logp), _ptr(spread), top, _ptr(best), _ptr(best_logp),
@@ -1079,7 +1093,8 @@ def log_probs_tensors(logits, tokens=None, scale=1.0, top=0, entropy=True, stats
 
 def log_probs_grad_tensors(logits, tokens, stats, scale=1.0, entropy=None, grad_logp=None, grad_entropy=None, out=None, stream=None):
     """Convenience for torch tensors: the gradient of log_probs_tensors with respect to its logits, from the stats (and, for grad_entropy, the entropy) it left.
-    grad_logp, grad_entropy: float32, one value per row or one for all, or None.  Returns out, of logits' shape and type (made if not given)."""
+    grad_logp, grad_entropy: float32, one value per row or one for all, or None.  Returns out, of logits' shape and type (made if not given); automatic
+    differentiation does not follow it."""
     import torch
     dtype, index = _float_type(logits), GP_I32 if tokens is None else _index_type(tokens)
     rows, ld = _rows_of_logits(logits, tokens)
@@ -1109,7 +1124,7 @@ def log_probs_grad_tensors(logits, tokens, stats, scale=1.0, entropy=None, grad_
 
 def _teacher(logits, teacher_index, teacher_logits):
     """(address, distance of rows, type) of a teacher's classes and of their logits, and the entries of a row."""
-    if tuple(teacher_index.shape[:-1]) != tuple(logits.shape[:-1]) or teacher_index.shape != teacher_logits.shape:
+    if teacher_index.shape[:-1] != logits.shape[:-1] or teacher_index.shape != teacher_logits.shape:
         raise ValueError("teacher_index and teacher_logits must be of one shape, with a row for every row of logits")
     index = _types()[1].get(teacher_index.dtype)
     if index is None:
@@ -1135,6 +1150,7 @@ def _differentiable_distill():
         @staticmethod
         @torch.autograd.function.once_differentiable
         def backward(ctx, grad):
+            _not_captured()
             logits, teacher_index, teacher_logits, stats = ctx.saved_tensors
             grad = grad if grad.is_contiguous() or not any(grad.stride()) else grad.contiguous()
             return distill_grad_tensors(logits, teacher_index, teacher_logits, stats, grad, ctx.temperature), None, None, None
@@ -1163,7 +1179,7 @@ def distill_tensors(logits, teacher_index, teacher_logits, temperature=1.0, grad
     to, ldg = (None, C) if out is None else _rows_for(out, logits.shape, logits.dtype, "out")
     _one_device(logits, teacher_index, teacher_logits, grad_loss, out, stats, workspace)
     with _on_stream(logits, stream) as handle:
-        loss = torch.empty(tuple(logits.shape[:-1]), dtype=torch.float32, device=logits.device)
+        loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
         if out is not None:
             _written(out)
         elif grad_loss is not None:
@@ -1179,7 +1195,8 @@ def distill_tensors(logits, teacher_index, teacher_logits, temperature=1.0, grad
 
 def distill_grad_tensors(logits, teacher_index, teacher_logits, stats, grad_loss, temperature=1.0, out=None, stream=None):
     """Convenience for torch tensors: the gradient of distill_tensors with respect to its logits, from the stats it left and grad_loss, the gradient of the
-    losses (float32, one value per row or one for all).  Returns out, of logits' shape and type (made if not given)."""
+    losses (float32, one value per row or one for all).  Returns out, of logits' shape and type (made if not given); automatic differentiation does not
+    follow it."""
     import torch
     dtype = _float_type(logits)
     rows, ld = _rows_of_logits(logits, None)

@@ -319,28 +319,32 @@ __global__ __launch_bounds__(1024) void gp_norm_grad_join(NormGradArgs a, int64_
 {
     __shared__ float lds[32][33];
     const int c = threadIdx.x & 31, s = threadIdx.x >> 5;
-    const int64_t j = (int64_t)blockIdx.x * 32 + c;
     const int64_t width = 2 * (int64_t)a.d;
-    float sum = 0.0f;
-    if (j < width) {
-        int64_t k = s;
-        for (; k + 96 < rows; k += 128) {
-            const float p = a.partial[k * width + j], q = a.partial[(k + 32) * width + j], t = a.partial[(k + 64) * width + j], o = a.partial[(k + 96) * width + j];
-            sum += (p + q) + (t + o);
+    for (int64_t first = (int64_t)blockIdx.x * 32; first < width; first += (int64_t)gridDim.x * 32) {
+        const int64_t j = first + c;
+        float sum = 0.0f;
+        if (j < width) {
+            int64_t k = s;
+            for (; k + 96 < rows; k += 128) {
+                const float p = a.partial[k * width + j], q = a.partial[(k + 32) * width + j], t = a.partial[(k + 64) * width + j], o = a.partial[(k + 96) * width + j];
+                sum += (p + q) + (t + o);
+            }
+            for (; k < rows; k += 32) sum += a.partial[k * width + j];
         }
-        for (; k < rows; k += 32) sum += a.partial[k * width + j];
+        lds[s][c] = sum;
+        __syncthreads();
+        if (s == 0 && j < width) {
+            float part[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) part[i] = lds[i][c];
+#pragma unroll
+            for (int n = 16; n > 0; n /= 2)
+#pragma unroll
+                for (int i = 0; i < n; ++i) part[i] += part[i + n];
+            write_sum(a, j < a.d, j < a.d ? j : j - a.d, part[0]);
+        }
+        __syncthreads();
     }
-    lds[s][c] = sum;
-    __syncthreads();
-    if (threadIdx.x >= 32 || j >= width) return;
-    float part[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) part[i] = lds[i][c];
-#pragma unroll
-    for (int n = 16; n > 0; n /= 2)
-#pragma unroll
-        for (int i = 0; i < n; ++i) part[i] += part[i + n];
-    write_sum(a, j < a.d, j < a.d ? j : j - a.d, part[0]);
 }
 
 // Rows too long for registers, first half: mean(u) and mean(u h) of a row.
@@ -470,7 +474,7 @@ gp_status launch_join(const NormGradArgs& a, int64_t rows, hipStream_t stream)
 {
     if (!a.weight_grad && !a.bias_grad) return GP_OK;
     profile_begin("gp_norm_grad_join", stream);
-    hipLaunchKernelGGL(gp_norm_grad_join, dim3((unsigned)((2 * (int64_t)a.d + 31) / 32)), dim3(1024), 0, stream, a, rows);
+    hipLaunchKernelGGL(gp_norm_grad_join, dim3((unsigned)std::min((2 * (int64_t)a.d + 31) / 32, kMaxBlocks)), dim3(1024), 0, stream, a, rows);
     profile_end(stream);
     GP_HIP(hipGetLastError());
     return GP_OK;
@@ -539,7 +543,7 @@ gp_status launch_norm_grad(NormGradArgs a, hipStream_t stream)
         a.chunk = (a.N + chunks - 1) / chunks;
         const int64_t used = (a.N + a.chunk - 1) / a.chunk;
         profile_begin("gp_norm_grad_columns", stream);
-        hipLaunchKernelGGL((gp_norm_grad_columns<TX, TG>), dim3((unsigned)((a.d + 255) / 256), (unsigned)used), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((gp_norm_grad_columns<TX, TG>), dim3((unsigned)(((int64_t)a.d + 255) / 256), (unsigned)used), dim3(256), 0, stream, a);
         profile_end(stream);
         GP_HIP(hipGetLastError());
         return launch_join(a, used, stream);

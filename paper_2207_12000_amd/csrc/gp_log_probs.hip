@@ -1405,7 +1405,7 @@ gp_status distill(const void* x, int64_t ld, gp_dtype dtype, int64_t N, int32_t 
     if (!known(teacher_dtype)) return fail(GP_ERR_INVALID_ARG, "unknown dtype %d", (int)teacher_dtype);
     if (K < 1 || ldi < K || ldt < K) return fail(GP_ERR_INVALID_ARG, "need K >= 1, ldi >= K, ldt >= K");
     if (K > kMostTop) return fail(GP_ERR_UNSUPPORTED, "more than %d entries", kMostTop);
-    if (!good_scale(T)) return fail(GP_ERR_INVALID_ARG, "need a temperature within 1e-30 .. 1e30");
+    if (!(T >= 1e-15f && T <= 1e15f)) return fail(GP_ERR_INVALID_ARG, "need a temperature within 1e-15 .. 1e15");  // (its square is a number too)
     if (grad && (ldg < C || (sg != 0 && sg != 1))) return fail(GP_ERR_INVALID_ARG, "need ldg >= C, a distance of 0 or 1");
     if (N == 0) return GP_OK;
     if (!x || !index || !teacher || (grad && !g)) return fail(GP_ERR_INVALID_ARG, "NULL argument");

@@ -72,7 +72,7 @@ for call in (distill, distill_grad):
     REFUSED += [(call, dict(logits_ptr=0), BAD), (call, dict(teacher_index_ptr=0), BAD), (call, dict(teacher_logits_ptr=0), BAD), (call, dict(grad_loss_ptr=0), BAD),
                 (call, dict(dtype=2), BAD), (call, dict(teacher_dtype=2), BAD), (call, dict(index=2), BAD), (call, dict(N=-1), BAD), (call, dict(C=0), BAD),
                 (call, dict(ld=7), BAD), (call, dict(ldg=7), BAD), (call, dict(ldi=2), BAD), (call, dict(ldt=2), BAD), (call, dict(K=0), BAD),
-                (call, dict(K=65, ldi=65, ldt=65), NO), (call, dict(temperature=0.0), BAD), (call, dict(temperature=NAN), BAD), (call, dict(stride_loss=2), BAD),
+                (call, dict(K=65, ldi=65, ldt=65), NO), (call, dict(temperature=0.0), BAD), (call, dict(temperature=NAN), BAD), (call, dict(temperature=1e16), BAD), (call, dict(stride_loss=2), BAD),
                 (call, dict(N=(1 << 40) + 1), NO), (call, dict(C=(1 << 28) + 1, ld=1 << 29, ldg=1 << 29), NO)]
 REFUSED += [(distill, dict(**LONG, ldg=1 << 20, workspace_ptr=0), BAD), (distill, dict(**LONG, ldg=1 << 20, workspace_bytes=gp.gp_distill_workspace(2, 1 << 20) - 1), BAD),
             (distill_grad, dict(stats_ptr=0), BAD), (distill_grad, dict(grad_ptr=0), BAD)]
@@ -137,7 +137,8 @@ def test_tensors_must_be_on_the_gpu_and_of_matching_shapes():
                 lambda: gp.distill_tensors(f, at.float(), of), lambda: gp.distill_tensors(f, at, of.double()), lambda: gp.distill_tensors(f, at, of, out=f.clone()),
                 lambda: gp.distill_tensors(f, at, of, grad_loss=g[:3]), lambda: gp.distill_tensors(f, at, of, grad_loss=g, out=f.bfloat16()),
                 lambda: gp.distill_grad_tensors(f, at, of, s, g), lambda: gp.distill_grad_tensors(f, at, of, None, g), lambda: gp.distill_grad_tensors(f, at, of, s, None),
-                lambda: gp.log_probs_tensors(f.clone().requires_grad_(), t, stream=1), lambda: gp.distill_tensors(f.clone().requires_grad_(), at, of, stream=1),
+                lambda: gp.log_probs_tensors(f.clone().requires_grad_(), t), lambda: gp.distill_tensors(f.clone().requires_grad_(), at, of),
+                lambda: gp.layer_norm_tensors(f, v.clone().requires_grad_()), lambda: gp.log_probs_tensors(f.clone().requires_grad_(), t, stream=1), lambda: gp.distill_tensors(f.clone().requires_grad_(), at, of, stream=1),
                 lambda: gp.layer_norm_tensors(f.clone().requires_grad_(), stream=1)):
         with pytest.raises(ValueError):
             bad()
