@@ -85,13 +85,17 @@ __device__ __forceinline__ float row_sum(float v, float* lds)
 
 // ---- forward ----------------------------------------------------------------------------------------------------
 
+// Lanes of a workgroup: teams of a wavefront or less come several to one, longer ones alone, since they meet at barriers.
+template <int TPR>
+constexpr int kNormBlock = TPR <= 64 ? 256 : TPR;
+
 // Vector t = v * TPR + lane of a row starts at column t * VEC; the last one is moved back to end with the row, and its first elements, which the
 // vector before has as well, take no part in sums.  NV is as small as holds the row, so only vectors v = NV - 1 may be that one or none.
 // y may be x: a row is read before it is written.
 template <typename TX, typename TY, int VEC, int NV, int TPR>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_norm_rows(NormArgs a)
+__global__ __launch_bounds__(kNormBlock<TPR>) void gp_norm_rows(NormArgs a)
 {
-    constexpr int BLOCK = TPR < 256 ? 256 : TPR, TEAMS = BLOCK / TPR;
+    constexpr int TEAMS = kNormBlock<TPR> / TPR;
     __shared__ float lds[3][16];
     const int lane = threadIdx.x % TPR;
     float w[NV][VEC], b[NV][VEC];
@@ -408,7 +412,7 @@ int team_lanes(int64_t N, int64_t nvec, int most)
 template <typename TX, typename TY, int VEC, int NV, int TPR>
 gp_status launch_norm(const NormArgs& a, hipStream_t stream)
 {
-    constexpr int BLOCK = TPR < 256 ? 256 : TPR, TEAMS = BLOCK / TPR;
+    constexpr int BLOCK = kNormBlock<TPR>, TEAMS = BLOCK / TPR;
     const int64_t blocks = std::min((a.N + TEAMS - 1) / TEAMS, kUnits * 2048 / BLOCK);
     profile_begin("gp_norm_rows", stream);
     hipLaunchKernelGGL((gp_norm_rows<TX, TY, VEC, NV, TPR>), dim3((unsigned)blocks), dim3(BLOCK), 0, stream, a);
@@ -442,14 +446,16 @@ gp_status launch_norm(NormArgs a, hipStream_t stream)
         return GP_OK;
     }
     a.nvec = (a.d + VEC - 1) / VEC;
-    switch (team_lanes(a.N, a.nvec, 16 / VEC)) {
+    // four vectors to a lane; two of narrow rows in bf16, whose parameters take more registers than the row (us, two / four: 507,001 x 100 48 / 54,
+    // 492,307 x 130 64 / 62, 64,000 x 1000 54 / 51, 62,135 x 1030 82 / 54, 15,609 x 4100 80 / 56)
+    switch (team_lanes(a.N, a.nvec, sizeof(TX) == 2 && a.nvec <= 16 ? 2 : 4)) {
     case 2: return launch_norm<TX, TY, VEC, 2>(a, stream);
     case 4: return launch_norm<TX, TY, VEC, 4>(a, stream);
     case 8: return launch_norm<TX, TY, VEC, 8>(a, stream);
     case 16: return launch_norm<TX, TY, VEC, 16>(a, stream);
     case 32: return launch_norm<TX, TY, VEC, 32>(a, stream);
     case 64: return launch_norm<TX, TY, VEC, 64>(a, stream);
-    case 128:
+    case 128: return launch_norm<TX, TY, VEC, 128>(a, stream);
     case 256: return launch_norm<TX, TY, VEC, 256>(a, stream);
     case 512: return launch_norm<TX, TY, VEC, 512>(a, stream);
     default: return launch_norm<TX, TY, VEC, 1024>(a, stream);
