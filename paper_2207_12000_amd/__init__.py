@@ -762,6 +762,7 @@ def gp_layer_norm(x_ptr: int, ldx: int, dtype: int, N: int, d: int, weight_ptr: 
     _check(st, "gp_layer_norm")
 
 
+@functools.lru_cache(maxsize=256)  # (of the sizes alone)
 def gp_layer_norm_grad_workspace(N: int, d: int) -> int:
     return lib().gp_layer_norm_grad_workspace(N, d)
 
@@ -776,6 +777,7 @@ def gp_layer_norm_grad(grad_ptr: int, ldg: int, grad_dtype: int, x_ptr: int, ldx
     _check(st, "gp_layer_norm_grad")
 
 
+@functools.lru_cache(maxsize=256)  # (of the sizes alone)
 def gp_log_probs_workspace(N: int, C: int, k: int = 0) -> int:
     return lib().gp_log_probs_workspace(N, C, k)
 
@@ -800,6 +802,7 @@ def gp_log_probs_grad(logits_ptr: int, ld: int, dtype: int, N: int, C: int, toke
     _check(st, "gp_log_probs_grad")
 
 
+@functools.lru_cache(maxsize=256)  # (of the sizes alone)
 def gp_distill_workspace(N: int, C: int) -> int:
     return lib().gp_distill_workspace(N, C)
 
