@@ -8,14 +8,15 @@
 // s (x_j - m) - log(sum), so that large logits cost no bits.  (m, log(sum)) are what a row's gradient needs.  A row whose logits are all -inf
 // keeps (0, 0): every p is 0 and every log p is -inf, without a case of its own.
 //
-// All are bound by memory: a row is read once, into the registers of a team of lanes, and where the gradient is asked for along with the
-// loss it is written from there.  Rows that 1,024 lanes cannot hold, and few long rows, are cut into parts, a workgroup each, whose
-// results a second launch joins.
+// All are bound by memory: a row is read once, into the registers of a team of lanes (as it is stored: widened it would take twice as many in bf16), and
+// where the gradient is asked for along with the loss it is written from there.  Rows that a workgroup cannot hold, and few long rows, are cut into
+// parts, a workgroup each, whose results a second launch joins.  us measured, and what the same bytes take a large copy: 4,096 rows of 32,768 in
+// bf16, eight alternatives 73 (58), loss and gradient 116 (116); 507,001 fp32 rows of 47, loss and gradient 61 (49); the gradient of 2.45 M of them 200 (213).
 //
-// Alternatives.  A logit and its class make one whole number (key_of), larger logits and then lower classes first, so no two are equal.  Teams of part of a
-// wavefront keep sorted lists in registers, into which every key is sorted by maxima and minima, and merge them.  Teams of a wavefront or more
+// Alternatives.  Teams of part of a wavefront sort their elements in registers, put their lists together and keep the largest.  A logit and its class make
+// one number there, larger logits and then lower classes first, so no two are equal (double_of, and key_of in memory).  Teams of a wavefront or more
 // compare with a bound instead: the k-th largest of 64 groups' maxima is no larger than the k-th largest logit, and few others
-// reach it (8.5 for 8, 44 for 32, 300 for 64, in any order that does not follow the groups); these are listed in LDS and ranked by counting.
+// reach it (8.5 for 8, 44 for 32, in any order that does not follow the groups; of 256 groups 74 for 64); these are listed in LDS and ranked by counting.
 // Where more reach it than the list has room for, as in rows of equal logits, the largest key below the last is looked for k times.
 #include <algorithm>
 #include <exception>
@@ -369,7 +370,7 @@ __device__ __forceinline__ void team_list(const uint64_t (&list)[L], uint64_t (&
 }
 
 // The same number, of which the compiler knows nothing: what is worked out from it stays where it is needed, and is not kept in registers from one
-// row to the next (60 instead of 99 for rows of 32,768 in bf16, so that a compute unit has four workgroups of 512 and not two).
+// row to the next (75 instead of 106 for rows of 32,768 in bf16, so that a compute unit has three workgroups of 512 and not two: answers 73 us and not 89).
 __device__ __forceinline__ int opaque(int v)
 {
     asm volatile("" : "+v"(v));
@@ -666,8 +667,8 @@ __device__ __forceinline__ RowSums join_parts(const float* partial, int parts, i
     return joined<64>(s, scale);
 }
 
-// Joins the parts of a row: its sums, and the largest of the parts' keys by the same bound as above, of 64 groups of lanes.  A wavefront for few
-// keys, a workgroup of 1,024 for many (one row of 190 parts by 20 keys 5 us; by 256 lanes 14).
+// Joins the parts of a row: its sums, and the largest of the parts' keys by the same bound as above, of 256 groups (place by place, so that each has
+// keys of every rank).  A wavefront for few keys, a workgroup of 1,024 for many (one row of 190 parts by 20 keys 5 us; by 256 lanes 14).
 template <typename T, int LANES>
 __global__ __launch_bounds__(LANES) void gp_answer_join(AnswerArgs a)
 {
@@ -883,7 +884,9 @@ struct Teacher {
     }
 };
 
-// Rows of part of a wavefront: the gradient goes through LDS, where the entries' shares are taken off, one after another.
+// Rows of part of a wavefront: the gradient goes through LDS, where the entries' shares are taken off, one after another, and leaves it in whole vectors (single
+// stores of a last vector's elements took 6 us of 66).  What is left above the bytes' time is waiting: 507,001 x 47, 390 instructions of the vector
+// unit a wavefront, 20 us of 57, and 9 us of a wavefront's life.  Asking for the next row ahead, with workgroups that walk, took longer (70 us), walking alone too (65).
 template <typename T, int VEC, int NV, int TPR, int PER>
 __global__ __launch_bounds__(256) void gp_distill_short(DistillArgs a)
 {
@@ -1079,7 +1082,7 @@ constexpr int64_t kFull = 256 * 16;      // wavefronts below which a row is spre
 constexpr int64_t kMostRows = INT64_C(1) << 40;
 constexpr int kMostClasses = 1 << kIndexBits;
 constexpr int64_t kFillParts = 512;      // workgroups that few long rows are cut into, at least
-constexpr int64_t kPartVectors = 512;    // vectors of such a part, at least
+constexpr int64_t kPartVectors = 512;    // vectors of such a part, at least (rows of fewer than eight such parts are left whole: a join takes 4 us)
 constexpr int kLongestRow = 1024 * 32;   // elements that a workgroup holds
 
 template <typename T>
@@ -1092,7 +1095,9 @@ int64_t row_parts(int64_t N, int64_t C, int vec)
     return std::max(parts, std::min(nvec / kPartVectors, (kFillParts + N - 1) / N));
 }
 
-// Lanes of a row's team: `least`, or as few as hold it in `most` vectors each; more, up to 32, where the rows make too few wavefronts.
+// Lanes of a row's team: `least`, or as few as hold it in `most` vectors each; more, up to `widest`, where the rows make too few wavefronts.  Answers go by 32
+// elements a lane (us, 32 / 16: 500,000 x 47 in bf16, eight best 31 / 43; 200,000 x 172, five best 38 / 47), sorted lists of more than eight places by 16, for
+// the registers; distillation by 4 vectors (100,000 x 300, 32 entries: 8 vectors 68, 4 vectors 63).
 int team_lanes(int64_t N, int64_t nvec, int least, int most, int widest = 32)
 {
     int lanes = least;

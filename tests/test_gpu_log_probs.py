@@ -46,7 +46,7 @@ def same(got, want, bound):
     got = wide(got)
     fine = np.isfinite(want)
     assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)])
-    off = np.abs(got - want)[fine]
+    off = np.abs(got[fine] - want[fine])
     bound = np.broadcast_to(bound, want.shape)[fine]
     assert (off <= bound).all(), f"worst {np.max(off / bound):.2f} of the bound"
 
