@@ -597,16 +597,29 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gp_answer_rows(AnswerAr
         }
         if (a.k > 0) {
             // whatever is not below the bound; -inf is no alternative, NaN above all
-            if (!(mine < bound) || s.total != s.total) {
+            const auto offer = [&](float y, int j) {
+                if (!(y < bound) && y != -infinity()) {
+                    const int at = atomicAdd(&lds.count, 1);
+                    if (at < TeamLds<TPR>::ROOM) lds.list[at] = key_of(y, j);
+                }
+            };
+            const bool some = !(mine < bound) || s.total != s.total;
+            uint64_t with = __ballot(some);
+            if (TPR > 64 && NV * VEC >= 32 && __popcll(with) <= 4) {
+                // few of a wavefront's lanes have one: all lanes look at a lane's elements, one each, as they are in memory (64 elements of every lane looked at
+                // by all took 300 of 930 instructions: 3,764 x 17,000 in bf16, five best 57 -> 49 us; of 8 elements less than the reads: 160 -> 184)
+                const int n = opaque(lane) & 63, v = n / VEC, i = n % VEC;
+                for (; with != 0; with &= with - 1) {
+                    const int from = (threadIdx.x & ~63) + __ffsll((unsigned long long)with) - 1, t = v * TPR + from;
+                    const int col = (int)e.column(v, from, len, hi - lo);
+                    if (n < NV * VEC && t < hi - lo && i >= t * VEC - col) offer(widen(x[off + col + i]), off + col + i);
+                }
+            } else if (some) {
                 const int here = opaque(lane);
 #pragma unroll
                 for (int v = 0; v < NV; ++v)
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i)
-                        if (!(e.at(v, i) < bound) && e.at(v, i) != -infinity()) {
-                            const int at = atomicAdd(&lds.count, 1);
-                            if (at < TeamLds<TPR>::ROOM) lds.list[at] = key_of(e.at(v, i), off + e.column(v, here, len, hi - lo) + i);
-                        }
+                    for (int i = 0; i < VEC; ++i) offer(e.at(v, i), off + (int)e.column(v, here, len, hi - lo) + i);
             }
             team_barrier<TPR>();
             const int count = __builtin_amdgcn_readfirstlane(lds.count);
@@ -1147,6 +1160,10 @@ gp_status launch_short(const AnswerArgs& a, hipStream_t stream)
     if constexpr (VEC < 8) return need <= 6 ? launch_short<T, VEC, 6, TPR>(a, stream) : launch_short<T, VEC, 8, TPR>(a, stream);
     return fail(GP_ERR_UNSUPPORTED, "no kernel for %d classes", a.C);
 }
+// Vectors of a row that a wavefront takes by itself: without barriers it is done sooner than a workgroup, where there are rows enough (us, a wavefront / 256 lanes:
+// 58,181 x 1100 in fp32, five best 86 / 160, loss and gradient 107 / 164; 25,000 x 2500 in bf16 59 / 82, 16,000 x 4000 38 / 53, 500 x 4000 8.7 / 6.2).
+int64_t one_wavefront(int64_t items) { return items >= 2048 ? 512 : 256; }
+
 template <typename T, int VEC, int NV, int TPR>
 gp_status launch_rows(const AnswerArgs& a, hipStream_t stream)
 {
@@ -1163,17 +1180,16 @@ gp_status launch_rows(const AnswerArgs& a, int64_t longest, hipStream_t stream)
 {
     if (longest <= TPR) return launch_rows<T, VEC, 1, TPR>(a, stream);
     if (longest <= 2 * TPR) return launch_rows<T, VEC, 2, TPR>(a, stream);
-    if (TPR < 512 || longest <= 4 * TPR) return launch_rows<T, VEC, 4, TPR>(a, stream);
-    if constexpr (TPR >= 512) return launch_rows<T, VEC, 8, TPR>(a, stream);
-    return GP_OK;
+    if (longest <= 4 * TPR) return launch_rows<T, VEC, 4, TPR>(a, stream);
+    return launch_rows<T, VEC, 8, TPR>(a, stream);
 }
-// Rows of a wavefront or more, or parts of them
+// Rows of a wavefront or more, or parts of them (us, 256 lanes / 512: 7,111 x 9000 in bf16, five best 51 / 62; 12,800 x 5000 in fp32 67 / 91)
 template <typename T>
 gp_status launch_rows(const AnswerArgs& a, hipStream_t stream)
 {
     const int64_t longest = (a.nvec + a.parts - 1) / a.parts;
-    if (longest <= 256) return launch_rows<T, kVec<T>, 64>(a, longest, stream);
-    if (longest <= 1024) return launch_rows<T, kVec<T>, 256>(a, longest, stream);
+    if (longest <= one_wavefront(a.N * a.parts)) return launch_rows<T, kVec<T>, 64>(a, longest, stream);
+    if (longest <= 2048) return launch_rows<T, kVec<T>, 256>(a, longest, stream);
     if (longest <= 4096) return launch_rows<T, kVec<T>, 512>(a, longest, stream);
     return launch_rows<float, kVec<float>, 1024>(a, longest, stream);
 }
@@ -1261,16 +1277,15 @@ gp_status launch_distill_rows(const DistillArgs& a, int64_t longest, hipStream_t
 {
     if (longest <= TPR) return launch_distill_rows<T, VEC, 1, TPR>(a, stream);
     if (longest <= 2 * TPR) return launch_distill_rows<T, VEC, 2, TPR>(a, stream);
-    if (TPR < 512 || longest <= 4 * TPR) return launch_distill_rows<T, VEC, 4, TPR>(a, stream);
-    if constexpr (TPR >= 512) return launch_distill_rows<T, VEC, 8, TPR>(a, stream);
-    return GP_OK;
+    if (longest <= 4 * TPR) return launch_distill_rows<T, VEC, 4, TPR>(a, stream);
+    return launch_distill_rows<T, VEC, 8, TPR>(a, stream);
 }
 template <typename T>
 gp_status launch_distill_rows(const DistillArgs& a, hipStream_t stream)
 {
     const int64_t longest = (a.nvec + a.parts - 1) / a.parts;
-    if (longest <= 256) return launch_distill_rows<T, kVec<T>, 64>(a, longest, stream);
-    if (longest <= 1024) return launch_distill_rows<T, kVec<T>, 256>(a, longest, stream);
+    if (longest <= one_wavefront(a.N * a.parts)) return launch_distill_rows<T, kVec<T>, 64>(a, longest, stream);
+    if (longest <= 2048) return launch_distill_rows<T, kVec<T>, 256>(a, longest, stream);
     if (longest <= 4096) return launch_distill_rows<T, kVec<T>, 512>(a, longest, stream);
     return launch_distill_rows<T, kVec<T>, 1024>(a, longest, stream);
 }

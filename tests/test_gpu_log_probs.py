@@ -80,7 +80,8 @@ def logits_of(N, C, dtype, pad=0, skew=0, seed=0, hide=0.0):
 # every team (4 to 64 lanes, 256, 1,024), rows below a vector, parts, odd widths
 SIZES = [(1, 1, 0, 0), (9, 2, 1, 1), (300, 3, 0, 1), (65, 7, 0, 0), (17, 8, 0, 0), (5000, 13, 0, 1), (20_000, 16, 0, 0), (3000, 40, 0, 0), (70_000, 47, 0, 0), (999, 64, 3, 1),
          (4001, 100, 0, 0), (2500, 172, 0, 0), (2000, 333, 1, 3), (40, 500, 0, 0), (700, 512, 0, 1), (300, 1000, 0, 0), (200, 1025, 5, 1), (90, 2047, 0, 0), (60, 3001, 0, 1),
-         (50, 8192, 0, 0), (33, 8193, 0, 1), (20, 20_001, 0, 0), (12, 32_768, 0, 0), (7, 32_771, 1, 1), (3, 100_003, 0, 0), (1, 16_384, 0, 0), (1, 391_000, 0, 0), (600, 33_000, 0, 0)]
+         (50, 8192, 0, 0), (33, 8193, 0, 1), (20, 20_001, 0, 0), (12, 32_768, 0, 0), (7, 32_771, 1, 1), (3, 100_003, 0, 0), (1, 16_384, 0, 0), (1, 391_000, 0, 0), (600, 33_000, 0, 0),
+         (2048, 1501, 1, 1), (2050, 4095, 0, 0)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
