@@ -7,8 +7,8 @@
 // squares are taken of (x - m) with the row at hand, so rows far from zero lose nothing.  A team is as few lanes as hold the row
 // in 16 to 32 elements each: few steps of a sum across lanes, and 64 bytes a lane in flight; more lanes where there are too few rows to fill the
 // chip.  Teams keep the columns' parameters from row to row (a workgroup for every few rows instead: 52 -> 102 us for 507,001 x 100 in bf16).  Rows too
-// long for 1,024 lanes are read again for each sum.  us measured, and what the same bytes take a large copy: 507,001 x 100 in bf16 49 (44); gradients of
-// 232,965 x 602 in fp32 349 (362), of 16,384 x 4,096 in bf16 88 (87).
+// long for 1,024 lanes are read again for each sum.  us measured, and what the same bytes take a large copy: 507,001 x 100 in bf16 46 (44); gradients of
+// 232,965 x 602 in fp32 347 (362), of 16,384 x 4,096 in bf16 82 (87).
 //
 // Gradients of weights: a team walks over every so-many-th row with the columns' sums in registers, a workgroup adds its teams' sums up in
 // LDS and leaves one row of them, and a second launch adds these rows in a fixed order: the same inputs give the same bits.

@@ -2,7 +2,7 @@
 
 Tolerances, u = 2^-24: log p as in the tests of log probabilities.  Of at most 64 entries v / T, with w their distance from the largest: log q is off by
 (4 |w| + 80 + 4 |log sum|) u, q by as much of itself and 4 u.  The loss is T^2 sum q (log q - log p): q's share of every difference, the differences' own
-errors, and 70 u of the terms.  The gradient g T (p - q): the errors of p and q, and 6 u of both.
+errors, and 70 u of the terms.  The gradient g T (p - q): the errors of p and q, 6 u of both, and 2^-126 (a smaller p is 0).
 """
 import numpy as np
 import pytest
@@ -49,7 +49,7 @@ def check(loss, grad, x, at, v, T, g):
         for k in range(K):
             np.add.at(q_of, (np.arange(N), c[:, k]), q[:, k])
             np.add.at(offq_of, (np.arange(N), c[:, k]), (q * (offq + 8 * U))[:, k])
-        b = np.abs(G)[:, None] * T * (p * (offp + 8 * U) + offq_of + 6 * U * (p + q_of)) + half_step(grad) * np.abs(wants) + 1e-37
+        b = np.abs(G)[:, None] * T * (p * (offp + 8 * U) + offq_of + 6 * U * (p + q_of) + 2.0 ** -126) + half_step(grad) * np.abs(wants) + 1e-37
         off = np.abs(wide(grad) - wants)
         assert (off <= b).all(), f"worst {np.max(off / b):.2f} of the bound"
 

@@ -3,7 +3,8 @@
 Tolerances, u = 2^-24.  With z = s (x - m), a term exp(z) is off by (4 |z| + 2) u of itself, and a sum of them by at most 32 additions in a lane, 10 steps among
 lanes and, for rows in parts, N_parts / 64 + 6 more: 64 u with what else happens to it (parts of up to 800 columns' groups: 80 u).  With Z the mean of |z| under p, the log of
 the sum is off by (80 + 4 Z + 4 |log|) u, log p by 4 u |z| more.  The entropy is log(sum) - weighted / sum: (160 + 170 Z + 4 mean(z^2) + 4 Z^2 + 4 |log| + 2 H) u.  The order
-of alternatives is that of the logits as they are stored: exact.  Gradients take what the forward pass kept as given to those bounds.  What is written in bf16 is
+of alternatives is that of the logits as they are stored: exact.  Gradients take what the forward pass kept as given to those bounds; a p below
+2^-126, the least normal number, is 0: off by as much.  What is written in bf16 is
 off by 2^-8 of itself besides.
 """
 import numpy as np
@@ -180,7 +181,7 @@ def check_gradient(got, logits, tokens, scale, g1, g2):
     named = (t >= 0) & (t < C)
     a1 = a1 * named
     size = np.abs(np.where(p > 0, lp, 0.0)) + H[:, None]
-    bound = s * (a1 * (p * (every + 4 * U) + 4 * U * (np.arange(C) == t)) + a2 * p * (size * (every + 8 * U) + every + offH)) + half_step(got) * np.abs(wants) + 1e-37
+    bound = s * (a1 * (p * (every + 4 * U) + 4 * U * (np.arange(C) == t)) + a2 * p * (size * (every + 8 * U) + every + offH) + 2.0 ** -126 * (a1 + a2 * size)) + half_step(got) * np.abs(wants) + 1e-37
     off = np.abs(wide(got) - wants)
     assert (off <= bound).all(), f"worst {np.max(off / bound):.2f} of the bound"
 
