@@ -122,13 +122,14 @@ struct RowSums {
 __device__ __forceinline__ float base_of(float m) { return m == -infinity() ? 0.0f : m; }
 
 // The sums of a row from those of its parts, one in each lane of a team of W, in every lane.  A part's are of exp(s (x - its own largest)): with
-// z = s (its largest - the row's), exp(z) times them, and z exp(z) times the total more of the weighted one.
+// z = s (its largest - the row's), exp(z) times them, and z exp(z) times the total more of the weighted one.  A part of classes that are ruled out adds
+// nothing: it has no largest to take z from (the distance of 0 to a row of the type's lowest values, times s, is infinite).
 template <int W>
 __device__ __forceinline__ RowSums joined(const RowSums& part, float scale)
 {
     RowSums s;
     s.m = team_largest<W>(part.m);
-    const float z = (base_of(part.m) - base_of(s.m)) * scale, f = part.total == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(z * kLog2e);
+    const float z = part.none() ? 0.0f : (base_of(part.m) - base_of(s.m)) * scale, f = part.none() ? 0.0f : __builtin_amdgcn_exp2f(z * kLog2e);
     s.total = team_sum<W>(f * part.total);
     s.weighted = team_sum<W>(f * (part.weighted + larger(z, -1e4f) * part.total));
     return s;
@@ -671,7 +672,8 @@ __device__ __forceinline__ RowSums join_parts(const float* partial, int parts, i
     RowSums s{-infinity(), 0.0f, 0.0f};
     for (int p = lane; p < parts; p += lanes) {
         const float4 q = *(const float4*)(partial + 4 * (int64_t)p);
-        const float m = larger(s.m, q.x), z = (base_of(s.m) - base_of(m)) * scale, y = (base_of(q.x) - base_of(m)) * scale;
+        const float m = larger(s.m, q.x);  // (as in `joined`: no distance where nothing is)
+        const float z = s.total == 0.0f ? 0.0f : (base_of(s.m) - base_of(m)) * scale, y = q.y == 0.0f ? 0.0f : (base_of(q.x) - base_of(m)) * scale;
         const float f = s.total == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(z * kLog2e), g = q.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(y * kLog2e);
         s.weighted = f * (s.weighted + larger(z, -1e4f) * s.total) + g * (q.z + larger(y, -1e4f) * q.y);
         s.total = f * s.total + g * q.y;
