@@ -955,14 +955,16 @@ __global__ __launch_bounds__(256) void gp_distill_short(DistillArgs a)
             }
         }
         team_barrier<64>();
-        // one lane of a team at a time, so that entries of one class go in their order
+        // one lane of a team at a time, so that entries of one class go in their order: a wavefront's additions in LDS are done in the order of its
+        // instructions, and the barrier keeps those of one turn ahead of the next one's (it is none but for the compiler, which might make one turn of all)
         for (int turn = 0; turn * PER < a.K; ++turn) {
-            if (lane != turn) continue;
+            if (lane == turn) {
 #pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (t.at[i] >= 0) atomicAdd(mine + t.at[i], -f * t.q[i]);
+                for (int i = 0; i < PER; ++i)
+                    if (t.at[i] >= 0) atomicAdd(mine + t.at[i], -f * t.q[i]);
+            }
+            team_barrier<64>();
         }
-        team_barrier<64>();
         T* const out = (T*)a.grad + row * a.ldg;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
