@@ -961,7 +961,7 @@ __global__ __launch_bounds__(256) void gp_distill_short(DistillArgs a)
             if (lane == turn) {
 #pragma unroll
                 for (int i = 0; i < PER; ++i)
-                    if (t.at[i] >= 0) atomicAdd(mine + t.at[i], -f * t.q[i]);
+                    if (t.some && t.at[i] >= 0) atomicAdd(mine + t.at[i], -f * t.q[i]);  // (0 times an f that is no number is none)
             }
             team_barrier<64>();
         }
