@@ -1195,7 +1195,9 @@ gp_status launch_rows(const AnswerArgs& a, hipStream_t stream)
     if (longest <= one_wavefront(a.N * a.parts)) return launch_rows<T, kVec<T>, 64>(a, longest, stream);
     if (longest <= 2048) return launch_rows<T, kVec<T>, 256>(a, longest, stream);
     if (longest <= 4096) return launch_rows<T, kVec<T>, 512>(a, longest, stream);
-    return launch_rows<float, kVec<float>, 1024>(a, longest, stream);
+    if constexpr (kLongestRow > 4096 * kVec<T>)  // (a part is of kLongestRow elements at most: in bf16 none comes here)
+        return launch_rows<T, kVec<T>, 1024>(a, longest, stream);
+    return fail(GP_ERR_UNSUPPORTED, "no kernel for %lld vectors in one part", (long long)longest);
 }
 
 template <typename T>
