@@ -556,6 +556,14 @@ def _on_stream(tensor, stream):
     return _other_stream(handle, tensor.device)
 
 
+def _no_tangent(*tensors):
+    """Derivatives in forward mode are not followed: a tensor that carries one is refused, as the result would be without."""
+    import torch
+    forward = torch.autograd.forward_ad
+    if getattr(forward, "_current_level", 0) >= 0 and any(t is not None and forward.unpack_dual(t).tangent is not None for t in tensors):
+        raise ValueError("forward-mode derivatives are not followed: give the primal tensors")
+
+
 @functools.lru_cache(maxsize=None)
 def _types():
     import torch
@@ -650,6 +658,7 @@ def embedding_tensors(table, tokens, scale=1.0, out=None, out_dtype=None, stream
     Where the table requires a gradient, the result does too: backward() takes it by embedding_grad_tensors, on the stream that was
     current here.  What is filled into out is a plain copy that automatic differentiation does not follow."""
     import torch
+    _no_tangent(table)
     if out is None and table.requires_grad and torch.is_grad_enabled():
         return _differentiable_lookup().apply(table, tokens, scale, out_dtype, stream)
     if table.dim() != 2:
@@ -938,6 +947,7 @@ def layer_norm_tensors(x, weight=None, bias=None, eps=1e-5, out=None, out_dtype=
     receives what layer_norm_grad_tensors needs.  Where x, weight or bias require a gradient, the result does too (not with out, stats or a stream of
     its own, nor in a capture)."""
     import torch
+    _no_tangent(x, weight, bias)
     if out is None and stats is None and (_followed(x, stream) or _followed(weight, stream) or _followed(bias, stream)):
         return _differentiable_norm().apply(x, weight, bias, eps, out_dtype)
     dtype, rows = _float_type(x), _as_rows(x, "x")
@@ -1070,6 +1080,7 @@ def log_probs_tensors(logits, tokens=None, scale=1.0, top=0, entropy=True, stats
     log_probs_grad_tensors needs.  workspace: a uint8 GPU tensor of gp_log_probs_workspace(rows, classes, top) bytes or more, kept by the caller.  Where
     logits require a gradient, logp and entropy do too (not with stats or a stream of its own, nor in a capture)."""
     import torch
+    _no_tangent(logits)
     if stats is None and _followed(logits, stream):
         return LogProbs(*_differentiable_log_probs().apply(logits, tokens, scale, top, entropy))
     dtype, index = _float_type(logits), GP_I32 if tokens is None else _index_type(tokens)
@@ -1169,6 +1180,7 @@ def distill_tensors(logits, teacher_index, teacher_logits, temperature=1.0, grad
     distill_grad_tensors needs.  workspace: a uint8 GPU tensor of gp_distill_workspace(rows, classes) bytes or more, kept by the caller.  Where logits
     require a gradient, the loss does too (not with grad_loss, stats or a stream of its own, nor in a capture); the teacher gets none."""
     import torch
+    _no_tangent(logits, teacher_logits)
     if stats is None and grad_loss is None and _followed(logits, stream):
         return _differentiable_distill().apply(logits, teacher_index, teacher_logits, temperature)
     dtype = _float_type(logits)
