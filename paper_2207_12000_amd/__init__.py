@@ -535,20 +535,27 @@ def _other_stream(handle, device):
 
 @functools.lru_cache(maxsize=None)
 def _current():
-    """(the handle of a device's current stream by its number, the current device): 1.7 us of a call's 11 are spent on torch's stream object, where its
-    handle cannot be had without one."""
+    """(the handle of a device's current stream by its number, the current device, whether torch records a trace): 1.7 us of a call's 11 are spent on torch's
+    stream object, where its handle cannot be had without one."""
     import torch
     bare = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return bare or (lambda index: torch.cuda.current_stream(index).cuda_stream), torch.cuda.current_device
+    return (bare or (lambda index: torch.cuda.current_stream(index).cuda_stream), torch.cuda.current_device,
+            getattr(torch._C, "_is_tracing", torch.jit.is_tracing))
+
+
+def _not_traced():
+    if _current()[2]():
+        raise ValueError("torch.jit.trace would record a result's memory and not the call that fills it")
 
 
 def _on_stream(tensor, stream):
     """Context: the tensor's device and the stream a call is enqueued on (torch's current one unless given) are current while what the
     call needs is allocated, so that torch gives its memory to no other stream before the call is done with it."""
+    _not_traced()
+    current_handle, current_device, _ = _current()
     if not tensor.is_cuda:
         raise ValueError("tensors must be on the GPU")
     index = tensor.get_device()
-    current_handle, current_device = _current()
     current = current_handle(index)
     handle = current if stream is None else int(stream)
     if handle == current and index == current_device():
@@ -557,8 +564,10 @@ def _on_stream(tensor, stream):
 
 
 def _no_tangent(*tensors):
-    """Derivatives in forward mode are not followed: a tensor that carries one is refused, as the result would be without."""
+    """Derivatives in forward mode are not followed: a tensor that carries one is refused, as the result would be without.  So are traces, here at the
+    beginning of a call whose arguments they would record first."""
     import torch
+    _not_traced()
     forward = torch.autograd.forward_ad
     if getattr(forward, "_current_level", 0) >= 0 and any(t is not None and forward.unpack_dual(t).tangent is not None for t in tensors):
         raise ValueError("forward-mode derivatives are not followed: give the primal tensors")

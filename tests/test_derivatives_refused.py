@@ -1,4 +1,4 @@
-"""What automatic differentiation cannot follow is refused, not dropped: tangents of forward mode."""
+"""What automatic differentiation cannot follow is refused, not dropped: tangents of forward mode, and traces that would keep a result's memory alone."""
 import pytest
 
 import paper_2207_12000_amd as gp
@@ -25,6 +25,15 @@ def test_tangents_are_refused(i):
             call(forward_ad.make_dual(x, torch.ones_like(x)))
         with pytest.raises(ValueError, match="on the GPU"):  # a level alone is none of the call's business
             call(x)
+
+
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("i", range(len(calls())))
+def test_traces_are_refused(i, grad):
+    import torch
+    call, x = calls()[i]
+    with pytest.raises(ValueError, match="torch.jit.trace"):
+        torch.jit.trace(call, (x.requires_grad_(grad),), check_trace=False)
 
 
 def test_transforms_of_functions_are_refused():
