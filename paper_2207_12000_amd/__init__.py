@@ -890,6 +890,43 @@ def _rows_for(t, shape, dtype, what):
     return t, _row_stride(t, what)
 
 
+def _memory(t):
+    """(address, bytes from row to row, bytes of a row, rows) of what a tensor takes; a contiguous one is a single row."""
+    size = t.element_size()
+    if t.dim() == 2 and t.stride(0) > 0 and not t.is_contiguous():
+        return t.data_ptr(), t.stride(0) * size, ((t.shape[1] - 1) * t.stride(1) + 1) * size, t.shape[0]
+    return t.data_ptr(), 0, (sum((n - 1) * step for n, step in zip(t.shape, t.stride())) + 1) * size, 1
+
+
+def _overlap(a, b):
+    """Whether two tensors share memory.  Rows of one distance may lie between each other's, as columns of one matrix do; of two distances they may not."""
+    if a.numel() == 0 or b.numel() == 0:
+        return False
+    (p, step, width, rows), (q, other_step, other_width, other_rows) = _memory(a), _memory(b)
+    if p >= q + (other_rows - 1) * other_step + other_width or q >= p + (rows - 1) * step + width:
+        return False
+    if rows > 1 and other_rows > 1 and step != other_step:
+        return True
+    if other_rows == 1:
+        (p, step, width, rows), (q, other_step, other_width, other_rows) = (q, other_step, other_width, other_rows), (p, step, width, rows)
+    if other_rows == 1:
+        return True
+    past = (p - q) % other_step  # of the other's rows that the first begins in or behind
+    return past < other_width or past + width > other_step
+
+
+def _apart(out, what, *inputs):
+    """Refuses a tensor to write that shares memory with what is read: another workgroup may read there after it was written."""
+    for t in inputs:
+        if t is not None and _overlap(out, t):
+            raise ValueError(f"{what} must not overlap what the call reads or writes besides")
+
+
+def _itself(out, t):
+    """Whether a call that writes out over t writes every element over itself."""
+    return out.dtype == t.dtype and _memory(out) == _memory(t)
+
+
 def _vector(t, n, what):
     if t is not None and (t.dim() != 1 or t.shape[0] != n or not t.is_contiguous()):
         raise ValueError(f"{what} must be a contiguous vector, one value per column")
@@ -952,7 +989,7 @@ def _differentiable_norm():
 def layer_norm_tensors(x, weight=None, bias=None, eps=1e-5, out=None, out_dtype=None, stats=None, stream=None):
     """Convenience for torch tensors: x is a float32 / bfloat16 GPU tensor whose last dimension is normalised (any distance of rows in two dimensions,
     contiguous in others), weight and bias vectors of float32 or bfloat16 (both of one type) or None.  Returns the normalised rows, of x's shape,
-    in out_dtype (x's unless given); out: a tensor of that shape, filled and returned (x itself will do).  stats: a (rows, 2) float32 tensor that
+    in out_dtype (x's unless given); out: a tensor of that shape, filled and returned (x itself will do, else it must not overlap the inputs).  stats: a (rows, 2) float32 tensor that
     receives what layer_norm_grad_tensors needs.  Where x, weight or bias require a gradient, the result does too (not with out, stats or a stream of
     its own, nor in a capture)."""
     import torch
@@ -972,6 +1009,8 @@ def layer_norm_tensors(x, weight=None, bias=None, eps=1e-5, out=None, out_dtype=
     if out is not None:
         to, ldy = _rows_for(out, x.shape, out_dtype or out.dtype, "out")
     _one_device(x, weight, bias, out, stats)
+    if out is not None:
+        _apart(to, "out", weight, bias, stats, None if _itself(to, rows) else rows)
     with _on_stream(x, stream) as handle:
         if out is None:
             out = _new_like(x, out_dtype)
@@ -988,7 +1027,8 @@ def layer_norm_tensors(x, weight=None, bias=None, eps=1e-5, out=None, out_dtype=
 def layer_norm_grad_tensors(grad, x, stats, weight=None, x_grad=None, weight_grad=None, bias_grad=None, accumulate=False, weight_dtype=None,
                             workspace=None, stream=None):
     """Convenience for torch tensors: the gradients of layer_norm_tensors from grad, the gradient of what it returned, and the stats it left.  Returns
-    (x_grad, weight_grad, bias_grad): each is made where None is given, filled where a tensor is, left out (None) where False is.  accumulate: weight_grad
+    (x_grad, weight_grad, bias_grad): each is made where None is given, filled where a tensor is, left out (None) where False is.  What is filled must not
+    overlap the inputs or each other, but for x_grad, which may be x or grad itself.  accumulate: weight_grad
     and bias_grad are added to (both given, or False).  weight_dtype: of the gradients that are made (weight's; float32 without one).  workspace: a uint8
     GPU tensor of gp_layer_norm_grad_workspace(rows, d) bytes or more, kept by the caller; without one the call takes its memory from torch.  Automatic
     differentiation does not follow it."""
@@ -1017,6 +1057,11 @@ def layer_norm_grad_tensors(grad, x, stats, weight=None, x_grad=None, weight_gra
         to, ldxg = _rows_for(x_grad, x.shape, x.dtype, "x_grad")
     outs = [None if t is False else t for t in (x_grad, weight_grad, bias_grad)]
     _one_device(x, grad, stats, weight, workspace, *outs)
+    if outs[0] is not None:
+        _apart(to, "x_grad", stats, weight, *(t for t in (rows, up) if not _itself(to, t)))
+    for t, what, others in ((outs[1], "weight_grad", outs[2:]), (outs[2], "bias_grad", ())):
+        if t is not None:
+            _apart(t, what, rows, up, stats, outs[0], *others)
     with _on_stream(x, stream) as handle:
         written = [t for t in outs if t is not None]
         if written:
@@ -1116,8 +1161,8 @@ def log_probs_tensors(logits, tokens=None, scale=1.0, top=0, entropy=True, stats
 
 def log_probs_grad_tensors(logits, tokens, stats, scale=1.0, entropy=None, grad_logp=None, grad_entropy=None, out=None, stream=None):
     """Convenience for torch tensors: the gradient of log_probs_tensors with respect to its logits, from the stats (and, for grad_entropy, the entropy) it left.
-    grad_logp, grad_entropy: float32, one value per row or one for all, or None.  Returns out, of logits' shape and type (made if not given); automatic
-    differentiation does not follow it."""
+    grad_logp, grad_entropy: float32, one value per row or one for all, or None.  Returns out, of logits' shape and type (made if not given; it must not
+    overlap the inputs); automatic differentiation does not follow it."""
     import torch
     dtype, index = _float_type(logits), GP_I32 if tokens is None else _index_type(tokens)
     rows, ld = _rows_of_logits(logits, tokens)
@@ -1134,6 +1179,8 @@ def log_probs_grad_tensors(logits, tokens, stats, scale=1.0, entropy=None, grad_
     if out is not None:
         to, ldg = _rows_for(out, logits.shape, logits.dtype, "out")
     _one_device(logits, tokens, stats, entropy, grad_logp, grad_entropy, out)
+    if out is not None:
+        _apart(to, "out", rows, tokens, stats, entropy, grad_logp, grad_entropy)
     with _on_stream(logits, stream) as handle:
         if out is None:
             out = _new_like(logits)
@@ -1185,7 +1232,7 @@ def distill_tensors(logits, teacher_index, teacher_logits, temperature=1.0, grad
     """Convenience for torch tensors: the loss of every row of logits (as log_probs_tensors takes them) against a teacher's best classes and their logits, each
     one row of up to 64 per row of logits (int32 / int64, -1 for none, and float32 / bfloat16: log_probs_tensors' top_index and top_logp will do).  Returns the
     float32 losses, of logits.shape[:-1]; with grad_loss (float32, one value per row or one for all) the gradient of the logits is made in the same
-    pass and (loss, gradient) returned, the gradient in out where that is given.  stats: a (rows, 2) float32 tensor that receives what
+    pass and (loss, gradient) returned, the gradient in out where that is given (not over the inputs).  stats: a (rows, 2) float32 tensor that receives what
     distill_grad_tensors needs.  workspace: a uint8 GPU tensor of gp_distill_workspace(rows, classes) bytes or more, kept by the caller.  Where logits
     require a gradient, the loss does too (not with grad_loss, stats or a stream of its own, nor in a capture); the teacher gets none."""
     import torch
@@ -1202,6 +1249,8 @@ def distill_tensors(logits, teacher_index, teacher_logits, temperature=1.0, grad
     grad_loss, stride = _per_row(grad_loss, N, "grad_loss")
     to, ldg = (None, C) if out is None else _rows_for(out, logits.shape, logits.dtype, "out")
     _one_device(logits, teacher_index, teacher_logits, grad_loss, out, stats, workspace)
+    if out is not None:
+        _apart(to, "out", rows, teacher_index, teacher_logits, grad_loss, stats)
     with _on_stream(logits, stream) as handle:
         loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
         if out is not None:
@@ -1219,8 +1268,8 @@ def distill_tensors(logits, teacher_index, teacher_logits, temperature=1.0, grad
 
 def distill_grad_tensors(logits, teacher_index, teacher_logits, stats, grad_loss, temperature=1.0, out=None, stream=None):
     """Convenience for torch tensors: the gradient of distill_tensors with respect to its logits, from the stats it left and grad_loss, the gradient of the
-    losses (float32, one value per row or one for all).  Returns out, of logits' shape and type (made if not given); automatic differentiation does not
-    follow it."""
+    losses (float32, one value per row or one for all).  Returns out, of logits' shape and type (made if not given; it must not overlap the inputs);
+    automatic differentiation does not follow it."""
     import torch
     dtype = _float_type(logits)
     rows, ld = _rows_of_logits(logits, None)
@@ -1233,6 +1282,8 @@ def distill_grad_tensors(logits, teacher_index, teacher_logits, stats, grad_loss
     if out is not None:
         to, ldg = _rows_for(out, logits.shape, logits.dtype, "out")
     _one_device(logits, teacher_index, teacher_logits, stats, grad_loss, out)
+    if out is not None:
+        _apart(to, "out", rows, teacher_index, teacher_logits, stats, grad_loss)
     with _on_stream(logits, stream) as handle:
         if out is None:
             out = _new_like(logits)
