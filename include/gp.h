@@ -489,8 +489,10 @@ gp_status gp_layer_norm(const void *x, int64_t ldx, gp_dtype dtype, int64_t N, i
  *     x_grad = r (u - mean(u) - h mean(u h)),   weight_grad = sum over rows of grad h,   bias_grad = sum over rows of grad
  *  grad    DEVICE, N x d of `grad_dtype`, rows ldg elements apart (ldg >= d, or 0: one row stands for all N).
  *  x, stats, weight  as gp_layer_norm had and left them.
- *  x_grad  DEVICE, N x d of `dtype`, rows ldxg elements apart; may be x or grad itself (same type and distance of rows); NULL: not wanted.
- *  weight_grad, bias_grad  DEVICE, d of `weight_dtype` each; NULL: not wanted.  accumulate = 1: added to what they hold.
+ *  x_grad  DEVICE, N x d of `dtype`, rows ldxg elements apart; may be x or grad itself (same type and distance of rows), else must not overlap
+ *          the inputs; NULL: not wanted.
+ *  weight_grad, bias_grad  DEVICE, d of `weight_dtype` each, which must overlap neither the inputs (weight among them) nor each other; NULL: not wanted.
+ *          accumulate = 1: added to what they hold.
  *  workspace  gp_layer_norm_grad_workspace bytes (0 for few rows); not needed where neither weight_grad nor bias_grad is wanted and d <= 16384.
  * Sums over rows are taken in an order that depends on N, d and the types alone.  N at most 2^40 (else UNSUPPORTED).  Enqueued on hip_stream.
  * Errors: INVALID_ARG, UNSUPPORTED, OOM_HOST, DEVICE.  gp_layer_norm_grad_workspace: -1 for sizes that the call rejects. */

@@ -1028,7 +1028,7 @@ def layer_norm_grad_tensors(grad, x, stats, weight=None, x_grad=None, weight_gra
                             workspace=None, stream=None):
     """Convenience for torch tensors: the gradients of layer_norm_tensors from grad, the gradient of what it returned, and the stats it left.  Returns
     (x_grad, weight_grad, bias_grad): each is made where None is given, filled where a tensor is, left out (None) where False is.  What is filled must not
-    overlap the inputs or each other, but for x_grad, which may be x or grad itself.  accumulate: weight_grad
+    overlap the inputs or each other, but for x_grad, which may be x or grad itself, and weight's and bias's, which may be written over weight.  accumulate: weight_grad
     and bias_grad are added to (both given, or False).  weight_dtype: of the gradients that are made (weight's; float32 without one).  workspace: a uint8
     GPU tensor of gp_layer_norm_grad_workspace(rows, d) bytes or more, kept by the caller; without one the call takes its memory from torch.  Automatic
     differentiation does not follow it."""
@@ -1079,6 +1079,8 @@ def layer_norm_grad_tensors(grad, x, stats, weight=None, x_grad=None, weight_gra
         need = gp_layer_norm_grad_workspace(N, d)
         ws = _workspace(workspace, need, x.device) if need > 0 else None
         kind = _types()[0].get(weight_dtype, -1)
+        if weight is not None and any(t is not None and _overlap(t, weight) for t in outs[1:]):
+            weight = weight.detach().clone()  # (few rows: workgroups that read it run beside those that write its gradient)
         gp_layer_norm_grad(up.data_ptr(), ldg, grad_dtype, rows.data_ptr(), ldx, dtype, N, d, stats.data_ptr(), _ptr(weight), kind, _ptr(to), ldxg,
                            _ptr(weight_grad), _ptr(bias_grad), accumulate, _ptr(ws), 0 if ws is None else ws.numel(), handle)
     return x_grad, weight_grad, bias_grad

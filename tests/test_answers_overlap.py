@@ -107,3 +107,37 @@ def test_an_empty_call_overlaps_nothing():
     x = torch.zeros(0, 8)
     with pytest.raises(ValueError, match="on the GPU"):
         gp.log_probs_grad_tensors(x, torch.zeros(0, dtype=torch.int32), torch.zeros(0, 2), grad_logp=torch.zeros(1), out=x)
+
+
+@pytest.mark.parametrize("over", ["weight", "bias", "both halves"])
+def test_gradients_written_over_the_weight_leave_the_call_a_copy_of_it(monkeypatch, over):
+    """Of few rows the workgroups that write the weight's gradient run beside those that read the weight: the call gets other memory to read it from."""
+    import contextlib
+
+    import torch
+    calls = []
+    monkeypatch.setattr(gp, "_on_stream", lambda tensor, stream: contextlib.nullcontext(0))
+    monkeypatch.setattr(gp, "gp_layer_norm_grad_workspace", lambda N, d: 0)
+    monkeypatch.setattr(gp, "gp_layer_norm_grad", lambda *a: calls.append((a, weights(a[9], a[7]))))
+
+    def weights(address, d):
+        import ctypes
+        return list((ctypes.c_float * d).from_address(address))
+
+    x, stats = torch.randn(4, 8), torch.ones(4, 2)
+    flat = torch.arange(24.0)
+    w = flat[8:16]
+    dw, db = {"weight": (w, None), "bias": (None, w), "both halves": (flat[4:12], flat[12:20])}[over]
+    for accumulate in (False, True):
+        gp.layer_norm_grad_tensors(x, x.clone(), stats, w, weight_grad=torch.zeros(8) if dw is None else dw, bias_grad=torch.zeros(8) if db is None else db, accumulate=accumulate)
+    gp.layer_norm_grad_tensors(x, x.clone(), stats, w)
+    for args, held in calls[:2]:
+        assert held == list(range(8, 16))
+        start = args[9]
+        for to in (args[13], args[14]):
+            assert to + 32 <= start or start + 32 <= to
+        if dw is not None:
+            assert args[13] == dw.data_ptr()
+        if db is not None:
+            assert args[14] == db.data_ptr()
+    assert calls[2][0][9] == w.data_ptr()
