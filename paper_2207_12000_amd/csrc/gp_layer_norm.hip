@@ -132,7 +132,8 @@ __global__ __launch_bounds__(kNormBlock<TPR>) void gp_norm_rows(NormArgs a)
             }
         // the mean again, of what is left: a sum of values far from zero is off by many times what one of them is
         rest = row_sum<TPR>(rest, lds[1]) * share;
-        const float r = 1.0f / sqrtf(fmaxf(row_sum<TPR>(squares, lds[2]) * share - rest * rest, 0.0f) + a.eps);
+        const float variance = row_sum<TPR>(squares, lds[2]) * share - rest * rest;
+        const float r = 1.0f / sqrtf((variance < 0.0f ? 0.0f : variance) + a.eps);  // (NaN stays)
         TY* const y = (TY*)a.y + row * a.ldy;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
