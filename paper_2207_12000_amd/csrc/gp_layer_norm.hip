@@ -159,7 +159,8 @@ __device__ __forceinline__ double workgroup_sum(double v, double* lds)
     return s;
 }
 
-// Rows too long for registers: a workgroup reads one three times.
+// Rows too long for registers: a workgroup reads one three times.  The mean is taken off in two parts, rounded to fp32 and what that left: a row far from zero
+// would lose half a step of its mean, times r, otherwise (us, in two parts / in one: 2,048 x 40,000 in fp32 271.2 / 270.9, in bf16 233.8 / 233.2).
 template <typename TX, typename TY>
 __global__ __launch_bounds__(1024) void gp_norm_long(NormArgs a)
 {
@@ -168,16 +169,17 @@ __global__ __launch_bounds__(1024) void gp_norm_long(NormArgs a)
         const TX* const x = (const TX*)a.x + row * a.ldx;
         double sum = 0.0;
         for (int64_t j = threadIdx.x; j < a.d; j += 1024) sum += widen(x[j]);
-        const float mean = (float)(workgroup_sum(sum, lds) / a.d);
+        const double m = workgroup_sum(sum, lds) / a.d;
+        const float mean = (float)m, rest = (float)(m - mean);
         double squares = 0.0;
         for (int64_t j = threadIdx.x; j < a.d; j += 1024) {
-            const float e = widen(x[j]) - mean;
+            const float e = (widen(x[j]) - mean) - rest;
             squares += e * e;
         }
         const float r = 1.0f / sqrtf((float)(workgroup_sum(squares, lds) / a.d) + a.eps);
         TY* const y = (TY*)a.y + row * a.ldy;
         for (int64_t j = threadIdx.x; j < a.d; j += 1024)
-            y[j] = narrow<TY>((widen(x[j]) - mean) * r * parameter(a.weight, a.wide_weights, (int)j, 1.0f) + parameter(a.bias, a.wide_weights, (int)j, 0.0f));
+            y[j] = narrow<TY>(((widen(x[j]) - mean) - rest) * r * parameter(a.weight, a.wide_weights, (int)j, 1.0f) + parameter(a.bias, a.wide_weights, (int)j, 0.0f));
         if (a.stats && threadIdx.x == 0) a.stats[2 * row] = mean, a.stats[2 * row + 1] = r;
     }
 }

@@ -31,3 +31,41 @@ def test_statistics_of_rows_that_are_no_numbers_are_none(d, dtype):
     assert bool(stats[5:].isfinite().all()) and bool(y[5:].isfinite().all())
     want = gp.layer_norm_tensors(x[5:].contiguous(), stats=torch.empty(2, 2, device="cuda"))
     assert torch.equal(y[5:], want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [d for d in WIDTHS if d >= 100])
+def test_rows_far_from_zero_lose_nothing(d, dtype):
+    """u = 2^-24.  Rows in registers: the first mean is off by at most e = 52 u mean|x| (50 u of a sum, two roundings), and x less it is exact or off by u of itself; the mean of
+    what is left is off by 52 u of its terms, f = 53 u (mean|x - m| + e).  The squares are of terms off by that mean, off by 54 u of themselves: of variance + e^2, taken from which
+    the mean's square is off by 104 u e (mean|x - m| + e): so r, by half of it over variance + eps, and 3 u.  h = (x - m) r is off by r f, r's part and 2 u, y by |w| times
+    that, two roundings of |h w|, one of y, and half a step of its type.  Rows beyond them have their mean in two parts, of which the second is off by u of itself, u^2 mean|x|,
+    and x - m by 2 u of itself; the squares are off by 4 u and a rounding, added up in fp64, r by half of that and 4 u."""
+    import torch
+    from oracle import answers
+    from test_gpu_layer_norm import U, half_step, wide
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    spread = torch.tensor([[1e-2], [1.0], [0.3], [30.0]], device="cuda")
+    far = torch.tensor([[1e4], [-3e5], [1e3], [-1e6]], device="cuda")
+    x = (far + spread * torch.randn(4, d, generator=gen, device="cuda")).to(types()[dtype])
+    w, b = torch.randn(d, generator=gen, device="cuda"), torch.randn(d, generator=gen, device="cuda")
+    stats = torch.empty(4, 2, device="cuda")
+    for out_dtype in (torch.float32, torch.bfloat16):
+        y = gp.layer_norm_tensors(x, w, b, eps=1e-6, out_dtype=out_dtype, stats=stats)
+        X, W = wide(x), np.abs(wide(w))
+        want, s = answers.layer_norm(X, wide(w), wide(b), float(np.float32(1e-6)))
+        m, r = s[:, :1], s[:, 1:]
+        h = np.abs((X - m) * r)
+        if d <= (16_384 if dtype == "f32" else 32_768):
+            near = np.abs(X - m).mean(1, keepdims=True)
+            e = 52 * U * np.abs(X).mean(1, keepdims=True)
+            f = 53 * U * (near + e)
+            variance = ((X - m) ** 2).mean(1, keepdims=True)
+            of_r = (54 * U * (variance + e ** 2) + 104 * U * e * (near + e)) * r ** 2 / 2 + 3 * U
+        else:
+            f, of_r = U ** 2 * np.abs(X).mean(1, keepdims=True), 7 * U
+        off_h = r * f + h * of_r + (2 if d <= 16_384 else 3) * U * h
+        bound = W * off_h + 2 * U * h * W + U * np.abs(want) + half_step(y) * np.abs(want)
+        off = np.abs(wide(y) - want)
+        assert (off <= bound).all(), f"worst {np.max(off / bound):.2f} of the bound"
+        assert (np.abs(wide(stats)[:, :1] - m) <= U * np.abs(m) * 2 + f).all() and (np.abs(wide(stats)[:, 1:] - r) <= r * (of_r + U)).all()
