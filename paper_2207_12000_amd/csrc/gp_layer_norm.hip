@@ -29,6 +29,7 @@ struct NormArgs {
     const void *weight, *bias;
     int wide_weights;  // weights, bias and their gradients are fp32 (else bf16)
     float eps;
+    double share;  // 1 / d
     void* y;
     int64_t ldy;
     float* stats;
@@ -91,14 +92,76 @@ __device__ __forceinline__ float row_sum(float v, float* lds)
 template <int TPR>
 constexpr int kNormBlock = TPR <= 64 ? 256 : TPR;
 
+// Wavefronts of a SIMD that a kernel is built for, by the types and the elements of a row that a lane holds: a launch is of eight workgroups of four to a compute
+// unit, and takes longer where they come in other rounds (us, five at a time / four: 492,307 x 130 in bf16 68 / 62, 15,609 x 4100 61.6 / 55.3).
+template <typename TX, typename TY, int E>
+constexpr int kNormWaves = E <= 12 ? 8 : E <= 16 ? (sizeof(TX) == sizeof(TY) ? 6 : 5) : E <= 24 || sizeof(TY) == 2 ? 4 : 3;
+
+// Whether a row's variance (with eps) is not to be had from sums in fp32: squares or sums beyond it (from |x - m| of 2^64 / sqrt(d) on, or an infinity or NaN).
+__device__ __forceinline__ bool beyond_fp32(float v) { return !(v < __builtin_inff()); }
+
+// Such a row: its sums in fp64, element by element from memory, a lane writing what it has read.  A row of one value is told by its variance, which is 0 or
+// 2^-63 of the mean's square and more where elements are 24 bits: below 2^-80 of it is what the mean's rounding left.  An infinity or NaN makes all NaN.  It
+// is rare, and takes as few registers as it can beside what the others keep: loops as they stand, no division or root in fp64.
+template <int TPR>
+__device__ __forceinline__ double far_sum(double v, int thread, double* lds)
+{
+#pragma unroll 1
+    for (int m = 4; m < (TPR < 64 ? TPR : 64) * 4; m *= 2) {
+        const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+        const unsigned low = __builtin_amdgcn_ds_bpermute((thread << 2) ^ m, (int)bits), high = __builtin_amdgcn_ds_bpermute((thread << 2) ^ m, (int)(bits >> 32));
+        v += __builtin_bit_cast(double, (uint64_t)high << 32 | low);
+    }
+    if constexpr (TPR > 64) {
+        __syncthreads();  // (whoever still reads the last sum)
+        if ((thread & 63) == 0) lds[thread >> 6] = v;
+        __syncthreads();
+        v = 0.0;
+#pragma unroll 1
+        for (int i = 0; i < TPR / 64; ++i) v += lds[i];
+    }
+    return v;
+}
+template <typename TX, typename TY, int TPR>
+__device__ __forceinline__ void norm_far_row(const NormArgs& a, int64_t row, double* lds)
+{
+    int thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));  // (so that nothing of it is worked out ahead and kept from row to row)
+    const int lane = thread % TPR;
+    const TX* const x = (const TX*)a.x + row * a.ldx;
+    TY* const y = (TY*)a.y + row * a.ldy;
+    double sum = 0.0, rest = 0.0, squares = 0.0;
+#pragma unroll 1
+    for (int64_t j = lane; j < a.d; j += TPR) sum += widen(x[j]);
+    const double mean = far_sum<TPR>(sum, thread, lds) * a.share;
+#pragma unroll 1
+    for (int64_t j = lane; j < a.d; j += TPR) {
+        const double e = widen(x[j]) - mean;
+        rest += e, squares += e * e;
+    }
+    rest = far_sum<TPR>(rest, thread, lds) * a.share;
+    double v = far_sum<TPR>(squares, thread, lds) * a.share - rest * rest;
+    const bool flat = v <= mean * mean * 0x1p-80;
+    v = (flat ? 0.0 : v) + a.eps;
+    double r = __builtin_amdgcn_rsq(v);  // (to 24 bits or more, 47 by one step)
+    r *= 1.5 - 0.5 * v * r * r;
+#pragma unroll 1
+    for (int64_t j = lane; j < a.d; j += TPR) {
+        const float h = flat ? 0.0f : (float)(((widen(x[j]) - mean) - rest) * r);
+        y[j] = narrow<TY>(h * parameter(a.weight, a.wide_weights, (int)j, 1.0f) + parameter(a.bias, a.wide_weights, (int)j, 0.0f));
+    }
+    if (a.stats && lane == 0) a.stats[2 * row] = (float)(mean + rest), a.stats[2 * row + 1] = (float)r;
+}
+
 // Vector t = v * TPR + lane of a row starts at column t * VEC; the last one is moved back to end with the row, and its first elements, which the
 // vector before has as well, take no part in sums.  NV is as small as holds the row, so only vectors v = NV - 1 may be that one or none.
 // y may be x: a row is read before it is written.
 template <typename TX, typename TY, int VEC, int NV, int TPR>
-__global__ __launch_bounds__(kNormBlock<TPR>) void gp_norm_rows(NormArgs a)
+__global__ __launch_bounds__(kNormBlock<TPR>) __attribute__((amdgpu_waves_per_eu(kNormWaves<TX, TY, NV * VEC>, kNormWaves<TX, TY, NV * VEC>))) void gp_norm_rows(NormArgs a)
 {
     constexpr int TEAMS = kNormBlock<TPR> / TPR;
     __shared__ float lds[3][16];
+    __shared__ double wide[TPR > 64 ? TPR / 64 : 1];
     const int lane = threadIdx.x % TPR;
     float w[NV][VEC], b[NV][VEC];
     int col[NV], first = 0;  // the first element of vector NV - 1 that counts
@@ -116,6 +179,9 @@ __global__ __launch_bounds__(kNormBlock<TPR>) void gp_norm_rows(NormArgs a)
         float e[NV][VEC], sum = 0.0f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) load_vec<TX, VEC>(x + col[v], e[v]);
+        // all of a row is asked for before any of it is used; where registers are tight the compiler's own order is better (us, with / without: 492,307 x 130 in
+        // fp32 112.5 / 119.2, in bf16 61.4 / 65.2; 16,384 x 4,096 in bf16 56.3 / 54.4, 30,000 x 3000 80.6 / 76.8)
+        if constexpr (sizeof(TX) == 4 || (NV <= 3 && TPR <= 64)) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
@@ -132,8 +198,12 @@ __global__ __launch_bounds__(kNormBlock<TPR>) void gp_norm_rows(NormArgs a)
             }
         // the mean again, of what is left: a sum of values far from zero is off by many times what one of them is
         rest = row_sum<TPR>(rest, lds[1]) * share;
-        const float variance = row_sum<TPR>(squares, lds[2]) * share - rest * rest;
-        const float r = 1.0f / sqrtf((variance < 0.0f ? 0.0f : variance) + a.eps);  // (NaN stays)
+        const float variance = row_sum<TPR>(squares, lds[2]) * share - rest * rest, v = (variance < 0.0f ? 0.0f : variance) + a.eps;
+        if (__builtin_expect(beyond_fp32(v), 0)) {  // (all lanes of a team alike)
+            norm_far_row<TX, TY, TPR>(a, row, wide);
+            continue;
+        }
+        const float r = 1.0f / sqrtf(v);
         TY* const y = (TY*)a.y + row * a.ldy;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -176,7 +246,12 @@ __global__ __launch_bounds__(1024) void gp_norm_long(NormArgs a)
             const float e = (widen(x[j]) - mean) - rest;
             squares += e * e;
         }
-        const float r = 1.0f / sqrtf((float)(workgroup_sum(squares, lds) / a.d) + a.eps);
+        const float v = (float)(workgroup_sum(squares, lds) / a.d) + a.eps;
+        if (beyond_fp32(v)) {
+            norm_far_row<TX, TY, 1024>(a, row, lds);
+            continue;
+        }
+        const float r = 1.0f / sqrtf(v);
         TY* const y = (TY*)a.y + row * a.ldy;
         for (int64_t j = threadIdx.x; j < a.d; j += 1024)
             y[j] = narrow<TY>(((widen(x[j]) - mean) - rest) * r * parameter(a.weight, a.wide_weights, (int)j, 1.0f) + parameter(a.bias, a.wide_weights, (int)j, 0.0f));
@@ -587,7 +662,7 @@ gp_status layer_norm(const void* x, int64_t ldx, gp_dtype dtype, int64_t N, int3
     if (N == 0) return GP_OK;
     if (!x || !y) return fail(GP_ERR_INVALID_ARG, "NULL argument");
     NormArgs a{};
-    a.x = x, a.ldx = ldx, a.N = N, a.d = d, a.weight = weight, a.bias = bias, a.wide_weights = weight_dtype == GP_F32, a.eps = eps, a.y = y, a.ldy = ldy,
+    a.x = x, a.ldx = ldx, a.N = N, a.d = d, a.weight = weight, a.bias = bias, a.wide_weights = weight_dtype == GP_F32, a.eps = eps, a.share = 1.0 / d, a.y = y, a.ldy = ldy,
     a.stats = stats;
     if (dtype == GP_F32) return out_dtype == GP_F32 ? launch_norm<float, float>(a, stream) : launch_norm<float, bf16_t>(a, stream);
     return out_dtype == GP_F32 ? launch_norm<bf16_t, float>(a, stream) : launch_norm<bf16_t, bf16_t>(a, stream);

@@ -69,3 +69,54 @@ def test_rows_far_from_zero_lose_nothing(d, dtype):
         off = np.abs(wide(y) - want)
         assert (off <= bound).all(), f"worst {np.max(off / bound):.2f} of the bound"
         assert (np.abs(wide(stats)[:, :1] - m) <= U * np.abs(m) * 2 + f).all() and (np.abs(wide(stats)[:, 1:] - r) <= r * (of_r + U)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_rows_whose_squares_or_sums_are_beyond_fp32(d, dtype):
+    """u = 2^-24.  The sums are taken in fp64; x - m is rounded once, r off by 3 u (the variance, its root, the quotient), h = (x - m) r by 5 u with its own rounding, y by two
+    roundings of |h w|, one of itself, and half a step of its type.  The statistics are rounded once, r below the least normal number by 2^-149 besides.  A row of one value is the bias."""
+    import torch
+    from oracle import answers
+    from test_gpu_layer_norm import U, check_backward, half_step, wide
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    ty = types()[dtype]
+    most = torch.finfo(ty).max
+    x = torch.randn(12, d, generator=gen, device="cuda").clamp(-3, 3)
+    x[0] *= 1e25
+    x[1] = x[1] * 1e30 + 1e32
+    x[2] *= 1.1e38                                                      # squares and sums
+    x[3] = torch.where(x[3] > 0, most, -most)                           # of both signs: x - m is beyond it too
+    x[4] = most                                                         # one value
+    x[5] = -most
+    x[5, d // 2] = -most * (1 - 2.0 ** -7)                              # but for one, a step of bf16 off
+    x[6] = 1e20 * torch.randint(0, 2, (d,), generator=gen, device="cuda")
+    x[7] = 0.0
+    x[7, d - 1] = most
+    x[8] *= -1e21
+    x[9] *= 1e22
+    x = x.to(ty)
+    w, b = torch.randn(d, generator=gen, device="cuda"), torch.randn(d, generator=gen, device="cuda")
+    for eps in (1e-5, 1e30):
+        eps = float(np.float32(eps))
+        alone = [gp.layer_norm_tensors(x[i:i + 1], w, b, eps=eps) for i in (10, 11)]
+        for out_dtype in (torch.float32, torch.bfloat16):
+            stats = torch.empty(12, 2, device="cuda")
+            y = gp.layer_norm_tensors(x, w, b, eps=eps, out_dtype=out_dtype, stats=stats)
+            X, W = wide(x), np.abs(wide(w))
+            want, s = answers.layer_norm(X, wide(w), wide(b), eps)
+            m, r = s[:, :1], s[:, 1:]
+            h = np.abs((X - m) * r)
+            bound = W * 6 * U * h + 2 * U * h * W + U * np.abs(want) + half_step(y) * np.abs(want) + 1e-37
+            off = np.abs(wide(y) - want)
+            assert (off <= bound)[:10].all(), f"worst {(off / bound)[:10].max(1)} of the bound"
+            assert (np.abs(wide(stats) - s)[:10] <= 4 * U * np.abs(s[:10]) + 2.0 ** -149).all()
+            assert torch.equal(y[4], b.to(out_dtype)) and bool(y.isfinite().all())
+            if out_dtype == ty:  # the rows beside them are left alone
+                assert torch.equal(y[10:], torch.cat(alone))
+                again = x.clone()
+                assert torch.equal(gp.layer_norm_tensors(again, w, b, eps=eps, out=again), y)
+        g = torch.randn(12, d, generator=gen, device="cuda")
+        fine = [0, 1, 6, 8, 9]
+        dx, _, _ = gp.layer_norm_grad_tensors(g, x, stats, w)
+        check_backward((dx[fine], None, None), g[fine], x[fine], stats[fine], w)
