@@ -481,7 +481,8 @@ gp_status gp_muon_step(const float *W, float *W_out, int64_t ldw, int64_t stride
  *  weight, bias  DEVICE, d of `weight_dtype` each; NULL: all 1, all 0.   eps: above 0, at most 1e30.
  *  y       DEVICE, N x d of `out_dtype`, rows ldy elements apart; may be x itself (same type and ldy), else must not overlap the inputs.
  *  stats   DEVICE, N x 2 fp32: (m, r) of every row, what the gradient needs; NULL: not wanted.
- * Any finite row has its y, though its squares are beyond fp32.  A row with an infinity or NaN gives NaN, in r too, and leaves the others alone.  Enqueued on hip_stream.  Errors: INVALID_ARG, OOM_HOST, DEVICE. */
+ * Any finite row has its y, though its squares are beyond fp32 or its values are one value far from zero.  A row with an infinity or NaN gives NaN, in r too,
+ * and leaves the others alone.  Enqueued on hip_stream.  Errors: INVALID_ARG, OOM_HOST, DEVICE. */
 gp_status gp_layer_norm(const void *x, int64_t ldx, gp_dtype dtype, int64_t N, int32_t d, const void *weight, const void *bias,
                         gp_dtype weight_dtype, float eps, void *y, int64_t ldy, gp_dtype out_dtype, float *stats, void *hip_stream);
 

@@ -97,8 +97,9 @@ constexpr int kNormBlock = TPR <= 64 ? 256 : TPR;
 template <typename TX, typename TY, int E>
 constexpr int kNormWaves = E <= 12 ? 8 : E <= 16 ? (sizeof(TX) == sizeof(TY) ? 6 : 5) : E <= 24 || sizeof(TY) == 2 ? 4 : 3;
 
-// Whether a row's variance (with eps) is not to be had from sums in fp32: squares or sums beyond it (from |x - m| of 2^64 / sqrt(d) on, or an infinity or NaN).
-__device__ __forceinline__ bool beyond_fp32(float v) { return !(v < __builtin_inff()); }
+// Whether a row's variance (with eps) is not to be had from sums in fp32: squares or sums beyond it (from |x - m| of 2^64 / sqrt(d) on, or an infinity or NaN),
+// or nothing but the rounding of its first mean, `rest` off, whose square is taken off it and known to 2^-17 or so: rows of one value far from zero.
+__device__ __forceinline__ bool beyond_fp32(float v, float rest) { return !(v < __builtin_inff()) || rest * rest > 32.0f * v; }
 
 // Such a row: its sums in fp64, element by element from memory, a lane writing what it has read.  A row of one value is told by its variance, which is 0 or
 // 2^-63 of the mean's square and more where elements are 24 bits: below 2^-80 of it is what the mean's rounding left.  An infinity or NaN makes all NaN.  It
@@ -199,7 +200,7 @@ __global__ __launch_bounds__(kNormBlock<TPR>) __attribute__((amdgpu_waves_per_eu
         // the mean again, of what is left: a sum of values far from zero is off by many times what one of them is
         rest = row_sum<TPR>(rest, lds[1]) * share;
         const float variance = row_sum<TPR>(squares, lds[2]) * share - rest * rest, v = (variance < 0.0f ? 0.0f : variance) + a.eps;
-        if (__builtin_expect(beyond_fp32(v), 0)) {  // (all lanes of a team alike)
+        if (__builtin_expect(beyond_fp32(v, rest), 0)) {  // (all lanes of a team alike)
             norm_far_row<TX, TY, TPR>(a, row, wide);
             continue;
         }
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(1024) void gp_norm_long(NormArgs a)
             squares += e * e;
         }
         const float v = (float)(workgroup_sum(squares, lds) / a.d) + a.eps;
-        if (beyond_fp32(v)) {
+        if (beyond_fp32(v, rest)) {
             norm_far_row<TX, TY, 1024>(a, row, lds);
             continue;
         }

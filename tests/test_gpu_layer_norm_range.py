@@ -120,3 +120,39 @@ def test_rows_whose_squares_or_sums_are_beyond_fp32(d, dtype):
         fine = [0, 1, 6, 8, 9]
         dx, _, _ = gp.layer_norm_grad_tensors(g, x, stats, w)
         check_backward((dx[fine], None, None), g[fine], x[fine], stats[fine], w)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_rows_of_one_value_and_rows_a_step_from_it(d, dtype):
+    """The bounds of rows far from zero, where a row in registers has its first mean off by no more than 6 sqrt(variance + eps) (it is done in fp64 from the square of that,
+    32 times variance + eps, on): e is the lesser of the two.  In 80 bits, since fp64 leaves a step of 2^-53 of the mean, times r."""
+    import torch
+    from test_gpu_layer_norm import U, wide
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    ty = types()[dtype]
+    step = torch.finfo(ty).eps
+    values = torch.tensor([1.1, -7.3e2, 1.37e4, -1.37e6, 1.37e8, 1.37e10, -1.37e12, 1.37e15, 1.37e18, 1.3e25, 3e38], device="cuda").to(ty).float()
+    one = values[:, None].expand(-1, d)
+    some = (torch.rand(len(values), d, generator=gen, device="cuda") < 0.3).float()
+    last = (torch.arange(d, device="cuda") == d - 1).float().expand(len(values), d)
+    x = torch.cat([one, one * (1 - step * some), one * (1 - 2 * step * last)]).to(ty)
+    w, b = torch.randn(d, generator=gen, device="cuda"), torch.randn(d, generator=gen, device="cuda")
+    stats = torch.empty(len(x), 2, device="cuda")
+    for eps in (1e-5, 1e-12):
+        y = gp.layer_norm_tensors(x, w, b, eps=eps, out_dtype=torch.float32, stats=stats)
+        X, W = wide(x).astype(np.longdouble), np.abs(wide(w))
+        m = X.mean(1, keepdims=True)
+        m = m + (X - m).mean(1, keepdims=True)
+        v = ((X - m) ** 2).mean(1, keepdims=True) + np.longdouble(np.float32(eps))
+        r = 1 / np.sqrt(v)
+        want = ((X - m) * r).astype(np.float64) * wide(w) + wide(b)
+        m, v, r, h = (a.astype(np.float64) for a in (m, v, r, np.abs((X - m) * r)))
+        near = np.abs(X - m).mean(1, keepdims=True).astype(np.float64)
+        e = np.minimum(52 * U * np.abs(m), 6 * np.sqrt(v))
+        f = 53 * U * (near + e)
+        of_r = (54 * U * (v + e ** 2) + 104 * U * e * (near + e)) * r ** 2 / 2 + 4 * U
+        bound = W * (r * f + h * of_r + 3 * U * h) + 2 * U * h * W + 2 * U * np.abs(want) + U * np.abs(wide(b)) + 1e-37
+        off = np.abs(wide(y) - want)
+        assert (off <= bound).all(), f"worst {(off / bound).max(1)} of the bound"
+        assert (np.abs(wide(stats)[:, 1:] - r) <= r * (of_r + U) + 2.0 ** -149).all() and (np.abs(wide(stats)[:, :1] - m) <= 2 * U * np.abs(m) + f).all()
