@@ -1107,9 +1107,9 @@ def _differentiable_log_probs():
 
     class Answers(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, logits, tokens, scale, top, entropy):
+        def forward(ctx, logits, tokens, scale, top, entropy, workspace):
             stats = torch.empty((logits.numel() // max(logits.shape[-1], 1), 2), dtype=torch.float32, device=logits.device)
-            a = log_probs_tensors(logits, tokens, scale, top, entropy, stats=stats)
+            a = log_probs_tensors(logits, tokens, scale, top, entropy, stats=stats, workspace=workspace)
             ctx.save_for_backward(logits, tokens, stats, a.entropy)
             ctx.scale = scale
             if top:
@@ -1123,7 +1123,7 @@ def _differentiable_log_probs():
             _not_captured()
             logits, tokens, stats, entropy = ctx.saved_tensors
             grads = [None if g is None else g if g.is_contiguous() or not any(g.stride()) else g.contiguous() for g in (grad_logp, grad_entropy)]
-            return log_probs_grad_tensors(logits, tokens, stats, ctx.scale, entropy, *grads), None, None, None, None
+            return log_probs_grad_tensors(logits, tokens, stats, ctx.scale, entropy, *grads), None, None, None, None, None
 
     return Answers
 
@@ -1138,7 +1138,7 @@ def log_probs_tensors(logits, tokens=None, scale=1.0, top=0, entropy=True, stats
     import torch
     _no_tangent(logits)
     if stats is None and _followed(logits, stream):
-        return LogProbs(*_differentiable_log_probs().apply(logits, tokens, scale, top, entropy))
+        return LogProbs(*_differentiable_log_probs().apply(logits, tokens, scale, top, entropy, workspace))
     dtype, index = _float_type(logits), GP_I32 if tokens is None else _index_type(tokens)
     rows, ld = _rows_of_logits(logits, tokens)
     N, C = rows.shape
@@ -1212,9 +1212,9 @@ def _differentiable_distill():
 
     class Distill(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, logits, teacher_index, teacher_logits, temperature):
+        def forward(ctx, logits, teacher_index, teacher_logits, temperature, workspace):
             stats = torch.empty((logits.numel() // max(logits.shape[-1], 1), 2), dtype=torch.float32, device=logits.device)
-            loss = distill_tensors(logits, teacher_index, teacher_logits, temperature, stats=stats)
+            loss = distill_tensors(logits, teacher_index, teacher_logits, temperature, stats=stats, workspace=workspace)
             ctx.save_for_backward(logits, teacher_index, teacher_logits, stats)
             ctx.temperature = temperature
             return loss
@@ -1225,7 +1225,7 @@ def _differentiable_distill():
             _not_captured()
             logits, teacher_index, teacher_logits, stats = ctx.saved_tensors
             grad = grad if grad.is_contiguous() or not any(grad.stride()) else grad.contiguous()
-            return distill_grad_tensors(logits, teacher_index, teacher_logits, stats, grad, ctx.temperature), None, None, None
+            return distill_grad_tensors(logits, teacher_index, teacher_logits, stats, grad, ctx.temperature), None, None, None, None
 
     return Distill
 
@@ -1240,7 +1240,7 @@ def distill_tensors(logits, teacher_index, teacher_logits, temperature=1.0, grad
     import torch
     _no_tangent(logits, teacher_logits)
     if stats is None and grad_loss is None and _followed(logits, stream):
-        return _differentiable_distill().apply(logits, teacher_index, teacher_logits, temperature)
+        return _differentiable_distill().apply(logits, teacher_index, teacher_logits, temperature, workspace)
     dtype = _float_type(logits)
     rows, ld = _rows_of_logits(logits, None)
     N, C = rows.shape
