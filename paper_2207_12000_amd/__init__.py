@@ -535,24 +535,23 @@ def _other_stream(handle, device):
 
 @functools.lru_cache(maxsize=None)
 def _current():
-    """(the handle of a device's current stream by its number, the current device, whether torch records a trace): 1.7 us of a call's 11 are spent on torch's
-    stream object, where its handle cannot be had without one."""
+    """(the handle of a device's current stream by its number, the current device, whether torch records a trace, torch's forward mode): 1.7 us of a call's 11
+    are spent on torch's stream object, where its handle cannot be had without one."""
     import torch
     bare = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return (bare or (lambda index: torch.cuda.current_stream(index).cuda_stream), torch.cuda.current_device,
-            getattr(torch._C, "_is_tracing", torch.jit.is_tracing))
+            getattr(torch._C, "_is_tracing", torch.jit.is_tracing), torch.autograd.forward_ad)
 
 
-def _not_traced():
-    if _current()[2]():
-        raise ValueError("torch.jit.trace would record a result's memory and not the call that fills it")
+_TRACED = "torch.jit.trace would record a result's memory and not the call that fills it"
 
 
 def _on_stream(tensor, stream):
     """Context: the tensor's device and the stream a call is enqueued on (torch's current one unless given) are current while what the
     call needs is allocated, so that torch gives its memory to no other stream before the call is done with it."""
-    _not_traced()
-    current_handle, current_device, _ = _current()
+    current_handle, current_device, tracing, _ = _current()
+    if tracing():
+        raise ValueError(_TRACED)
     if not tensor.is_cuda:
         raise ValueError("tensors must be on the GPU")
     index = tensor.get_device()
@@ -564,11 +563,8 @@ def _on_stream(tensor, stream):
 
 
 def _no_tangent(*tensors):
-    """Derivatives in forward mode are not followed: a tensor that carries one is refused, as the result would be without.  So are traces, here at the
-    beginning of a call whose arguments they would record first."""
-    import torch
-    _not_traced()
-    forward = torch.autograd.forward_ad
+    """Derivatives in forward mode are not followed: a tensor that carries one is refused, as the result would be without."""
+    forward = _current()[3]
     if getattr(forward, "_current_level", 0) >= 0 and any(t is not None and forward.unpack_dual(t).tangent is not None for t in tensors):
         raise ValueError("forward-mode derivatives are not followed: give the primal tensors")
 
@@ -849,9 +845,13 @@ def gp_distill_grad(logits_ptr: int, ld: int, dtype: int, N: int, C: int, teache
 def _followed(t, stream):
     """Whether automatic differentiation is to follow a call on t.  Its backward pass runs on the stream that is current at the call, and may meet
     leaves that a graph outside a capture has as well, which ends the process: so neither another stream nor a capture goes with it."""
-    import torch
-    if t is None or not (t.requires_grad and torch.is_grad_enabled()):
+    if t is None or not t.requires_grad:
         return False
+    import torch
+    if not torch.is_grad_enabled():
+        return False
+    if _current()[2]():
+        raise ValueError(_TRACED)
     if not t.is_cuda:
         raise ValueError("tensors must be on the GPU")
     if stream is not None:
@@ -992,7 +992,6 @@ def layer_norm_tensors(x, weight=None, bias=None, eps=1e-5, out=None, out_dtype=
     in out_dtype (x's unless given); out: a tensor of that shape, filled and returned (x itself will do, else it must not overlap the inputs).  stats: a (rows, 2) float32 tensor that
     receives what layer_norm_grad_tensors needs.  Where x, weight or bias require a gradient, the result does too (not with out, stats or a stream of
     its own, nor in a capture)."""
-    import torch
     _no_tangent(x, weight, bias)
     if out is None and stats is None and (_followed(x, stream) or _followed(weight, stream) or _followed(bias, stream)):
         return _differentiable_norm().apply(x, weight, bias, eps, out_dtype)
@@ -1059,9 +1058,9 @@ def layer_norm_grad_tensors(grad, x, stats, weight=None, x_grad=None, weight_gra
     _one_device(x, grad, stats, weight, workspace, *outs)
     if outs[0] is not None:
         _apart(to, "x_grad", stats, weight, *(t for t in (rows, up) if not _itself(to, t)))
-    for t, what, others in ((outs[1], "weight_grad", outs[2:]), (outs[2], "bias_grad", ())):
-        if t is not None:
-            _apart(t, what, rows, up, stats, outs[0], *others)
+    sums = [t for t in outs[1:] if t is not None]
+    for i, t in enumerate(sums):
+        _apart(t, "weight_grad or bias_grad", rows, up, stats, outs[0], *sums[:i])
     with _on_stream(x, stream) as handle:
         written = [t for t in outs if t is not None]
         if written:
@@ -1079,7 +1078,7 @@ def layer_norm_grad_tensors(grad, x, stats, weight=None, x_grad=None, weight_gra
         need = gp_layer_norm_grad_workspace(N, d)
         ws = _workspace(workspace, need, x.device) if need > 0 else None
         kind = _types()[0].get(weight_dtype, -1)
-        if weight is not None and any(t is not None and _overlap(t, weight) for t in outs[1:]):
+        if sums and weight is not None and any(_overlap(t, weight) for t in sums):
             weight = weight.detach().clone()  # (few rows: workgroups that read it run beside those that write its gradient)
         gp_layer_norm_grad(up.data_ptr(), ldg, grad_dtype, rows.data_ptr(), ldx, dtype, N, d, stats.data_ptr(), _ptr(weight), kind, _ptr(to), ldxg,
                            _ptr(weight_grad), _ptr(bias_grad), accumulate, _ptr(ws), 0 if ws is None else ws.numel(), handle)
@@ -1165,7 +1164,6 @@ def log_probs_grad_tensors(logits, tokens, stats, scale=1.0, entropy=None, grad_
     """Convenience for torch tensors: the gradient of log_probs_tensors with respect to its logits, from the stats (and, for grad_entropy, the entropy) it left.
     grad_logp, grad_entropy: float32, one value per row or one for all, or None.  Returns out, of logits' shape and type (made if not given; it must not
     overlap the inputs); automatic differentiation does not follow it."""
-    import torch
     dtype, index = _float_type(logits), GP_I32 if tokens is None else _index_type(tokens)
     rows, ld = _rows_of_logits(logits, tokens)
     N, C = rows.shape
@@ -1272,7 +1270,6 @@ def distill_grad_tensors(logits, teacher_index, teacher_logits, stats, grad_loss
     """Convenience for torch tensors: the gradient of distill_tensors with respect to its logits, from the stats it left and grad_loss, the gradient of the
     losses (float32, one value per row or one for all).  Returns out, of logits' shape and type (made if not given; it must not overlap the inputs);
     automatic differentiation does not follow it."""
-    import torch
     dtype = _float_type(logits)
     rows, ld = _rows_of_logits(logits, None)
     N, C = rows.shape
