@@ -889,13 +889,14 @@ struct Teacher {
             q[i] = some ? q[i] / total : 0.0f;
         }
     }
+    // T^2 q (log q - log p), with T taken into both: (logit - base) / T may be beyond fp32 where T times it is not (a class at the type's lowest value, T below 1)
     __device__ __forceinline__ float loss(float T, float base, float log_total) const
     {
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            if (!(q[i] == 0.0f)) sum += q[i] * (logq[i] - ((logit[i] - base) / T - log_total));
-        return T * T * team_sum<W>(sum);
+            if (!(q[i] == 0.0f)) sum += T * q[i] * (T * (logq[i] + log_total) - (logit[i] - base));
+        return team_sum<W>(sum);
     }
 };
 
