@@ -8,6 +8,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import math
 import os
 from typing import Any, NamedTuple, Optional
 
@@ -590,8 +591,9 @@ def _index_type(tokens):
 
 
 def _one_device(first, *others):
+    device = first.device
     for t in others:
-        if t is not None and t.device != first.device:
+        if t is not None and t.device != device:
             raise ValueError("tensors must be on one device")
 
 
@@ -881,10 +883,7 @@ def _as_rows(t, what):
 
 def _rows_for(t, shape, dtype, what):
     """(view, distance of rows) of a tensor that rows are written to: of `shape`, or two-dimensional with as many rows."""
-    N = 1
-    for n in shape[:-1]:
-        N *= n
-    if (tuple(t.shape) != tuple(shape) and tuple(t.shape) != (N, shape[-1])) or t.dtype != dtype:
+    if (t.shape != shape and tuple(t.shape) != (math.prod(shape[:-1]), shape[-1])) or t.dtype != dtype:
         raise ValueError(f"{what} must be of the rows' shape and of the right type")
     t = _as_rows(t, what)
     return t, _row_stride(t, what)
@@ -915,16 +914,36 @@ def _overlap(a, b):
     return past < other_width or past + width > other_step
 
 
+def _end(t):
+    address, step, width, rows = _memory(t)
+    return address + (rows - 1) * step + width
+
+
+def _clear(*tensors):
+    """Whether no two tensors share memory, as far as their ends tell (None: left out)."""
+    last = 0
+    for at, end in sorted([(t.data_ptr(), t.data_ptr() + t.nbytes if t.is_contiguous() else _end(t)) for t in tensors if t is not None]):
+        if at < last:
+            return False
+        last = end
+    return True
+
+
 def _apart(out, what, *inputs):
     """Refuses a tensor to write that shares memory with what is read: another workgroup may read there after it was written."""
+    start = out.data_ptr()
+    end = start + out.nbytes if out.is_contiguous() else _end(out)
     for t in inputs:
-        if t is not None and _overlap(out, t):
+        if t is None:
+            continue
+        at = t.data_ptr()
+        if at < end and not (at < start and t.is_contiguous() and at + t.nbytes <= start) and _overlap(out, t):
             raise ValueError(f"{what} must not overlap what the call reads or writes besides")
 
 
 def _itself(out, t):
-    """Whether a call that writes out over t writes every element over itself."""
-    return out.dtype == t.dtype and _memory(out) == _memory(t)
+    """Whether a call that writes out over t writes every element over itself (both matrices)."""
+    return out.data_ptr() == t.data_ptr() and out.dtype == t.dtype and out.shape == t.shape and (out.stride() == t.stride() or out.is_contiguous() and t.is_contiguous())
 
 
 def _vector(t, n, what):
@@ -1056,15 +1075,19 @@ def layer_norm_grad_tensors(grad, x, stats, weight=None, x_grad=None, weight_gra
         to, ldxg = _rows_for(x_grad, x.shape, x.dtype, "x_grad")
     outs = [None if t is False else t for t in (x_grad, weight_grad, bias_grad)]
     _one_device(x, grad, stats, weight, workspace, *outs)
-    if outs[0] is not None:
-        _apart(to, "x_grad", stats, weight, *(t for t in (rows, up) if not _itself(to, t)))
-    sums = [t for t in outs[1:] if t is not None]
-    for i, t in enumerate(sums):
-        _apart(t, "weight_grad or bias_grad", rows, up, stats, outs[0], *sums[:i])
+    given = [t for t in outs if t is not None]
+    other = [t for t in (rows, up) if outs[0] is None or not _itself(to, t)]
+    over_weight = False
+    if given and not _clear(*given, *other, stats, weight):
+        if outs[0] is not None:
+            _apart(to, "x_grad", *other, stats, weight)
+        sums = [t for t in outs[1:] if t is not None]
+        for i, t in enumerate(sums):
+            _apart(t, "weight_grad or bias_grad", rows, up, stats, outs[0], *sums[:i])
+        over_weight = weight is not None and any(_overlap(t, weight) for t in sums)
     with _on_stream(x, stream) as handle:
-        written = [t for t in outs if t is not None]
-        if written:
-            _written(*written)
+        if given:
+            _written(*given)
         if x_grad is None:
             x_grad = _new_like(x)
             to, ldxg = x_grad, d
@@ -1078,7 +1101,7 @@ def layer_norm_grad_tensors(grad, x, stats, weight=None, x_grad=None, weight_gra
         need = gp_layer_norm_grad_workspace(N, d)
         ws = _workspace(workspace, need, x.device) if need > 0 else None
         kind = _types()[0].get(weight_dtype, -1)
-        if sums and weight is not None and any(_overlap(t, weight) for t in sums):
+        if over_weight:
             weight = weight.detach().clone()  # (few rows: workgroups that read it run beside those that write its gradient)
         gp_layer_norm_grad(up.data_ptr(), ldg, grad_dtype, rows.data_ptr(), ldx, dtype, N, d, stats.data_ptr(), _ptr(weight), kind, _ptr(to), ldxg,
                            _ptr(weight_grad), _ptr(bias_grad), accumulate, _ptr(ws), 0 if ws is None else ws.numel(), handle)
