@@ -4,10 +4,10 @@
 //   h = (x - m) r,  u = w g:   dx = r (u - mean(u) - h mean(u h)),   dw = sum over rows of g h,   db = sum over rows of g
 //
 // Both directions are bound by memory: a row is read once, kept in the registers of a team of lanes, and written once.  Mean and
-// squares are taken of (x - m) with the row at hand, so rows far from zero lose nothing.  A team is as few lanes as hold the row
+// squares are taken of (x - m) with the row at hand, so rows far from zero lose nothing; the few that fp32 cannot do are done again in fp64.  A team is as few lanes as hold the row
 // in 16 to 32 elements each: few steps of a sum across lanes, and 64 bytes a lane in flight; more lanes where there are too few rows to fill the
 // chip.  Teams keep the columns' parameters from row to row (a workgroup for every few rows instead: 52 -> 102 us for 507,001 x 100 in bf16).  Rows too
-// long for 1,024 lanes are read again for each sum.  us measured, and what the same bytes take a large copy: 507,001 x 100 in bf16 46 (44); gradients of
+// long for 1,024 lanes are read again for each sum (2,048 x 40,000 in fp32 271, a copy 141).  us measured, and what the same bytes take a large copy: 507,001 x 100 in bf16 45 (44); gradients of
 // 232,965 x 602 in fp32 347 (362), of 16,384 x 4,096 in bf16 82 (87).
 //
 // Gradients of weights: a team walks over every so-many-th row with the columns' sums in registers, a workgroup adds its teams' sums up in
