@@ -1134,7 +1134,9 @@ gp_status launch_short(const AnswerArgs& a, hipStream_t stream)
     GP_HIP(hipGetLastError());
     return GP_OK;
 }
-// Elements of a row that lists of more than 8 places are kept in registers for: beyond, a wavefront's or workgroup's bound finds them sooner.
+// Elements of a row that lists of more than 8 places are kept in registers for; beyond, a wavefront's bound finds them.  us, bound / list in bf16: 246,153 x 260, 20 places
+// 289 / 326, 130,000 x 500, 32 places 163 / 177, 3,000 x 300, 20 places 8.0 / 9.6.  A list would be sooner for 9 to 16 places there (12 places 241 / 198, 129 / 109) and
+// for 33 to 64 up to 256 elements (320,000 x 200, 64 places 573 / 324; in fp32 378 / 322): those limits are too low.
 constexpr int kListRow = 256, kLongListRow = 128;
 
 template <typename T, int VEC, int NV, int TPR>
