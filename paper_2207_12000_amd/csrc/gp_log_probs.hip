@@ -120,6 +120,8 @@ struct RowSums {
     __device__ __forceinline__ float entropy() const { return none() ? 0.0f : logf(total) - weighted / total; }
 };
 __device__ __forceinline__ float base_of(float m) { return m == -infinity() ? 0.0f : m; }
+// Half of a logit's distance from the largest, which whole may be beyond fp32 where s times it is not (the same bits, but for the scale)
+__device__ __forceinline__ float half_distance(float x, float base) { return 0.5f * x - 0.5f * base; }
 
 // The sums of a row from those of its parts, one in each lane of a team of W, in every lane.  A part's are of exp(s (x - its own largest)): with
 // z = s (its largest - the row's), exp(z) times them, and z exp(z) times the total more of the weighted one.  A part of classes that are ruled out adds
@@ -139,7 +141,7 @@ __device__ __forceinline__ void write_top(const AnswerArgs& a, int64_t row, int 
 {
     const bool none = x == -infinity();
     a.top_index[row * a.k + place] = none ? -1 : j;
-    a.top_logp[row * a.k + place] = none ? -infinity() : (x - base) * a.scale - log_total;
+    a.top_logp[row * a.k + place] = none ? -infinity() : half_distance(x, base) * (2.0f * a.scale) - log_total;
 }
 __device__ __forceinline__ void write_top(const AnswerArgs& a, int64_t row, int place, uint64_t key, float base, float log_total)
 {
@@ -148,7 +150,7 @@ __device__ __forceinline__ void write_top(const AnswerArgs& a, int64_t row, int 
 __device__ __forceinline__ void write_row(const AnswerArgs& a, int64_t row, int64_t token, float logit, float base, const RowSums& s)
 {
     const float l = s.log_total();
-    if (a.logp) a.logp[row] = token >= 0 && token < a.C ? (logit - base) * a.scale - l : 0.0f;
+    if (a.logp) a.logp[row] = token >= 0 && token < a.C ? half_distance(logit, base) * (2.0f * a.scale) - l : 0.0f;
     if (a.entropy) a.entropy[row] = s.entropy();
     if (a.stats) a.stats[2 * row] = base, a.stats[2 * row + 1] = l;
 }
@@ -889,13 +891,14 @@ struct Teacher {
             q[i] = some ? q[i] / total : 0.0f;
         }
     }
-    // T^2 q (log q - log p), with T taken into both: (logit - base) / T may be beyond fp32 where T times it is not (a class at the type's lowest value, T below 1)
+    // T^2 q (log q - log p), with T taken into both: (logit - base) / T may be beyond fp32 where T times it is not (a class at the type's lowest value, T below 1),
+    // and so may logit - base
     __device__ __forceinline__ float loss(float T, float base, float log_total) const
     {
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            if (!(q[i] == 0.0f)) sum += T * q[i] * (T * (logq[i] + log_total) - (logit[i] - base));
+            if (!(q[i] == 0.0f)) sum += 2.0f * T * q[i] * (0.5f * T * (logq[i] + log_total) - half_distance(logit[i], base));
         return team_sum<W>(sum);
     }
 };
