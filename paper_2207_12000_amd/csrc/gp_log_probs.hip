@@ -891,15 +891,16 @@ struct Teacher {
             q[i] = some ? q[i] / total : 0.0f;
         }
     }
-    // T^2 q (log q - log p), with T taken into both: (logit - base) / T may be beyond fp32 where T times it is not (a class at the type's lowest value, T below 1),
-    // and so may logit - base
+    // T^2 q (log q - log p) as 4 T q (T (log q + log(sum)) - (logit - base)) / 4, in quarters: (logit - base) / T may be beyond fp32 where the loss is not (a class at the
+    // type's lowest value, T below 1), and so may logit - base and a sum of such
     __device__ __forceinline__ float loss(float T, float base, float log_total) const
     {
+        const float t = 0.25f * T, b = 0.25f * base;
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            if (!(q[i] == 0.0f)) sum += 2.0f * T * q[i] * (0.5f * T * (logq[i] + log_total) - half_distance(logit[i], base));
-        return team_sum<W>(sum);
+            if (!(q[i] == 0.0f)) sum += q[i] * (t * (logq[i] + log_total) - (0.25f * logit[i] - b));
+        return 4.0f * T * team_sum<W>(sum);
     }
 };
 
