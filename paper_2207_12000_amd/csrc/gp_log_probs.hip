@@ -11,7 +11,7 @@
 // All are bound by memory: a row is read once, into the registers of a team of lanes (as it is stored: widened it would take twice as many in bf16), and
 // where the gradient is asked for along with the loss it is written from there.  Rows that a workgroup cannot hold, and few long rows, are cut into
 // parts, a workgroup each, whose results a second launch joins.  us measured, and what the same bytes take a large copy: 4,096 rows of 32,768 in
-// bf16, eight alternatives 63 (58), loss and gradient 110 (116); 507,001 fp32 rows of 47, loss and gradient 58 (49); the gradient of 2.45 M of them 200 (213).
+// bf16, eight alternatives 63 (58), loss and gradient 109 (116); 507,001 fp32 rows of 47, loss and gradient 59 (49); the gradient of 2.45 M of them 200 (213).
 //
 // Alternatives.  Teams of part of a wavefront sort their elements in registers, put their lists together and keep the largest.  A logit and its class make
 // one number there, larger logits and then lower classes first, so no two are equal (double_of, and key_of in memory).  Teams of a wavefront or more
